@@ -2,42 +2,17 @@
 // workspace layout and kernel launches.  See include/mtgr_hstu.h and include/mtgr_embedding.h
 // for the contract.
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <mutex>
 #include <string>
 
 #include "../../include/mtgr_embedding.h"
 #include "../../include/mtgr_hstu.h"
+#include "api_util.h"
 #include "mtgr_internal.h"
 
 namespace {
 
-thread_local std::string g_last_error;
-
-mtgr_status_t fail(mtgr_status_t st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-mtgr_status_t fail(mtgr_status_t st, const char* fmt, ...) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof(buf), fmt, ap);
-    va_end(ap);
-    g_last_error = buf;
-    return st;
-}
-
-mtgr_status_t ok() {
-    g_last_error.clear();
-    return MTGR_SUCCESS;
-}
-
-mtgr_status_t device_fail(hipError_t e, const char* where) {
-    return fail(MTGR_ERROR_DEVICE, "%s: %s", where, hipGetErrorString(e));
-}
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+using namespace mtgr_api;
 
 constexpr int MAX_SEQLEN = (mtgr::SCHED_BUCKETS - 1) * 64;
 

@@ -96,7 +96,19 @@ __global__ __launch_bounds__(256) void add_kernel(long long rows, int cols, cons
     }
 }
 
+// Zero rows of `chunks` 16-byte chunks, `ld` chunks apart.
+__global__ __launch_bounds__(256) void zero_rows_kernel(long long rows, int chunks, uint4* p, long long ld) {
+    for (long long r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int c = threadIdx.x; c < chunks; c += 256) p[r * ld + c] = make_uint4(0, 0, 0, 0);
+}
+
 }  // namespace
+
+hipError_t launch_zero_rows(long long rows, int chunks, void* p, long long ld, hipStream_t s) {
+    if (rows <= 0) return hipSuccess;
+    zero_rows_kernel<<<(int)(rows < 16384 ? rows : 16384), 256, 0, s>>>(rows, chunks, (uint4*)p, ld);
+    return hipGetLastError();
+}
 
 hipError_t launch_add(long long rows, int cols, bool bf16, const void* a, long long lda, const void* b,
                       long long ldb, void* out, long long ldo, hipStream_t s) {

@@ -1,0 +1,386 @@
+// Softmax cross entropy of token rows against a set of class rows, in pieces of the classes, without
+// keeping the logits:
+//   z_nc = scale x_n . w_c + b_c,  lse_n = log sum_c exp z_nc,  loss_n = lse_n - z_n,t(n)
+// and its gradients
+//   dz_nc = g_n (exp(z_nc - lse_n) - [c = t(n)]),  dx = scale dz W,  dW = scale dz^T x,  db = sum_n dz.
+//
+// Only rows with a label (0 <= t < V) take part.  They are gathered once into consecutive rows, so that
+// the products' cost follows their number, which stays on the device (no synchronisation): the grids are
+// laid out for N rows and the kernels stop at the count.
+//
+// Forward: x W^T on the matrix cores (gemm_wide.h), whose epilogue leaves the maximum and the sum of
+// exponentials of every row and 64 classes; a second kernel joins them.  2 n V d operations; written are
+// 8 bytes per row and 64 classes, a sixteenth of the logits in bf16.
+// Backward, per piece of classes: x W^T again, its epilogue turning the products into dz (rounded to bf16
+// as operand of the next two products; the bias gradient is summed from dz before that rounding), then
+// dx += dz W (fp32, over the pieces) and the piece's dW = dz^T x.  6 n V d operations.
+#include "gemm_wide.h"
+
+namespace mtgr {
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int ROWS_PER_BLOCK = 256;               // of the gather
+constexpr int GROUP_M = 4;                        // see gemm_wide.h (tile_of)
+
+struct SmPlan {
+    int piece;                // classes per piece, a multiple of 256
+    int pieces;
+    int vpad;                 // V rounded up to whole tiles
+    size_t rows, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
+};
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Pieces of the classes: the statistics (forward, 8 bytes per row and 64 classes) or dz (backward, 2 bytes
+// per row and class) of one piece take about half or one gigabyte.
+SmPlan sm_plan(long long N, int V, int d, bool backward) {
+    SmPlan p{};
+    const long long mblocks = (N + WBM - 1) / WBM, npad = mblocks * WBM;
+    const long long blocks = (V + WBN - 1ll) / WBN;
+    const long long budget = backward ? (1ll << 30) / (npad * 2 * WBN) : (512ll << 20) / (npad * 32);
+    long long per = std::max(1ll, std::min(budget, blocks));
+    p.pieces = (int)((blocks + per - 1) / per);
+    per = (blocks + p.pieces - 1) / p.pieces;     // pieces of equal size
+    p.piece = (int)(per * WBN);
+    p.vpad = (int)(blocks * WBN);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += align256(bytes);
+        return here;
+    };
+    p.rows = take(256);
+    p.index = take(sizeof(int) * npad);
+    p.bias = take(sizeof(float) * p.vpad);
+    p.xc = take((size_t)npad * d * 2);
+    if (!backward) {
+        p.stats = take((size_t)(p.piece / 64) * N * sizeof(float2));
+        p.running = take((size_t)N * sizeof(float2));
+    } else {
+        p.info = take(sizeof(int4) * npad);
+        p.dz = take((size_t)N * p.piece * 2);
+        // fp32 partials of both products: one split, or as many as make at most 256 tiles
+        const size_t nblocks = (size_t)((d + WBN - 1) / WBN), tile = WBM * WBN * sizeof(float);
+        p.dxp = take(std::max<size_t>(mblocks * nblocks, 256) * tile);
+        p.dwp = take(std::max<size_t>(per * nblocks, 256) * tile);
+        p.colp = take((size_t)2 * mblocks * p.piece * sizeof(float));
+    }
+    p.total = at;
+    return p;
+}
+
+template <class T>
+__device__ __forceinline__ int label_of(const void* targets, long long i, int V) {
+    const T t = ((const T*)targets)[i];
+    return t >= 0 && t < V ? (int)t : -1;
+}
+
+// Gathers the rows with a label (index[k] = row, xc[k] = x[row]) in order, counts them, and finishes the
+// rows without one: loss = lse = 0 (forward), dx = 0 (backward).  A workgroup has 256 rows and counts the
+// labels before them itself.  The last workgroups write the padded class bias, in units of log 2.
+template <class T, bool BWD>
+__global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* rows, int* index, uint16_t* xc,
+                                                       float* bias2, int4* info, int vpad, int row_blocks) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if ((int)blockIdx.x >= row_blocks) {
+        const int c = ((int)blockIdx.x - row_blocks) * 1024 + tid;
+        if (c < vpad) bias2[c] = c >= a.V ? -__builtin_inff() : a.bias ? a.bias[c] * LOG2E : 0.f;
+        return;
+    }
+    __shared__ int counts[16], own[4], list[ROWS_PER_BLOCK], off[ROWS_PER_BLOCK];
+    const long long r0 = (long long)blockIdx.x * ROWS_PER_BLOCK;
+    int before = 0;
+#pragma unroll 8
+    for (long long i = tid; i < r0; i += 1024) before += label_of<T>(a.targets, i, a.V) >= 0;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) before += __shfl_xor(before, o, 64);
+    if (lane == 0) counts[w] = before;
+    const long long r = r0 + tid;
+    const int t = tid < ROWS_PER_BLOCK && r < a.N ? label_of<T>(a.targets, r, a.V) : -1;
+    const unsigned long long on = __ballot(t >= 0);
+    if (lane == 0 && w < 4) own[w] = __popcll(on);
+    __syncthreads();
+    before = 0;
+#pragma unroll
+    for (int i = 0; i < 16; i++) before += counts[i];
+    int at = 0, n = 0;                                   // labelled rows of the waves before, of the workgroup
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if (i < w) at += own[i];
+        n += own[i];
+    }
+    const int in_block = (int)min((long long)ROWS_PER_BLOCK, a.N - r0);
+    if (tid < in_block) {
+        const int lower = __popcll(on & ((1ull << lane) - 1ull));
+        if (t >= 0) {
+            const int k = at + lower;
+            list[k] = tid;
+            index[before + k] = (int)r;
+            if (BWD) {
+                // an empty row (no class that counts: lse = -inf) has no gradient
+                const float lse = a.lse[r] * LOG2E, g = a.dloss[r];
+                const bool empty = lse == -__builtin_inff();
+                info[before + k] = make_int4(__float_as_int(empty ? __builtin_inff() : lse),
+                                             __float_as_int(empty ? 0.f : g), t, 0);
+            }
+        } else {
+            off[tid - at - lower] = tid;                 // (64 w + lane rows before, at + lower of them labelled)
+            if (!BWD) {
+                a.loss[r] = 0.f;
+                a.lse[r] = 0.f;
+            }
+        }
+    }
+    __syncthreads();
+    const int ch = a.d / 8;
+    for (int i = tid; i < n * ch; i += 1024) {
+        const int k = i / ch, c = i % ch;
+        *(uint4*)(xc + (long long)(before + k) * a.d + 8 * c) =
+            *(const uint4*)((const uint16_t*)a.x + (r0 + list[k]) * a.ld_x + 8 * c);
+    }
+    if (BWD)
+        for (int i = tid; i < (in_block - n) * ch; i += 1024)
+            *(uint4*)((uint16_t*)a.dx + (r0 + off[i / ch]) * a.ld_x + 8 * (i % ch)) = make_uint4(0, 0, 0, 0);
+    if ((int)blockIdx.x == row_blocks - 1) {
+        const int total = before + n;
+        if (tid == 0) *rows = total;
+        // rows up to the end of the last tile: no gradient
+        if (BWD && total + tid < (total + WBM - 1) / WBM * WBM)
+            info[total + tid] = make_int4(__float_as_int(__builtin_inff()), 0, -1, 0);
+    }
+}
+
+__device__ __forceinline__ float2 join(float2 p, float2 q) {
+    const float top = fmaxf(p.x, q.x);
+    return make_float2(top, p.y * __builtin_amdgcn_exp2f(p.x - top) + q.y * __builtin_amdgcn_exp2f(q.x - top));
+}
+
+// Joins a piece's statistics, [parts][N], of 16 rows per workgroup (64 threads a row, so that a large class
+// set is not one thread's chain of loads), with those of the pieces before.  After the last piece: loss and
+// lse, the label's logit from its own product.
+template <class T>
+__global__ __launch_bounds__(1024) void sm_join_kernel(SoftmaxLossArgs a, const int* rows, const int* index,
+                                                       const uint16_t* xc, const float* bias2, const float2* stats,
+                                                       int parts, float2* running, bool first, bool last) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, count = *rows;
+    const int r0 = (int)blockIdx.x * 16;
+    if (r0 >= count) return;
+    __shared__ float2 part[16][16];
+    __shared__ float zt[16];
+    const int r = r0 + (tid & 15);
+    float2 s = make_float2(-3.402823466e38f, 0.f);
+    if (r < count) {
+#pragma unroll 4
+        for (int p = tid >> 4; p < parts; p += 64) s = join(s, stats[(long long)p * a.N + r]);
+    }
+#pragma unroll
+    for (int o = 16; o <= 32; o <<= 1) s = join(s, make_float2(__shfl_xor(s.x, o, 64), __shfl_xor(s.y, o, 64)));
+    if (lane < 16) part[w][lane] = s;
+    if (last && r0 + w < count) {
+        const long long row = index[r0 + w];
+        const int t = label_of<T>(a.targets, row, a.V);
+        const uint16_t *x = xc + (long long)(r0 + w) * a.d, *c = (const uint16_t*)a.w + (long long)t * a.ld_w;
+        float dot = 0.f;
+        for (int i = lane; i < a.d; i += 64) dot = fmaf(bf16_to_f32(x[i]), bf16_to_f32(c[i]), dot);
+        dot = wave_sum(dot);
+        if (lane == 0) zt[w] = fmaf(dot, a.scale * LOG2E, bias2[t]);
+    }
+    __syncthreads();
+    if (tid < 16 && r < count) {
+        s = part[0][tid];
+#pragma unroll
+        for (int i = 1; i < 16; i++) s = join(s, part[i][tid]);
+        if (!first) s = join(s, running[r]);
+        if (!last) {
+            running[r] = s;
+        } else {
+            const long long row = index[r];
+            const float lse = s.x + __builtin_amdgcn_logf(s.y);
+            const bool empty = s.y == 0.f;               // no class counts
+            a.lse[row] = empty ? -__builtin_inff() : lse * LN2;
+            a.loss[row] = empty ? 0.f : (lse - zt[tid]) * LN2;
+        }
+    }
+}
+
+// dx of the rows with a label: the K splits' sums, scaled and rounded once.
+__global__ __launch_bounds__(256) void sm_dx_kernel(SoftmaxLossArgs a, const int* rows, const int* index,
+                                                    const float* partial) {
+    const int count = *rows, ch = a.d / 8;
+    const int splits = acc_splits((count + WBM - 1) / WBM * ((a.d + WBN - 1) / WBN));
+    const long long per = (long long)count * a.d;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)count * ch;
+         i += (long long)gridDim.x * 256) {
+        const long long r = i / ch;
+        const int c = (int)(i % ch) * 8;
+        const float* p = partial + r * a.d + c;
+        floatx4 lo = *(const floatx4*)p, hi = *(const floatx4*)(p + 4);
+        for (int k = 1; k < splits; k++) {
+            lo += *(const floatx4*)(p + k * per);
+            hi += *(const floatx4*)(p + k * per + 4);
+        }
+        lo *= a.scale;
+        hi *= a.scale;
+        *(uint4*)((uint16_t*)a.dx + index[r] * a.ld_x + c) =
+            make_uint4(pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3]));
+    }
+}
+
+// A piece's dW = scale sum of the K splits, rounded once; the last workgroups add up its bias gradient.
+__global__ __launch_bounds__(256) void sm_dw_kernel(SoftmaxLossArgs a, const int* rows, const float* partial,
+                                                    int splits, int v0, int nv, const float* colp, int ld_col,
+                                                    int sum_blocks) {
+    if ((int)blockIdx.x >= sum_blocks) {
+        const int c = ((int)blockIdx.x - sum_blocks) * 256 + threadIdx.x;
+        if (c >= nv) return;
+        const int parts = 2 * ((*rows + WBM - 1) / WBM);
+        float s = 0.f;
+#pragma unroll 8
+        for (int p = 0; p < parts; p++) s += colp[(long long)p * ld_col + c];
+        a.dbias[v0 + c] = s;
+        return;
+    }
+    const int ch = a.d / 4;
+    const long long per = (long long)nv * a.d;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)nv * ch; i += (long long)sum_blocks * 256) {
+        const long long r = i / ch;
+        const int c = (int)(i % ch) * 4;
+        floatx4 s = *(const floatx4*)(partial + r * a.d + c);
+        for (int k = 1; k < splits; k++) s += *(const floatx4*)(partial + k * per + r * a.d + c);
+        s *= a.scale;
+        *(uint2*)((uint16_t*)a.dw + (v0 + r) * a.ld_w + c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
+    }
+}
+
+template <bool BWD>
+hipError_t launch_rows(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, hipStream_t s) {
+    const int rb = (int)((a.N + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK), bb = (p.vpad + 1023) / 1024;
+    int *rows = (int*)(ws + p.rows), *index = (int*)(ws + p.index);
+    uint16_t* xc = (uint16_t*)(ws + p.xc);
+    float* bias2 = (float*)(ws + p.bias);
+    int4* info = (int4*)(ws + p.info);
+    if (a.targets64) sm_rows_kernel<int64_t, BWD><<<rb + bb, 1024, 0, s>>>(a, rows, index, xc, bias2, info, p.vpad, rb);
+    else sm_rows_kernel<int, BWD><<<rb + bb, 1024, 0, s>>>(a, rows, index, xc, bias2, info, p.vpad, rb);
+    return hipGetLastError();
+}
+
+// x W^T of the piece at class v0.
+GemmArgs logits_product(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, int v0) {
+    GemmArgs g{};
+    g.layout = GEMM_NT;
+    g.M = a.N;
+    g.N = std::min(p.piece, p.vpad - v0);
+    g.K = a.d;
+    g.A = ws + p.xc;
+    g.lda = a.d;
+    g.B = (const uint16_t*)a.w + v0 * a.ld_w;
+    g.ldb = a.ld_w;
+    g.bias = (const float*)(ws + p.bias) + v0;
+    g.scale = a.scale * LOG2E;
+    g.rows = (const int*)(ws + p.rows);
+    g.b_rows = std::min(p.piece, a.V - v0);
+    g.class0 = v0;
+    g.group_m = GROUP_M;
+    g.mblocks = (int)((a.N + WBM - 1) / WBM);
+    g.nblocks = (int)(g.N / WBN);
+    g.splits = 1;
+    g.ks_per_split = (a.d + WBK - 1) / WBK;
+    return g;
+}
+
+}  // namespace
+
+size_t softmax_loss_workspace_bytes(long long N, int V, int d, bool backward) {
+    return N > 0 && V > 0 ? sm_plan(N, V, d, backward).total : 0;
+}
+
+hipError_t launch_softmax_loss_fwd(const SoftmaxLossArgs& a, void* workspace, hipStream_t s) {
+    const SmPlan p = sm_plan(a.N, a.V, a.d, false);
+    char* ws = (char*)workspace;
+    hipError_t e = launch_rows<false>(a, p, ws, s);
+    for (int i = 0; i < p.pieces && e == hipSuccess; i++) {
+        GemmArgs g = logits_product(a, p, ws, i * p.piece);
+        g.stats = (float2*)(ws + p.stats);
+        if ((e = wide_launch<GEMM_NT, GEMM_EPI_SM_STATS, false>(g, s)) != hipSuccess) break;
+        const int blocks = (int)((a.N + 15) / 16);
+        const bool first = i == 0, last = i == p.pieces - 1;
+        const int *rows = (const int*)(ws + p.rows), *index = (const int*)(ws + p.index);
+        const uint16_t* xc = (const uint16_t*)(ws + p.xc);
+        const float* bias2 = (const float*)(ws + p.bias);
+        float2* running = (float2*)(ws + p.running);
+        if (a.targets64) sm_join_kernel<int64_t><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, 4 * g.nblocks, running, first, last);
+        else sm_join_kernel<int><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, 4 * g.nblocks, running, first, last);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hipStream_t s) {
+    if (a.N == 0) {
+        const hipError_t z = launch_zero_rows(a.V, a.d / 8, a.dw, a.ld_w / 8, s);
+        return z != hipSuccess || !a.dbias ? z : launch_fill_f32(a.dbias, a.V, 0.f, s);
+    }
+    const SmPlan p = sm_plan(a.N, a.V, a.d, true);
+    char* ws = (char*)workspace;
+    const int* rows = (const int*)(ws + p.rows);
+    hipError_t e = launch_rows<true>(a, p, ws, s);
+    for (int i = 0; i < p.pieces && e == hipSuccess; i++) {
+        const int v0 = i * p.piece;
+        GemmArgs g = logits_product(a, p, ws, v0);
+        const int nv = g.b_rows;
+        g.C = ws + p.dz;
+        g.ldc = p.piece;
+        g.row_info = (const int4*)(ws + p.info);
+        g.col_partial = a.dbias ? (float*)(ws + p.colp) : nullptr;
+        if ((e = wide_launch<GEMM_NT, GEMM_EPI_SM_GRAD, false>(g, s)) != hipSuccess) break;
+
+        GemmArgs x{};                                    // dx += dz W
+        x.layout = GEMM_NN;
+        x.M = a.N;
+        x.N = a.d;
+        x.K = (nv + WBK - 1) / WBK * WBK;                // (dz is zero behind the last class)
+        x.A = ws + p.dz;
+        x.lda = p.piece;
+        x.B = g.B;
+        x.ldb = a.ld_w;
+        x.rows = rows;
+        x.b_rows = nv;
+        x.accumulate = i > 0;
+        x.partial = (float*)(ws + p.dxp);
+        x.mblocks = g.mblocks;
+        x.nblocks = (a.d + WBN - 1) / WBN;
+        x.splits = 1;
+        const int xgrid = XCDS * ((std::max(x.mblocks * x.nblocks, 256) + XCDS - 1) / XCDS);
+        gemm_wide_kernel<GEMM_NN, GEMM_EPI_ACC, false><<<xgrid, 512, 0, s>>>(x);
+        if ((e = hipGetLastError()) != hipSuccess) break;
+
+        GemmArgs w{};                                    // the piece's dW = dz^T x
+        w.layout = GEMM_TN;
+        w.M = nv;
+        w.N = a.d;
+        w.K = a.N;
+        w.A = ws + p.dz;
+        w.lda = p.piece;
+        w.B = ws + p.xc;
+        w.ldb = a.d;
+        w.rows = rows;
+        w.partial = (float*)(ws + p.dwp);
+        w.mblocks = (nv + WBM - 1) / WBM;
+        w.nblocks = x.nblocks;
+        const long long nks = (a.N + WBK - 1) / WBK;
+        w.splits = (int)std::max(1ll, std::min({256ll / (w.mblocks * w.nblocks), nks / 8, 64ll}));
+        if ((e = wide_launch<GEMM_TN, GEMM_EPI_ROWS, false>(w, s)) != hipSuccess) break;
+        const int sums = (int)std::min(((long long)nv * a.d / 4 + 255) / 256, 8192ll);
+        const int cols = a.dbias ? (nv + 255) / 256 : 0;
+        sm_dw_kernel<<<sums + cols, 256, 0, s>>>(a, rows, w.partial, w.splits, v0, nv, g.col_partial, (int)g.N, sums);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+    const int grid = (int)std::min((a.N * (a.d / 8) + 255) / 256, 8192ll);
+    sm_dx_kernel<<<grid, 256, 0, s>>>(a, rows, (const int*)(ws + p.index), (const float*)(ws + p.dxp));
+    return hipGetLastError();
+}
+
+}  // namespace mtgr

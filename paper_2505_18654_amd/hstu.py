@@ -54,6 +54,8 @@ EXPORTED = (
     "mtgr_embedding_lookup_workspace_size", "mtgr_embedding_lookup", "mtgr_embedding_gather",
     "mtgr_embedding_sgd_workspace_size", "mtgr_embedding_sgd", "mtgr_embedding_evict",
     "mtgr_embedding_rehash",
+    "mtgr_gated_ffn_workspace_size", "mtgr_gated_ffn_fwd", "mtgr_gated_ffn_bwd", "mtgr_dropout",
+    "mtgr_softmax_loss_workspace_size", "mtgr_softmax_loss_fwd", "mtgr_softmax_loss_bwd",
 )
 
 
@@ -83,6 +85,21 @@ class GlnProblem(ctypes.Structure):
         ("num_tokens", ctypes.c_int64), ("dim", ctypes.c_int32), ("num_groups", ctypes.c_int32),
         ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
         ("ld_x", ctypes.c_int64), ("ld_u", ctypes.c_int64), ("ld_y", ctypes.c_int64),
+    ]
+
+
+class GatedFfnProblem(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int64), ("dim", ctypes.c_int32), ("hidden", ctypes.c_int32),
+        ("ld_x", ctypes.c_int64), ("ld_w_in", ctypes.c_int64), ("ld_w_out", ctypes.c_int64),
+        ("ld_y", ctypes.c_int64), ("ld_r", ctypes.c_int64), ("ld_pre", ctypes.c_int64), ("ld_h", ctypes.c_int64),
+    ]
+
+
+class SoftmaxLossProblem(ctypes.Structure):
+    _fields_ = [
+        ("num_rows", ctypes.c_int64), ("num_classes", ctypes.c_int64), ("dim", ctypes.c_int32),
+        ("target_bits", ctypes.c_int32), ("scale", ctypes.c_float), ("ld_x", ctypes.c_int64), ("ld_w", ctypes.c_int64),
     ]
 
 
@@ -141,6 +158,15 @@ def lib() -> ctypes.CDLL:
         L.mtgr_embedding_sgd.argtypes = [E, i64, vp, vp, vp, i64, i64, vp, vp, ctypes.c_float, vp, sz, vp]
         L.mtgr_embedding_evict.argtypes = [E, i32, ctypes.c_uint32, vp, vp]
         L.mtgr_embedding_rehash.argtypes = [E, E, vp]
+        F, S = ctypes.POINTER(GatedFfnProblem), ctypes.POINTER(SoftmaxLossProblem)
+        L.mtgr_gated_ffn_workspace_size.argtypes = [F, ctypes.c_int, ctypes.POINTER(sz)]
+        L.mtgr_gated_ffn_fwd.argtypes = [F, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mtgr_gated_ffn_bwd.argtypes = [F, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mtgr_dropout.argtypes = [i64, i32, ctypes.c_int, vp, i64, ctypes.c_double, vp, ctypes.c_uint32, vp, i64, vp,
+                                   i64, vp]
+        L.mtgr_softmax_loss_workspace_size.argtypes = [S, ctypes.c_int, ctypes.POINTER(sz)]
+        L.mtgr_softmax_loss_fwd.argtypes = [S, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mtgr_softmax_loss_bwd.argtypes = [S, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         for name in EXPORTED:
             if name not in ("mtgr_status_string", "mtgr_last_error_message", "mtgr_version"):
                 getattr(L, name).restype = ctypes.c_int
@@ -409,3 +435,46 @@ def mtgr_embedding_evict(table, threshold, min_count, num_evicted, stream=None) 
 
 def mtgr_embedding_rehash(src, dst, stream=None) -> None:
     _check(lib().mtgr_embedding_rehash(ctypes.byref(src), ctypes.byref(dst), _stream(stream)))
+
+
+# ------------------------------------------------------------------ feed-forward block, dropout, softmax loss
+
+def mtgr_gated_ffn_workspace_size(problem: GatedFfnProblem, backward: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().mtgr_gated_ffn_workspace_size(ctypes.byref(problem), int(backward), ctypes.byref(out)))
+    return int(out.value)
+
+
+def mtgr_gated_ffn_fwd(problem, x, w_in, w_out, residual, y, pre, h, workspace, workspace_bytes, stream=None) -> None:
+    _check(lib().mtgr_gated_ffn_fwd(ctypes.byref(problem), _ptr(x), _ptr(w_in), _ptr(w_out), _ptr(residual), _ptr(y),
+                                    _ptr(pre), _ptr(h), _ptr(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def mtgr_gated_ffn_bwd(problem, dy, x, pre, h, w_in, w_out, dx, dw_in, dw_out, workspace, workspace_bytes,
+                       stream=None) -> None:
+    _check(lib().mtgr_gated_ffn_bwd(ctypes.byref(problem), _ptr(dy), _ptr(x), _ptr(pre), _ptr(h), _ptr(w_in),
+                                    _ptr(w_out), _ptr(dx), _ptr(dw_in), _ptr(dw_out), _ptr(workspace),
+                                    int(workspace_bytes), _stream(stream)))
+
+
+def mtgr_dropout(rows, cols, dtype, x, ld_x, prob, rng, site, residual, ld_residual, out, ld_out, stream=None) -> None:
+    _check(lib().mtgr_dropout(int(rows), int(cols), int(dtype), _ptr(x), int(ld_x), float(prob), _ptr(rng), int(site),
+                              _ptr(residual), int(ld_residual), _ptr(out), int(ld_out), _stream(stream)))
+
+
+def mtgr_softmax_loss_workspace_size(problem: SoftmaxLossProblem, backward: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().mtgr_softmax_loss_workspace_size(ctypes.byref(problem), int(backward), ctypes.byref(out)))
+    return int(out.value)
+
+
+def mtgr_softmax_loss_fwd(problem, x, w, targets, bias, loss, lse, workspace, workspace_bytes, stream=None) -> None:
+    _check(lib().mtgr_softmax_loss_fwd(ctypes.byref(problem), _ptr(x), _ptr(w), _ptr(targets), _ptr(bias), _ptr(loss),
+                                       _ptr(lse), _ptr(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def mtgr_softmax_loss_bwd(problem, dloss, x, w, targets, bias, lse, dx, dw, dbias, workspace, workspace_bytes,
+                          stream=None) -> None:
+    _check(lib().mtgr_softmax_loss_bwd(ctypes.byref(problem), _ptr(dloss), _ptr(x), _ptr(w), _ptr(targets), _ptr(bias),
+                                       _ptr(lse), _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(workspace),
+                                       int(workspace_bytes), _stream(stream)))

@@ -302,3 +302,160 @@ def add(a, b, out=None):
     hstu.mtgr_add(rows, cols, _dtype_code(a), a, _token_stride(a, cols), b, _token_stride(b, cols), out,
                   _token_stride(out, cols))
     return out
+
+
+# ------------------------------------------------------------------ feed-forward block, dropout, softmax loss
+
+def _matrix(name: str, t, shape, dtype, like=None) -> int:
+    """Checks a 2-D operand (shape, type, dense rows that do not overlap, the current device) and returns its
+    row stride; `like`: the strides that a gradient shares."""
+    if not isinstance(t, torch.Tensor) or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        got = f"{tuple(t.shape)} {t.dtype}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise ValueError(f"{name} is [{shape[0]}, {shape[1]}] of {dtype}, got {got}")
+    _on_device(name, t)
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"the rows of {name} overlap")
+    ld = _token_stride(t, shape[1])
+    if like is not None and ld != like:
+        raise ValueError(f"{name} must share the row stride of its primal")
+    return ld
+
+
+def _vector(name: str, t, n: int, dtypes) -> None:
+    if not isinstance(t, torch.Tensor) or tuple(t.shape) != (n,) or t.dtype not in dtypes or not t.is_contiguous():
+        raise ValueError(f"{name} is a dense [{n}] of {' or '.join(str(d) for d in dtypes)}")
+    _on_device(name, t)
+
+
+def _on_device(name: str, t) -> None:
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+
+
+def _scratch(workspace, need: int, device):
+    """The caller's workspace, or a new one of at least `need` bytes."""
+    if workspace is None:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("a workspace is a dense uint8 tensor")
+    _on_device("workspace", workspace)
+    return workspace
+
+
+def _two_dims(name: str, t):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} is a matrix")
+    return t.shape
+
+
+def gated_ffn_problem(tokens: int, dim: int, hidden: int, ld_x=None, ld_w_in=None, ld_w_out=None, ld_y=None, ld_r=None,
+                      ld_pre=None, ld_h=None) -> hstu.GatedFfnProblem:
+    return hstu.GatedFfnProblem(tokens, dim, hidden, ld_x or dim, ld_w_in or 2 * hidden, ld_w_out or dim, ld_y or dim,
+                                ld_r or dim, ld_pre or 2 * hidden, ld_h or hidden)
+
+
+def gated_ffn_workspace(tokens: int, dim: int, hidden: int, device="cuda", backward: bool = False) -> torch.Tensor:
+    """A workspace for gated_ffn_fwd (serving) or gated_ffn_bwd of up to `tokens` tokens."""
+    n = hstu.mtgr_gated_ffn_workspace_size(gated_ffn_problem(tokens, dim, hidden), backward)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def gated_ffn_fwd(x, w_in, w_out, residual=None, save: bool = False, out=None, workspace=None):
+    """y = (silu(x W_gate) * (x W_up)) W_out (+ residual), bf16: x [T, d], w_in [d, 2f] = gate | up columns,
+    w_out [f, d]; d and f multiples of 32.  Returns y, or with save=True (y, pre [T, 2f], h [T, f]), the last two
+    for gated_ffn_bwd."""
+    (T, d), f = _two_dims("x", x), _two_dims("w_out", w_out)[0]
+    bf = torch.bfloat16
+    if out is None:
+        out = torch.empty((T, d), dtype=bf, device=x.device)
+    pre = torch.empty((T, 2 * f), dtype=bf, device=x.device) if save else None
+    h = torch.empty((T, f), dtype=bf, device=x.device) if save else None
+    p = gated_ffn_problem(T, d, f, _matrix("x", x, (T, d), bf), _matrix("w_in", w_in, (d, 2 * f), bf),
+                          _matrix("w_out", w_out, (f, d), bf), _matrix("out", out, (T, d), bf),
+                          _matrix("residual", residual, (T, d), bf) if residual is not None else None)
+    n = 0
+    if not save:
+        workspace = _scratch(workspace, hstu.mtgr_gated_ffn_workspace_size(p), x.device)
+        n = workspace.numel()
+    hstu.mtgr_gated_ffn_fwd(p, x, w_in, w_out, residual, out, pre, h, None if save else workspace, n)
+    return (out, pre, h) if save else out
+
+
+def gated_ffn_bwd(dy, x, pre, h, w_in, w_out, grads=None, workspace=None):
+    """Gradients of gated_ffn_fwd: (dx, dw_in, dw_out), in the layouts of x, w_in and w_out (`grads`: the tensors to
+    write).  A residual's gradient is dy itself."""
+    (T, d), f = _two_dims("x", x), _two_dims("w_out", w_out)[0]
+    bf = torch.bfloat16
+    dx, dw_in, dw_out = grads if grads is not None else (_like_layout(t) for t in (x, w_in, w_out))
+    p = gated_ffn_problem(T, d, f, _matrix("x", x, (T, d), bf), _matrix("w_in", w_in, (d, 2 * f), bf),
+                          _matrix("w_out", w_out, (f, d), bf), _matrix("dy", dy, (T, d), bf), None,
+                          _matrix("pre", pre, (T, 2 * f), bf), _matrix("h", h, (T, f), bf))
+    _matrix("dx", dx, (T, d), bf, p.ld_x)
+    _matrix("dw_in", dw_in, (d, 2 * f), bf, p.ld_w_in)
+    _matrix("dw_out", dw_out, (f, d), bf, p.ld_w_out)
+    workspace = _scratch(workspace, hstu.mtgr_gated_ffn_workspace_size(p, True), x.device)
+    hstu.mtgr_gated_ffn_bwd(p, dy, x, pre, h, w_in, w_out, dx, dw_in, dw_out, workspace, workspace.numel())
+    return dx, dw_in, dw_out
+
+
+def dropout(x, p: float, rng, site: int = 0, residual=None, out=None):
+    """[residual +] dropout(x) of a [rows, cols] matrix, bf16 or fp32.  The mask follows from rng (a device int64 [2]:
+    seed, step), `site` and the element alone and is not stored: the backward pass is dropout(dout, p, rng, site)
+    with the same rng.  A program advances the step between its steps (rng[1] += 1)."""
+    rows, cols = _two_dims("x", x)
+    code = _dtype_code(x)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    ld_x, ld_out = _matrix("x", x, (rows, cols), x.dtype), _matrix("out", out, (rows, cols), x.dtype)
+    ld_r = _matrix("residual", residual, (rows, cols), x.dtype) if residual is not None else cols
+    _vector("rng", rng, 2, (torch.int64,))
+    if not 0 <= site < 1 << 32:
+        raise ValueError("site is a 32-bit number")
+    hstu.mtgr_dropout(rows, cols, code, x, ld_x, p, rng, site, residual, ld_r, out, ld_out)
+    return out
+
+
+def _softmax_loss_problem(x, w, targets, bias, scale: float) -> hstu.SoftmaxLossProblem:
+    (N, d), V = _two_dims("x", x), _two_dims("w", w)[0]
+    ld_x, ld_w = _matrix("x", x, (N, d), torch.bfloat16), _matrix("w", w, (V, d), torch.bfloat16)
+    _vector("targets", targets, N, (torch.int64, torch.int32))
+    if bias is not None:
+        _vector("bias", bias, V, (torch.float32,))
+    return hstu.SoftmaxLossProblem(N, V, d, 64 if targets.dtype == torch.int64 else 32, scale, ld_x, ld_w)
+
+
+def softmax_loss_workspace(rows: int, classes: int, dim: int, device="cuda", backward: bool = False) -> torch.Tensor:
+    """A workspace for softmax_loss_fwd or softmax_loss_bwd of these sizes."""
+    p = hstu.SoftmaxLossProblem(rows, classes, dim, 64, 1.0, dim, dim)
+    n = hstu.mtgr_softmax_loss_workspace_size(p, backward)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def softmax_loss_fwd(x, w, targets, bias=None, scale: float = 1.0, workspace=None):
+    """Softmax cross entropy of the rows of x [N, d] against the classes w [V, d] (bf16), with the logits
+    z = scale x w^T + bias (bias [V] fp32), which are never kept: (loss [N], lse [N]) fp32.  A row whose target lies
+    outside 0 .. V-1 has no label: loss and lse 0.  A bias of -inf takes a class out."""
+    p = _softmax_loss_problem(x, w, targets, bias, scale)
+    loss = torch.empty(p.num_rows, dtype=torch.float32, device=x.device)
+    lse = torch.empty_like(loss)
+    workspace = _scratch(workspace, hstu.mtgr_softmax_loss_workspace_size(p), x.device)
+    hstu.mtgr_softmax_loss_fwd(p, x, w, targets, bias, loss, lse, workspace, workspace.numel())
+    return loss, lse
+
+
+def softmax_loss_bwd(dloss, x, w, targets, lse, bias=None, scale: float = 1.0, grads=None, workspace=None):
+    """Gradients of softmax_loss_fwd for dloss [N] fp32 (that of the mean over n labels: 1 / n) and the forward's lse:
+    (dx, dw, dbias or None), dx and dw in the layouts of x and w (`grads`: the tensors to write)."""
+    p = _softmax_loss_problem(x, w, targets, bias, scale)
+    _vector("dloss", dloss, p.num_rows, (torch.float32,))
+    _vector("lse", lse, p.num_rows, (torch.float32,))
+    if grads is None:
+        grads = _like_layout(x), _like_layout(w), torch.empty_like(bias) if bias is not None else None
+    dx, dw, dbias = grads
+    _matrix("dx", dx, x.shape, torch.bfloat16, p.ld_x)
+    _matrix("dw", dw, w.shape, torch.bfloat16, p.ld_w)
+    if dbias is not None:
+        _vector("dbias", dbias, p.num_classes, (torch.float32,))
+    workspace = _scratch(workspace, hstu.mtgr_softmax_loss_workspace_size(p, True), x.device)
+    hstu.mtgr_softmax_loss_bwd(p, dloss, x, w, targets, bias, lse, dx, dw, dbias, workspace, workspace.numel())
+    return dx, dw, dbias
