@@ -22,7 +22,7 @@ LIB_PATH = os.path.join(HERE, LIB_NAME)
 SOURCES = ["api.hip", "schedule.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_bwd_dq.hip",
            "attn_bwd_dkdv.hip", "attn_bwd_dqds.hip", "group_ln.hip", "validate.hip",
            "pointwise.hip", "embedding.hip", "gemm.hip", "gemm_wide.hip", "clock.hip",
-           "dropout.hip", "ffn.hip", "softmax_loss.hip", "api_block.hip"]
+           "dropout.hip", "ffn.hip", "ffn_rows.hip", "softmax_loss.hip", "api_block.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

@@ -13,6 +13,8 @@
 
 namespace mtgr {
 
+constexpr int FEW_ROWS = 1024;
+
 static void tiles_of(GemmArgs* g, int ntile) {
     g->mblocks = (int)((g->M + WBM - 1) / WBM);
     g->nblocks = (int)((g->N + ntile - 1) / ntile);
@@ -22,6 +24,7 @@ static void tiles_of(GemmArgs* g, int ntile) {
 }
 
 hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t s) {
+    if (a.T <= FEW_ROWS) return launch_ffn_rows(a, s);
     GemmArgs g{};
     g.layout = GEMM_NN;
     g.M = a.T;

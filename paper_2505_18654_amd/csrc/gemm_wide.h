@@ -617,19 +617,21 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
             }
         } else if constexpr (!RESIDUAL) {
             if constexpr (GRAD) {
-                // dz = g (exp(z - lse) - [column = label]) in place of the products, and its column sums
+                // dz = g (exp(z - lse) - [column = label]) / max |g| in place of the products, and its column sums
+                const float top = ((const float*)g.rows)[1];     // the largest |g|
                 floatx4 cs[WNN];
 #pragma unroll
                 for (int a = 0; a < WNN; a++) cs[a] = floatx4{};
 #pragma unroll
                 for (int b = 0; b < WNM; b++) {
-                    const float lse = __int_as_float(ri[b].x), gr = __int_as_float(ri[b].y);
+                    const float lse = __int_as_float(ri[b].x), gr = __int_as_float(ri[b].y) / top;
+                    const float gp = gr * __int_as_float(ri[b].w);
                     const int label = ri[b].z - g.class0 - en;
 #pragma unroll
                     for (int a = 0; a < WNN; a++)
 #pragma unroll
                         for (int e = 0; e < 4; e++)
-                            acc[a][b][e] = gr * __builtin_amdgcn_exp2f(fmaf(acc[a][b][e], g.scale, bi[a][e]) - lse);
+                            acc[a][b][e] = gp * __builtin_amdgcn_exp2f(fmaf(acc[a][b][e], g.scale, bi[a][e]) - lse);
                     if (__any((unsigned)label < 64u)) {
 #pragma unroll
                         for (int a = 0; a < WNN; a++)

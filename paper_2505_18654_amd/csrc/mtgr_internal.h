@@ -151,14 +151,15 @@ struct GemmArgs {
     int mblocks, nblocks, splits, ks_per_split;
     bool wide;                // 256 x 256 tiles, k steps of 64 (gemm_wide.hip)
     // The products of the softmax loss:
-    const int* rows;          // number of token rows on the device (at most M, or K of TN)
+    const int* rows;          // number of token rows on the device (at most M, or K of TN); SM_GRAD: a float
+                              // behind it, the largest gradient of a row's loss
     int b_rows;               // rows of B (classes), where they are fewer than N or K
     int class0;               // first class of the piece
     int group_m;              // m blocks that an XCD's workgroups share
     int accumulate;           // ACC: add to the partials of the calls before
     float scale;              // z = scale acc + bias, in units of log 2
     float2* stats;            // SM_STATS: [4 nblocks][M] (maximum, sum) per row and 64 classes
-    const int4* row_info;     // SM_GRAD: per row (lse, gradient of its loss, label), whole m blocks
+    const int4* row_info;     // SM_GRAD: per row (lse, gradient of its loss, label, factor 2^-low of lse), whole m blocks
     float* col_partial;       // SM_GRAD: [2 mblocks][N] column sums, or NULL
 };
 hipError_t launch_clock_probe(int iters, int blocks, long long* out, hipStream_t s);
@@ -203,6 +204,7 @@ struct FfnArgs {
     long long ld_x, ld_win, ld_wout, ld_y, ld_r, ld_pre, ld_h;
 };
 hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t s);
+hipError_t launch_ffn_rows(const FfnArgs& a, hipStream_t s);      // its form for few tokens (ffn_rows.hip)
 size_t ffn_bwd_workspace_bytes(long long T, int d, int f);
 hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s);
 

@@ -13,7 +13,9 @@
 // 8 bytes per row and 64 classes, a sixteenth of the logits in bf16.
 // Backward, per piece of classes: x W^T again, its epilogue turning the products into dz (rounded to bf16
 // as operand of the next two products; the bias gradient is summed from dz before that rounding), then
-// dx += dz W (fp32, over the pieces) and the piece's dW = dz^T x.  6 n V d operations.
+// dx += dz W (fp32, over the pieces) and the piece's dW = dz^T x.  6 n V d operations.  dz is kept divided by
+// the largest |g| of the rows, which multiplies the finished sums: under a mean the g are one number, whose
+// rounding error would be common to all labels' terms (-g), and a label's own term -1 is exact.
 #include "gemm_wide.h"
 
 namespace mtgr {
@@ -21,6 +23,7 @@ namespace mtgr {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LOG2E_LOW = (float)(1.4426950408889634 - (double)LOG2E);
 constexpr int ROWS_PER_BLOCK = 256;               // of the gather
 constexpr int GROUP_M = 4;                        // see gemm_wide.h (tile_of)
 
@@ -28,7 +31,7 @@ struct SmPlan {
     int piece;                // classes per piece, a multiple of 256
     int pieces;
     int vpad;                 // V rounded up to whole tiles
-    size_t rows, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
+    size_t rows /* their count, the largest |g| */, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -90,6 +93,7 @@ __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* r
         return;
     }
     __shared__ int counts[16], own[4], list[ROWS_PER_BLOCK], off[ROWS_PER_BLOCK];
+    __shared__ float tops[16];
     const long long r0 = (long long)blockIdx.x * ROWS_PER_BLOCK;
     int before = 0;
 #pragma unroll 8
@@ -120,10 +124,13 @@ __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* r
             index[before + k] = (int)r;
             if (BWD) {
                 // an empty row (no class that counts: lse = -inf) has no gradient
-                const float lse = a.lse[r] * LOG2E, g = a.dloss[r];
+                // lse in units of log 2: what its rounding (an error common to the row's terms) leaves out goes
+                // into the factor 2^-low
+                const float lse = a.lse[r], g = a.dloss[r], high = lse * LOG2E;
                 const bool empty = lse == -__builtin_inff();
-                info[before + k] = make_int4(__float_as_int(empty ? __builtin_inff() : lse),
-                                             __float_as_int(empty ? 0.f : g), t, 0);
+                const float low = fmaf(lse, LOG2E_LOW, fmaf(lse, LOG2E, -high));
+                info[before + k] = make_int4(__float_as_int(empty ? __builtin_inff() : high), __float_as_int(empty ? 0.f : g),
+                                             t, __float_as_int(empty ? 0.f : __builtin_amdgcn_exp2f(-low)));
             }
         } else {
             off[tid - at - lower] = tid;                 // (64 w + lane rows before, at + lower of them labelled)
@@ -145,6 +152,21 @@ __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* r
             *(uint4*)((uint16_t*)a.dx + (r0 + off[i / ch]) * a.ld_x + 8 * (i % ch)) = make_uint4(0, 0, 0, 0);
     if ((int)blockIdx.x == row_blocks - 1) {
         const int total = before + n;
+        if (BWD) {
+            float top = 0.f;
+#pragma unroll 4
+            for (long long i = tid; i < a.N; i += 1024)
+                if (label_of<T>(a.targets, i, a.V) >= 0) top = fmaxf(top, fabsf(a.dloss[i]));
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+            if (lane == 0) tops[w] = top;
+            __syncthreads();
+            if (tid == 0) {
+#pragma unroll
+                for (int i = 1; i < 16; i++) top = fmaxf(top, tops[i]);
+                ((float*)rows)[1] = top > 0.f ? top : 1.f;
+            }
+        }
         if (tid == 0) *rows = total;
         // rows up to the end of the last tile: no gradient
         if (BWD && total + tid < (total + WBM - 1) / WBM * WBM)
@@ -209,6 +231,7 @@ __global__ __launch_bounds__(1024) void sm_join_kernel(SoftmaxLossArgs a, const 
 __global__ __launch_bounds__(256) void sm_dx_kernel(SoftmaxLossArgs a, const int* rows, const int* index,
                                                     const float* partial) {
     const int count = *rows, ch = a.d / 8;
+    const float factor = a.scale * ((const float*)rows)[1];
     const int splits = acc_splits((count + WBM - 1) / WBM * ((a.d + WBN - 1) / WBN));
     const long long per = (long long)count * a.d;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)count * ch;
@@ -221,8 +244,8 @@ __global__ __launch_bounds__(256) void sm_dx_kernel(SoftmaxLossArgs a, const int
             lo += *(const floatx4*)(p + k * per);
             hi += *(const floatx4*)(p + k * per + 4);
         }
-        lo *= a.scale;
-        hi *= a.scale;
+        lo *= factor;
+        hi *= factor;
         *(uint4*)((uint16_t*)a.dx + index[r] * a.ld_x + c) =
             make_uint4(pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3]));
     }
@@ -239,17 +262,18 @@ __global__ __launch_bounds__(256) void sm_dw_kernel(SoftmaxLossArgs a, const int
         float s = 0.f;
 #pragma unroll 8
         for (int p = 0; p < parts; p++) s += colp[(long long)p * ld_col + c];
-        a.dbias[v0 + c] = s;
+        a.dbias[v0 + c] = s * ((const float*)rows)[1];
         return;
     }
     const int ch = a.d / 4;
+    const float factor = a.scale * ((const float*)rows)[1];
     const long long per = (long long)nv * a.d;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)nv * ch; i += (long long)sum_blocks * 256) {
         const long long r = i / ch;
         const int c = (int)(i % ch) * 4;
         floatx4 s = *(const floatx4*)(partial + r * a.d + c);
         for (int k = 1; k < splits; k++) s += *(const floatx4*)(partial + k * per + r * a.d + c);
-        s *= a.scale;
+        s *= factor;
         *(uint2*)((uint16_t*)a.dw + (v0 + r) * a.ld_w + c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
     }
 }

@@ -141,10 +141,13 @@ def softmax_loss(x, w, targets, bias=None, scale=1.0, dloss=None):
     e_dz = (e_p + 2 * U * q.abs()) * g.abs()[:, None]
     if empty:
         dz, e_dz = torch.zeros_like(dz), torch.zeros_like(e_dz)
-    e16 = e_dz + half_step(dz) + half_step(e_dz)
+    # The operand is dz / G, G = max |g|, rounded to bf16 and multiplied by G after the sums: off by half a step of
+    # dz / G times G (up to twice half a step of dz itself, whose binade is another), and U of dz for the division.
+    top = g.abs().max() if len(t) and bool((g != 0).any()) else 1.0
+    e16 = e_dz + top * (half_step(dz / top) + half_step(e_dz / top)) + 2 * U * dz.abs()
     s = abs(scale)
     vals.update(dx=whole(scale * (dz @ W)), dw=scale * (dz.t().contiguous() @ X), dbias=dz.sum(0))
-    errs.update(dx=whole(s * (e16 @ W.abs() + (V + 80) * U * (dz.abs() @ W.abs()))),
-                dw=s * (e16.t().contiguous() @ X.abs() + (len(t) + 80) * U * (dz.abs().t().contiguous() @ X.abs())),
-                dbias=e_dz.sum(0) + (len(t) + 20) * U * dz.abs().sum(0))
+    errs.update(dx=whole(s * (e16 @ W.abs() + (V + 82) * U * (dz.abs() @ W.abs()))),
+                dw=s * (e16.t().contiguous() @ X.abs() + (len(t) + 82) * U * (dz.abs().t().contiguous() @ X.abs())),
+                dbias=e_dz.sum(0) + (len(t) + 24) * U * dz.abs().sum(0))
     return vals, errs
