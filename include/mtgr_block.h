@@ -38,8 +38,14 @@ typedef struct {
     int64_t ld_h;             /* h */
 } mtgr_gated_ffn_problem_t;
 
-/* Workspace bytes of the forward (backward = 0) or the backward pass. */
-mtgr_status_t mtgr_gated_ffn_workspace_size(const mtgr_gated_ffn_problem_t* p, int backward, size_t* bytes);
+typedef enum {
+    MTGR_FFN_SERVING = 0,     /* forward, pre and h not kept */
+    MTGR_FFN_BACKWARD = 1,
+    MTGR_FFN_TRAINING = 2     /* forward that keeps pre and h */
+} mtgr_ffn_pass_t;
+
+/* Workspace bytes of a pass. */
+mtgr_status_t mtgr_gated_ffn_workspace_size(const mtgr_gated_ffn_problem_t* p, mtgr_ffn_pass_t pass, size_t* bytes);
 
 /* Forward.  residual may be NULL, and may be y itself.  For the backward pass, pre and h are kept: both
  * given.  For serving, both NULL: h then lives in the workspace. */

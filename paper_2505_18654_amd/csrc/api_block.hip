@@ -56,7 +56,9 @@ mtgr_status_t check_ffn(const mtgr_gated_ffn_problem_t* p) {
     return MTGR_SUCCESS;
 }
 
-size_t ffn_fwd_workspace(const mtgr_gated_ffn_problem_t* p) { return align256((size_t)p->num_tokens * p->hidden * 2); }
+size_t ffn_fwd_workspace(const mtgr_gated_ffn_problem_t* p, bool save) {
+    return align256(mtgr::ffn_fwd_workspace_bytes(p->num_tokens, p->dim, p->hidden, save));
+}
 
 mtgr_status_t check_loss(const mtgr_softmax_loss_problem_t* p) {
     if (!p) return fail(MTGR_ERROR_NULL_POINTER, "problem is NULL");
@@ -118,12 +120,15 @@ size_t loss_workspace(const mtgr_softmax_loss_problem_t* p, bool backward) {
 
 extern "C" {
 
-mtgr_status_t mtgr_gated_ffn_workspace_size(const mtgr_gated_ffn_problem_t* p, int backward, size_t* bytes) {
+mtgr_status_t mtgr_gated_ffn_workspace_size(const mtgr_gated_ffn_problem_t* p, mtgr_ffn_pass_t pass, size_t* bytes) {
     if (!bytes) return fail(MTGR_ERROR_NULL_POINTER, "bytes is NULL");
     CHECK(check_ffn(p));
+    if (pass != MTGR_FFN_SERVING && pass != MTGR_FFN_BACKWARD && pass != MTGR_FFN_TRAINING)
+        return fail(MTGR_ERROR_INVALID_ARGUMENT, "pass %d unknown", (int)pass);
     *bytes = p->num_tokens == 0 ? 0
-             : backward         ? align256(mtgr::ffn_bwd_workspace_bytes(p->num_tokens, p->dim, p->hidden))
-                                : ffn_fwd_workspace(p);
+             : pass == MTGR_FFN_BACKWARD
+                 ? align256(mtgr::ffn_bwd_workspace_bytes(p->num_tokens, p->dim, p->hidden))
+                 : ffn_fwd_workspace(p, pass == MTGR_FFN_TRAINING);
     return ok();
 }
 
@@ -139,16 +144,13 @@ mtgr_status_t mtgr_gated_ffn_fwd(const mtgr_gated_ffn_problem_t* p, const void* 
     if (residual) CHECK(check_matrix(residual, "residual", p->ld_r, p->dim));
     if ((pre == nullptr) != (h == nullptr))
         return fail(MTGR_ERROR_NULL_POINTER, "pre and h are kept together: %s is NULL", pre ? "h" : "pre");
-    mtgr::FfnArgs a{};
-    a.ld_h = p->hidden;
     if (pre) {
         CHECK(check_matrix(pre, "pre", p->ld_pre, 2ll * p->hidden));
         CHECK(check_matrix(h, "h", p->ld_h, p->hidden));
-        a.ld_h = p->ld_h;
-    } else {
-        CHECK(check_workspace(workspace, workspace_bytes, ffn_fwd_workspace(p)));
-        h = workspace;
     }
+    CHECK(check_workspace(workspace, workspace_bytes, ffn_fwd_workspace(p, pre != nullptr)));
+    mtgr::FfnArgs a{};
+    a.ld_h = p->ld_h;
     a.T = p->num_tokens;
     a.d = p->dim;
     a.f = p->hidden;
@@ -165,7 +167,7 @@ mtgr_status_t mtgr_gated_ffn_fwd(const mtgr_gated_ffn_problem_t* p, const void* 
     a.ld_y = p->ld_y;
     a.ld_r = p->ld_r;
     a.ld_pre = p->ld_pre;
-    const hipError_t e = mtgr::launch_ffn_fwd(a, (hipStream_t)stream);
+    const hipError_t e = mtgr::launch_ffn_fwd(a, workspace, (hipStream_t)stream);
     if (e != hipSuccess) return device_fail(e, "gated feed-forward");
     return ok();
 }

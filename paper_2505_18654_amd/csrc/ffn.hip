@@ -9,65 +9,181 @@
 // columns of the same numbers, in the same lanes), and so are dh and dpre: neither the pre-activations
 // (in serving) nor dh go through memory.  Roundings to bf16: h and dpre, as operands of the next product;
 // pre, which the forward keeps for the backward (its tensors of the kind are bf16).
-#include "gemm_wide.h"
+#include "gemm_mid.h"
 
 namespace mtgr {
 
-constexpr int FEW_ROWS = 1024;
+namespace {
 
-static void tiles_of(GemmArgs* g, int ntile) {
-    g->mblocks = (int)((g->M + WBM - 1) / WBM);
-    g->nblocks = (int)((g->N + ntile - 1) / ntile);
-    g->splits = 1;
-    g->ks_per_split = (int)((g->K + WBK - 1) / WBK);
-    g->wide = true;
+// Tiles and K splits of a product, and its kernel: 256 x 256 tiles, one workgroup per CU, or 128 x 128 tiles,
+// two per CU.  Whichever is estimated to end first: rounds of workgroups that fill the chip, each of its k steps
+// of 64 and a start and an end, and with K splits their fp32 partials, written and read by another kernel.
+// The figures are measured ones (T = 312 .. 69,563, d = 256 .. 1024, f = 704 .. 2816).
+struct Tiles {
+    bool mid;
+    int mblocks, nblocks, splits;
+    double us;
+};
+
+Tiles tiles_of(bool mid, long long M, long long N, long long K, int n_factor, int splits, bool partials) {
+    Tiles t{};
+    t.mid = mid;
+    const int side = mid ? MBM : WBM;
+    t.mblocks = (int)((M + side - 1) / side);
+    t.nblocks = (int)((N + side / n_factor - 1) / (side / n_factor));
+    t.splits = splits;
+    const long long steps = ((K + WBK - 1) / WBK + splits - 1) / splits, slots = mid ? MID_WORKGROUPS : WIDE_WORKGROUPS;
+    const long long items = (long long)t.mblocks * t.nblocks * splits, rounds = (items + slots - 1) / slots;
+    t.us = rounds * (mid ? 4.0 + (items > WIDE_WORKGROUPS ? 1.0 : 0.8) * steps : 7.0 + 1.3 * steps);
+    if (partials) t.us += 4.0 + (double)splits * M * N * 8 / 8e6;
+    return t;
 }
 
-hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t s) {
-    if (a.T <= FEW_ROWS) return launch_ffn_rows(a, s);
+Tiles plan(long long M, long long N, long long K, int n_factor) {
+    const Tiles wide = tiles_of(false, M, N, K, n_factor, 1, false), mid = tiles_of(true, M, N, K, n_factor, 1, false);
+    return mid.us < wide.us ? mid : wide;
+}
+
+// The same with K splits of the 128 x 128 tiles.
+Tiles plan_deep(long long M, long long N, long long K) {
+    Tiles best = plan(M, N, K, 1);
+    const long long most = std::min(16ll, (K + WBK - 1) / WBK / 4);
+    for (int s = 2; s <= most; s++) {
+        const Tiles t = tiles_of(true, M, N, K, 1, s, true);
+        if (t.us < best.us) best = t;
+    }
+    return best;
+}
+
+// A weight gradient (K = tokens) is always split.
+Tiles plan_split(long long M, long long N, long long K) {
+    Tiles best{};
+    best.us = 1e30;
+    const long long most = std::min(64ll, std::max(1ll, (K + WBK - 1) / WBK / 4));
+    for (int mid = 0; mid < 2; mid++)
+        for (int s = 1; s <= most; s++) {
+            const Tiles t = tiles_of(mid, M, N, K, 1, s, true);
+            if (t.us < best.us) best = t;
+        }
+    return best;
+}
+
+size_t partial_bytes(const Tiles& t, long long M, long long N) {
+    return t.splits > 1 ? (size_t)t.splits * M * N * sizeof(float) : 0;
+}
+
+// out = sum of the K splits' partials (+ residual), rounded once.
+__global__ __launch_bounds__(256) void ffn_sum_kernel(const float* partial, int splits, long long rows, int cols, uint16_t* out,
+                                                      long long ld_out, const uint16_t* residual, long long ld_r) {
+    const int ch = cols / 4;
+    const long long n = rows * ch;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const long long r = i / ch;
+        const int c = (int)(i % ch) * 4;
+        floatx4 s = ((const floatx4*)partial)[i];
+#pragma unroll 4
+        for (int k = 1; k < splits; k++) s += ((const floatx4*)partial)[k * n + i];
+        if (residual) {
+            const uint2 v = *(const uint2*)(residual + r * ld_r + c);
+            s += floatx4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                         __uint_as_float(v.y & 0xffff0000u)};
+        }
+        *(uint2*)(out + r * ld_out + c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
+    }
+}
+
+void set_tiles(GemmArgs* g, const Tiles& t) {
+    g->mblocks = t.mblocks;
+    g->nblocks = t.nblocks;
+    g->splits = t.splits;
+    g->ks_per_split = (int)(((g->K + WBK - 1) / WBK + t.splits - 1) / t.splits);
+    // (the 256 x 256 kernel wants every split to have k)
+    if (!t.mid) g->splits = (int)(((g->K + WBK - 1) / WBK + g->ks_per_split - 1) / g->ks_per_split);
+    g->wide = !t.mid;
+}
+
+GemmArgs product(int layout, long long M, long long N, long long K, const void* A, long long lda, const void* B,
+                 long long ldb, void* C, long long ldc) {
     GemmArgs g{};
-    g.layout = GEMM_NN;
-    g.M = a.T;
-    g.N = a.f;
-    g.K = a.d;
-    g.A = a.x;
-    g.lda = a.ld_x;
-    g.B = a.w_in;
-    g.ldb = a.ld_win;
-    g.C = a.pre;
-    g.ldc = a.ld_pre;
-    g.C2 = a.h;
-    g.ldc2 = a.ld_h;
-    tiles_of(&g, WBN / 2);
-    hipError_t e = a.pre ? wide_launch<GEMM_NN, GEMM_EPI_GATED_SAVE, false>(g, s)
-                         : wide_launch<GEMM_NN, GEMM_EPI_GATED, false>(g, s);
+    g.layout = layout;
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.A = A;
+    g.lda = lda;
+    g.B = B;
+    g.ldb = ldb;
+    g.C = C;
+    g.ldc = ldc;
+    return g;
+}
+
+}  // namespace
+
+// C = A B (NN) or A B^T (NT), plus the residual R where there is one; `partial` holds the K splits' sums.
+template <int LAYOUT>
+static hipError_t deep_product(GemmArgs g, float* partial, hipStream_t s) {
+    const Tiles t = plan_deep(g.M, g.N, g.K);
+    if (!t.mid && (LAYOUT == GEMM_NT || !g.R)) {
+        gemm_plan(&g);
+        return launch_gemm_bf16(g, s);
+    }
+    set_tiles(&g, t);
+    if constexpr (LAYOUT == GEMM_NN) {
+        if (!t.mid) return wide_launch<GEMM_NN, GEMM_EPI_RESIDUAL, false>(g, s);
+        if (t.splits == 1 && g.R) return mid_launch<GEMM_NN, GEMM_EPI_RESIDUAL>(g, s);
+    }
+    if (t.splits == 1) return mid_launch<LAYOUT, GEMM_EPI_NONE>(g, s);
+    g.partial = partial;
+    const hipError_t e = mid_launch<LAYOUT, GEMM_EPI_PART>(g, s);
     if (e != hipSuccess) return e;
-    g = GemmArgs{};
-    g.layout = GEMM_NN;
-    g.M = a.T;
-    g.N = a.d;
-    g.K = a.f;
-    g.A = a.h;
-    g.lda = a.ld_h;
-    g.B = a.w_out;
-    g.ldb = a.ld_wout;
-    g.C = a.y;
-    g.ldc = a.ld_y;
+    const int grid = (int)std::min((g.M * (g.N / 4) + 255) / 256, 8192ll);
+    ffn_sum_kernel<<<grid, 256, 0, s>>>(partial, g.splits, g.M, (int)g.N, (uint16_t*)g.C, g.ldc, (const uint16_t*)g.R, g.ldr);
+    return hipGetLastError();
+}
+
+static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Workspace of the forward: h, where the caller does not keep it, and the second product's partials.
+size_t ffn_fwd_workspace_bytes(long long T, int d, int f, bool save) {
+    const bool few = ffn_rows_fit(T, d, FFN_OUT_COLUMNS);
+    return (save ? 0 : align256((size_t)T * f * 2)) + (few ? 0 : partial_bytes(plan_deep(T, d, f), T, d));
+}
+
+hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
+    FfnArgs a = f;
+    float* partial = (float*)workspace;
+    if (!a.pre) {
+        a.h = workspace;
+        a.ld_h = a.f;
+        partial = (float*)((char*)workspace + align256((size_t)a.T * a.f * 2));
+    }
+    hipError_t e;
+    if (ffn_rows_fit(a.T, a.f, FFN_HIDDEN_COLUMNS)) {
+        e = launch_ffn_rows_hidden(a, s);
+    } else {
+        GemmArgs g = product(GEMM_NN, a.T, a.f, a.d, a.x, a.ld_x, a.w_in, a.ld_win, a.pre, a.ld_pre);
+        g.C2 = a.h;
+        g.ldc2 = a.ld_h;
+        const Tiles t = plan(a.T, a.f, a.d, 2);
+        set_tiles(&g, t);
+        if (t.mid) e = a.pre ? mid_launch<GEMM_NN, GEMM_EPI_GATED_SAVE>(g, s) : mid_launch<GEMM_NN, GEMM_EPI_GATED>(g, s);
+        else e = a.pre ? wide_launch<GEMM_NN, GEMM_EPI_GATED_SAVE, false>(g, s) : wide_launch<GEMM_NN, GEMM_EPI_GATED, false>(g, s);
+    }
+    if (e != hipSuccess) return e;
+    if (ffn_rows_fit(a.T, a.d, FFN_OUT_COLUMNS)) return launch_ffn_rows_out(a, s);
+    GemmArgs g = product(GEMM_NN, a.T, a.d, a.f, a.h, a.ld_h, a.w_out, a.ld_wout, a.y, a.ld_y);
     g.R = a.residual;
     g.ldr = a.ld_r;
-    if (a.residual) {
-        tiles_of(&g, WBN);
-        return wide_launch<GEMM_NN, GEMM_EPI_RESIDUAL, false>(g, s);
-    }
-    gemm_plan(&g);
-    return launch_gemm_bf16(g, s);
+    return deep_product<GEMM_NN>(g, partial, s);
 }
 
-// Workspace of the backward: dpre [T, 2f] bf16, then the larger of the weight gradients' partials.
-static size_t dpre_bytes(long long T, int f) { return ((size_t)T * 2 * f * 2 + 255) & ~(size_t)255; }
-
+// Workspace of the backward: dpre [T, 2f] bf16, then the largest of the three products' partials.
 size_t ffn_bwd_workspace_bytes(long long T, int d, int f) {
-    return dpre_bytes(T, f) + std::max(gemm_workspace_bytes(GEMM_TN, d, 2ll * f, T), gemm_workspace_bytes(GEMM_TN, f, d, T));
+    const size_t weights = (size_t)d * f * sizeof(float);
+    return align256((size_t)T * 2 * f * 2) +
+           std::max({plan_split(d, 2ll * f, T).splits * 2 * weights, plan_split(f, d, T).splits * weights,
+                     partial_bytes(plan_deep(T, d, 2ll * f), T, d)});
 }
 
 hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
@@ -75,45 +191,27 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
         const hipError_t z = launch_zero_rows(a.d, a.f / 4, a.dw_in, a.ld_win / 8, s);
         return z != hipSuccess ? z : launch_zero_rows(a.f, a.d / 8, a.dw_out, a.ld_wout / 8, s);
     }
+    const long long f2 = 2ll * a.f;
     char* dpre = (char*)workspace;
-    float* partial = (float*)(dpre + dpre_bytes(a.T, a.f));
-    GemmArgs g{};
-    g.layout = GEMM_NT;
-    g.M = a.T;
-    g.N = a.f;
-    g.K = a.d;
-    g.A = a.dy;
-    g.lda = a.ld_y;
-    g.B = a.w_out;
-    g.ldb = a.ld_wout;
-    g.C = dpre;
-    g.ldc = 2ll * a.f;
+    float* partial = (float*)(dpre + align256((size_t)a.T * f2 * 2));
+    GemmArgs g = product(GEMM_NT, a.T, a.f, a.d, a.dy, a.ld_y, a.w_out, a.ld_wout, dpre, f2);
     g.R = a.pre;
     g.ldr = a.ld_pre;
-    tiles_of(&g, WBN);
-    hipError_t e = wide_launch<GEMM_NT, GEMM_EPI_GATED_BWD, false>(g, s);
+    const Tiles t = plan(a.T, a.f, a.d, 1);
+    set_tiles(&g, t);
+    hipError_t e = t.mid ? mid_launch<GEMM_NT, GEMM_EPI_GATED_BWD>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_GATED_BWD, false>(g, s);
     if (e != hipSuccess) return e;
-    auto product = [&](int layout, long long M, long long N, long long K, const void* A, long long lda, const void* B,
-                       long long ldb, void* C, long long ldc) {
-        GemmArgs p{};
-        p.layout = layout;
-        p.M = M;
-        p.N = N;
-        p.K = K;
-        p.A = A;
-        p.lda = lda;
-        p.B = B;
-        p.ldb = ldb;
-        p.C = C;
-        p.ldc = ldc;
-        gemm_plan(&p);
-        p.partial = partial;
-        return launch_gemm_bf16(p, s);
+    e = deep_product<GEMM_NT>(product(GEMM_NT, a.T, a.d, f2, dpre, f2, a.w_in, a.ld_win, a.dx, a.ld_x), partial, s);
+    if (e != hipSuccess) return e;
+    auto gradient = [&](GemmArgs w) {
+        const Tiles q = plan_split(w.M, w.N, w.K);
+        set_tiles(&w, q);
+        w.partial = partial;
+        const hipError_t r = q.mid ? mid_launch<GEMM_TN, GEMM_EPI_NONE>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_NONE, false>(w, s);
+        return r != hipSuccess ? r : launch_split_reduce(w, s);
     };
-    const long long f2 = 2ll * a.f;
-    if ((e = product(GEMM_NT, a.T, a.d, f2, dpre, f2, a.w_in, a.ld_win, a.dx, a.ld_x)) != hipSuccess) return e;
-    if ((e = product(GEMM_TN, a.d, f2, a.T, a.x, a.ld_x, dpre, f2, a.dw_in, a.ld_win)) != hipSuccess) return e;
-    return product(GEMM_TN, a.f, a.d, a.T, a.h, a.ld_h, a.dy, a.ld_y, a.dw_out, a.ld_wout);
+    if ((e = gradient(product(GEMM_TN, a.d, f2, a.T, a.x, a.ld_x, dpre, f2, a.dw_in, a.ld_win))) != hipSuccess) return e;
+    return gradient(product(GEMM_TN, a.f, a.d, a.T, a.h, a.ld_h, a.dy, a.ld_y, a.dw_out, a.ld_wout));
 }
 
 }  // namespace mtgr

@@ -149,7 +149,14 @@ hipError_t rows_launch(const RowsArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_ffn_rows(const FfnArgs& f, hipStream_t s) {
+// Up to one workgroup of 64 rows per CU: beyond that the tiles of gemm_mid.h read the weights less often (312
+// tokens, d = 768, f = 2048: hidden, 320 workgroups, 15.2 us here and 12.2 there; output, 120 workgroups,
+// 11.4 and 25.7; 1,024 tokens, d = 512, f = 1408: 704 workgroups, 18 and 9.4; 256 workgroups, 10 and 20).
+bool ffn_rows_fit(long long T, int N, int columns) {
+    return T <= 16384 && (T + 63) / 64 * ((N + columns - 1) / columns) <= 256;
+}
+
+hipError_t launch_ffn_rows_hidden(const FfnArgs& f, hipStream_t s) {
     RowsArgs a{};
     a.T = (int)f.T;
     a.K = f.d;
@@ -162,8 +169,12 @@ hipError_t launch_ffn_rows(const FfnArgs& f, hipStream_t s) {
     a.ld_out = f.ld_h;
     a.pre = (uint16_t*)f.pre;
     a.ld_pre = f.ld_pre;
-    const hipError_t e = f.pre ? rows_launch<FR_SAVE, 4>(a, s) : rows_launch<FR_GATED, 4>(a, s);
-    if (e != hipSuccess) return e;
+    return f.pre ? rows_launch<FR_SAVE, 4>(a, s) : rows_launch<FR_GATED, 4>(a, s);
+}
+
+hipError_t launch_ffn_rows_out(const FfnArgs& f, hipStream_t s) {
+    RowsArgs a{};
+    a.T = (int)f.T;
     a.K = f.f;
     a.N = f.d;
     a.x = (const uint16_t*)f.h;

@@ -573,6 +573,13 @@ static hipError_t gemm_launch(const GemmArgs& g, hipStream_t s) {
     return hipGetLastError();
 }
 
+hipError_t launch_split_reduce(const GemmArgs& g, hipStream_t s) {
+    const int sums = (int)min((g.M * g.N / 4 + 255) / 256, 8192ll);
+    const int cols = g.colsum ? (int)((g.N + 255) / 256) : 0;
+    gemm_split_reduce_kernel<<<sums + cols, 256, 0, s>>>(g, sums);
+    return hipGetLastError();
+}
+
 hipError_t launch_gemm_bf16(const GemmArgs& g, hipStream_t s) {
     hipError_t e = hipSuccess;
     if (g.wide && g.layout != GEMM_TN) return launch_gemm_wide(g, s);
@@ -591,12 +598,7 @@ hipError_t launch_gemm_bf16(const GemmArgs& g, hipStream_t s) {
             e = g.wide ? launch_gemm_wide(g, s)
                 : g.colsum ? gemm_launch<GEMM_TN, GEMM_EPI_NONE, true>(g, s) : gemm_launch<GEMM_TN, GEMM_EPI_NONE, false>(g, s);
             if (e != hipSuccess) return e;
-            {
-                const int sums = (int)min((g.M * g.N / 4 + 255) / 256, 8192ll);
-                const int cols = g.colsum ? (int)((g.N + 255) / 256) : 0;
-                gemm_split_reduce_kernel<<<sums + cols, 256, 0, s>>>(g, sums);
-            }
-            return hipGetLastError();
+            return launch_split_reduce(g, s);
         default: return hipErrorInvalidValue;
     }
 }

@@ -1,0 +1,332 @@
+// The products of the feed-forward block and the softmax loss on 128 x 128 tiles, for sizes whose 256 x 256
+// tiles (gemm_wide.h: the same layouts, epilogues and arguments) do not fill the chip.
+//
+// A workgroup of 4 waves computes a tile in k steps of 64, wave w the 64 x 64 part (m half w % 2, n half w / 2)
+// as 4 x 4 blocks of 16 x 16, transposed as in gemm_wide.h.  Two LDS stages (64 KB) let two workgroups share a
+// CU, so that one's barriers, copies and epilogue run under the other's matrix instructions.  One barrier per
+// step: it hands over the stage that has landed and frees the other one for the copies of the next step.
+// (A workgroup alone on its CU takes 0.85 us per step, for 0.2 us of matrix work; four stages, or operands read
+// a half step ahead, did not change that, so products of few tiles are split over k instead.)  Epilogues work on a lane's four consecutive columns of a row, without staging: at
+// these sizes the results stay in the L2 caches, which join the 32-byte pieces.
+#pragma once
+
+#include <type_traits>
+
+#include "gemm_wide.h"
+
+namespace mtgr {
+
+namespace {
+
+constexpr int MBM = 128, MBN = 128, MBK = 64;
+constexpr uint32_t MSLOT = MBM * MBK * 2;
+
+// Workgroups per tile grid that fill the chip once: two per CU.
+constexpr int MID_WORKGROUPS = 512;
+
+}  // namespace
+
+template <int LAYOUT, int EPI>
+__global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
+    constexpr bool A_KR = LAYOUT == GEMM_TN, B_KR = LAYOUT != GEMM_NT;
+    constexpr bool ACC = EPI == GEMM_EPI_ACC, SPLIT = LAYOUT == GEMM_TN || ACC || EPI == GEMM_EPI_PART;
+    constexpr bool GATED = EPI == GEMM_EPI_GATED || EPI == GEMM_EPI_GATED_SAVE;
+    constexpr bool STATS = EPI == GEMM_EPI_SM_STATS, GRAD = EPI == GEMM_EPI_SM_GRAD, B_SHORT = STATS || GRAD;
+    constexpr bool DYN = B_SHORT || ACC || EPI == GEMM_EPI_ROWS;
+    constexpr int NTILE = GATED ? MBN / 2 : MBN;
+    constexpr uint32_t OFF_B = 2 * MSLOT;
+    __shared__ __align__(1024) char sm[4 * MSLOT];           // A 0, A 1, B 0, B 1
+
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wm = w & 1, wn = w >> 1;
+    const int lr = lane & 15, lg = lane >> 4;
+    int M = (int)g.M, K = (int)g.K, mblocks = g.mblocks;
+    const int N = (int)g.N;
+    if constexpr (DYN) {
+        if constexpr (LAYOUT == GEMM_TN) {
+            K = min(*g.rows, K);
+        } else {
+            M = min(*g.rows, M);
+            mblocks = (M + MBM - 1) / MBM;
+        }
+    }
+    // items (split, m block, n block), a share of consecutive ones per XCD
+    const int tiles = mblocks * g.nblocks, items = tiles * g.splits, share = (items + XCDS - 1) / XCDS;
+    const int it = blockIdx.x % XCDS * share + blockIdx.x / XCDS;
+    if ((int)(blockIdx.x / XCDS) >= share || it >= items) return;
+    const int split = it / tiles, mb = it % tiles / g.nblocks, nb = it % g.nblocks;
+    const int m0 = mb * MBM, n0 = nb * NTILE;
+    const int nks = (K + MBK - 1) / MBK, per = (nks + g.splits - 1) / g.splits;
+    const int ks0 = split * per, nk = min(nks, ks0 + per) - ks0;      // at most 0: a split without k
+
+    const uint32_t lds0 = lds_address(sm), ldsw = lds0 + __builtin_amdgcn_readfirstlane((uint32_t)w * 1024u);
+    // copies: instruction q of wave w fills the 1 KB block 4 q + w of a slot, as in gemm_wide.h
+    auto kc_offsets = [&](uint32_t* vo, long long ld, int rvalid, int kvalid) {
+        const int r = 8 * w + (lane >> 3), c = min((lane & 7) ^ swz<8>(r), (kvalid >> 3) - 1);
+#pragma unroll
+        for (int q = 0; q < 4; q++) vo[q] = (uint32_t)(min(32 * q + r, rvalid - 1) * ld + 8 * c) * 2u;
+    };
+    auto kr_offsets = [&](uint32_t* vo, long long ld, int cvalid, int kvalid) {
+        const int r = 4 * w + (lane >> 4), c = min((lane & 15) ^ swz<16>(r), ((cvalid + 7) >> 3) - 1);
+#pragma unroll
+        for (int q = 0; q < 4; q++) vo[q] = (uint32_t)(min(16 * q + r, kvalid - 1) * ld + 8 * c) * 2u;
+    };
+    auto gated_offsets = [&](uint32_t* vo, long long ld, int hvalid, int kvalid) {
+        const int r = 4 * w + (lane >> 4), c = (lane & 15) ^ swz<16>(r);
+        const int col = 8 * min(4 * (c >> 3) + (c & 3), (hvalid >> 3) - 1) + n0 + ((c & 4) ? N : 0);
+#pragma unroll
+        for (int q = 0; q < 4; q++) vo[q] = (uint32_t)(min(16 * q + r, kvalid - 1) * ld + col) * 2u;
+    };
+    auto offsets_a = [&](uint32_t* vo, int kvalid) {
+        if constexpr (A_KR) kr_offsets(vo, g.lda, M - m0, kvalid);
+        else kc_offsets(vo, g.lda, min(MBM, M - m0), kvalid);
+    };
+    auto offsets_b = [&](uint32_t* vo, int kvalid) {
+        if constexpr (GATED) gated_offsets(vo, g.ldb, N - n0, kvalid);
+        else if constexpr (B_KR) kr_offsets(vo, g.ldb, N - n0, kvalid);
+        else kc_offsets(vo, g.ldb, min(MBN, (B_SHORT ? g.b_rows : N) - n0), kvalid);
+    };
+    const long long stepA = 2ll * (A_KR ? MBK * g.lda : MBK), stepB = 2ll * (B_KR ? MBK * g.ldb : MBK);
+    const char* pa = (const char*)g.A + 2 * (A_KR ? (long long)m0 : (long long)m0 * g.lda) + ks0 * stepA;
+    const char* pb = (const char*)g.B + 2 * (GATED ? 0ll : B_KR ? (long long)n0 : (long long)n0 * g.ldb) + ks0 * stepB;
+    uint32_t voA[4], voB[4];
+    offsets_a(voA, MBK);
+    offsets_b(voB, MBK);
+    auto copy = [&](int i) {
+        const int valid = K - (ks0 + i) * MBK;             // k left; fewer than 64 in the last step of a ragged K
+        uint32_t ra[4], rb[4];
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            ra[q] = voA[q];
+            rb[q] = voB[q];
+        }
+        if (valid < MBK) {
+            offsets_a(ra, valid);
+            offsets_b(rb, valid);
+        }
+        // (the A of these products is padded with zeros in k: only the rows of B end early)
+        if constexpr (ACC) {
+            if ((ks0 + i + 1) * MBK > g.b_rows) offsets_b(rb, g.b_rows - (ks0 + i) * MBK);
+        }
+        const uint32_t slot = (uint32_t)(i & 1) * MSLOT;
+#pragma unroll
+        for (int q = 0; q < 4; q++) lds_dma16(ldsw + slot + 4096u * q, pa, ra[q]);
+#pragma unroll
+        for (int q = 0; q < 4; q++) lds_dma16(ldsw + OFF_B + slot + 4096u * q, pb, rb[q]);
+        pa += stepA;
+        pb += stepB;
+    };
+    // zeros in the k past a ragged K, in both operands
+    auto zero_tail = [&](int i) {
+        const int valid = K - (ks0 + i) * MBK;
+        auto clear = [&](bool kr, char* t) {
+            if (kr) {
+                for (int c = valid * 16 + tid; c < MBK * 16; c += 256) ((uint4*)t)[c] = make_uint4(0, 0, 0, 0);
+            } else {
+                for (int c = tid; c < MBM * 8; c += 256)
+                    if (((c & 7) ^ swz<8>(c >> 3)) >= (valid >> 3)) ((uint4*)t)[c] = make_uint4(0, 0, 0, 0);
+            }
+        };
+        clear(A_KR, sm + (i & 1) * MSLOT);
+        clear(B_KR, sm + OFF_B + (i & 1) * MSLOT);
+        lds_barrier();
+    };
+    // operand reads, as in gemm_wide.h; a k-row slot has 16 chunks per row
+    auto kc_base = [&](int r0) { return lds0 + 16u * (uint32_t)((r0 + lr) * 8 + (lg ^ swz<8>(lr))); };
+    auto kr_base = [&](int c0, int half) {
+        const int row = 8 * lg + 4 * half + (lr >> 2), colx = c0 + 4 * (lr & 3);
+        return lds0 + 16u * (uint32_t)tile_chunk<16>(row, colx >> 3) + 2u * (uint32_t)(colx & 7);
+    };
+    uint32_t rm[2], rn[2];
+    rm[0] = A_KR ? kr_base(64 * wm, 0) : kc_base(64 * wm);
+    rm[1] = A_KR ? kr_base(64 * wm, 1) : 0;
+    rn[0] = OFF_B + (B_KR ? kr_base(64 * wn, 0) : kc_base(64 * wn));
+    rn[1] = OFF_B + (B_KR ? kr_base(64 * wn, 1) : 0);
+    typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+    auto read_frag = [&](auto kr, const uint32_t (&r)[2], uint32_t slot, int part, int blk) {
+        if constexpr (decltype(kr)::value) {
+            const uint32_t o0 = ((r[0] + slot) ^ (32u * blk)) + 8192u * part, o1 = ((r[1] + slot) ^ (32u * blk)) + 8192u * part;
+            const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(uintptr_t)o0);
+            const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(uintptr_t)o1);
+            const short __attribute__((ext_vector_type(8))) v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            return __builtin_bit_cast(bf16x8, v);
+        } else {
+            return *(const lds_bf16x8*)(uintptr_t)(((r[0] + slot) ^ (64u * part)) + 2048u * blk);
+        }
+    };
+    using AK = std::integral_constant<bool, A_KR>;
+    using BK = std::integral_constant<bool, B_KR>;
+
+    floatx4 acc[4][4];
+#pragma unroll
+    for (int a = 0; a < 4; a++)
+#pragma unroll
+        for (int b = 0; b < 4; b++) acc[a][b] = floatx4{};
+    if (nk > 0) copy(0);
+    for (int i = 0; i < nk; i++) {
+        wait_vmem();
+        lds_barrier();
+        if (i + 1 < nk) copy(i + 1);
+        if (K - (ks0 + i) * MBK < MBK) zero_tail(i);
+        const uint32_t slot = (uint32_t)(i & 1) * MSLOT;
+#pragma unroll
+        for (int p = 0; p < 2; p++) {
+            bf16x8 fm[4], fn[4];
+#pragma unroll
+            for (int b = 0; b < 4; b++) fm[b] = read_frag(AK{}, rm, slot, p, b);
+#pragma unroll
+            for (int a = 0; a < 4; a++) fn[a] = read_frag(BK{}, rn, slot, p, a);
+#pragma unroll
+            for (int a = 0; a < 4; a++)
+#pragma unroll
+                for (int b = 0; b < 4; b++)
+                    acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fn[a], fm[b], acc[a][b], 0, 0, 0);
+        }
+    }
+
+    // ---- epilogue: acc[a][b] holds row em + 16 b + l % 16, columns en + 16 a + 4 (l / 16) + 0..3
+    const int em = m0 + 64 * wm + lr, en = n0 + 64 * wn + 4 * lg;
+    auto pack = [](floatx4 v) { return make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); };
+    auto unpack = [](uint2 u) {
+        return floatx4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                       __uint_as_float(u.y & 0xffff0000u)};
+    };
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int b = 0; b < 4; b++)
+#pragma unroll
+            for (int a = 0; a < 4; a++) {
+                const int gm = em + 16 * b, gn = en + 16 * a;
+                if (gm >= M || gn >= N) continue;
+                floatx4* dst = (floatx4*)(g.partial + ((long long)split * M + gm) * N + gn);
+                *dst = ACC && g.accumulate ? *dst + acc[a][b] : acc[a][b];
+            }
+    } else if constexpr (STATS) {
+        floatx4 bias[4];
+#pragma unroll
+        for (int a = 0; a < 4; a++) bias[a] = *(const floatx4*)(g.bias + en + 16 * a);
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            float top = -3.402823466e38f, sum = 0.f;
+#pragma unroll
+            for (int a = 0; a < 4; a++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    acc[a][b][e] = fmaf(acc[a][b][e], g.scale, bias[a][e]);
+                    top = fmaxf(top, acc[a][b][e]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+#pragma unroll
+            for (int a = 0; a < 4; a++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) sum += __builtin_amdgcn_exp2f(acc[a][b][e] - top);
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            const int gm = em + 16 * b;
+            if (lg == 0 && gm < M) g.stats[(long long)(2 * nb + wn) * g.M + gm] = make_float2(top, sum);
+        }
+    } else if constexpr (GRAD) {
+        const float top = ((const float*)g.rows)[1];
+        floatx4 bias[4], cs[4];
+        int4 ri[4];
+#pragma unroll
+        for (int b = 0; b < 4; b++) ri[b] = g.row_info[em + 16 * b];
+#pragma unroll
+        for (int a = 0; a < 4; a++) {
+            bias[a] = *(const floatx4*)(g.bias + en + 16 * a);
+            cs[a] = floatx4{};
+        }
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            const float lse = __int_as_float(ri[b].x), gr = __int_as_float(ri[b].y) / top;
+            const float gp = gr * __int_as_float(ri[b].w);
+            const int label = ri[b].z - g.class0 - en, gm = em + 16 * b;
+#pragma unroll
+            for (int a = 0; a < 4; a++) {
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    acc[a][b][e] = gp * __builtin_amdgcn_exp2f(fmaf(acc[a][b][e], g.scale, bias[a][e]) - lse);
+                    if (label == 16 * a + e) acc[a][b][e] -= gr;
+                }
+                cs[a] += acc[a][b];
+                if (gm < M) *(uint2*)((uint16_t*)g.C + gm * g.ldc + en + 16 * a) = pack(acc[a][b]);
+            }
+        }
+        if (g.col_partial != nullptr) {
+#pragma unroll
+            for (int a = 0; a < 4; a++) {
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    float v = dpp_add<0xB1>(cs[a][e]);
+                    v = dpp_add<0x4E>(v);
+                    v = dpp_add<0x141>(v);
+                    cs[a][e] = dpp_add<0x140>(v);
+                }
+                if (lr == 0) *(floatx4*)(g.col_partial + (long long)(2 * mb + wm) * g.N + en + 16 * a) = cs[a];
+            }
+        }
+    } else if constexpr (GATED) {
+#pragma unroll
+        for (int b = 0; b < 4; b++)
+#pragma unroll
+            for (int a = 0; a < 2; a++) {
+                const int gm = em + 16 * b, gn = n0 + 32 * wn + 16 * a + 4 * lg;
+                if (gm >= M || gn >= N) continue;
+                const floatx4 z = acc[a][b], u = acc[a + 2][b];
+                if constexpr (EPI == GEMM_EPI_GATED_SAVE) {
+                    uint16_t* p = (uint16_t*)g.C + gm * g.ldc + gn;
+                    *(uint2*)p = pack(z);
+                    *(uint2*)(p + N) = pack(u);
+                }
+                const floatx4 h = {silu(z[0]) * u[0], silu(z[1]) * u[1], silu(z[2]) * u[2], silu(z[3]) * u[3]};
+                *(uint2*)((uint16_t*)g.C2 + gm * g.ldc2 + gn) = pack(h);
+            }
+    } else {
+        // (what the epilogue reads is loaded before the first store)
+        uint2 r0[EPI == GEMM_EPI_NONE ? 1 : 4][4], r1[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][4];
+        if constexpr (EPI != GEMM_EPI_NONE) {
+#pragma unroll
+            for (int b = 0; b < 4; b++)
+#pragma unroll
+                for (int a = 0; a < 4; a++) {
+                    const uint16_t* r = (const uint16_t*)g.R + min(em + 16 * b, M - 1) * g.ldr + min(en + 16 * a, N - 4);
+                    r0[a][b] = *(const uint2*)r;
+                    if constexpr (EPI == GEMM_EPI_GATED_BWD) r1[a][b] = *(const uint2*)(r + N);
+                }
+        }
+#pragma unroll
+        for (int b = 0; b < 4; b++)
+#pragma unroll
+            for (int a = 0; a < 4; a++) {
+                const int gm = em + 16 * b, gn = en + 16 * a;
+                if (gm >= M || gn >= N) continue;
+                floatx4 v = acc[a][b];
+                uint16_t* dst = (uint16_t*)g.C + gm * g.ldc + gn;
+                if constexpr (EPI == GEMM_EPI_GATED_BWD) {
+                    const floatx4 z = unpack(r0[a][b]), u = unpack(r1[a][b]);
+                    floatx4 dz, du;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const float sg = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z[e]));
+                        const float s = v[e] * sg;
+                        du[e] = s * z[e];
+                        dz[e] = s * u[e] * (1.0f + z[e] * (1.0f - sg));
+                    }
+                    *(uint2*)dst = pack(dz);
+                    *(uint2*)(dst + N) = pack(du);
+                } else {
+                    if constexpr (EPI == GEMM_EPI_RESIDUAL) v += unpack(r0[a][b]);
+                    *(uint2*)dst = pack(v);
+                }
+            }
+    }
+}
+
+template <int LAYOUT, int EPI>
+static hipError_t mid_launch(const GemmArgs& g, hipStream_t s) {
+    const int items = g.mblocks * g.nblocks * g.splits;
+    gemm_mid_kernel<LAYOUT, EPI><<<XCDS * ((items + XCDS - 1) / XCDS), 256, 0, s>>>(g);
+    return hipGetLastError();
+}
+
+}  // namespace mtgr

@@ -43,14 +43,14 @@ constexpr int WBM = 256, WBN = 256, WBK = 64;
 constexpr int WNM = 8, WNN = 4;                 // 16 x 16 blocks per wave (m, n)
 constexpr uint32_t WSLOT = WBM * WBK * 2;       // bytes of one operand's stage
 constexpr int WQ = 4;                           // copy instructions per wave, operand and stage
-// Slots: A 0, A 1, B 0, B 1, A 2; the epilogue stages in the last one.
+// Slots: A 0, A 1, B 0, B 1 and the third stage of the deep operand; the epilogue stages in the last one.
 constexpr uint32_t WSTAGING = 4 * WSLOT;
 
 template <int V>
 using IC = std::integral_constant<int, V>;
 
 __device__ __forceinline__ uint32_t slot_a(int r) { return r == 2 ? 4u * WSLOT : (uint32_t)r * WSLOT; }
-__device__ __forceinline__ uint32_t slot_b(int r) { return (2u + (uint32_t)r) * WSLOT; }
+__device__ __forceinline__ uint32_t slot_b(int r) { return (2u + (uint32_t)r) * WSLOT; }      // (4: the third stage)
 
 __device__ __forceinline__ float silu(float z) {
     return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
@@ -71,6 +71,13 @@ __device__ __forceinline__ float bf16_half(uint32_t w, int hi) {
 // K splits of a product with `tiles` tiles whose rows are counted on the device: the chip filled once.
 __device__ __forceinline__ int acc_splits(int tiles) { return max(1, min(256 / max(tiles, 1), 64)); }
 
+// Columns of items of the softmax statistics: about 16 items per CU, so that the last round of them is short,
+// each of as many class tiles as that leaves (their statistics stay in registers in between).
+__device__ __forceinline__ int stat_chunks(int mblocks, int nblocks) {
+    const int per_item = min(max(mblocks * nblocks / 4096, 1), 32);
+    return (nblocks + per_item - 1) / per_item;
+}
+
 // LDS hand-off between the lanes of one wave (its LDS operations run in order).
 __device__ __forceinline__ void wave_lds_fence() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -83,14 +90,18 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
     constexpr bool A_KR = LAYOUT == GEMM_TN;      // A stored [K][M]
     constexpr bool B_KR = LAYOUT != GEMM_NT;      // B stored [K][N]
     constexpr bool ACC = EPI == GEMM_EPI_ACC;     // fp32 partials added up over calls
-    constexpr bool SPLIT = LAYOUT == GEMM_TN || ACC;     // fp32 partials per K split, one tile per workgroup
+    constexpr bool DIRECT = EPI == GEMM_EPI_ROWS_DIRECT;
+    constexpr bool SPLIT = (LAYOUT == GEMM_TN && !DIRECT) || ACC;     // fp32 partials per K split, one tile per workgroup
     constexpr bool GATED = EPI == GEMM_EPI_GATED || EPI == GEMM_EPI_GATED_SAVE;
     constexpr bool RESIDUAL = EPI == GEMM_EPI_BIAS_RESIDUAL || EPI == GEMM_EPI_RESIDUAL;
     constexpr bool STATS = EPI == GEMM_EPI_SM_STATS, GRAD = EPI == GEMM_EPI_SM_GRAD;
     // The number of token rows is on the device (g.rows): M, or K of a weight gradient.
-    constexpr bool DYN = STATS || GRAD || ACC || EPI == GEMM_EPI_ROWS;
+    constexpr bool DYN = STATS || GRAD || ACC || EPI == GEMM_EPI_ROWS || DIRECT;
     // The rows of B end before N (its last columns of C are formed from copies of the last row).
     constexpr bool B_SHORT = STATS || GRAD;
+    // Which operand is copied two k steps ahead, into three stages: A, which streams while B (weights) stays
+    // in the XCD's L2; the softmax products stream the classes (B) past a few m blocks of rows.
+    constexpr bool DEEP_B = B_SHORT;
     constexpr int NTILE = GATED ? WBN / 2 : WBN;  // columns of C per tile
     __shared__ __align__(1024) char sm[5 * WSLOT];
 
@@ -109,7 +120,10 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
     // Items (split, m block, n block), an equal share of consecutive ones per XCD (workgroup % 8):
     // an XCD's 32 workgroups share a few m blocks' rows (NN / NT) or few k ranges (TN) in its L2.
     const int x = blockIdx.x % XCDS, tiles = mblocks * g.nblocks;
-    const int splits = ACC ? acc_splits(tiles) : g.splits, items = tiles * splits;
+    const int splits = ACC ? acc_splits(tiles) : g.splits;
+    // SM_STATS: an item is an m block and every chunks-th n block
+    const int chunks = STATS ? stat_chunks(mblocks, g.nblocks) : g.nblocks;
+    const int items = STATS ? mblocks * chunks : tiles * splits;
     const int share = (items + XCDS - 1) / XCDS;
     int j = blockIdx.x / XCDS, mb, nb;            // j: item within the share
     auto tile_of = [&](int jj) {
@@ -118,7 +132,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
         if constexpr (B_SHORT) {
             // Groups of g.group_m m blocks, m fastest: an XCD's workgroups share the rows of a few m
             // blocks and of a few n blocks (a class set is far larger than an L2).
-            const int per = g.group_m * g.nblocks, r = it % per, m = it / per * g.group_m;
+            const int per = g.group_m * chunks, r = it % per, m = it / per * g.group_m;
             const int in_group = min(g.group_m, mblocks - m);
             mb = m + r % in_group;
             nb = r / in_group;
@@ -140,6 +154,18 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
                 const int gm = mb * WBM + c / (WBN / 4), gn = nb * WBN + 4 * (c % (WBN / 4));
                 if (gm < M && gn < N) *(floatx4*)(g.partial + ((long long)split * M + gm) * N + gn) = floatx4{};
             }
+            return;
+        }
+    }
+    if constexpr (DIRECT) {
+        if (nk <= 0) {                            // no rows: no gradient
+            do {
+                for (int c = tid; c < WBM * WBN / 8; c += 512) {
+                    const int gm = mb * WBM + c / (WBN / 8), gn = nb * WBN + 8 * (c % (WBN / 8));
+                    if (gm < M && gn < N) *(uint4*)((uint16_t*)g.C + gm * g.ldc + gn) = make_uint4(0, 0, 0, 0);
+                }
+                j += gridDim.x / XCDS;
+            } while (tile_of(j));
             return;
         }
     }
@@ -218,6 +244,8 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
     };
     using A_ = std::true_type;
     using B_ = std::false_type;
+    using X_ = std::integral_constant<bool, !DEEP_B>;      // the deep operand, and the other one
+    using Y_ = std::integral_constant<bool, DEEP_B>;
     auto copy_a = [&](int i, int r) { copy(IC<0>{}, IC<WQ>{}, A_{}, slot_a(r), i); };
     auto copy_b = [&](int i, int r) { copy(IC<0>{}, IC<WQ>{}, B_{}, slot_b(r), i); };
     // The k past K of a ragged last stage hold copies of valid values; zeros in both operands add
@@ -309,8 +337,9 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
     // Stores of a full tile's epilogue per wave.  The waits below count on at least as many memory
     // operations behind the copies of stage 1 (more only make them stricter).
     constexpr int NOUT = EPI == GEMM_EPI_BIAS_SILU ? 2 : 1;
-    constexpr int NSTORE = STATS ? 8 : EPI == GEMM_EPI_GATED ? 8 : EPI == GEMM_EPI_GATED_SAVE ? 24
+    constexpr int NSTORE = STATS ? 0 : EPI == GEMM_EPI_GATED ? 8 : EPI == GEMM_EPI_GATED_SAVE ? 24
                            : EPI == GEMM_EPI_GATED_BWD ? 32 : 16 * NOUT;
+    constexpr int NBIAS = B_SHORT ? WNN : 0;     // loads of a tile's class bias
     start_tile();
     copy_b(0, 0);
     copy_a(0, 0);
@@ -319,13 +348,22 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
         copy_a(1, 1);
     }
     bool counted = false;      // the previous tile of this workgroup was a full one
+    float ref[STATS ? WNM : 1], sum[STATS ? WNM : 1];      // this lane's columns of an item's rows
+    bool fresh = true;
     for (;;) {
+        floatx4 cbias[B_SHORT ? WNN : 1];
+        if constexpr (B_SHORT) {
+            const char* cb = (const char*)(g.bias + n0);
+            const uint32_t off = 256u * (uint32_t)wn + 16u * (uint32_t)(once(lane) >> 4);
+#pragma unroll
+            for (int a = 0; a < WNN; a++) cbias[a] = *(const floatx4*)(cb + (off + 64u * a));
+        }
         // Stage 0 has landed (a full tile's NSTORE stores and the copies of stage 1 may be in
-        // flight behind it), and slot A 2, where the epilogue staged, is free.
-        if (counted && nk > 1) wait_vmcnt<NSTORE + 2 * WQ>();
+        // flight behind it), and the fifth slot, where the epilogue staged, is free.
+        if (counted && nk > 1) wait_vmcnt<NSTORE + 2 * WQ + NBIAS>();
         else wait_vmem();
         lds_barrier();
-        if (nk > 2) copy_a(2, 2);
+        if (nk > 2) copy(IC<0>{}, IC<WQ>{}, X_{}, slot_a(2), 2);
         if (ragged && nk == 1) zero_tail(slot_a(0), slot_b(0));
 #pragma unroll
         for (int a = 0; a < WNN; a++)
@@ -345,34 +383,34 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
         fm[1] = read_frag(AK{}, rm, slot_a(0), IC<0>{}, IC<1>{});
         fm[2] = read_frag(AK{}, rm, slot_a(0), IC<0>{}, IC<2>{});
         fm[3] = read_frag(AK{}, rm, slot_a(0), IC<0>{}, IC<3>{});
-        // Step i: copies of the second half of B(i+1), then A(i+2), then, behind the barrier that
-        // frees its slot, the first half of B(i+2).
-        uint32_t sa = slot_a(0), sb = slot_b(0), sa1 = slot_a(1), sa2 = slot_a(2), sb1 = slot_b(1);
+        // Step i, with X the deep operand (A) and Y the other one: copies of the second half of Y(i+1), then
+        // X(i+2), then, behind the barrier that frees its slot, the first half of Y(i+2).
+        uint32_t sa = slot_a(0), sb = slot_b(0), sa1 = slot_a(1), sb1 = slot_b(1), sx2 = slot_a(2);
         for (int i = 0; i < nk; i++) {
             const bool cb = i > 0 && i + 1 < nk, ca = i > 0 && i + 2 < nk, cn = i + 2 < nk;
             colsum_step(sb);
             slot(IC<0>{}, IC<0>{}, sa, sa, sb);
-            if (cb) copy(IC<2>{}, IC<3>{}, B_{}, sb1, i + 1);
+            if (cb) copy(IC<2>{}, IC<3>{}, Y_{}, DEEP_B ? sa1 : sb1, i + 1);
             slot(IC<0>{}, IC<1>{}, sa, sa, sb);
             slot(IC<0>{}, IC<2>{}, sa, sa, sb);
-            if (cb) copy(IC<3>{}, IC<4>{}, B_{}, sb1, i + 1);
+            if (cb) copy(IC<3>{}, IC<4>{}, Y_{}, DEEP_B ? sa1 : sb1, i + 1);
             slot(IC<0>{}, IC<3>{}, sa, sa, sb);
             slot(IC<0>{}, IC<4>{}, sa, sa, sb);
-            if (ca) copy(IC<0>{}, IC<1>{}, A_{}, sa2, i + 2);
+            if (ca) copy(IC<0>{}, IC<1>{}, X_{}, sx2, i + 2);
             slot(IC<0>{}, IC<5>{}, sa, sa, sb);
             slot(IC<0>{}, IC<6>{}, sa, sa, sb);
-            if (ca) copy(IC<1>{}, IC<2>{}, A_{}, sa2, i + 2);
+            if (ca) copy(IC<1>{}, IC<2>{}, X_{}, sx2, i + 2);
             slot(IC<0>{}, IC<7>{}, sa, sa, sb);
             slot(IC<1>{}, IC<0>{}, sa, sa1, sb1);
-            if (ca) copy(IC<2>{}, IC<3>{}, A_{}, sa2, i + 2);
+            if (ca) copy(IC<2>{}, IC<3>{}, X_{}, sx2, i + 2);
             slot(IC<1>{}, IC<1>{}, sa, sa1, sb1);
             slot(IC<1>{}, IC<2>{}, sa, sa1, sb1);
-            if (ca) copy(IC<3>{}, IC<4>{}, A_{}, sa2, i + 2);
+            if (ca) copy(IC<3>{}, IC<4>{}, X_{}, sx2, i + 2);
             slot(IC<1>{}, IC<3>{}, sa, sa1, sb1);
-            // stage i + 1 has landed; A(i+2) may still be in flight, in step 0 also the previous
-            // tile's stores, which were issued between the copies of stage 1 and A(2)
+            // stage i + 1 has landed; X(i+2) may still be in flight, in step 0 also the previous
+            // tile's stores (and the class bias), which were issued between the copies of stage 1 and X(2)
             if (cn) {
-                if (i == 0) wait_vmcnt<NSTORE + WQ>();
+                if (i == 0) wait_vmcnt<NSTORE + WQ + NBIAS>();
                 else wait_vmcnt<WQ>();
             } else if (i + 1 < nk) {
                 wait_vmem();
@@ -382,22 +420,21 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
             // (after the last step the reads touch a slot that may be changing and are not used)
             slot(IC<1>{}, IC<4>{}, sa, sa1, sb1);
             slot(IC<1>{}, IC<5>{}, sa, sa1, sb1);
-            if (cn) copy(IC<0>{}, IC<1>{}, B_{}, sb, i + 2);
+            if (cn) copy(IC<0>{}, IC<1>{}, Y_{}, DEEP_B ? sa : sb, i + 2);
             slot(IC<1>{}, IC<6>{}, sa, sa1, sb1);
-            if (cn) copy(IC<1>{}, IC<2>{}, B_{}, sb, i + 2);
+            if (cn) copy(IC<1>{}, IC<2>{}, Y_{}, DEEP_B ? sa : sb, i + 2);
             slot(IC<1>{}, IC<7>{}, sa, sa1, sb1);
-            const uint32_t t = sa;
+            const uint32_t t = sa, u = sb;
             sa = sa1;
-            sa1 = sa2;
-            sa2 = t;
-            const uint32_t u = sb;
             sb = sb1;
-            sb1 = u;
+            sa1 = DEEP_B ? t : sx2;
+            sb1 = DEEP_B ? sx2 : u;
+            sx2 = DEEP_B ? u : t;
         }
 
         // ---- epilogue.  acc[a][b] holds C of row m0 + 128 wm + 16 b + l % 16, columns
         // n0 + 64 wn + 16 a + 4 (l / 16) + 0..3.  Each wave passes its part through 4 KB of its own
-        // in slot A 2 (no barrier), so that a store instruction writes whole 128-byte lines (or
+        // in the fifth slot (no barrier), so that a store instruction writes whole 128-byte lines (or
         // 256-byte rows of fp32 partials), and the first stages of the workgroup's next tile are
         // copied meanwhile.
         const int el = once(lane), er = el & 15, eg = el >> 4;
@@ -452,31 +489,26 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
             }
             wait_vmcnt_seen<0>();                      // (before the copies, which it would wait for)
         }
-        // class bias of this lane's columns (padded to whole tiles) and, for the gradient, its rows
-        int4 ri[GRAD ? WNM : 1];
-        if constexpr (B_SHORT) {
+        int4 ri[GRAD ? WNM : 1];                       // the rows of this lane
+        if constexpr (GRAD) {
 #pragma unroll
-            for (int a = 0; a < WNN; a++) bi[a] = *(const floatx4*)(g.bias + en + 16 * a + 4 * eg);
-            if constexpr (GRAD) {
-#pragma unroll
-                for (int b = 0; b < WNM; b++) ri[b] = g.row_info[em + 16 * b + er];
-            }
-            wait_vmcnt_seen<0>();
+            for (int b = 0; b < WNM; b++) ri[b] = g.row_info[em + 16 * b + er];
         }
-        // gate and up values of row 8 q + l / 8 of block b, chunk l % 8, two blocks ahead
-        uint4 pg[EPI == GEMM_EPI_GATED_BWD ? 2 : 1][2], pu[EPI == GEMM_EPI_GATED_BWD ? 2 : 1][2];
+        if constexpr (B_SHORT) wait_vmcnt_seen<0>();   // (before the copies)
+        // gate and up values of row 8 q + l / 8 of block b, chunk l % 8, four blocks ahead
+        uint4 pg[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][2], pu[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][2];
         auto load_pre = [&](int b) {
             const uint16_t* R = (const uint16_t*)g.R + min(en + 8 * (el & 7), N - 8);
 #pragma unroll
             for (int q = 0; q < 2; q++) {
                 const uint16_t* r = R + min(em + 16 * b + 8 * q + (el >> 3), M - 1) * g.ldr;
-                pg[b & 1][q] = *(const uint4*)r;
-                pu[b & 1][q] = *(const uint4*)(r + N);
+                pg[b & 3][q] = *(const uint4*)r;
+                pu[b & 3][q] = *(const uint4*)(r + N);
             }
         };
         if constexpr (EPI == GEMM_EPI_GATED_BWD) {
-            load_pre(0);
-            load_pre(1);
+#pragma unroll
+            for (int b = 0; b < 4; b++) load_pre(b);
         }
         // residual rows (row 8 q + l / 8 of block b, chunk l % 8), four blocks ahead, and their
         // columns' bias
@@ -498,8 +530,15 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
 #pragma unroll
             for (int b = 0; b < 4; b++) load_residual(b);
         }
-        j += gridDim.x / XCDS;
-        const bool more = tile_of(j);
+        bool more, last_of_item = true;
+        if (STATS && nb + chunks < g.nblocks) {
+            nb += chunks;
+            more = true;
+            last_of_item = false;
+        } else {
+            j += gridDim.x / XCDS;
+            more = tile_of(j);
+        }
         if (more) {
             start_tile();
             copy_b(0, 0);
@@ -511,26 +550,68 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
         }
         counted = full;
         if constexpr (STATS) {
-            // Softmax statistics of this wave's 64 columns, in units of log 2: z = scale log2(e) x.w + bias.
-            // The maximum starts at the lowest number, so that columns of -inf alone leave a sum of 0.
+            // Softmax statistics in units of log 2, z = scale log2(e) x.w + bias: sum of 2^(z - ref) over the
+            // columns of a row that this lane has seen in the item.  ref is the lane's maximum in the item's
+            // first tile.  Later tiles cost no maximum: terms far below ref do not count beside it, and
+            // terms far above are noticed in their sum, which the float range holds up to 2^127 times ref.
+            // It starts at the lowest number, so that columns of -inf alone leave a sum of 0.
+            bool high = fresh;
+            float part[WNM];
+            if (fresh) {
 #pragma unroll
-            for (int b = 0; b < WNM; b++) {
-                float z[4 * WNN], top = -3.402823466e38f, sum = 0.f;
+                for (int b = 0; b < WNM; b++) {
+                    ref[b] = -3.402823466e38f;
+                    sum[b] = 0.f;
+                }
+            } else {
 #pragma unroll
-                for (int a = 0; a < WNN; a++)
+                for (int b = 0; b < WNM; b++) {
+                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        z[4 * a + e] = fmaf(acc[a][b][e], g.scale, bi[a][e]);
-                        top = fmaxf(top, z[4 * a + e]);
-                    }
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                    for (int a = 0; a < WNN; a++)
 #pragma unroll
-                for (int i = 0; i < 4 * WNN; i++) sum += __builtin_amdgcn_exp2f(z[i] - top);
-                sum += __shfl_xor(sum, 16, 64);
-                sum += __shfl_xor(sum, 32, 64);
-                const int gm = em + 16 * b + er;
-                if (eg == 0 && gm < M) g.stats[(long long)(4 * tile_nb + wn) * g.M + gm] = make_float2(top, sum);
+                        for (int e = 0; e < 4; e++)
+                            s4[e] += __builtin_amdgcn_exp2f(fmaf(acc[a][b][e], g.scale, cbias[a][e]) - ref[b]);
+                    part[b] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    high |= !(part[b] < 0x1p100f);
+                }
+            }
+            if (__any(high)) {
+#pragma unroll
+                for (int b = 0; b < WNM; b++) {
+                    float top = ref[b];
+#pragma unroll
+                    for (int a = 0; a < WNN; a++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            acc[a][b][e] = fmaf(acc[a][b][e], g.scale, cbias[a][e]);
+                            top = fmaxf(top, acc[a][b][e]);
+                        }
+                    float s = sum[b] * __builtin_amdgcn_exp2f(ref[b] - top);
+#pragma unroll
+                    for (int a = 0; a < WNN; a++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) s += __builtin_amdgcn_exp2f(acc[a][b][e] - top);
+                    sum[b] = s;
+                    ref[b] = top;
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < WNM; b++) sum[b] += part[b];
+            }
+            fresh = last_of_item;
+            if (last_of_item) {
+                // the four lanes of a row together, to slot (chunk, wave)
+#pragma unroll
+                for (int b = 0; b < WNM; b++) {
+                    float top = fmaxf(ref[b], __shfl_xor(ref[b], 16, 64));
+                    top = fmaxf(top, __shfl_xor(top, 32, 64));
+                    float s = sum[b] * __builtin_amdgcn_exp2f(ref[b] - top);
+                    s += __shfl_xor(s, 16, 64);
+                    s += __shfl_xor(s, 32, 64);
+                    const int gm = em + 16 * b + er;
+                    if (eg == 0 && gm < M) g.stats[(long long)(4 * (tile_nb % chunks) + wn) * g.M + gm] = make_float2(top, s);
+                }
             }
         } else if constexpr (EPI == GEMM_EPI_GATED_BWD) {
             // dh passes through LDS in fp32, one block at a time, so that a lane has 8 columns of a row:
@@ -543,8 +624,8 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
                     const int row = 8 * q + (el >> 3), ch = el & 7, gm = em + 16 * b + row, gn = en + 8 * ch;
                     const floatx4 x0 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch) ^ row));
                     const floatx4 x1 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch + 1) ^ row));
-                    const uint32_t gw[4] = {pg[b & 1][q].x, pg[b & 1][q].y, pg[b & 1][q].z, pg[b & 1][q].w};
-                    const uint32_t uw[4] = {pu[b & 1][q].x, pu[b & 1][q].y, pu[b & 1][q].z, pu[b & 1][q].w};
+                    const uint32_t gw[4] = {pg[b & 3][q].x, pg[b & 3][q].y, pg[b & 3][q].z, pg[b & 3][q].w};
+                    const uint32_t uw[4] = {pu[b & 3][q].x, pu[b & 3][q].y, pu[b & 3][q].z, pu[b & 3][q].w};
                     float dg[8], du[8];
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
@@ -564,7 +645,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
                         store_nt16(dst + N, &ou);
                     }
                 }
-                if (b < 6) load_pre(b + 2);
+                if (b < 4) load_pre(b + 4);
                 wave_lds_fence();
             }
         } else if constexpr (GATED) {
@@ -631,7 +712,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
                     for (int a = 0; a < WNN; a++)
 #pragma unroll
                         for (int e = 0; e < 4; e++)
-                            acc[a][b][e] = gp * __builtin_amdgcn_exp2f(fmaf(acc[a][b][e], g.scale, bi[a][e]) - lse);
+                            acc[a][b][e] = gp * __builtin_amdgcn_exp2f(fmaf(acc[a][b][e], g.scale, cbias[a][e]) - lse);
                     if (__any((unsigned)label < 64u)) {
 #pragma unroll
                         for (int a = 0; a < WNN; a++)
@@ -639,8 +720,10 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
                             for (int e = 0; e < 4; e++)
                                 if (label == 16 * a + 4 * eg + e) acc[a][b][e] -= gr;
                     }
+                    if (g.col_partial != nullptr) {
 #pragma unroll
-                    for (int a = 0; a < WNN; a++) cs[a] += acc[a][b];
+                        for (int a = 0; a < WNN; a++) cs[a] += acc[a][b];
+                    }
                 }
                 if (g.col_partial != nullptr) {
 #pragma unroll
@@ -657,6 +740,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
                     }
                 }
             }
+            const float factor = DIRECT ? g.scale * ((const float*)g.rows)[1] : 0.f;
             // bf16, 32 rows (two blocks) at a time: 16-byte chunk c (of 8) of row r at c ^ (r & 7)
 #pragma unroll
             for (int rd = 0; rd < WNM / 2; rd++)
@@ -667,6 +751,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
 #pragma unroll
                         for (int a = 0; a < WNN; a++) {
                             floatx4 v = acc[a][2 * rd + bb];
+                            if constexpr (DIRECT) v *= factor;
                             if (out == 1) {
 #pragma unroll
                                 for (int e = 0; e < 4; e++) v[e] = silu(v[e] + bi[a][e]);
@@ -727,7 +812,7 @@ template <int LAYOUT, int EPI, bool COLSUM>
 static hipError_t wide_launch(const GemmArgs& g, hipStream_t s) {
     // NN / NT: one workgroup per CU (those without a tile end at once); TN: one per (split, tile)
     const int items = g.mblocks * g.nblocks * g.splits;
-    const int gx = LAYOUT == GEMM_TN ? XCDS * ((items + XCDS - 1) / XCDS) : WIDE_WORKGROUPS;
+    const int gx = LAYOUT == GEMM_TN && EPI != GEMM_EPI_ROWS_DIRECT ? XCDS * ((items + XCDS - 1) / XCDS) : WIDE_WORKGROUPS;
     gemm_wide_kernel<LAYOUT, EPI, COLSUM><<<gx, 512, 0, s>>>(g);
     return hipGetLastError();
 }

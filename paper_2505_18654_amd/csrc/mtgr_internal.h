@@ -128,9 +128,10 @@ constexpr int GEMM_NN = 0, GEMM_NT = 1, GEMM_TN = 2;
 constexpr int GEMM_EPI_NONE = 0, GEMM_EPI_BIAS_SILU = 1, GEMM_EPI_BIAS_RESIDUAL = 2;
 // Epilogues of gemm_wide.h alone (ffn.hip, softmax_loss.hip): C = acc + R; the gated products; softmax
 // statistics and gradient of a class tile; fp32 partials that add up over calls; a weight gradient
-// over rows counted on the device.
+// over rows counted on the device, as fp32 partials or finished; fp32 partials of an NN or NT product.
 constexpr int GEMM_EPI_RESIDUAL = 3, GEMM_EPI_GATED = 4, GEMM_EPI_GATED_SAVE = 5, GEMM_EPI_GATED_BWD = 6,
-              GEMM_EPI_SM_STATS = 7, GEMM_EPI_SM_GRAD = 8, GEMM_EPI_ACC = 9, GEMM_EPI_ROWS = 10;
+              GEMM_EPI_SM_STATS = 7, GEMM_EPI_SM_GRAD = 8, GEMM_EPI_ACC = 9, GEMM_EPI_ROWS = 10, GEMM_EPI_ROWS_DIRECT = 11,
+              GEMM_EPI_PART = 12;
 struct GemmArgs {
     int layout, epilogue;
     long long M, N, K;
@@ -157,8 +158,8 @@ struct GemmArgs {
     int class0;               // first class of the piece
     int group_m;              // m blocks that an XCD's workgroups share
     int accumulate;           // ACC: add to the partials of the calls before
-    float scale;              // z = scale acc + bias, in units of log 2
-    float2* stats;            // SM_STATS: [4 nblocks][M] (maximum, sum) per row and 64 classes
+    float scale;              // z = scale acc + bias, in units of log 2; ROWS_DIRECT: C = scale max |g| acc
+    float2* stats;            // SM_STATS: [4 chunks][M] (reference, sum) per row and wave
     const int4* row_info;     // SM_GRAD: per row (lse, gradient of its loss, label, factor 2^-low of lse), whole m blocks
     float* col_partial;       // SM_GRAD: [2 mblocks][N] column sums, or NULL
 };
@@ -168,6 +169,7 @@ void gemm_plan(GemmArgs* g);
 size_t gemm_workspace_bytes(int layout, long long M, long long N, long long K);
 hipError_t launch_gemm_bf16(const GemmArgs& g, hipStream_t s);
 hipError_t launch_gemm_wide(const GemmArgs& g, hipStream_t s);      // the products with g.wide
+hipError_t launch_split_reduce(const GemmArgs& g, hipStream_t s);   // C and colsum from a TN product's partials
 constexpr int WIDE_WORKGROUPS = 256;                                   // of its persistent NN / NT form: one per CU
 
 // Elementwise out = a + b (bf16 or fp32) on [rows, cols] with row strides.
@@ -203,8 +205,13 @@ struct FfnArgs {
     void *dx, *dw_in, *dw_out;
     long long ld_x, ld_win, ld_wout, ld_y, ld_r, ld_pre, ld_h;
 };
-hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t s);
-hipError_t launch_ffn_rows(const FfnArgs& a, hipStream_t s);      // its form for few tokens (ffn_rows.hip)
+size_t ffn_fwd_workspace_bytes(long long T, int d, int f, bool save);
+hipError_t launch_ffn_fwd(const FfnArgs& a, void* workspace, hipStream_t s);
+// Its two products for few tokens (ffn_rows.hip), of so many columns per workgroup.
+constexpr int FFN_HIDDEN_COLUMNS = 32, FFN_OUT_COLUMNS = 32;
+bool ffn_rows_fit(long long T, int N, int columns);
+hipError_t launch_ffn_rows_hidden(const FfnArgs& a, hipStream_t s);
+hipError_t launch_ffn_rows_out(const FfnArgs& a, hipStream_t s);
 size_t ffn_bwd_workspace_bytes(long long T, int d, int f);
 hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s);
 

@@ -8,9 +8,10 @@
 // the products' cost follows their number, which stays on the device (no synchronisation): the grids are
 // laid out for N rows and the kernels stop at the count.
 //
-// Forward: x W^T on the matrix cores (gemm_wide.h), whose epilogue leaves the maximum and the sum of
-// exponentials of every row and 64 classes; a second kernel joins them.  2 n V d operations; written are
-// 8 bytes per row and 64 classes, a sixteenth of the logits in bf16.
+// Forward: x W^T on the matrix cores (gemm_wide.h).  A workgroup walks class tiles of its rows, and every lane
+// keeps a reference and a sum of exponentials for the columns that it saw of a row; a second kernel joins
+// them.  2 n V d operations; written are at most 8 bytes per row and 64 classes, a sixteenth of the logits in
+// bf16.
 // Backward, per piece of classes: x W^T again, its epilogue turning the products into dz (rounded to bf16
 // as operand of the next two products; the bias gradient is summed from dz before that rounding), then
 // dx += dz W (fp32, over the pieces) and the piece's dW = dz^T x.  6 n V d operations.  dz is kept divided by
@@ -31,7 +32,7 @@ struct SmPlan {
     int piece;                // classes per piece, a multiple of 256
     int pieces;
     int vpad;                 // V rounded up to whole tiles
-    size_t rows /* their count, the largest |g| */, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
+    size_t rows /* their count, the largest |g| */, counts, tops, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -55,6 +56,8 @@ SmPlan sm_plan(long long N, int V, int d, bool backward) {
         return here;
     };
     p.rows = take(256);
+    p.counts = take(sizeof(int) * mblocks);
+    p.tops = take(sizeof(float) * mblocks);
     p.index = take(sizeof(int) * npad);
     p.bias = take(sizeof(float) * p.vpad);
     p.xc = take((size_t)npad * d * 2);
@@ -80,24 +83,49 @@ __device__ __forceinline__ int label_of(const void* targets, long long i, int V)
     return t >= 0 && t < V ? (int)t : -1;
 }
 
-// Gathers the rows with a label (index[k] = row, xc[k] = x[row]) in order, counts them, and finishes the
-// rows without one: loss = lse = 0 (forward), dx = 0 (backward).  A workgroup has 256 rows and counts the
-// labels before them itself.  The last workgroups write the padded class bias, in units of log 2.
+// Labels of every 256 rows, their largest |g| (backward), and the padded class bias in units of log 2 (the last
+// workgroups).
 template <class T, bool BWD>
-__global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* rows, int* index, uint16_t* xc,
-                                                       float* bias2, int4* info, int vpad, int row_blocks) {
+__global__ __launch_bounds__(256) void sm_count_kernel(SoftmaxLossArgs a, int* counts, float* tops, float* bias2, int vpad,
+                                                       int row_blocks) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     if ((int)blockIdx.x >= row_blocks) {
-        const int c = ((int)blockIdx.x - row_blocks) * 1024 + tid;
+        const int c = ((int)blockIdx.x - row_blocks) * 256 + tid;
         if (c < vpad) bias2[c] = c >= a.V ? -__builtin_inff() : a.bias ? a.bias[c] * LOG2E : 0.f;
         return;
     }
+    __shared__ int n[4];
+    __shared__ float top[4];
+    const long long r = (long long)blockIdx.x * ROWS_PER_BLOCK + tid;
+    const bool on = r < a.N && label_of<T>(a.targets, r, a.V) >= 0;
+    float g = BWD && on ? fabsf(a.dloss[r]) : 0.f;
+    if (BWD) {
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) g = fmaxf(g, __shfl_xor(g, o, 64));
+    }
+    const int k = __popcll(__ballot(on));
+    if (lane == 0) {
+        n[w] = k;
+        top[w] = g;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        counts[blockIdx.x] = n[0] + n[1] + n[2] + n[3];
+        if (BWD) tops[blockIdx.x] = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    }
+}
+
+// Gathers the rows with a label (index[k] = row, xc[k] = x[row]) in order, counts them, and finishes the
+// rows without one: loss = lse = 0 (forward), dx = 0 (backward).  A workgroup has 256 rows.
+template <class T, bool BWD>
+__global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* rows, const int* block_counts,
+                                                       const float* block_tops, int* index, uint16_t* xc, int4* info) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, row_blocks = gridDim.x;
     __shared__ int counts[16], own[4], list[ROWS_PER_BLOCK], off[ROWS_PER_BLOCK];
     __shared__ float tops[16];
     const long long r0 = (long long)blockIdx.x * ROWS_PER_BLOCK;
     int before = 0;
-#pragma unroll 8
-    for (long long i = tid; i < r0; i += 1024) before += label_of<T>(a.targets, i, a.V) >= 0;
+    for (int i = tid; i < (int)blockIdx.x; i += 1024) before += block_counts[i];
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) before += __shfl_xor(before, o, 64);
     if (lane == 0) counts[w] = before;
@@ -154,9 +182,7 @@ __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* r
         const int total = before + n;
         if (BWD) {
             float top = 0.f;
-#pragma unroll 4
-            for (long long i = tid; i < a.N; i += 1024)
-                if (label_of<T>(a.targets, i, a.V) >= 0) top = fmaxf(top, fabsf(a.dloss[i]));
+            for (int i = tid; i < row_blocks; i += 1024) top = fmaxf(top, block_tops[i]);
 #pragma unroll
             for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
             if (lane == 0) tops[w] = top;
@@ -185,8 +211,9 @@ __device__ __forceinline__ float2 join(float2 p, float2 q) {
 template <class T>
 __global__ __launch_bounds__(1024) void sm_join_kernel(SoftmaxLossArgs a, const int* rows, const int* index,
                                                        const uint16_t* xc, const float* bias2, const float2* stats,
-                                                       int parts, float2* running, bool first, bool last) {
+                                                       int nblocks, float2* running, bool first, bool last) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, count = *rows;
+    const int parts = 4 * stat_chunks((count + WBM - 1) / WBM, nblocks);
     const int r0 = (int)blockIdx.x * 16;
     if (r0 >= count) return;
     __shared__ float2 part[16][16];
@@ -280,13 +307,19 @@ __global__ __launch_bounds__(256) void sm_dw_kernel(SoftmaxLossArgs a, const int
 
 template <bool BWD>
 hipError_t launch_rows(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, hipStream_t s) {
-    const int rb = (int)((a.N + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK), bb = (p.vpad + 1023) / 1024;
+    const int rb = (int)((a.N + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK), bb = p.vpad / 256;
+    int* counts = (int*)(ws + p.counts);
+    float* tops = (float*)(ws + p.tops);
     int *rows = (int*)(ws + p.rows), *index = (int*)(ws + p.index);
     uint16_t* xc = (uint16_t*)(ws + p.xc);
     float* bias2 = (float*)(ws + p.bias);
     int4* info = (int4*)(ws + p.info);
-    if (a.targets64) sm_rows_kernel<int64_t, BWD><<<rb + bb, 1024, 0, s>>>(a, rows, index, xc, bias2, info, p.vpad, rb);
-    else sm_rows_kernel<int, BWD><<<rb + bb, 1024, 0, s>>>(a, rows, index, xc, bias2, info, p.vpad, rb);
+    if (a.targets64) sm_count_kernel<int64_t, BWD><<<rb + bb, 256, 0, s>>>(a, counts, tops, bias2, p.vpad, rb);
+    else sm_count_kernel<int, BWD><<<rb + bb, 256, 0, s>>>(a, counts, tops, bias2, p.vpad, rb);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (a.targets64) sm_rows_kernel<int64_t, BWD><<<rb, 1024, 0, s>>>(a, rows, counts, tops, index, xc, info);
+    else sm_rows_kernel<int, BWD><<<rb, 1024, 0, s>>>(a, rows, counts, tops, index, xc, info);
     return hipGetLastError();
 }
 
@@ -334,8 +367,8 @@ hipError_t launch_softmax_loss_fwd(const SoftmaxLossArgs& a, void* workspace, hi
         const uint16_t* xc = (const uint16_t*)(ws + p.xc);
         const float* bias2 = (const float*)(ws + p.bias);
         float2* running = (float2*)(ws + p.running);
-        if (a.targets64) sm_join_kernel<int64_t><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, 4 * g.nblocks, running, first, last);
-        else sm_join_kernel<int><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, 4 * g.nblocks, running, first, last);
+        if (a.targets64) sm_join_kernel<int64_t><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, g.nblocks, running, first, last);
+        else sm_join_kernel<int><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, g.nblocks, running, first, last);
         e = hipGetLastError();
     }
     return e;
@@ -395,9 +428,16 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         w.nblocks = x.nblocks;
         const long long nks = (a.N + WBK - 1) / WBK;
         w.splits = (int)std::max(1ll, std::min({256ll / (w.mblocks * w.nblocks), nks / 8, 64ll}));
-        if ((e = wide_launch<GEMM_TN, GEMM_EPI_ROWS, false>(w, s)) != hipSuccess) break;
-        const int sums = (int)std::min(((long long)nv * a.d / 4 + 255) / 256, 8192ll);
+        w.scale = a.scale;
+        w.C = (uint16_t*)a.dw + v0 * a.ld_w;
+        w.ldc = a.ld_w;
+        // (without a split the sums are finished in place)
+        const bool direct = w.splits == 1;
+        e = direct ? wide_launch<GEMM_TN, GEMM_EPI_ROWS_DIRECT, false>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_ROWS, false>(w, s);
+        if (e != hipSuccess) break;
+        const int sums = direct ? 0 : (int)std::min(((long long)nv * a.d / 4 + 255) / 256, 8192ll);
         const int cols = a.dbias ? (nv + 255) / 256 : 0;
+        if (sums + cols == 0) continue;
         sm_dw_kernel<<<sums + cols, 256, 0, s>>>(a, rows, w.partial, w.splits, v0, nv, g.col_partial, (int)g.N, sums);
         e = hipGetLastError();
     }

@@ -37,6 +37,7 @@ MTGR_VALIDATE_SCRATCH_BYTES = 64
 MTGR_NOALLOC_SCRATCH_BYTES = 16 * 1024 * 1024
 MTGR_GEMM_NN, MTGR_GEMM_NT, MTGR_GEMM_TN = 0, 1, 2
 MTGR_GEMM_EPI_NONE, MTGR_GEMM_EPI_BIAS_SILU, MTGR_GEMM_EPI_BIAS_RESIDUAL = 0, 1, 2
+MTGR_FFN_SERVING, MTGR_FFN_BACKWARD, MTGR_FFN_TRAINING = 0, 1, 2
 MTGR_EMB_KEY_EMPTY = 0xFFFFFFFFFFFFFFFF
 MTGR_EMB_KEY_DELETED = 0xFFFFFFFFFFFFFFFE
 MTGR_EMB_STATE_WORDS = 8
@@ -439,9 +440,9 @@ def mtgr_embedding_rehash(src, dst, stream=None) -> None:
 
 # ------------------------------------------------------------------ feed-forward block, dropout, softmax loss
 
-def mtgr_gated_ffn_workspace_size(problem: GatedFfnProblem, backward: bool = False) -> int:
+def mtgr_gated_ffn_workspace_size(problem: GatedFfnProblem, which: int = MTGR_FFN_SERVING) -> int:
     out = ctypes.c_size_t(0)
-    _check(lib().mtgr_gated_ffn_workspace_size(ctypes.byref(problem), int(backward), ctypes.byref(out)))
+    _check(lib().mtgr_gated_ffn_workspace_size(ctypes.byref(problem), int(which), ctypes.byref(out)))
     return int(out.value)
 
 

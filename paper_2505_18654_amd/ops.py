@@ -355,8 +355,9 @@ def gated_ffn_problem(tokens: int, dim: int, hidden: int, ld_x=None, ld_w_in=Non
 
 
 def gated_ffn_workspace(tokens: int, dim: int, hidden: int, device="cuda", backward: bool = False) -> torch.Tensor:
-    """A workspace for gated_ffn_fwd (serving) or gated_ffn_bwd of up to `tokens` tokens."""
-    n = hstu.mtgr_gated_ffn_workspace_size(gated_ffn_problem(tokens, dim, hidden), backward)
+    """A workspace for gated_ffn_fwd (with save or without) or gated_ffn_bwd of these sizes."""
+    n = hstu.mtgr_gated_ffn_workspace_size(gated_ffn_problem(tokens, dim, hidden),
+                                           hstu.MTGR_FFN_BACKWARD if backward else hstu.MTGR_FFN_SERVING)
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
@@ -373,11 +374,9 @@ def gated_ffn_fwd(x, w_in, w_out, residual=None, save: bool = False, out=None, w
     p = gated_ffn_problem(T, d, f, _matrix("x", x, (T, d), bf), _matrix("w_in", w_in, (d, 2 * f), bf),
                           _matrix("w_out", w_out, (f, d), bf), _matrix("out", out, (T, d), bf),
                           _matrix("residual", residual, (T, d), bf) if residual is not None else None)
-    n = 0
-    if not save:
-        workspace = _scratch(workspace, hstu.mtgr_gated_ffn_workspace_size(p), x.device)
-        n = workspace.numel()
-    hstu.mtgr_gated_ffn_fwd(p, x, w_in, w_out, residual, out, pre, h, None if save else workspace, n)
+    need = hstu.mtgr_gated_ffn_workspace_size(p, hstu.MTGR_FFN_TRAINING if save else hstu.MTGR_FFN_SERVING)
+    workspace = _scratch(workspace, need, x.device)
+    hstu.mtgr_gated_ffn_fwd(p, x, w_in, w_out, residual, out, pre, h, workspace, workspace.numel())
     return (out, pre, h) if save else out
 
 
@@ -393,7 +392,7 @@ def gated_ffn_bwd(dy, x, pre, h, w_in, w_out, grads=None, workspace=None):
     _matrix("dx", dx, (T, d), bf, p.ld_x)
     _matrix("dw_in", dw_in, (d, 2 * f), bf, p.ld_w_in)
     _matrix("dw_out", dw_out, (f, d), bf, p.ld_w_out)
-    workspace = _scratch(workspace, hstu.mtgr_gated_ffn_workspace_size(p, True), x.device)
+    workspace = _scratch(workspace, hstu.mtgr_gated_ffn_workspace_size(p, hstu.MTGR_FFN_BACKWARD), x.device)
     hstu.mtgr_gated_ffn_bwd(p, dy, x, pre, h, w_in, w_out, dx, dw_in, dw_out, workspace, workspace.numel())
     return dx, dw_in, dw_out
 

@@ -77,7 +77,7 @@ def test_ffn_backward_refuses_each_matrix(name):
 
 
 def test_ffn_backward_workspace():
-    need = hstu.mtgr_gated_ffn_workspace_size(ffn(), True)
+    need = hstu.mtgr_gated_ffn_workspace_size(ffn(), hstu.MTGR_FFN_BACKWARD)
     assert need >= 100 * 2 * 96 * 2
     assert status_of(ffn_bwd, ffn(), workspace_bytes=need - 1) == SMALL
     assert status_of(ffn_bwd, ffn(), workspace=None) == NULL
@@ -90,7 +90,12 @@ def test_ffn_null_problem_and_empty():
     assert L.mtgr_gated_ffn_workspace_size(ctypes.byref(ffn()), 0, None) == NULL
     assert L.mtgr_gated_ffn_fwd(None, *[None] * 8, 0, None) == NULL
     assert L.mtgr_gated_ffn_bwd(None, *[None] * 10, 0, None) == NULL
+    assert L.mtgr_gated_ffn_workspace_size(ctypes.byref(ffn()), 3, ctypes.byref(n)) == INVALID
     assert hstu.mtgr_gated_ffn_workspace_size(ffn(tokens=0)) == 0
+    for T in (1, 100, 700, 5000, 70000):                 # the forward that keeps h needs no more than serving
+        p = ffn(tokens=T, dim=512, hidden=1408)
+        keep = hstu.mtgr_gated_ffn_workspace_size(p, hstu.MTGR_FFN_TRAINING)
+        assert keep <= hstu.mtgr_gated_ffn_workspace_size(p) - 2 * T * 1408
     ffn_fwd(ffn(tokens=0), x=None, w_in=None, w_out=None, y=None, workspace=None, workspace_bytes=0)
 
 
