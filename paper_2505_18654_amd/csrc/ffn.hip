@@ -15,63 +15,6 @@ namespace mtgr {
 
 namespace {
 
-// Tiles and K splits of a product, and its kernel: 256 x 256 tiles, one workgroup per CU, or 128 x 128 tiles,
-// two per CU.  Whichever is estimated to end first: rounds of workgroups that fill the chip, each of its k steps
-// of 64 and a start and an end, and with K splits their fp32 partials, written and read by another kernel.
-// The figures are measured ones (T = 312 .. 69,563, d = 256 .. 1024, f = 704 .. 2816).
-struct Tiles {
-    bool mid;
-    int mblocks, nblocks, splits;
-    double us;
-};
-
-Tiles tiles_of(bool mid, long long M, long long N, long long K, int n_factor, int splits, bool partials) {
-    Tiles t{};
-    t.mid = mid;
-    const int side = mid ? MBM : WBM;
-    t.mblocks = (int)((M + side - 1) / side);
-    t.nblocks = (int)((N + side / n_factor - 1) / (side / n_factor));
-    t.splits = splits;
-    const long long steps = ((K + WBK - 1) / WBK + splits - 1) / splits, slots = mid ? MID_WORKGROUPS : WIDE_WORKGROUPS;
-    const long long items = (long long)t.mblocks * t.nblocks * splits, rounds = (items + slots - 1) / slots;
-    t.us = rounds * (mid ? 4.0 + (items > WIDE_WORKGROUPS ? 1.0 : 0.8) * steps : 7.0 + 1.3 * steps);
-    if (partials) t.us += 4.0 + (double)splits * M * N * 8 / 8e6;
-    return t;
-}
-
-Tiles plan(long long M, long long N, long long K, int n_factor) {
-    const Tiles wide = tiles_of(false, M, N, K, n_factor, 1, false), mid = tiles_of(true, M, N, K, n_factor, 1, false);
-    return mid.us < wide.us ? mid : wide;
-}
-
-// The same with K splits of the 128 x 128 tiles.
-Tiles plan_deep(long long M, long long N, long long K) {
-    Tiles best = plan(M, N, K, 1);
-    const long long most = std::min(16ll, (K + WBK - 1) / WBK / 4);
-    for (int s = 2; s <= most; s++) {
-        const Tiles t = tiles_of(true, M, N, K, 1, s, true);
-        if (t.us < best.us) best = t;
-    }
-    return best;
-}
-
-// A weight gradient (K = tokens) is always split.
-Tiles plan_split(long long M, long long N, long long K) {
-    Tiles best{};
-    best.us = 1e30;
-    const long long most = std::min(64ll, std::max(1ll, (K + WBK - 1) / WBK / 4));
-    for (int mid = 0; mid < 2; mid++)
-        for (int s = 1; s <= most; s++) {
-            const Tiles t = tiles_of(mid, M, N, K, 1, s, true);
-            if (t.us < best.us) best = t;
-        }
-    return best;
-}
-
-size_t partial_bytes(const Tiles& t, long long M, long long N) {
-    return t.splits > 1 ? (size_t)t.splits * M * N * sizeof(float) : 0;
-}
-
 // out = sum of the K splits' partials (+ residual), rounded once.
 __global__ __launch_bounds__(256) void ffn_sum_kernel(const float* partial, int splits, long long rows, int cols, uint16_t* out,
                                                       long long ld_out, const uint16_t* residual, long long ld_r) {
@@ -90,16 +33,6 @@ __global__ __launch_bounds__(256) void ffn_sum_kernel(const float* partial, int 
         }
         *(uint2*)(out + r * ld_out + c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
     }
-}
-
-void set_tiles(GemmArgs* g, const Tiles& t) {
-    g->mblocks = t.mblocks;
-    g->nblocks = t.nblocks;
-    g->splits = t.splits;
-    g->ks_per_split = (int)(((g->K + WBK - 1) / WBK + t.splits - 1) / t.splits);
-    // (the 256 x 256 kernel wants every split to have k)
-    if (!t.mid) g->splits = (int)(((g->K + WBK - 1) / WBK + g->ks_per_split - 1) / g->ks_per_split);
-    g->wide = !t.mid;
 }
 
 GemmArgs product(int layout, long long M, long long N, long long K, const void* A, long long lda, const void* B,
@@ -182,7 +115,7 @@ hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
 size_t ffn_bwd_workspace_bytes(long long T, int d, int f) {
     const size_t weights = (size_t)d * f * sizeof(float);
     return align256((size_t)T * 2 * f * 2) +
-           std::max({plan_split(d, 2ll * f, T).splits * 2 * weights, plan_split(f, d, T).splits * weights,
+           std::max({plan_split(d, 2ll * f, T, true).splits * 2 * weights, plan_split(f, d, T, true).splits * weights,
                      partial_bytes(plan_deep(T, d, 2ll * f), T, d)});
 }
 
@@ -204,7 +137,7 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
     e = deep_product<GEMM_NT>(product(GEMM_NT, a.T, a.d, f2, dpre, f2, a.w_in, a.ld_win, a.dx, a.ld_x), partial, s);
     if (e != hipSuccess) return e;
     auto gradient = [&](GemmArgs w) {
-        const Tiles q = plan_split(w.M, w.N, w.K);
+        const Tiles q = plan_split(w.M, w.N, w.K, true);
         set_tiles(&w, q);
         w.partial = partial;
         const hipError_t r = q.mid ? mid_launch<GEMM_TN, GEMM_EPI_NONE>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_NONE, false>(w, s);

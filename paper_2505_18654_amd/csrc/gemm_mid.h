@@ -329,4 +329,77 @@ static hipError_t mid_launch(const GemmArgs& g, hipStream_t s) {
     return hipGetLastError();
 }
 
+// ---------------------------------------------------------------- which tiles
+
+// Tiles and K splits of a product, and its kernel: 256 x 256 tiles, one workgroup per CU, or 128 x 128 tiles,
+// two per CU.  Whichever is estimated to end first: rounds of workgroups that fill the chip, each of its k steps
+// of 64 and a start and an end, and with K splits their fp32 partials, written and read by another kernel.
+// The figures are measured ones (T = 312 .. 69,563, d = 256 .. 1024, f = 704 .. 2816).
+struct Tiles {
+    bool mid;
+    int mblocks, nblocks, splits;
+    double us;
+};
+
+static inline Tiles tiles_of(bool mid, long long M, long long N, long long K, int n_factor, int splits, bool partials) {
+    Tiles t{};
+    t.mid = mid;
+    const int side = mid ? MBM : WBM;
+    t.mblocks = (int)((M + side - 1) / side);
+    t.nblocks = (int)((N + side / n_factor - 1) / (side / n_factor));
+    t.splits = splits;
+    const long long steps = ((K + WBK - 1) / WBK + splits - 1) / splits, slots = mid ? MID_WORKGROUPS : WIDE_WORKGROUPS;
+    const long long items = (long long)t.mblocks * t.nblocks * splits, rounds = (items + slots - 1) / slots;
+    t.us = rounds * (mid ? 4.0 + (items > WIDE_WORKGROUPS ? 1.0 : 0.8) * steps : 7.0 + 1.3 * steps);
+    if (partials) t.us += 4.0 + (double)splits * M * N * 8 / 8e6;
+    return t;
+}
+
+static inline Tiles plan(long long M, long long N, long long K, int n_factor) {
+    const Tiles wide = tiles_of(false, M, N, K, n_factor, 1, false), mid = tiles_of(true, M, N, K, n_factor, 1, false);
+    return mid.us < wide.us ? mid : wide;
+}
+
+// The same with K splits of the 128 x 128 tiles.
+static inline Tiles plan_deep(long long M, long long N, long long K) {
+    Tiles best = plan(M, N, K, 1);
+    const long long most = std::min(16ll, (K + WBK - 1) / WBK / 4);
+    if (best.us < 12.0) return best;              // (about what a split's start and end and its sum take)
+    for (int s = 2; s <= most; s++) {
+        const Tiles t = tiles_of(true, M, N, K, 1, s, true);
+        if (t.us < best.us) best = t;
+    }
+    return best;
+}
+
+// A product of fp32 partials, or (not `always`) one that 256 x 256 tiles without a split finish in place.
+static inline Tiles plan_split(long long M, long long N, long long K, bool always) {
+    static const int candidates[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+    Tiles best{};
+    best.us = 1e30;
+    const long long most = std::max(1ll, (K + WBK - 1) / WBK / 4);
+    for (int s : candidates) {
+        if (s > most) break;
+        for (int mid = 0; mid < 2; mid++) {
+            const Tiles t = tiles_of(mid, M, N, K, 1, s, always || mid || s > 1);
+            if (t.us < best.us) best = t;
+        }
+    }
+    return best;
+}
+
+static inline size_t partial_bytes(const Tiles& t, long long M, long long N) {
+    return t.splits > 1 ? (size_t)t.splits * M * N * sizeof(float) : 0;
+}
+
+static inline void set_tiles(GemmArgs* g, const Tiles& t) {
+    g->mblocks = t.mblocks;
+    g->nblocks = t.nblocks;
+    g->splits = t.splits;
+    g->ks_per_split = (int)(((g->K + WBK - 1) / WBK + t.splits - 1) / t.splits);
+    // (the 256 x 256 kernel wants every split to have k)
+    if (!t.mid) g->splits = (int)(((g->K + WBK - 1) / WBK + g->ks_per_split - 1) / g->ks_per_split);
+    g->wide = !t.mid;
+}
+
 }  // namespace mtgr

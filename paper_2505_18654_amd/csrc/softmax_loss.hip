@@ -17,7 +17,7 @@
 // dx += dz W (fp32, over the pieces) and the piece's dW = dz^T x.  6 n V d operations.  dz is kept divided by
 // the largest |g| of the rows, which multiplies the finished sums: under a mean the g are one number, whose
 // rounding error would be common to all labels' terms (-g), and a label's own term -1 is exact.
-#include "gemm_wide.h"
+#include "gemm_mid.h"
 
 namespace mtgr {
 
@@ -32,6 +32,8 @@ struct SmPlan {
     int piece;                // classes per piece, a multiple of 256
     int pieces;
     int vpad;                 // V rounded up to whole tiles
+    Tiles logits;             // of x W^T (forward and backward), dx and dW; which kernel
+    Tiles dx, dw;
     size_t rows /* their count, the largest |g| */, counts, tops, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
 };
 
@@ -49,6 +51,12 @@ SmPlan sm_plan(long long N, int V, int d, bool backward) {
     per = (blocks + p.pieces - 1) / p.pieces;     // pieces of equal size
     p.piece = (int)(per * WBN);
     p.vpad = (int)(blocks * WBN);
+    // The number of labels is not known here: x W^T is planned for all rows, dx and dW for half of them.
+    const long long half = (N + 1) / 2;
+    const Tiles lw = tiles_of(false, N, p.piece, d, 1, 1, false), lm = tiles_of(true, N, p.piece, d, 1, 1, false);
+    p.logits = lm.us < lw.us ? lm : lw;
+    p.dx = plan_split(half, d, p.piece, true);
+    p.dw = plan_split(p.piece, d, half, false);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -67,11 +75,11 @@ SmPlan sm_plan(long long N, int V, int d, bool backward) {
     } else {
         p.info = take(sizeof(int4) * npad);
         p.dz = take((size_t)N * p.piece * 2);
-        // fp32 partials of both products: one split, or as many as make at most 256 tiles
-        const size_t nblocks = (size_t)((d + WBN - 1) / WBN), tile = WBM * WBN * sizeof(float);
-        p.dxp = take(std::max<size_t>(mblocks * nblocks, 256) * tile);
-        p.dwp = take(std::max<size_t>(per * nblocks, 256) * tile);
-        p.colp = take((size_t)2 * mblocks * p.piece * sizeof(float));
+        // fp32 partials (of the wide dx kernel: one split, or as many as make at most 256 tiles)
+        const size_t tiles = (size_t)mblocks * ((d + WBN - 1) / WBN);
+        p.dxp = take(std::max<size_t>(std::max<size_t>(tiles, 256) * WBM * WBN, (size_t)p.dx.splits * N * d) * sizeof(float));
+        p.dwp = take((size_t)p.dw.splits * p.piece * d * sizeof(float));
+        p.colp = take((size_t)(p.logits.mid ? 4 : 2) * mblocks * p.piece * sizeof(float));
     }
     p.total = at;
     return p;
@@ -83,17 +91,17 @@ __device__ __forceinline__ int label_of(const void* targets, long long i, int V)
     return t >= 0 && t < V ? (int)t : -1;
 }
 
-// Labels of every 256 rows, their largest |g| (backward), and the padded class bias in units of log 2 (the last
-// workgroups).
+// The class bias in units of log 2, padded to whole tiles with classes that do not count.
+__device__ __forceinline__ void padded_bias(const SoftmaxLossArgs& a, float* bias2, int vpad, int c) {
+    if (c < vpad) bias2[c] = c >= a.V ? -__builtin_inff() : a.bias ? a.bias[c] * LOG2E : 0.f;
+}
+
+// Labels of every 256 rows, their largest |g| (backward), and the class bias (the last workgroups).
 template <class T, bool BWD>
 __global__ __launch_bounds__(256) void sm_count_kernel(SoftmaxLossArgs a, int* counts, float* tops, float* bias2, int vpad,
                                                        int row_blocks) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    if ((int)blockIdx.x >= row_blocks) {
-        const int c = ((int)blockIdx.x - row_blocks) * 256 + tid;
-        if (c < vpad) bias2[c] = c >= a.V ? -__builtin_inff() : a.bias ? a.bias[c] * LOG2E : 0.f;
-        return;
-    }
+    if ((int)blockIdx.x >= row_blocks) return padded_bias(a, bias2, vpad, ((int)blockIdx.x - row_blocks) * 256 + tid);
     __shared__ int n[4];
     __shared__ float top[4];
     const long long r = (long long)blockIdx.x * ROWS_PER_BLOCK + tid;
@@ -116,16 +124,41 @@ __global__ __launch_bounds__(256) void sm_count_kernel(SoftmaxLossArgs a, int* c
 }
 
 // Gathers the rows with a label (index[k] = row, xc[k] = x[row]) in order, counts them, and finishes the
-// rows without one: loss = lse = 0 (forward), dx = 0 (backward).  A workgroup has 256 rows.
-template <class T, bool BWD>
+// rows without one: loss = lse = 0 (forward), dx = 0 (backward).  A workgroup has 256 rows.  SCAN: the labels
+// before them, and the last workgroup's largest |g|, are counted here instead of by sm_count_kernel, and the
+// last workgroups write the class bias (up to SCAN_ROWS rows: at 6,418 rows the two kernels take 7 us, this
+// one 5; at 69,563 20 and 23, and 28 and 85 in the backward).
+constexpr int SCAN_ROWS = 8192;
+template <class T, bool BWD, bool SCAN>
 __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* rows, const int* block_counts,
-                                                       const float* block_tops, int* index, uint16_t* xc, int4* info) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, row_blocks = gridDim.x;
+                                                       const float* block_tops, int* index, uint16_t* xc, int4* info,
+                                                       float* bias2, int vpad, int row_blocks) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (SCAN && (int)blockIdx.x >= row_blocks)
+        return padded_bias(a, bias2, vpad, ((int)blockIdx.x - row_blocks) * 1024 + tid);
     __shared__ int counts[16], own[4], list[ROWS_PER_BLOCK], off[ROWS_PER_BLOCK];
     __shared__ float tops[16];
     const long long r0 = (long long)blockIdx.x * ROWS_PER_BLOCK;
+    const bool last = (int)blockIdx.x == row_blocks - 1;
+    float top = 0.f;                                     // the largest |g| of all rows (backward, last workgroup)
+    if (BWD && last) {
+        if (SCAN) {
+#pragma unroll 8
+            for (int i = tid; i < (int)a.N; i += 1024) {
+                const float g = fabsf(a.dloss[i]);
+                top = fmaxf(top, label_of<T>(a.targets, i, a.V) >= 0 ? g : 0.f);
+            }
+        } else {
+            for (int i = tid; i < row_blocks; i += 1024) top = fmaxf(top, block_tops[i]);
+        }
+    }
     int before = 0;
-    for (int i = tid; i < (int)blockIdx.x; i += 1024) before += block_counts[i];
+    if (SCAN) {
+#pragma unroll 8
+        for (int i = tid; i < (int)r0; i += 1024) before += label_of<T>(a.targets, i, a.V) >= 0;
+    } else {
+        for (int i = tid; i < (int)blockIdx.x; i += 1024) before += block_counts[i];
+    }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) before += __shfl_xor(before, o, 64);
     if (lane == 0) counts[w] = before;
@@ -178,11 +211,9 @@ __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* r
     if (BWD)
         for (int i = tid; i < (in_block - n) * ch; i += 1024)
             *(uint4*)((uint16_t*)a.dx + (r0 + off[i / ch]) * a.ld_x + 8 * (i % ch)) = make_uint4(0, 0, 0, 0);
-    if ((int)blockIdx.x == row_blocks - 1) {
+    if (last) {
         const int total = before + n;
         if (BWD) {
-            float top = 0.f;
-            for (int i = tid; i < row_blocks; i += 1024) top = fmaxf(top, block_tops[i]);
 #pragma unroll
             for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
             if (lane == 0) tops[w] = top;
@@ -211,9 +242,9 @@ __device__ __forceinline__ float2 join(float2 p, float2 q) {
 template <class T>
 __global__ __launch_bounds__(1024) void sm_join_kernel(SoftmaxLossArgs a, const int* rows, const int* index,
                                                        const uint16_t* xc, const float* bias2, const float2* stats,
-                                                       int nblocks, float2* running, bool first, bool last) {
+                                                       bool mid, int nblocks, float2* running, bool first, bool last) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, count = *rows;
-    const int parts = 4 * stat_chunks((count + WBM - 1) / WBM, nblocks);
+    const int parts = mid ? 2 * nblocks : 4 * stat_chunks((count + WBM - 1) / WBM, nblocks);
     const int r0 = (int)blockIdx.x * 16;
     if (r0 >= count) return;
     __shared__ float2 part[16][16];
@@ -256,10 +287,10 @@ __global__ __launch_bounds__(1024) void sm_join_kernel(SoftmaxLossArgs a, const 
 
 // dx of the rows with a label: the K splits' sums, scaled and rounded once.
 __global__ __launch_bounds__(256) void sm_dx_kernel(SoftmaxLossArgs a, const int* rows, const int* index,
-                                                    const float* partial) {
+                                                    const float* partial, int mid_splits) {
     const int count = *rows, ch = a.d / 8;
     const float factor = a.scale * ((const float*)rows)[1];
-    const int splits = acc_splits((count + WBM - 1) / WBM * ((a.d + WBN - 1) / WBN));
+    const int splits = mid_splits > 0 ? mid_splits : acc_splits((count + WBM - 1) / WBM * ((a.d + WBN - 1) / WBN));
     const long long per = (long long)count * a.d;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)count * ch;
          i += (long long)gridDim.x * 256) {
@@ -281,15 +312,16 @@ __global__ __launch_bounds__(256) void sm_dx_kernel(SoftmaxLossArgs a, const int
 // A piece's dW = scale sum of the K splits, rounded once; the last workgroups add up its bias gradient.
 __global__ __launch_bounds__(256) void sm_dw_kernel(SoftmaxLossArgs a, const int* rows, const float* partial,
                                                     int splits, int v0, int nv, const float* colp, int ld_col,
-                                                    int sum_blocks) {
+                                                    int row_tile, int sum_blocks) {
     if ((int)blockIdx.x >= sum_blocks) {
         const int c = ((int)blockIdx.x - sum_blocks) * 256 + threadIdx.x;
         if (c >= nv) return;
-        const int parts = 2 * ((*rows + WBM - 1) / WBM);
-        float s = 0.f;
+        const int parts = 2 * ((*rows + row_tile - 1) / row_tile);
+        // (in 64 bits: softmax sums and label counts cancel, and the parts are hundreds)
+        double s = 0.;
 #pragma unroll 8
         for (int p = 0; p < parts; p++) s += colp[(long long)p * ld_col + c];
-        a.dbias[v0 + c] = s * ((const float*)rows)[1];
+        a.dbias[v0 + c] = (float)(s * ((const float*)rows)[1]);
         return;
     }
     const int ch = a.d / 4;
@@ -307,20 +339,27 @@ __global__ __launch_bounds__(256) void sm_dw_kernel(SoftmaxLossArgs a, const int
 
 template <bool BWD>
 hipError_t launch_rows(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, hipStream_t s) {
-    const int rb = (int)((a.N + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK), bb = p.vpad / 256;
+    const int rb = (int)((a.N + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK);
     int* counts = (int*)(ws + p.counts);
     float* tops = (float*)(ws + p.tops);
     int *rows = (int*)(ws + p.rows), *index = (int*)(ws + p.index);
     uint16_t* xc = (uint16_t*)(ws + p.xc);
     float* bias2 = (float*)(ws + p.bias);
     int4* info = (int4*)(ws + p.info);
-    if (a.targets64) sm_count_kernel<int64_t, BWD><<<rb + bb, 256, 0, s>>>(a, counts, tops, bias2, p.vpad, rb);
-    else sm_count_kernel<int, BWD><<<rb + bb, 256, 0, s>>>(a, counts, tops, bias2, p.vpad, rb);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (a.targets64) sm_rows_kernel<int64_t, BWD><<<rb, 1024, 0, s>>>(a, rows, counts, tops, index, xc, info);
-    else sm_rows_kernel<int, BWD><<<rb, 1024, 0, s>>>(a, rows, counts, tops, index, xc, info);
-    return hipGetLastError();
+    auto launch = [&](auto type) {
+        typedef decltype(type) T;
+        if (a.N <= SCAN_ROWS) {
+            sm_rows_kernel<T, BWD, true><<<rb + (p.vpad + 1023) / 1024, 1024, 0, s>>>(a, rows, counts, tops, index, xc, info,
+                                                                                   bias2, p.vpad, rb);
+            return hipGetLastError();
+        }
+        sm_count_kernel<T, BWD><<<rb + p.vpad / 256, 256, 0, s>>>(a, counts, tops, bias2, p.vpad, rb);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        sm_rows_kernel<T, BWD, false><<<rb, 1024, 0, s>>>(a, rows, counts, tops, index, xc, info, bias2, p.vpad, rb);
+        return hipGetLastError();
+    };
+    return a.targets64 ? launch(int64_t{}) : launch(int{});
 }
 
 // x W^T of the piece at class v0.
@@ -340,8 +379,9 @@ GemmArgs logits_product(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, int
     g.b_rows = std::min(p.piece, a.V - v0);
     g.class0 = v0;
     g.group_m = GROUP_M;
-    g.mblocks = (int)((a.N + WBM - 1) / WBM);
-    g.nblocks = (int)(g.N / WBN);
+    const int side = p.logits.mid ? MBM : WBM;
+    g.mblocks = (int)((a.N + side - 1) / side);
+    g.nblocks = (g.b_rows + side - 1) / side;
     g.splits = 1;
     g.ks_per_split = (a.d + WBK - 1) / WBK;
     return g;
@@ -360,15 +400,16 @@ hipError_t launch_softmax_loss_fwd(const SoftmaxLossArgs& a, void* workspace, hi
     for (int i = 0; i < p.pieces && e == hipSuccess; i++) {
         GemmArgs g = logits_product(a, p, ws, i * p.piece);
         g.stats = (float2*)(ws + p.stats);
-        if ((e = wide_launch<GEMM_NT, GEMM_EPI_SM_STATS, false>(g, s)) != hipSuccess) break;
+        e = p.logits.mid ? mid_launch<GEMM_NT, GEMM_EPI_SM_STATS>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_SM_STATS, false>(g, s);
+        if (e != hipSuccess) break;
         const int blocks = (int)((a.N + 15) / 16);
         const bool first = i == 0, last = i == p.pieces - 1;
         const int *rows = (const int*)(ws + p.rows), *index = (const int*)(ws + p.index);
         const uint16_t* xc = (const uint16_t*)(ws + p.xc);
         const float* bias2 = (const float*)(ws + p.bias);
         float2* running = (float2*)(ws + p.running);
-        if (a.targets64) sm_join_kernel<int64_t><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, g.nblocks, running, first, last);
-        else sm_join_kernel<int><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, g.nblocks, running, first, last);
+        if (a.targets64) sm_join_kernel<int64_t><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, p.logits.mid, g.nblocks, running, first, last);
+        else sm_join_kernel<int><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, p.logits.mid, g.nblocks, running, first, last);
         e = hipGetLastError();
     }
     return e;
@@ -391,7 +432,8 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         g.ldc = p.piece;
         g.row_info = (const int4*)(ws + p.info);
         g.col_partial = a.dbias ? (float*)(ws + p.colp) : nullptr;
-        if ((e = wide_launch<GEMM_NT, GEMM_EPI_SM_GRAD, false>(g, s)) != hipSuccess) break;
+        e = p.logits.mid ? mid_launch<GEMM_NT, GEMM_EPI_SM_GRAD>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_SM_GRAD, false>(g, s);
+        if (e != hipSuccess) break;
 
         GemmArgs x{};                                    // dx += dz W
         x.layout = GEMM_NN;
@@ -406,12 +448,20 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         x.b_rows = nv;
         x.accumulate = i > 0;
         x.partial = (float*)(ws + p.dxp);
-        x.mblocks = g.mblocks;
-        x.nblocks = (a.d + WBN - 1) / WBN;
-        x.splits = 1;
-        const int xgrid = XCDS * ((std::max(x.mblocks * x.nblocks, 256) + XCDS - 1) / XCDS);
-        gemm_wide_kernel<GEMM_NN, GEMM_EPI_ACC, false><<<xgrid, 512, 0, s>>>(x);
-        if ((e = hipGetLastError()) != hipSuccess) break;
+        if (p.dx.mid) {
+            x.mblocks = (int)((a.N + MBM - 1) / MBM);
+            x.nblocks = (a.d + MBN - 1) / MBN;
+            x.splits = p.dx.splits;
+            e = mid_launch<GEMM_NN, GEMM_EPI_ACC>(x, s);
+        } else {
+            x.mblocks = (int)((a.N + WBM - 1) / WBM);
+            x.nblocks = (a.d + WBN - 1) / WBN;
+            x.splits = 1;
+            const int grid = XCDS * ((std::max(x.mblocks * x.nblocks, 256) + XCDS - 1) / XCDS);
+            gemm_wide_kernel<GEMM_NN, GEMM_EPI_ACC, false><<<grid, 512, 0, s>>>(x);
+            e = hipGetLastError();
+        }
+        if (e != hipSuccess) break;
 
         GemmArgs w{};                                    // the piece's dW = dz^T x
         w.layout = GEMM_TN;
@@ -424,26 +474,28 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         w.ldb = a.d;
         w.rows = rows;
         w.partial = (float*)(ws + p.dwp);
-        w.mblocks = (nv + WBM - 1) / WBM;
-        w.nblocks = x.nblocks;
-        const long long nks = (a.N + WBK - 1) / WBK;
-        w.splits = (int)std::max(1ll, std::min({256ll / (w.mblocks * w.nblocks), nks / 8, 64ll}));
+        w.splits = p.dw.splits;
         w.scale = a.scale;
         w.C = (uint16_t*)a.dw + v0 * a.ld_w;
         w.ldc = a.ld_w;
-        // (without a split the sums are finished in place)
-        const bool direct = w.splits == 1;
-        e = direct ? wide_launch<GEMM_TN, GEMM_EPI_ROWS_DIRECT, false>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_ROWS, false>(w, s);
+        const int side = p.dw.mid ? MBM : WBM;
+        w.mblocks = (nv + side - 1) / side;
+        w.nblocks = (a.d + side - 1) / side;
+        // (without a split the 256 x 256 tiles finish the sums in place)
+        const bool direct = w.splits == 1 && !p.dw.mid;
+        e = p.dw.mid ? mid_launch<GEMM_TN, GEMM_EPI_ROWS>(w, s)
+            : direct ? wide_launch<GEMM_TN, GEMM_EPI_ROWS_DIRECT, false>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_ROWS, false>(w, s);
         if (e != hipSuccess) break;
         const int sums = direct ? 0 : (int)std::min(((long long)nv * a.d / 4 + 255) / 256, 8192ll);
         const int cols = a.dbias ? (nv + 255) / 256 : 0;
         if (sums + cols == 0) continue;
-        sm_dw_kernel<<<sums + cols, 256, 0, s>>>(a, rows, w.partial, w.splits, v0, nv, g.col_partial, (int)g.N, sums);
+        sm_dw_kernel<<<sums + cols, 256, 0, s>>>(a, rows, w.partial, w.splits, v0, nv, g.col_partial, (int)g.N, p.logits.mid ? MBM : WBM, sums);
         e = hipGetLastError();
     }
     if (e != hipSuccess) return e;
     const int grid = (int)std::min((a.N * (a.d / 8) + 255) / 256, 8192ll);
-    sm_dx_kernel<<<grid, 256, 0, s>>>(a, rows, (const int*)(ws + p.index), (const float*)(ws + p.dxp));
+    sm_dx_kernel<<<grid, 256, 0, s>>>(a, rows, (const int*)(ws + p.index), (const float*)(ws + p.dxp),
+                                   p.dx.mid ? p.dx.splits : 0);
     return hipGetLastError();
 }
 

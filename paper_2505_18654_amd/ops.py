@@ -306,39 +306,44 @@ def add(a, b, out=None):
 
 # ------------------------------------------------------------------ feed-forward block, dropout, softmax loss
 
-def _matrix(name: str, t, shape, dtype, like=None) -> int:
-    """Checks a 2-D operand (shape, type, dense rows that do not overlap, the current device) and returns its
-    row stride; `like`: the strides that a gradient shares."""
-    if not isinstance(t, torch.Tensor) or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        got = f"{tuple(t.shape)} {t.dtype}" if isinstance(t, torch.Tensor) else type(t).__name__
-        raise ValueError(f"{name} is [{shape[0]}, {shape[1]}] of {dtype}, got {got}")
-    _on_device(name, t)
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+def _device() -> int:
+    """The current device; the operands below have to be on it (the stream is its current one)."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2     # (no tensor's device number)
+
+
+def _matrix(name: str, t, rows: int, cols: int, dtype, dev: int, like: Optional[int] = None) -> int:
+    """Checks a 2-D operand (shape, type, device, dense rows that do not overlap) and returns its row stride;
+    `like`: the row stride that a gradient shares with its primal."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != (rows, cols):
+        got = f"{list(t.shape)} {t.dtype}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise ValueError(f"{name} is [{rows}, {cols}] of {dtype}, got {got}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"the rows of {name} are not dense")
+    if rows <= 1:
+        ld = cols
+    elif ld < cols:
         raise ValueError(f"the rows of {name} overlap")
-    ld = _token_stride(t, shape[1])
     if like is not None and ld != like:
         raise ValueError(f"{name} must share the row stride of its primal")
     return ld
 
 
-def _vector(name: str, t, n: int, dtypes) -> None:
-    if not isinstance(t, torch.Tensor) or tuple(t.shape) != (n,) or t.dtype not in dtypes or not t.is_contiguous():
+def _vector(name: str, t, n: int, dtypes, dev: int) -> None:
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} is a dense [{n}] of {' or '.join(str(d) for d in dtypes)}")
-    _on_device(name, t)
-
-
-def _on_device(name: str, t) -> None:
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() != dev:
         raise ValueError(f"{name} is on {t.device}, not on the current device")
 
 
-def _scratch(workspace, need: int, device):
-    """The caller's workspace, or a new one of at least `need` bytes."""
+def _scratch(workspace, need: int, like) -> torch.Tensor:
+    """The caller's workspace, or a new one of at least `need` bytes beside the operand `like`."""
     if workspace is None:
-        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
-    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-        raise ValueError("a workspace is a dense uint8 tensor")
-    _on_device("workspace", workspace)
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
+    if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != like.get_device():
+        raise ValueError("a workspace is a dense uint8 tensor on the device of the operands")
     return workspace
 
 
@@ -366,16 +371,16 @@ def gated_ffn_fwd(x, w_in, w_out, residual=None, save: bool = False, out=None, w
     w_out [f, d]; d and f multiples of 32.  Returns y, or with save=True (y, pre [T, 2f], h [T, f]), the last two
     for gated_ffn_bwd."""
     (T, d), f = _two_dims("x", x), _two_dims("w_out", w_out)[0]
-    bf = torch.bfloat16
+    bf, dev = torch.bfloat16, _device()
     if out is None:
         out = torch.empty((T, d), dtype=bf, device=x.device)
     pre = torch.empty((T, 2 * f), dtype=bf, device=x.device) if save else None
     h = torch.empty((T, f), dtype=bf, device=x.device) if save else None
-    p = gated_ffn_problem(T, d, f, _matrix("x", x, (T, d), bf), _matrix("w_in", w_in, (d, 2 * f), bf),
-                          _matrix("w_out", w_out, (f, d), bf), _matrix("out", out, (T, d), bf),
-                          _matrix("residual", residual, (T, d), bf) if residual is not None else None)
+    p = hstu.GatedFfnProblem(T, d, f, _matrix("x", x, T, d, bf, dev), _matrix("w_in", w_in, d, 2 * f, bf, dev),
+                             _matrix("w_out", w_out, f, d, bf, dev), _matrix("out", out, T, d, bf, dev),
+                             _matrix("residual", residual, T, d, bf, dev) if residual is not None else d, 2 * f, f)
     need = hstu.mtgr_gated_ffn_workspace_size(p, hstu.MTGR_FFN_TRAINING if save else hstu.MTGR_FFN_SERVING)
-    workspace = _scratch(workspace, need, x.device)
+    workspace = _scratch(workspace, need, x)
     hstu.mtgr_gated_ffn_fwd(p, x, w_in, w_out, residual, out, pre, h, workspace, workspace.numel())
     return (out, pre, h) if save else out
 
@@ -384,15 +389,15 @@ def gated_ffn_bwd(dy, x, pre, h, w_in, w_out, grads=None, workspace=None):
     """Gradients of gated_ffn_fwd: (dx, dw_in, dw_out), in the layouts of x, w_in and w_out (`grads`: the tensors to
     write).  A residual's gradient is dy itself."""
     (T, d), f = _two_dims("x", x), _two_dims("w_out", w_out)[0]
-    bf = torch.bfloat16
+    bf, dev = torch.bfloat16, _device()
     dx, dw_in, dw_out = grads if grads is not None else (_like_layout(t) for t in (x, w_in, w_out))
-    p = gated_ffn_problem(T, d, f, _matrix("x", x, (T, d), bf), _matrix("w_in", w_in, (d, 2 * f), bf),
-                          _matrix("w_out", w_out, (f, d), bf), _matrix("dy", dy, (T, d), bf), None,
-                          _matrix("pre", pre, (T, 2 * f), bf), _matrix("h", h, (T, f), bf))
-    _matrix("dx", dx, (T, d), bf, p.ld_x)
-    _matrix("dw_in", dw_in, (d, 2 * f), bf, p.ld_w_in)
-    _matrix("dw_out", dw_out, (f, d), bf, p.ld_w_out)
-    workspace = _scratch(workspace, hstu.mtgr_gated_ffn_workspace_size(p, hstu.MTGR_FFN_BACKWARD), x.device)
+    p = hstu.GatedFfnProblem(T, d, f, _matrix("x", x, T, d, bf, dev), _matrix("w_in", w_in, d, 2 * f, bf, dev),
+                             _matrix("w_out", w_out, f, d, bf, dev), _matrix("dy", dy, T, d, bf, dev), d,
+                             _matrix("pre", pre, T, 2 * f, bf, dev), _matrix("h", h, T, f, bf, dev))
+    _matrix("dx", dx, T, d, bf, dev, p.ld_x)
+    _matrix("dw_in", dw_in, d, 2 * f, bf, dev, p.ld_w_in)
+    _matrix("dw_out", dw_out, f, d, bf, dev, p.ld_w_out)
+    workspace = _scratch(workspace, hstu.mtgr_gated_ffn_workspace_size(p, hstu.MTGR_FFN_BACKWARD), x)
     hstu.mtgr_gated_ffn_bwd(p, dy, x, pre, h, w_in, w_out, dx, dw_in, dw_out, workspace, workspace.numel())
     return dx, dw_in, dw_out
 
@@ -402,12 +407,12 @@ def dropout(x, p: float, rng, site: int = 0, residual=None, out=None):
     seed, step), `site` and the element alone and is not stored: the backward pass is dropout(dout, p, rng, site)
     with the same rng.  A program advances the step between its steps (rng[1] += 1)."""
     rows, cols = _two_dims("x", x)
-    code = _dtype_code(x)
+    code, dt, dev = _dtype_code(x), x.dtype, _device()
     if out is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    ld_x, ld_out = _matrix("x", x, (rows, cols), x.dtype), _matrix("out", out, (rows, cols), x.dtype)
-    ld_r = _matrix("residual", residual, (rows, cols), x.dtype) if residual is not None else cols
-    _vector("rng", rng, 2, (torch.int64,))
+        out = torch.empty((rows, cols), dtype=dt, device=x.device)
+    ld_x, ld_out = _matrix("x", x, rows, cols, dt, dev), _matrix("out", out, rows, cols, dt, dev)
+    ld_r = _matrix("residual", residual, rows, cols, dt, dev) if residual is not None else cols
+    _vector("rng", rng, 2, (torch.int64,), dev)
     if not 0 <= site < 1 << 32:
         raise ValueError("site is a 32-bit number")
     hstu.mtgr_dropout(rows, cols, code, x, ld_x, p, rng, site, residual, ld_r, out, ld_out)
@@ -416,10 +421,11 @@ def dropout(x, p: float, rng, site: int = 0, residual=None, out=None):
 
 def _softmax_loss_problem(x, w, targets, bias, scale: float) -> hstu.SoftmaxLossProblem:
     (N, d), V = _two_dims("x", x), _two_dims("w", w)[0]
-    ld_x, ld_w = _matrix("x", x, (N, d), torch.bfloat16), _matrix("w", w, (V, d), torch.bfloat16)
-    _vector("targets", targets, N, (torch.int64, torch.int32))
+    dev = _device()
+    ld_x, ld_w = _matrix("x", x, N, d, torch.bfloat16, dev), _matrix("w", w, V, d, torch.bfloat16, dev)
+    _vector("targets", targets, N, (torch.int64, torch.int32), dev)
     if bias is not None:
-        _vector("bias", bias, V, (torch.float32,))
+        _vector("bias", bias, V, (torch.float32,), dev)
     return hstu.SoftmaxLossProblem(N, V, d, 64 if targets.dtype == torch.int64 else 32, scale, ld_x, ld_w)
 
 
@@ -437,7 +443,7 @@ def softmax_loss_fwd(x, w, targets, bias=None, scale: float = 1.0, workspace=Non
     p = _softmax_loss_problem(x, w, targets, bias, scale)
     loss = torch.empty(p.num_rows, dtype=torch.float32, device=x.device)
     lse = torch.empty_like(loss)
-    workspace = _scratch(workspace, hstu.mtgr_softmax_loss_workspace_size(p), x.device)
+    workspace = _scratch(workspace, hstu.mtgr_softmax_loss_workspace_size(p), x)
     hstu.mtgr_softmax_loss_fwd(p, x, w, targets, bias, loss, lse, workspace, workspace.numel())
     return loss, lse
 
@@ -446,15 +452,16 @@ def softmax_loss_bwd(dloss, x, w, targets, lse, bias=None, scale: float = 1.0, g
     """Gradients of softmax_loss_fwd for dloss [N] fp32 (that of the mean over n labels: 1 / n) and the forward's lse:
     (dx, dw, dbias or None), dx and dw in the layouts of x and w (`grads`: the tensors to write)."""
     p = _softmax_loss_problem(x, w, targets, bias, scale)
-    _vector("dloss", dloss, p.num_rows, (torch.float32,))
-    _vector("lse", lse, p.num_rows, (torch.float32,))
+    dev = x.get_device()
+    _vector("dloss", dloss, p.num_rows, (torch.float32,), dev)
+    _vector("lse", lse, p.num_rows, (torch.float32,), dev)
     if grads is None:
         grads = _like_layout(x), _like_layout(w), torch.empty_like(bias) if bias is not None else None
     dx, dw, dbias = grads
-    _matrix("dx", dx, x.shape, torch.bfloat16, p.ld_x)
-    _matrix("dw", dw, w.shape, torch.bfloat16, p.ld_w)
+    _matrix("dx", dx, *x.shape, torch.bfloat16, dev, p.ld_x)
+    _matrix("dw", dw, *w.shape, torch.bfloat16, dev, p.ld_w)
     if dbias is not None:
-        _vector("dbias", dbias, p.num_classes, (torch.float32,))
-    workspace = _scratch(workspace, hstu.mtgr_softmax_loss_workspace_size(p, True), x.device)
+        _vector("dbias", dbias, p.num_classes, (torch.float32,), dev)
+    workspace = _scratch(workspace, hstu.mtgr_softmax_loss_workspace_size(p, True), x)
     hstu.mtgr_softmax_loss_bwd(p, dloss, x, w, targets, bias, lse, dx, dw, dbias, workspace, workspace.numel())
     return dx, dw, dbias
