@@ -11,6 +11,12 @@ library's HIP kernels.  IDs are int64 tensors holding the bit patterns of uint64
     table.sgd(batch, grad_out, lr=0.05)          # sparse update of the batch's rows
     table.evict(threshold=t - window)            # drop IDs not seen since the threshold
     table.evict(threshold=0, min_count=3)        # drop IDs seen fewer than 3 times
+
+Next-item training against the batch's own items (bf16 tables, dim a multiple of 32):
+
+    out, batch = table.lookup(ids, now=t)
+    loss, saved = table.item_loss(x, batch, labels)      # labels: positions in ids, -1 for none
+    dx, grad_out = table.item_loss_bwd(dloss, saved)     # grad_out goes to table.sgd, dx to the encoder
 """
 from __future__ import annotations
 
@@ -18,7 +24,7 @@ from dataclasses import dataclass
 
 import torch
 
-from . import hstu
+from . import hstu, ops
 
 
 def _next_pow2(n: int) -> int:
@@ -133,6 +139,35 @@ class DynamicEmbedding:
         new = self._descriptor(keys, key_rows, int(key_capacity))
         hstu.mtgr_embedding_rehash(old, new)
         self.keys, self.key_rows, self.key_capacity, self.table = keys, key_rows, int(key_capacity), new
+
+    # -------------------------------------------------------------- loss over the batch's items
+    def item_loss(self, x: torch.Tensor, batch: Batch, labels: torch.Tensor, scale: float = 1.0):
+        """Softmax cross entropy of the rows of x [N, dim] against the batch's distinct items, each item's logit
+        corrected by the log of its share of the batch (popular items would be pushed down as classes for being
+        there more often).  labels [N] int64: the position in the batch's IDs of the row's label, outside 0 .. n-1 for
+        a row without one; a label whose ID the table does not hold counts as none.  Nothing synchronises.
+        Returns (loss [N], saved for item_loss_bwd)."""
+        at = torch.arange(batch.n_max, device=self.device)
+        known = (at < batch.num_unique) & (batch.rows >= 0)
+        rows = torch.where(known, batch.rows, torch.full_like(batch.rows, -1))
+        w = torch.empty(batch.n_max, self.dim, dtype=self.dtype, device=self.device)
+        hstu.mtgr_embedding_gather(self.table, batch.n_max, at.to(torch.int32), rows, w, w.stride(0))
+        share = batch.occurrences.clamp(min=1).float() / max(batch.n, 1)
+        bias = torch.where(known, -torch.log(share), torch.full_like(share, float("-inf")))
+        has = (labels >= 0) & (labels < batch.n)
+        item = batch.inverse.long()[torch.where(has, labels, torch.zeros_like(labels))]
+        targets = torch.where(has & known[item.clamp(0, batch.n_max - 1)], item, torch.full_like(item, -1))
+        loss, lse = ops.softmax_loss_fwd(x, w, targets, bias=bias, scale=scale)
+        return loss, (x, w, targets, lse, bias, scale, batch)
+
+    def item_loss_bwd(self, dloss: torch.Tensor, saved):
+        """(dx [N, dim], grad_out [n, dim]) of item_loss: grad_out, for sgd(), gives each of an item's positions
+        its share of the item's gradient."""
+        x, w, targets, lse, bias, scale, batch = saved
+        dx, dw, _ = ops.softmax_loss_bwd(dloss, x, w, targets, lse, bias=bias, scale=scale,
+                                         grads=(ops._like_layout(x), torch.empty_like(w), None))
+        item = batch.inverse[:batch.n].long()
+        return dx, (dw[item].float() / batch.occurrences[item].float()[:, None]).to(self.dtype)
 
     # -------------------------------------------------------------- state (synchronising)
     def stats(self) -> dict:

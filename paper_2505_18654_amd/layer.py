@@ -105,3 +105,42 @@ def layer_bwd(dx_out: torch.Tensor, ctx: dict, jag: ops.Jagged, P: LayerParams, 
     if keep is not None:
         keep.update(dh=da, dxt=dxt, dx_gln=dx)
     return g
+
+
+@dataclass
+class FfnParams:
+    gamma: torch.Tensor      # [G, d] fp32, of the input Group-LN
+    beta: torch.Tensor       # [G, d] fp32
+    w_in: torch.Tensor       # [d, 2f] bf16: columns gate | up
+    w_out: torch.Tensor      # [f, d] bf16
+
+
+def ffn_fwd(x: torch.Tensor, jag: ops.Jagged, P: FfnParams, rng=None, p_drop: float = 0.0, site: int = 0,
+            eps: float = 1e-5, save: bool = True):
+    """The feed-forward block that may follow an encoder layer, with its residual branch:
+
+        X' = X + dropout((silu(Xt W_gate) (*) (Xt W_up)) W_out),   Xt = GroupLN(X)
+
+    Returns (x_out [T, d], ctx for ffn_bwd), with save=False (serving) (x_out, None).  `rng` (device int64 [2]:
+    seed, step) and `site` fix the dropped elements and have to be the same in ffn_bwd (ops.dropout)."""
+    xt, m, r = ops.gln_fwd(x, None, jag.seg, P.gamma, P.beta, eps)
+    drops = p_drop > 0.0
+    out = ops.gated_ffn_fwd(xt, P.w_in, P.w_out, residual=None if drops else x, save=save)
+    y, pre, h = out if save else (out, None, None)
+    if drops:
+        ops.dropout(y, p_drop, rng, site, residual=x, out=y)
+    return y, dict(x=x, xt=xt, m=m, r=r, pre=pre, h=h) if save else None
+
+
+def ffn_bwd(dx_out: torch.Tensor, ctx: dict, jag: ops.Jagged, P: FfnParams, rng=None, p_drop: float = 0.0,
+            site: int = 0, eps: float = 1e-5) -> dict:
+    """Gradients of ffn_fwd: dict with x and every FfnParams field."""
+    dy = ops.dropout(dx_out, p_drop, rng, site) if p_drop > 0.0 else dx_out
+    g = {}
+    dxt, g["w_in"], g["w_out"] = ops.gated_ffn_bwd(dy, ctx["xt"], ctx["pre"], ctx["h"], P.w_in, P.w_out)
+    # (one pass adds the residual branch's gradient, unless X is a view with gaps between its rows)
+    one_pass = ctx["x"].is_contiguous() and dx_out.is_contiguous()
+    dx, _, g["gamma"], g["beta"] = ops.gln_bwd(dxt, ctx["x"], None, jag.seg, P.gamma, ctx["m"], ctx["r"], eps,
+                                               residual=dx_out if one_pass else None)
+    g["x"] = dx if one_pass else ops.add(dx, dx_out)
+    return g
