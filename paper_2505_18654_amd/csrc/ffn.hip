@@ -16,23 +16,66 @@ namespace mtgr {
 namespace {
 
 // out = sum of the K splits' partials (+ residual), rounded once.
-__global__ __launch_bounds__(256) void ffn_sum_kernel(const float* partial, int splits, long long rows, int cols, uint16_t* out,
-                                                      long long ld_out, const uint16_t* residual, long long ld_r) {
-    const int ch = cols / 4;
-    const long long n = rows * ch;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+struct SumArgs {
+    const float* partial;
+    int splits, cols;
+    long long rows;
+    uint16_t* out;
+    long long ld_out;
+    const uint16_t* residual;
+    long long ld_r;
+};
+
+__device__ __forceinline__ void sum_splits(const SumArgs& a, int block, int blocks) {
+    const int ch = a.cols / 4;
+    const long long n = a.rows * ch;
+    for (long long i = (long long)block * 256 + threadIdx.x; i < n; i += (long long)blocks * 256) {
         const long long r = i / ch;
         const int c = (int)(i % ch) * 4;
-        floatx4 s = ((const floatx4*)partial)[i];
+        floatx4 s = ((const floatx4*)a.partial)[i];
 #pragma unroll 4
-        for (int k = 1; k < splits; k++) s += ((const floatx4*)partial)[k * n + i];
-        if (residual) {
-            const uint2 v = *(const uint2*)(residual + r * ld_r + c);
+        for (int k = 1; k < a.splits; k++) s += ((const floatx4*)a.partial)[k * n + i];
+        if (a.residual) {
+            const uint2 v = *(const uint2*)(a.residual + r * a.ld_r + c);
             s += floatx4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
                          __uint_as_float(v.y & 0xffff0000u)};
         }
-        *(uint2*)(out + r * ld_out + c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
+        *(uint2*)(a.out + r * a.ld_out + c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
     }
+}
+
+// One or two products' sums; the second one's workgroups from `first` on.
+__global__ __launch_bounds__(256) void ffn_sum_kernel(SumArgs a, SumArgs b, int first) {
+    if ((int)blockIdx.x < first) sum_splits(a, blockIdx.x, first);
+    else sum_splits(b, blockIdx.x - first, gridDim.x - first);
+}
+
+SumArgs sum_of(const GemmArgs& g) {
+    return {g.partial, g.splits, (int)g.N, g.M, (uint16_t*)g.C, g.ldc, (const uint16_t*)g.R, g.ldr};
+}
+
+int sum_grid(const GemmArgs& g) { return (int)std::min((g.M * (g.N / 4) + 255) / 256, 4096ll); }
+
+// Both weight gradients' tiles and K splits where they share a launch: 128 x 128 tiles, the same split of the
+// tokens for both.
+Tiles plan_both(long long d, long long f, long long T) {
+    static const int candidates[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+    Tiles best{};
+    best.us = 1e30;
+    const long long steps = (T + WBK - 1) / WBK, most = std::max(1ll, steps / 4);
+    const long long tiles = ((d + MBM - 1) / MBM) * ((2 * f + MBN - 1) / MBN) + ((f + MBM - 1) / MBM) * ((d + MBN - 1) / MBN);
+    for (int s : candidates) {
+        if (s > most) break;
+        const long long rounds = (tiles * s + MID_WORKGROUPS - 1) / MID_WORKGROUPS;
+        const double us = rounds * (4.0 + (tiles * s > WIDE_WORKGROUPS ? 1.0 : 0.8) * ((steps + s - 1) / s)) + 4.0 +
+                          (double)s * 3 * d * f * 8 / 8e6;
+        if (us < best.us) {
+            best.us = us;
+            best.splits = s;
+        }
+    }
+    best.mid = true;
+    return best;
 }
 
 GemmArgs product(int layout, long long M, long long N, long long K, const void* A, long long lda, const void* B,
@@ -70,8 +113,7 @@ static hipError_t deep_product(GemmArgs g, float* partial, hipStream_t s) {
     g.partial = partial;
     const hipError_t e = mid_launch<LAYOUT, GEMM_EPI_PART>(g, s);
     if (e != hipSuccess) return e;
-    const int grid = (int)std::min((g.M * (g.N / 4) + 255) / 256, 8192ll);
-    ffn_sum_kernel<<<grid, 256, 0, s>>>(partial, g.splits, g.M, (int)g.N, (uint16_t*)g.C, g.ldc, (const uint16_t*)g.R, g.ldr);
+    ffn_sum_kernel<<<sum_grid(g), 256, 0, s>>>(sum_of(g), SumArgs{}, sum_grid(g));
     return hipGetLastError();
 }
 
@@ -111,12 +153,32 @@ hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
     return deep_product<GEMM_NN>(g, partial, s);
 }
 
-// Workspace of the backward: dpre [T, 2f] bf16, then the largest of the three products' partials.
+// The weight gradients of the backward: in one launch, or one after the other.
+struct GradientPlan {
+    bool both;
+    Tiles in, out;
+};
+
+static GradientPlan plan_gradients(long long T, int d, int f) {
+    GradientPlan p{};
+    p.in = plan_split(d, 2ll * f, T, true);
+    p.out = plan_split(f, d, T, true);
+    const Tiles both = plan_both(d, f, T);
+    p.both = both.us < p.in.us + p.out.us;
+    if (p.both) {
+        p.in = tiles_of(true, d, 2ll * f, T, 1, both.splits, true);
+        p.out = tiles_of(true, f, d, T, 1, both.splits, true);
+    }
+    return p;
+}
+
+// Workspace of the backward: dpre [T, 2f] bf16, then the partials of dx or of the weight gradients.
 size_t ffn_bwd_workspace_bytes(long long T, int d, int f) {
     const size_t weights = (size_t)d * f * sizeof(float);
+    const GradientPlan p = plan_gradients(T, d, f);
+    const size_t in = p.in.splits * 2 * weights, out = p.out.splits * weights;
     return align256((size_t)T * 2 * f * 2) +
-           std::max({plan_split(d, 2ll * f, T, true).splits * 2 * weights, plan_split(f, d, T, true).splits * weights,
-                     partial_bytes(plan_deep(T, d, 2ll * f), T, d)});
+           std::max(p.both ? in + out : std::max(in, out), partial_bytes(plan_deep(T, d, 2ll * f), T, d));
 }
 
 hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
@@ -136,15 +198,25 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
     if (e != hipSuccess) return e;
     e = deep_product<GEMM_NT>(product(GEMM_NT, a.T, a.d, f2, dpre, f2, a.w_in, a.ld_win, a.dx, a.ld_x), partial, s);
     if (e != hipSuccess) return e;
-    auto gradient = [&](GemmArgs w) {
-        const Tiles q = plan_split(w.M, w.N, w.K, true);
-        set_tiles(&w, q);
-        w.partial = partial;
-        const hipError_t r = q.mid ? mid_launch<GEMM_TN, GEMM_EPI_NONE>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_NONE, false>(w, s);
+    const GradientPlan p = plan_gradients(a.T, a.d, a.f);
+    GemmArgs wi = product(GEMM_TN, a.d, f2, a.T, a.x, a.ld_x, dpre, f2, a.dw_in, a.ld_win);
+    GemmArgs wo = product(GEMM_TN, a.f, a.d, a.T, a.h, a.ld_h, a.dy, a.ld_y, a.dw_out, a.ld_wout);
+    set_tiles(&wi, p.in);
+    set_tiles(&wo, p.out);
+    wi.partial = wo.partial = partial;
+    if (p.both) {
+        wo.partial = partial + (size_t)wi.splits * a.d * f2;
+        gemm_mid_pair_kernel<GEMM_TN, GEMM_EPI_NONE><<<mid_grid(wi) + mid_grid(wo), 256, 0, s>>>(wi, wo, mid_grid(wi));
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        ffn_sum_kernel<<<sum_grid(wi) + sum_grid(wo), 256, 0, s>>>(sum_of(wi), sum_of(wo), sum_grid(wi));
+        return hipGetLastError();
+    }
+    auto gradient = [&](const GemmArgs& w) {
+        const hipError_t r = w.wide ? wide_launch<GEMM_TN, GEMM_EPI_NONE, false>(w, s) : mid_launch<GEMM_TN, GEMM_EPI_NONE>(w, s);
         return r != hipSuccess ? r : launch_split_reduce(w, s);
     };
-    if ((e = gradient(product(GEMM_TN, a.d, f2, a.T, a.x, a.ld_x, dpre, f2, a.dw_in, a.ld_win))) != hipSuccess) return e;
-    return gradient(product(GEMM_TN, a.f, a.d, a.T, a.h, a.ld_h, a.dy, a.ld_y, a.dw_out, a.ld_wout));
+    e = gradient(wi);
+    return e != hipSuccess ? e : gradient(wo);
 }
 
 }  // namespace mtgr

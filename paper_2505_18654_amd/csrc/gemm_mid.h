@@ -19,23 +19,23 @@ namespace mtgr {
 namespace {
 
 constexpr int MBM = 128, MBN = 128, MBK = 64;
-constexpr uint32_t MSLOT = MBM * MBK * 2;
+constexpr uint32_t MSLOT = MBM * MBK * 2, MID_LDS = 4 * MSLOT;
 
 // Workgroups per tile grid that fill the chip once: two per CU.
 constexpr int MID_WORKGROUPS = 512;
 
 }  // namespace
 
+// The tile of workgroup `block` of a product's own grid; sm: MID_LDS bytes.
 template <int LAYOUT, int EPI>
-__global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
+__device__ __forceinline__ void mid_tile(const GemmArgs& g, int block, char* sm) {
     constexpr bool A_KR = LAYOUT == GEMM_TN, B_KR = LAYOUT != GEMM_NT;
     constexpr bool ACC = EPI == GEMM_EPI_ACC, SPLIT = LAYOUT == GEMM_TN || ACC || EPI == GEMM_EPI_PART;
     constexpr bool GATED = EPI == GEMM_EPI_GATED || EPI == GEMM_EPI_GATED_SAVE;
     constexpr bool STATS = EPI == GEMM_EPI_SM_STATS, GRAD = EPI == GEMM_EPI_SM_GRAD, B_SHORT = STATS || GRAD;
     constexpr bool DYN = B_SHORT || ACC || EPI == GEMM_EPI_ROWS;
     constexpr int NTILE = GATED ? MBN / 2 : MBN;
-    constexpr uint32_t OFF_B = 2 * MSLOT;
-    __shared__ __align__(1024) char sm[4 * MSLOT];           // A 0, A 1, B 0, B 1
+    constexpr uint32_t OFF_B = 2 * MSLOT;                    // stages A 0, A 1, B 0, B 1
 
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wm = w & 1, wn = w >> 1;
     const int lr = lane & 15, lg = lane >> 4;
@@ -51,8 +51,8 @@ __global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
     }
     // items (split, m block, n block), a share of consecutive ones per XCD
     const int tiles = mblocks * g.nblocks, items = tiles * g.splits, share = (items + XCDS - 1) / XCDS;
-    const int it = blockIdx.x % XCDS * share + blockIdx.x / XCDS;
-    if ((int)(blockIdx.x / XCDS) >= share || it >= items) return;
+    const int it = block % XCDS * share + block / XCDS;
+    if (block / XCDS >= share || it >= items) return;
     const int split = it / tiles, mb = it % tiles / g.nblocks, nb = it % g.nblocks;
     const int m0 = mb * MBM, n0 = nb * NTILE;
     const int nks = (K + MBK - 1) / MBK, per = (nks + g.splits - 1) / g.splits;
@@ -156,6 +156,20 @@ __global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
     using AK = std::integral_constant<bool, A_KR>;
     using BK = std::integral_constant<bool, B_KR>;
 
+    // acc[a][b] will hold row em + 16 b, columns en + 16 a + 0..3; what the epilogue reads there is loaded first
+    const int em = m0 + 64 * wm + lr, en = n0 + 64 * wn + 4 * lg;
+    constexpr bool READS = EPI == GEMM_EPI_RESIDUAL || EPI == GEMM_EPI_GATED_BWD;
+    uint2 r0[READS ? 4 : 1][4], r1[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][4];
+    if constexpr (READS) {
+#pragma unroll
+        for (int b = 0; b < 4; b++)
+#pragma unroll
+            for (int a = 0; a < 4; a++) {
+                const uint16_t* r = (const uint16_t*)g.R + min(em + 16 * b, M - 1) * g.ldr + min(en + 16 * a, N - 4);
+                r0[a][b] = *(const uint2*)r;
+                if constexpr (EPI == GEMM_EPI_GATED_BWD) r1[a][b] = *(const uint2*)(r + N);
+            }
+    }
     floatx4 acc[4][4];
 #pragma unroll
     for (int a = 0; a < 4; a++)
@@ -183,8 +197,7 @@ __global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
         }
     }
 
-    // ---- epilogue: acc[a][b] holds row em + 16 b + l % 16, columns en + 16 a + 4 (l / 16) + 0..3
-    const int em = m0 + 64 * wm + lr, en = n0 + 64 * wn + 4 * lg;
+    // ---- epilogue
     auto pack = [](floatx4 v) { return make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); };
     auto unpack = [](uint2 u) {
         return floatx4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
@@ -282,18 +295,6 @@ __global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
                 *(uint2*)((uint16_t*)g.C2 + gm * g.ldc2 + gn) = pack(h);
             }
     } else {
-        // (what the epilogue reads is loaded before the first store)
-        uint2 r0[EPI == GEMM_EPI_NONE ? 1 : 4][4], r1[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][4];
-        if constexpr (EPI != GEMM_EPI_NONE) {
-#pragma unroll
-            for (int b = 0; b < 4; b++)
-#pragma unroll
-                for (int a = 0; a < 4; a++) {
-                    const uint16_t* r = (const uint16_t*)g.R + min(em + 16 * b, M - 1) * g.ldr + min(en + 16 * a, N - 4);
-                    r0[a][b] = *(const uint2*)r;
-                    if constexpr (EPI == GEMM_EPI_GATED_BWD) r1[a][b] = *(const uint2*)(r + N);
-                }
-        }
 #pragma unroll
         for (int b = 0; b < 4; b++)
 #pragma unroll
@@ -323,9 +324,24 @@ __global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
 }
 
 template <int LAYOUT, int EPI>
+__global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
+    __shared__ __align__(1024) char sm[MID_LDS];
+    mid_tile<LAYOUT, EPI>(g, blockIdx.x, sm);
+}
+
+// Two products in one launch, the second one from workgroup `first` (a multiple of the XCDs) on.
+template <int LAYOUT, int EPI>
+__global__ __launch_bounds__(256, 2) void gemm_mid_pair_kernel(GemmArgs g, GemmArgs h, int first) {
+    __shared__ __align__(1024) char sm[MID_LDS];
+    if ((int)blockIdx.x < first) mid_tile<LAYOUT, EPI>(g, blockIdx.x, sm);
+    else mid_tile<LAYOUT, EPI>(h, blockIdx.x - first, sm);
+}
+
+static inline int mid_grid(const GemmArgs& g) { return XCDS * ((g.mblocks * g.nblocks * g.splits + XCDS - 1) / XCDS); }
+
+template <int LAYOUT, int EPI>
 static hipError_t mid_launch(const GemmArgs& g, hipStream_t s) {
-    const int items = g.mblocks * g.nblocks * g.splits;
-    gemm_mid_kernel<LAYOUT, EPI><<<XCDS * ((items + XCDS - 1) / XCDS), 256, 0, s>>>(g);
+    gemm_mid_kernel<LAYOUT, EPI><<<mid_grid(g), 256, 0, s>>>(g);
     return hipGetLastError();
 }
 

@@ -494,7 +494,6 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
 #pragma unroll
             for (int b = 0; b < WNM; b++) ri[b] = g.row_info[em + 16 * b + er];
         }
-        if constexpr (B_SHORT) wait_vmcnt_seen<0>();   // (before the copies)
         // gate and up values of row 8 q + l / 8 of block b, chunk l % 8, four blocks ahead
         uint4 pg[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][2], pu[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][2];
         auto load_pre = [&](int b) {
@@ -539,8 +538,9 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
             j += gridDim.x / XCDS;
             more = tile_of(j);
         }
+        if (more) start_tile();
+        if constexpr (B_SHORT) wait_vmcnt_seen<0>();   // (before the copies, which it would wait for)
         if (more) {
-            start_tile();
             copy_b(0, 0);
             copy_a(0, 0);
             if (nk > 1) {
