@@ -69,7 +69,7 @@ mtgr_status_t mtgr_gated_ffn_bwd(const mtgr_gated_ffn_problem_t* p, const void* 
  * captured graph.  site numbers the places of a model that drop, so that their masks differ; the step
  * counts modulo 2^32.  Element e is kept when word e % 4 of Philox4x32-7 with the key seed and the counter
  * (e / 4 low, e / 4 high, site, step) is at least floor(prob 2^32).  0 <= prob < 1.  cols is a multiple of
- * 16 bytes.  A dropped element counts as 0 whatever x holds.  out may be x or the residual. */
+ * 16 bytes, rows * cols below 2^50.  A dropped element counts as 0 whatever x holds.  out may be x or the residual. */
 mtgr_status_t mtgr_dropout(int64_t rows, int32_t cols, mtgr_dtype_t dtype, const void* x, int64_t ld_x, double prob,
                            const uint64_t* rng, uint32_t site, const void* residual, int64_t ld_residual, void* out,
                            int64_t ld_out, mtgr_stream_t stream);

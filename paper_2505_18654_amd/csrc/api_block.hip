@@ -218,7 +218,7 @@ mtgr_status_t mtgr_dropout(int64_t rows, int32_t cols, mtgr_dtype_t dtype, const
                            int64_t ld_out, mtgr_stream_t stream) {
     if (dtype != MTGR_DTYPE_BF16 && dtype != MTGR_DTYPE_FP32) return fail(MTGR_ERROR_UNSUPPORTED, "dtype %d", (int)dtype);
     const int esize = dtype == MTGR_DTYPE_BF16 ? 2 : 4, per = 16 / esize;
-    if (rows < 0 || cols <= 0 || rows >= (1ll << 40))
+    if (rows < 0 || cols <= 0 || rows >= (1ll << 50) / cols)
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "rows = %lld, cols = %d", (long long)rows, cols);
     if (cols % per != 0) return fail(MTGR_ERROR_INVALID_ARGUMENT, "cols = %d is not a multiple of %d", cols, per);
     if (!(prob >= 0.0 && prob < 1.0)) return fail(MTGR_ERROR_INVALID_ARGUMENT, "prob = %g outside [0, 1)", prob);

@@ -91,6 +91,9 @@ __device__ __forceinline__ int label_of(const void* targets, long long i, int V)
     return t >= 0 && t < V ? (int)t : -1;
 }
 
+// |g| for the largest of a batch: an infinite or NaN gradient stays that of its own row.
+__device__ __forceinline__ float size_of(float g) { return fabsf(g) < __builtin_inff() ? fabsf(g) : 0.f; }
+
 // The class bias in units of log 2, padded to whole tiles with classes that do not count.
 __device__ __forceinline__ void padded_bias(const SoftmaxLossArgs& a, float* bias2, int vpad, int c) {
     if (c < vpad) bias2[c] = c >= a.V ? -__builtin_inff() : a.bias ? a.bias[c] * LOG2E : 0.f;
@@ -106,7 +109,7 @@ __global__ __launch_bounds__(256) void sm_count_kernel(SoftmaxLossArgs a, int* c
     __shared__ float top[4];
     const long long r = (long long)blockIdx.x * ROWS_PER_BLOCK + tid;
     const bool on = r < a.N && label_of<T>(a.targets, r, a.V) >= 0;
-    float g = BWD && on ? fabsf(a.dloss[r]) : 0.f;
+    float g = BWD && on ? size_of(a.dloss[r]) : 0.f;
     if (BWD) {
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) g = fmaxf(g, __shfl_xor(g, o, 64));
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* r
         if (SCAN) {
 #pragma unroll 8
             for (int i = tid; i < (int)a.N; i += 1024) {
-                const float g = fabsf(a.dloss[i]);
+                const float g = size_of(a.dloss[i]);
                 top = fmaxf(top, label_of<T>(a.targets, i, a.V) >= 0 ? g : 0.f);
             }
         } else {

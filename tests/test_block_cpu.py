@@ -114,7 +114,7 @@ def drop(**kw):
     (dict(prob=float("nan")), INVALID), (dict(x=None), NULL), (dict(out=None), NULL), (dict(rng=None), NULL),
     (dict(rng=FAKE + 4), INVALID), (dict(x=FAKE + 8), INVALID), (dict(ld_x=56), INVALID), (dict(ld_out=68), INVALID),
     (dict(residual=FAKE, ld_residual=32), INVALID), (dict(residual=FAKE + 2, ld_residual=64), INVALID),
-    (dict(ld_x=1 << 22), UNSUPPORTED), (dict(rows=1 << 40), INVALID),
+    (dict(ld_x=1 << 22), UNSUPPORTED), (dict(rows=1 << 44), INVALID),
 ])
 def test_dropout_refused(kw, status):
     assert status_of(drop, **kw) == status

@@ -112,6 +112,20 @@ def test_classes_taken_out():
     assert not any(v.any() for v in ops.softmax_loss_bwd(dloss, x, w, t, s4, bias=none))
 
 
+def test_one_infinite_gradient_stays_in_its_row():
+    x, w, t, b, dloss = make(300, 200, 64, 1.0, False)
+    _, lse = ops.softmax_loss_fwd(x, w, t)
+    want, _, _ = ops.softmax_loss_bwd(dloss, x, w, t, lse)
+    bad = dloss.clone()
+    bad[7] = float("inf")
+    got, _, _ = ops.softmax_loss_bwd(bad, x, w, t, lse)
+    rest = torch.arange(300, device="cuda") != 7
+    assert not torch.isfinite(got[7]).all()
+    # (both are within a bf16 rounding of each product's operand; dz is kept relative to the largest gradient)
+    assert torch.isfinite(got[rest]).all()
+    assert float((got[rest].double() - want[rest].double()).norm() / want[rest].double().norm()) < 2.0 ** -7
+
+
 def test_large_logits():
     """Logits of a thousand and more: the maximum is taken out first; confident rows have losses near 0."""
     x, w, t, b, dloss = make(200, 500, 128, 1.0, False, spread=60.0)
