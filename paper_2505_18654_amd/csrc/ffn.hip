@@ -44,10 +44,11 @@ __device__ __forceinline__ void sum_splits(const SumArgs& a, int block, int bloc
     }
 }
 
-// One or two products' sums; the second one's workgroups from `first` on.
-__global__ __launch_bounds__(256) void ffn_sum_kernel(SumArgs a, SumArgs b, int first) {
+// Up to three products' sums; the second one's workgroups from `first` on, the third one's from `second` on.
+__global__ __launch_bounds__(256) void ffn_sum_kernel(SumArgs a, SumArgs b, SumArgs c, int first, int second) {
     if ((int)blockIdx.x < first) sum_splits(a, blockIdx.x, first);
-    else sum_splits(b, blockIdx.x - first, gridDim.x - first);
+    else if ((int)blockIdx.x < second) sum_splits(b, blockIdx.x - first, second - first);
+    else sum_splits(c, blockIdx.x - second, gridDim.x - second);
 }
 
 SumArgs sum_of(const GemmArgs& g) {
@@ -55,28 +56,6 @@ SumArgs sum_of(const GemmArgs& g) {
 }
 
 int sum_grid(const GemmArgs& g) { return (int)std::min((g.M * (g.N / 4) + 255) / 256, 4096ll); }
-
-// Both weight gradients' tiles and K splits where they share a launch: 128 x 128 tiles, the same split of the
-// tokens for both.
-Tiles plan_both(long long d, long long f, long long T) {
-    static const int candidates[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
-    Tiles best{};
-    best.us = 1e30;
-    const long long steps = (T + WBK - 1) / WBK, most = std::max(1ll, steps / 4);
-    const long long tiles = ((d + MBM - 1) / MBM) * ((2 * f + MBN - 1) / MBN) + ((f + MBM - 1) / MBM) * ((d + MBN - 1) / MBN);
-    for (int s : candidates) {
-        if (s > most) break;
-        const long long rounds = (tiles * s + MID_WORKGROUPS - 1) / MID_WORKGROUPS;
-        const double us = rounds * (4.0 + (tiles * s > WIDE_WORKGROUPS ? 1.0 : 0.8) * ((steps + s - 1) / s)) + 4.0 +
-                          (double)s * 3 * d * f * 8 / 8e6;
-        if (us < best.us) {
-            best.us = us;
-            best.splits = s;
-        }
-    }
-    best.mid = true;
-    return best;
-}
 
 GemmArgs product(int layout, long long M, long long N, long long K, const void* A, long long lda, const void* B,
                  long long ldb, void* C, long long ldc) {
@@ -98,8 +77,7 @@ GemmArgs product(int layout, long long M, long long N, long long K, const void* 
 
 // C = A B (NN) or A B^T (NT), plus the residual R where there is one; `partial` holds the K splits' sums.
 template <int LAYOUT>
-static hipError_t deep_product(GemmArgs g, float* partial, hipStream_t s) {
-    const Tiles t = plan_deep(g.M, g.N, g.K);
+static hipError_t deep_product(GemmArgs g, const Tiles& t, float* partial, hipStream_t s) {
     if (!t.mid && (LAYOUT == GEMM_NT || !g.R)) {
         gemm_plan(&g);
         return launch_gemm_bf16(g, s);
@@ -113,7 +91,7 @@ static hipError_t deep_product(GemmArgs g, float* partial, hipStream_t s) {
     g.partial = partial;
     const hipError_t e = mid_launch<LAYOUT, GEMM_EPI_PART>(g, s);
     if (e != hipSuccess) return e;
-    ffn_sum_kernel<<<sum_grid(g), 256, 0, s>>>(sum_of(g), SumArgs{}, sum_grid(g));
+    ffn_sum_kernel<<<sum_grid(g), 256, 0, s>>>(sum_of(g), SumArgs{}, SumArgs{}, sum_grid(g), sum_grid(g));
     return hipGetLastError();
 }
 
@@ -140,7 +118,7 @@ hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
         GemmArgs g = product(GEMM_NN, a.T, a.f, a.d, a.x, a.ld_x, a.w_in, a.ld_win, a.pre, a.ld_pre);
         g.C2 = a.h;
         g.ldc2 = a.ld_h;
-        const Tiles t = plan(a.T, a.f, a.d, 2);
+        const Tiles t = plan(a.T, a.f, a.d, WBN / 2);
         set_tiles(&g, t);
         if (t.mid) e = a.pre ? mid_launch<GEMM_NN, GEMM_EPI_GATED_SAVE>(g, s) : mid_launch<GEMM_NN, GEMM_EPI_GATED>(g, s);
         else e = a.pre ? wide_launch<GEMM_NN, GEMM_EPI_GATED_SAVE, false>(g, s) : wide_launch<GEMM_NN, GEMM_EPI_GATED, false>(g, s);
@@ -150,35 +128,64 @@ hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
     GemmArgs g = product(GEMM_NN, a.T, a.d, a.f, a.h, a.ld_h, a.w_out, a.ld_wout, a.y, a.ld_y);
     g.R = a.residual;
     g.ldr = a.ld_r;
-    return deep_product<GEMM_NN>(g, partial, s);
+    return deep_product<GEMM_NN>(g, plan_deep(g.M, g.N, g.K), partial, s);
 }
 
-// The weight gradients of the backward: in one launch, or one after the other.
-struct GradientPlan {
-    bool both;
-    Tiles in, out;
+namespace {
+
+// The three products behind dpre: dx, dW_in and dW_out, one after the other, or in one launch on 128 x 128 tiles,
+// their k cut into about equal numbers of steps, and one launch that adds up all partials.
+struct BackwardPlan {
+    bool together;
+    Tiles dx, in, out;
+    size_t bytes;             // of the partials
 };
 
-static GradientPlan plan_gradients(long long T, int d, int f) {
-    GradientPlan p{};
+BackwardPlan plan_backward(long long T, int d, int f) {
+    BackwardPlan p{};
+    p.dx = plan_deep(T, d, 2ll * f);
     p.in = plan_split(d, 2ll * f, T, true);
     p.out = plan_split(f, d, T, true);
-    const Tiles both = plan_both(d, f, T);
-    p.both = both.us < p.in.us + p.out.us;
-    if (p.both) {
-        p.in = tiles_of(true, d, 2ll * f, T, 1, both.splits, true);
-        p.out = tiles_of(true, f, d, T, 1, both.splits, true);
+    const Tiles x = tiles_of(true, T, d, 2ll * f, WBN, 1, false), i = tiles_of(true, d, 2ll * f, T, WBN, 1, false),
+                o = tiles_of(true, f, d, T, WBN, 1, false);
+    const double tx = (double)x.mblocks * x.nblocks, tg = (double)i.mblocks * i.nblocks + (double)o.mblocks * o.nblocks;
+    const unsigned nx = (2u * f + WBK - 1) / WBK, ng = (unsigned)((T + WBK - 1) / WBK);
+    double best = p.dx.us + p.in.us + p.out.us;
+    int sx = 0, sg = 0;
+    for (unsigned steps = 4; steps <= 128; steps += steps / 2 < 4 ? 2 : steps / 4) {
+        const unsigned a = (nx + steps - 1) / steps, b = (ng + steps - 1) / steps;
+        const double qx = (nx + a - 1) / a, qg = (ng + b - 1) / b, items = tx * a + tg * b, top = std::max(qx, qg);
+        // (beyond one round a workgroup follows another as soon as it can: the mean, and half of a last one)
+        const double us = (items <= MID_WORKGROUPS ? MID_START + (items > WIDE_WORKGROUPS ? MID_STEP : MID_STEP_ALONE) * top
+                           : (tx * a * (MID_START + MID_STEP * qx) + tg * b * (MID_START + MID_STEP * qg)) / MID_WORKGROUPS +
+                                 0.5 * (MID_START + MID_STEP * top)) +
+                          partials_us((double)a * T * d + 3.0 * b * d * f);
+        if (us < best && a <= 64 && b <= 64) {
+            best = us;
+            sx = (int)a;
+            sg = (int)b;
+        }
+    }
+    const size_t weights = (size_t)d * f * sizeof(float);
+    p.together = sx > 0;
+    if (p.together) {
+        p.dx = x;
+        p.in = i;
+        p.out = o;
+        p.dx.splits = sx;
+        p.in.splits = p.out.splits = sg;
+        p.bytes = (size_t)sx * T * d * sizeof(float) + 3 * sg * weights;
+    } else {
+        p.bytes = std::max({partial_bytes(p.dx, T, d), 2 * p.in.splits * weights, p.out.splits * weights});
     }
     return p;
 }
 
-// Workspace of the backward: dpre [T, 2f] bf16, then the partials of dx or of the weight gradients.
+}  // namespace
+
+// Workspace of the backward: dpre [T, 2f] bf16, then the partials.
 size_t ffn_bwd_workspace_bytes(long long T, int d, int f) {
-    const size_t weights = (size_t)d * f * sizeof(float);
-    const GradientPlan p = plan_gradients(T, d, f);
-    const size_t in = p.in.splits * 2 * weights, out = p.out.splits * weights;
-    return align256((size_t)T * 2 * f * 2) +
-           std::max(p.both ? in + out : std::max(in, out), partial_bytes(plan_deep(T, d, 2ll * f), T, d));
+    return align256((size_t)T * 2 * f * 2) + plan_backward(T, d, f).bytes;
 }
 
 hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
@@ -192,27 +199,31 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
     GemmArgs g = product(GEMM_NT, a.T, a.f, a.d, a.dy, a.ld_y, a.w_out, a.ld_wout, dpre, f2);
     g.R = a.pre;
     g.ldr = a.ld_pre;
-    const Tiles t = plan(a.T, a.f, a.d, 1);
+    const Tiles t = plan(a.T, a.f, a.d);
     set_tiles(&g, t);
     hipError_t e = t.mid ? mid_launch<GEMM_NT, GEMM_EPI_GATED_BWD>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_GATED_BWD, false>(g, s);
     if (e != hipSuccess) return e;
-    e = deep_product<GEMM_NT>(product(GEMM_NT, a.T, a.d, f2, dpre, f2, a.w_in, a.ld_win, a.dx, a.ld_x), partial, s);
-    if (e != hipSuccess) return e;
-    const GradientPlan p = plan_gradients(a.T, a.d, a.f);
+    const BackwardPlan p = plan_backward(a.T, a.d, a.f);
+    GemmArgs x = product(GEMM_NT, a.T, a.d, f2, dpre, f2, a.w_in, a.ld_win, a.dx, a.ld_x);
     GemmArgs wi = product(GEMM_TN, a.d, f2, a.T, a.x, a.ld_x, dpre, f2, a.dw_in, a.ld_win);
     GemmArgs wo = product(GEMM_TN, a.f, a.d, a.T, a.h, a.ld_h, a.dy, a.ld_y, a.dw_out, a.ld_wout);
     set_tiles(&wi, p.in);
     set_tiles(&wo, p.out);
-    wi.partial = wo.partial = partial;
-    if (p.both) {
-        wo.partial = partial + (size_t)wi.splits * a.d * f2;
-        gemm_mid_pair_kernel<GEMM_TN, GEMM_EPI_NONE><<<mid_grid(wi) + mid_grid(wo), 256, 0, s>>>(wi, wo, mid_grid(wi));
+    if (p.together) {
+        set_tiles(&x, p.dx);
+        x.partial = partial;
+        wi.partial = x.partial + (size_t)x.splits * a.T * a.d;
+        wo.partial = wi.partial + (size_t)wi.splits * a.d * f2;
+        const int first = mid_grid(x), second = first + mid_grid(wi), sx = sum_grid(x), si = sx + sum_grid(wi);
+        gemm_mid_trio_kernel<GEMM_NT, GEMM_EPI_PART, GEMM_TN, GEMM_EPI_PART><<<second + mid_grid(wo), 256, 0, s>>>(x, wi, wo, first, second);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        ffn_sum_kernel<<<sum_grid(wi) + sum_grid(wo), 256, 0, s>>>(sum_of(wi), sum_of(wo), sum_grid(wi));
+        ffn_sum_kernel<<<si + sum_grid(wo), 256, 0, s>>>(sum_of(x), sum_of(wi), sum_of(wo), sx, si);
         return hipGetLastError();
     }
+    if ((e = deep_product<GEMM_NT>(x, p.dx, partial, s)) != hipSuccess) return e;
+    wi.partial = wo.partial = partial;
     auto gradient = [&](const GemmArgs& w) {
-        const hipError_t r = w.wide ? wide_launch<GEMM_TN, GEMM_EPI_NONE, false>(w, s) : mid_launch<GEMM_TN, GEMM_EPI_NONE>(w, s);
+        const hipError_t r = w.wide ? wide_launch<GEMM_TN, GEMM_EPI_NONE, false>(w, s) : mid_launch<GEMM_TN, GEMM_EPI_PART>(w, s);
         return r != hipSuccess ? r : launch_split_reduce(w, s);
     };
     e = gradient(wi);

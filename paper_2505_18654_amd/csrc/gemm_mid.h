@@ -329,12 +329,19 @@ __global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
     mid_tile<LAYOUT, EPI>(g, blockIdx.x, sm);
 }
 
-// Two products in one launch, the second one from workgroup `first` (a multiple of the XCDs) on.
-template <int LAYOUT, int EPI>
+// Several products in one launch, each from a workgroup of its own on (a multiple of the XCDs).
+template <int LAYOUT0, int EPI0, int LAYOUT1, int EPI1>
 __global__ __launch_bounds__(256, 2) void gemm_mid_pair_kernel(GemmArgs g, GemmArgs h, int first) {
     __shared__ __align__(1024) char sm[MID_LDS];
-    if ((int)blockIdx.x < first) mid_tile<LAYOUT, EPI>(g, blockIdx.x, sm);
-    else mid_tile<LAYOUT, EPI>(h, blockIdx.x - first, sm);
+    if ((int)blockIdx.x < first) mid_tile<LAYOUT0, EPI0>(g, blockIdx.x, sm);
+    else mid_tile<LAYOUT1, EPI1>(h, blockIdx.x - first, sm);
+}
+
+template <int LAYOUT0, int EPI0, int LAYOUT1, int EPI1>
+__global__ __launch_bounds__(256, 2) void gemm_mid_trio_kernel(GemmArgs g, GemmArgs h, GemmArgs k, int first, int second) {
+    __shared__ __align__(1024) char sm[MID_LDS];
+    if ((int)blockIdx.x < first) mid_tile<LAYOUT0, EPI0>(g, blockIdx.x, sm);
+    else mid_tile<LAYOUT1, EPI1>((int)blockIdx.x < second ? h : k, blockIdx.x - ((int)blockIdx.x < second ? first : second), sm);
 }
 
 static inline int mid_grid(const GemmArgs& g) { return XCDS * ((g.mblocks * g.nblocks * g.splits + XCDS - 1) / XCDS); }
@@ -357,32 +364,44 @@ struct Tiles {
     double us;
 };
 
-static inline Tiles tiles_of(bool mid, long long M, long long N, long long K, int n_factor, int splits, bool partials) {
+constexpr double MID_START = 4.0, MID_STEP = 1.0, MID_STEP_ALONE = 0.8;     // us; two workgroups on a CU, or one
+constexpr double WIDE_START = 7.0, WIDE_STEP = 1.3;
+
+// Writing and reading `elements` of fp32 partials, and the launch that adds them.
+static inline double partials_us(double elements) { return 4.0 + elements * 8 / 8e6; }
+
+// n_cols: columns of the result per 256 columns of B (128 for the gated products).
+static inline Tiles tiles_of(bool mid, long long M, long long N, long long K, int n_cols, int splits, bool partials) {
     Tiles t{};
     t.mid = mid;
-    const int side = mid ? MBM : WBM;
-    t.mblocks = (int)((M + side - 1) / side);
-    t.nblocks = (int)((N + side / n_factor - 1) / (side / n_factor));
+    const int side = mid ? MBM : WBM, cols = mid ? n_cols / 2 : n_cols;
+    t.mblocks = (int)((unsigned long long)(M + side - 1) / (unsigned)side);
+    t.nblocks = (int)((unsigned long long)(N + cols - 1) / (unsigned)cols);
     t.splits = splits;
-    const long long steps = ((K + WBK - 1) / WBK + splits - 1) / splits, slots = mid ? MID_WORKGROUPS : WIDE_WORKGROUPS;
-    const long long items = (long long)t.mblocks * t.nblocks * splits, rounds = (items + slots - 1) / slots;
-    t.us = rounds * (mid ? 4.0 + (items > WIDE_WORKGROUPS ? 1.0 : 0.8) * steps : 7.0 + 1.3 * steps);
-    if (partials) t.us += 4.0 + (double)splits * M * N * 8 / 8e6;
+    const unsigned all = (unsigned)((K + WBK - 1) / WBK), steps = (all + splits - 1) / (unsigned)splits;
+    const long long items = (long long)t.mblocks * t.nblocks * splits;
+    if (mid) t.us = (double)((items + MID_WORKGROUPS - 1) / MID_WORKGROUPS) *
+                    (MID_START + (items > WIDE_WORKGROUPS ? MID_STEP : MID_STEP_ALONE) * steps);
+    else t.us = (double)((items + WIDE_WORKGROUPS - 1) / WIDE_WORKGROUPS) * (WIDE_START + WIDE_STEP * steps);
+    if (partials) t.us += partials_us((double)splits * M * N);
     return t;
 }
 
-static inline Tiles plan(long long M, long long N, long long K, int n_factor) {
-    const Tiles wide = tiles_of(false, M, N, K, n_factor, 1, false), mid = tiles_of(true, M, N, K, n_factor, 1, false);
+static inline Tiles plan(long long M, long long N, long long K, int n_cols = WBN) {
+    const Tiles wide = tiles_of(false, M, N, K, n_cols, 1, false), mid = tiles_of(true, M, N, K, n_cols, 1, false);
     return mid.us < wide.us ? mid : wide;
 }
 
+constexpr int SPLITS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+
 // The same with K splits of the 128 x 128 tiles.
 static inline Tiles plan_deep(long long M, long long N, long long K) {
-    Tiles best = plan(M, N, K, 1);
-    const long long most = std::min(16ll, (K + WBK - 1) / WBK / 4);
+    Tiles best = plan(M, N, K);
     if (best.us < 12.0) return best;              // (about what a split's start and end and its sum take)
-    for (int s = 2; s <= most; s++) {
-        const Tiles t = tiles_of(true, M, N, K, 1, s, true);
+    for (int s : SPLITS) {
+        if (s == 1) continue;
+        if (s > 16 || s * 4 * WBK > K) break;
+        const Tiles t = tiles_of(true, M, N, K, WBN, s, true);
         if (t.us < best.us) best = t;
     }
     return best;
@@ -390,14 +409,12 @@ static inline Tiles plan_deep(long long M, long long N, long long K) {
 
 // A product of fp32 partials, or (not `always`) one that 256 x 256 tiles without a split finish in place.
 static inline Tiles plan_split(long long M, long long N, long long K, bool always) {
-    static const int candidates[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
     Tiles best{};
     best.us = 1e30;
-    const long long most = std::max(1ll, (K + WBK - 1) / WBK / 4);
-    for (int s : candidates) {
-        if (s > most) break;
+    for (int s : SPLITS) {
+        if (s > 1 && s * 4ll * WBK > K) break;
         for (int mid = 0; mid < 2; mid++) {
-            const Tiles t = tiles_of(mid, M, N, K, 1, s, always || mid || s > 1);
+            const Tiles t = tiles_of(mid, M, N, K, WBN, s, always || mid || s > 1);
             if (t.us < best.us) best = t;
         }
     }

@@ -53,7 +53,7 @@ SmPlan sm_plan(long long N, int V, int d, bool backward) {
     p.vpad = (int)(blocks * WBN);
     // The number of labels is not known here: x W^T is planned for all rows, dx and dW for half of them.
     const long long half = (N + 1) / 2;
-    const Tiles lw = tiles_of(false, N, p.piece, d, 1, 1, false), lm = tiles_of(true, N, p.piece, d, 1, 1, false);
+    const Tiles lw = tiles_of(false, N, p.piece, d, WBN, 1, false), lm = tiles_of(true, N, p.piece, d, WBN, 1, false);
     p.logits = lm.us < lw.us ? lm : lw;
     p.dx = plan_split(half, d, p.piece, true);
     p.dw = plan_split(p.piece, d, half, false);
@@ -288,55 +288,66 @@ __global__ __launch_bounds__(1024) void sm_join_kernel(SoftmaxLossArgs a, const 
     }
 }
 
-// dx of the rows with a label: the K splits' sums, scaled and rounded once.
-__global__ __launch_bounds__(256) void sm_dx_kernel(SoftmaxLossArgs a, const int* rows, const int* index,
-                                                    const float* partial, int mid_splits) {
-    const int count = *rows, ch = a.d / 8;
-    const float factor = a.scale * ((const float*)rows)[1];
-    const int splits = mid_splits > 0 ? mid_splits : acc_splits((count + WBM - 1) / WBM * ((a.d + WBN - 1) / WBN));
+// What ends a piece: its dW (the K splits' sums, unless finished in place), its bias gradient and, with the last
+// piece, dx of the rows with a label; each scaled and rounded once.  Each has workgroups of its own.
+struct FinishArgs {
+    const int* rows;
+    const int* index;
+    const float *dw_partial, *col_partial, *dx_partial;
+    int dw_splits, dx_splits; // dx_splits 0: those of the wide kernel
+    int v0, nv, ld_col;
+    bool mid;                 // col_partial is that of 128-row tiles
+    int dw_blocks, col_blocks;
+};
+
+__global__ __launch_bounds__(256) void sm_finish_kernel(SoftmaxLossArgs a, FinishArgs f) {
+    const float top = ((const float*)f.rows)[1], factor = a.scale * top;
+    int block = blockIdx.x;
+    if (block < f.dw_blocks) {
+        const int ch = a.d / 4;
+        const long long per = (long long)f.nv * a.d;
+        for (long long i = (long long)block * 256 + threadIdx.x; i < (long long)f.nv * ch; i += (long long)f.dw_blocks * 256) {
+            const long long r = i / ch;
+            const int c = (int)(i % ch) * 4;
+            const float* p = f.dw_partial + r * a.d + c;
+            floatx4 s = *(const floatx4*)p;
+            for (int k = 1; k < f.dw_splits; k++) s += *(const floatx4*)(p + k * per);
+            s *= factor;
+            *(uint2*)((uint16_t*)a.dw + (f.v0 + r) * a.ld_w + c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
+        }
+        return;
+    }
+    block -= f.dw_blocks;
+    const int count = *f.rows;
+    if (block < f.col_blocks) {
+        const int c = block * 256 + threadIdx.x;
+        if (c >= f.nv) return;
+        const int side = f.mid ? MBM : WBM, parts = 2 * ((count + side - 1) / side);
+        // (in 64 bits: softmax sums and label counts cancel, and the parts are hundreds)
+        double s = 0.;
+#pragma unroll 8
+        for (int p = 0; p < parts; p++) s += f.col_partial[(long long)p * f.ld_col + c];
+        a.dbias[f.v0 + c] = (float)(s * top);
+        return;
+    }
+    block -= f.col_blocks;
+    const int blocks = gridDim.x - f.dw_blocks - f.col_blocks, ch = a.d / 8;
+    const int splits = f.dx_splits > 0 ? f.dx_splits : acc_splits((count + WBM - 1) / WBM * ((a.d + WBN - 1) / WBN));
     const long long per = (long long)count * a.d;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)count * ch;
-         i += (long long)gridDim.x * 256) {
+    for (long long i = (long long)block * 256 + threadIdx.x; i < (long long)count * ch; i += (long long)blocks * 256) {
         const long long r = i / ch;
         const int c = (int)(i % ch) * 8;
-        const float* p = partial + r * a.d + c;
+        const float* p = f.dx_partial + r * a.d + c;
         floatx4 lo = *(const floatx4*)p, hi = *(const floatx4*)(p + 4);
+#pragma unroll 4
         for (int k = 1; k < splits; k++) {
             lo += *(const floatx4*)(p + k * per);
             hi += *(const floatx4*)(p + k * per + 4);
         }
         lo *= factor;
         hi *= factor;
-        *(uint4*)((uint16_t*)a.dx + index[r] * a.ld_x + c) =
+        *(uint4*)((uint16_t*)a.dx + f.index[r] * a.ld_x + c) =
             make_uint4(pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3]));
-    }
-}
-
-// A piece's dW = scale sum of the K splits, rounded once; the last workgroups add up its bias gradient.
-__global__ __launch_bounds__(256) void sm_dw_kernel(SoftmaxLossArgs a, const int* rows, const float* partial,
-                                                    int splits, int v0, int nv, const float* colp, int ld_col,
-                                                    int row_tile, int sum_blocks) {
-    if ((int)blockIdx.x >= sum_blocks) {
-        const int c = ((int)blockIdx.x - sum_blocks) * 256 + threadIdx.x;
-        if (c >= nv) return;
-        const int parts = 2 * ((*rows + row_tile - 1) / row_tile);
-        // (in 64 bits: softmax sums and label counts cancel, and the parts are hundreds)
-        double s = 0.;
-#pragma unroll 8
-        for (int p = 0; p < parts; p++) s += colp[(long long)p * ld_col + c];
-        a.dbias[v0 + c] = (float)(s * ((const float*)rows)[1]);
-        return;
-    }
-    const int ch = a.d / 4;
-    const float factor = a.scale * ((const float*)rows)[1];
-    const long long per = (long long)nv * a.d;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)nv * ch; i += (long long)sum_blocks * 256) {
-        const long long r = i / ch;
-        const int c = (int)(i % ch) * 4;
-        floatx4 s = *(const floatx4*)(partial + r * a.d + c);
-        for (int k = 1; k < splits; k++) s += *(const floatx4*)(partial + k * per + r * a.d + c);
-        s *= factor;
-        *(uint2*)((uint16_t*)a.dw + (v0 + r) * a.ld_w + c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
     }
 }
 
@@ -451,21 +462,6 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         x.b_rows = nv;
         x.accumulate = i > 0;
         x.partial = (float*)(ws + p.dxp);
-        if (p.dx.mid) {
-            x.mblocks = (int)((a.N + MBM - 1) / MBM);
-            x.nblocks = (a.d + MBN - 1) / MBN;
-            x.splits = p.dx.splits;
-            e = mid_launch<GEMM_NN, GEMM_EPI_ACC>(x, s);
-        } else {
-            x.mblocks = (int)((a.N + WBM - 1) / WBM);
-            x.nblocks = (a.d + WBN - 1) / WBN;
-            x.splits = 1;
-            const int grid = XCDS * ((std::max(x.mblocks * x.nblocks, 256) + XCDS - 1) / XCDS);
-            gemm_wide_kernel<GEMM_NN, GEMM_EPI_ACC, false><<<grid, 512, 0, s>>>(x);
-            e = hipGetLastError();
-        }
-        if (e != hipSuccess) break;
-
         GemmArgs w{};                                    // the piece's dW = dz^T x
         w.layout = GEMM_TN;
         w.M = nv;
@@ -484,22 +480,53 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         const int side = p.dw.mid ? MBM : WBM;
         w.mblocks = (nv + side - 1) / side;
         w.nblocks = (a.d + side - 1) / side;
-        // (without a split the 256 x 256 tiles finish the sums in place)
-        const bool direct = w.splits == 1 && !p.dw.mid;
-        e = p.dw.mid ? mid_launch<GEMM_TN, GEMM_EPI_ROWS>(w, s)
-            : direct ? wide_launch<GEMM_TN, GEMM_EPI_ROWS_DIRECT, false>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_ROWS, false>(w, s);
+        // (without a split the 256 x 256 tiles finish dW in place)
+        const bool direct = w.splits == 1 && !p.dw.mid, last = i == p.pieces - 1;
+        if (p.dx.mid) {
+            x.mblocks = (int)((a.N + MBM - 1) / MBM);
+            x.nblocks = (a.d + MBN - 1) / MBN;
+            x.splits = p.dx.splits;
+        } else {
+            x.mblocks = (int)((a.N + WBM - 1) / WBM);
+            x.nblocks = (a.d + WBN - 1) / WBN;
+            x.splits = 1;                                // (chosen on the device, from the rows with a label)
+        }
+        if (p.dx.mid && p.dw.mid) {
+            gemm_mid_pair_kernel<GEMM_NN, GEMM_EPI_ACC, GEMM_TN, GEMM_EPI_ROWS><<<mid_grid(x) + mid_grid(w), 256, 0, s>>>(x, w, mid_grid(x));
+            e = hipGetLastError();
+        } else {
+            if (p.dx.mid) {
+                e = mid_launch<GEMM_NN, GEMM_EPI_ACC>(x, s);
+            } else {
+                const int grid = XCDS * ((std::max(x.mblocks * x.nblocks, 256) + XCDS - 1) / XCDS);
+                gemm_wide_kernel<GEMM_NN, GEMM_EPI_ACC, false><<<grid, 512, 0, s>>>(x);
+                e = hipGetLastError();
+            }
+            if (e != hipSuccess) break;
+            e = p.dw.mid ? mid_launch<GEMM_TN, GEMM_EPI_ROWS>(w, s)
+                : direct ? wide_launch<GEMM_TN, GEMM_EPI_ROWS_DIRECT, false>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_ROWS, false>(w, s);
+        }
         if (e != hipSuccess) break;
-        const int sums = direct ? 0 : (int)std::min(((long long)nv * a.d / 4 + 255) / 256, 8192ll);
-        const int cols = a.dbias ? (nv + 255) / 256 : 0;
-        if (sums + cols == 0) continue;
-        sm_dw_kernel<<<sums + cols, 256, 0, s>>>(a, rows, w.partial, w.splits, v0, nv, g.col_partial, (int)g.N, p.logits.mid ? MBM : WBM, sums);
+        FinishArgs f{};
+        f.rows = rows;
+        f.index = (const int*)(ws + p.index);
+        f.dw_partial = w.partial;
+        f.col_partial = g.col_partial;
+        f.dx_partial = x.partial;
+        f.dw_splits = w.splits;
+        f.dx_splits = p.dx.mid ? p.dx.splits : 0;
+        f.v0 = v0;
+        f.nv = nv;
+        f.ld_col = (int)g.N;
+        f.mid = p.logits.mid;
+        f.dw_blocks = direct ? 0 : (int)std::min(((long long)nv * a.d / 4 + 255) / 256, 8192ll);
+        f.col_blocks = a.dbias ? (nv + 255) / 256 : 0;
+        const int dx_blocks = last ? (int)std::min((a.N * (a.d / 8) + 255) / 256, 8192ll) : 0;
+        if (f.dw_blocks + f.col_blocks + dx_blocks == 0) continue;
+        sm_finish_kernel<<<f.dw_blocks + f.col_blocks + dx_blocks, 256, 0, s>>>(a, f);
         e = hipGetLastError();
     }
-    if (e != hipSuccess) return e;
-    const int grid = (int)std::min((a.N * (a.d / 8) + 255) / 256, 8192ll);
-    sm_dx_kernel<<<grid, 256, 0, s>>>(a, rows, (const int*)(ws + p.index), (const float*)(ws + p.dxp),
-                                   p.dx.mid ? p.dx.splits : 0);
-    return hipGetLastError();
+    return e;
 }
 
 }  // namespace mtgr
