@@ -97,10 +97,18 @@ static hipError_t deep_product(GemmArgs g, const Tiles& t, float* partial, hipSt
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Whether the second product is done by the kernel for few rows.  Its waves go through k alone (no launch adds
+// partials), so that a deep k favours the tiles split over k: 64 .. 128 tokens, f = 1408: 8.7 us, 11.2 there; f = 2816:
+// 15, 11.3; up to 32 tokens, f = 2816: 7.5 .. 10.8, 9.6 .. 10.1; 312 tokens, f = 2048: 11.5, 14.4.
+static bool rows_output(long long T, int d, int f) {
+    if (!ffn_rows_fit(T, d, FFN_OUT_COLUMNS)) return false;
+    const double us = T <= 16 ? 1.0 + 1.4 * f / 512 : 1.5 + (T <= 32 ? 0.85 : 1.25) * f / 256;
+    return us < plan_deep(T, d, f).us;
+}
+
 // Workspace of the forward: h, where the caller does not keep it, and the second product's partials.
 size_t ffn_fwd_workspace_bytes(long long T, int d, int f, bool save) {
-    const bool few = ffn_rows_fit(T, d, FFN_OUT_COLUMNS);
-    return (save ? 0 : align256((size_t)T * f * 2)) + (few ? 0 : partial_bytes(plan_deep(T, d, f), T, d));
+    return (save ? 0 : align256((size_t)T * f * 2)) + (rows_output(T, d, f) ? 0 : partial_bytes(plan_deep(T, d, f), T, d));
 }
 
 hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
@@ -124,7 +132,7 @@ hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
         else e = a.pre ? wide_launch<GEMM_NN, GEMM_EPI_GATED_SAVE, false>(g, s) : wide_launch<GEMM_NN, GEMM_EPI_GATED, false>(g, s);
     }
     if (e != hipSuccess) return e;
-    if (ffn_rows_fit(a.T, a.d, FFN_OUT_COLUMNS)) return launch_ffn_rows_out(a, s);
+    if (rows_output(a.T, a.d, a.f)) return launch_ffn_rows_out(a, s);
     GemmArgs g = product(GEMM_NN, a.T, a.d, a.f, a.h, a.ld_h, a.w_out, a.ld_wout, a.y, a.ld_y);
     g.R = a.residual;
     g.ldr = a.ld_r;

@@ -149,9 +149,10 @@ hipError_t rows_launch(const RowsArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Up to one workgroup of 64 rows per CU: beyond that the tiles of gemm_mid.h read the weights less often (312
-// tokens, d = 768, f = 2048: hidden, 320 workgroups, 15.2 us here and 12.2 there; output, 120 workgroups,
-// 11.4 and 25.7; 1,024 tokens, d = 512, f = 1408: 704 workgroups, 18 and 9.4; 256 workgroups, 10 and 20).
+// Up to one workgroup of 64 rows per CU: beyond that the tiles of gemm_mid.h read the weights less often (gated
+// product of 64 tokens, d = 1024, f = 2816, 176 workgroups: 10.9 us here and 13.0 there; 600 tokens, d = 256,
+// f = 704, 220: 6.3 and 6.3; 312 tokens, d = 768, f = 2048, 320: 15.2 and 12.2; 1,024 tokens, d = 512, f = 1408,
+// 704: 18 and 9.4).
 bool ffn_rows_fit(long long T, int N, int columns) {
     return T <= 16384 && (T + 63) / 64 * ((N + columns - 1) / columns) <= 256;
 }

@@ -5,9 +5,12 @@
 // as 4 x 4 blocks of 16 x 16, transposed as in gemm_wide.h.  Two LDS stages (64 KB) let two workgroups share a
 // CU, so that one's barriers, copies and epilogue run under the other's matrix instructions.  One barrier per
 // step: it hands over the stage that has landed and frees the other one for the copies of the next step.
-// (A workgroup alone on its CU takes 0.85 us per step, for 0.2 us of matrix work; four stages, or operands read
-// a half step ahead, did not change that, so products of few tiles are split over k instead.)  Epilogues work on a lane's four consecutive columns of a row, without staging: at
-// these sizes the results stay in the L2 caches, which join the 32-byte pieces.
+// (A workgroup alone on its CU takes 0.8 us per step, for 0.2 us of matrix work: a chain of the wait, the barrier,
+// the copies and the reads.  Without the matrix instructions or the reads it was as long, without the copies
+// 0.15 us shorter.  Four stages, operands read a half step ahead, eight waves, and copies spread between the matrix
+// instructions, 2 to 15 % slower, gained nothing, so products of few tiles are split over k instead.)  Epilogues
+// work on a lane's four consecutive columns of a row, without staging: at these sizes the results stay in the L2
+// caches, which join the 32-byte pieces.
 #pragma once
 
 #include <type_traits>

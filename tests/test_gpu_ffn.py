@@ -53,7 +53,7 @@ def check_forward(T, d, f, residual=False, wide=0):
 @pytest.mark.parametrize("T, d, f", [
     (1, 32, 32), (1, 512, 1408), (2, 96, 160), (5, 1024, 2816), (15, 64, 96), (16, 256, 704), (17, 256, 704),
     (31, 544, 416), (64, 128, 352), (65, 768, 2048), (255, 160, 288), (256, 64, 128), (257, 96, 1120), (700, 512, 1408),
-    (2049, 256, 672), (9000, 128, 352), (20011, 64, 704),
+    (2049, 256, 672), (9000, 128, 352), (20011, 64, 704), (33, 96, 2816), (127, 1024, 2848),
 ])
 def test_forward(T, d, f):
     check_forward(T, d, f, residual=T % 2 == 1)
