@@ -103,10 +103,11 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
     // in the XCD's L2; the softmax products stream the classes (B) past a few m blocks of rows.
     constexpr bool DEEP_B = B_SHORT;
     constexpr int NTILE = GATED ? WBN / 2 : WBN;  // columns of C per tile
+    constexpr int WAVE_M = GATED ? 64 : 128, WAVE_N = GATED ? 128 : 64;      // a wave's part of a tile
     __shared__ __align__(1024) char sm[5 * WSLOT];
 
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int wm = w & 1, wn = w >> 1;
+    const int wm = GATED ? w & 3 : w & 1, wn = GATED ? w >> 2 : w >> 1;
     int M = (int)g.M, K = (int)g.K, mblocks = g.mblocks;
     const int N = (int)g.N;
     if constexpr (DYN) {
@@ -190,11 +191,11 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
 #pragma unroll
         for (int q = 0; q < WQ; q++) vo[q] = (uint32_t)(min(16 * q + r, kvalid - 1) * ld + 8 * c) * 2u;
     };
-    // The gated product's B: the wave quarter q of a stage holds gate columns 32 q .. + 31 of the tile,
-    // then the up columns of the same numbers (hidden columns past `hvalid` clamp)
+    // The gated product's B: half q of a stage's columns holds gate columns 64 q .. + 63 of the tile, then the
+    // up columns of the same numbers (hidden columns past `hvalid` clamp)
     auto gated_offsets = [&](uint32_t* vo, long long ld, int h0, int hvalid, int kvalid) {
         const int ln = once(lane), r = 2 * w + (ln >> 5), c = (ln & 31) ^ swz<32>(r);
-        const int col = 8 * min(4 * (c >> 3) + (c & 3), (hvalid >> 3) - 1) + h0 + ((c & 4) ? N : 0);
+        const int col = 8 * min(8 * (c >> 4) + (c & 7), (hvalid >> 3) - 1) + h0 + ((c & 8) ? N : 0);
 #pragma unroll
         for (int q = 0; q < WQ; q++) vo[q] = (uint32_t)(min(16 * q + r, kvalid - 1) * ld + col) * 2u;
     };
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
     // k-contiguous rows r0 + 16 b: chunk (4 p + l / 16) ^ swz(r0) for k32 part p, i.e. the offset of
     // part 0 XOR 64 p, block b at + 2048 b.
     // k-row column block c0 + 16 b: supplier rows of the two halves (k + 0..3, + 4..7) of part 0;
-    // part 1 is 16384 bytes further, block b the offset XOR 32 b (c0 is a multiple of 64).
+    // part 1 is 16384 bytes further, block b the offset XOR 32 b (c0 is a multiple of its 64 or 128 columns).
     const int lr = lane & 15, lg = lane >> 4;
     auto kc_base = [&](int r0) { return lds0 + 16u * (uint32_t)((r0 + lr) * 8 + (lg ^ swz<8>(lr))); };
     auto kr_base = [&](int c0, int half) {
@@ -278,10 +279,10 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
         return lds0 + 16u * (uint32_t)tile_chunk<32>(row, colx >> 3) + 2u * (uint32_t)(colx & 7);
     };
     uint32_t rm[2], rn[2];
-    rm[0] = A_KR ? kr_base(128 * wm, 0) : kc_base(128 * wm);
-    rm[1] = A_KR ? kr_base(128 * wm, 1) : 0;
-    rn[0] = B_KR ? kr_base(64 * wn, 0) : kc_base(64 * wn);
-    rn[1] = B_KR ? kr_base(64 * wn, 1) : 0;
+    rm[0] = A_KR ? kr_base(WAVE_M * wm, 0) : kc_base(WAVE_M * wm);
+    rm[1] = A_KR ? kr_base(WAVE_M * wm, 1) : 0;
+    rn[0] = B_KR ? kr_base(WAVE_N * wn, 0) : kc_base(WAVE_N * wn);
+    rn[1] = B_KR ? kr_base(WAVE_N * wn, 1) : 0;
     typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
     auto read_frag = [&](auto kr, const uint32_t (&r)[2], uint32_t slot, auto pc, auto bc) {
         constexpr uint32_t P = decltype(pc)::value, BL = decltype(bc)::value;
@@ -296,11 +297,14 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
             return *(const lds_bf16x8*)(uintptr_t)(((r[0] + slot) ^ (64u * P)) + 2048u * BL);
         }
     };
-    using AK = std::integral_constant<bool, A_KR>;
-    using BK = std::integral_constant<bool, B_KR>;
+    auto read_a = [&](uint32_t slot, auto pc, auto bc) { return read_frag(std::integral_constant<bool, A_KR>{}, rm, slot, pc, bc); };
+    auto read_b = [&](uint32_t slot, auto pc, auto bc) { return read_frag(std::integral_constant<bool, B_KR>{}, rn, slot, pc, bc); };
+    // the operand of the wave's eight blocks (A; B in the gated products) and that of its four
+    auto read_m = [&](uint32_t slot, auto pc, auto bc) { if constexpr (GATED) return read_b(slot, pc, bc); else return read_a(slot, pc, bc); };
+    auto read_n = [&](uint32_t slot, auto pc, auto bc) { if constexpr (GATED) return read_a(slot, pc, bc); else return read_b(slot, pc, bc); };
 
     floatx4 acc[WNN][WNM];
-    bf16x8 fm[WNM], fn[2][WNN];       // operands: m blocks (four ahead), n blocks of both k32 parts
+    bf16x8 fm[WNM], fn[2][WNN];       // operands: the eight blocks (four ahead), the four blocks of both k32 parts
     float csum[8];
     const bool colsum = COLSUM && mb == 0;
     auto colsum_step = [&](uint32_t sb) {
@@ -315,22 +319,22 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
             }
         }
     };
-    // Slot b of k32 part P: the four MFMAs of m block b, m block b + 4 read ahead (from part NP in
-    // slot nsa once past the part's end), and in slots 4 and 5 the n blocks of the next part.
-    auto slot = [&](auto pc, auto bc, uint32_t csa, uint32_t nsa, uint32_t nsb) {
+    // Slot b of k32 part P: the four MFMAs of m block b (gated: n block b), block b + 4 read ahead (from part NP in
+    // slot nsm once past the part's end), and in slots 4 and 5 the other operand's blocks of the next part.
+    auto slot = [&](auto pc, auto bc, uint32_t csm, uint32_t nsm, uint32_t nsn) {
         constexpr int P = decltype(pc)::value, b = decltype(bc)::value, NP = P ^ 1;
         if constexpr (b < 4) {
-            fm[b + 4] = read_frag(AK{}, rm, csa, IC<P>{}, IC<b + 4>{});
+            fm[b + 4] = read_m(csm, IC<P>{}, IC<b + 4>{});
         } else {
             if constexpr (b < 6) {
-                fn[NP][2 * (b - 4)] = read_frag(BK{}, rn, nsb, IC<NP>{}, IC<2 * (b - 4)>{});
-                fn[NP][2 * (b - 4) + 1] = read_frag(BK{}, rn, nsb, IC<NP>{}, IC<2 * (b - 4) + 1>{});
+                fn[NP][2 * (b - 4)] = read_n(nsn, IC<NP>{}, IC<2 * (b - 4)>{});
+                fn[NP][2 * (b - 4) + 1] = read_n(nsn, IC<NP>{}, IC<2 * (b - 4) + 1>{});
             }
-            fm[b - 4] = read_frag(AK{}, rm, nsa, IC<NP>{}, IC<b - 4>{});
+            fm[b - 4] = read_m(nsm, IC<NP>{}, IC<b - 4>{});
         }
 #pragma unroll
         for (int a = 0; a < WNN; a++)
-            acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fn[P][a], fm[b], acc[a][b], 0, 0, 0);
+            acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(GATED ? fm[b] : fn[P][a], GATED ? fn[P][a] : fm[b], acc[a][b], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
 
@@ -375,38 +379,40 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
 #pragma unroll
             for (int e = 0; e < 8; e++) csum[e] = 0.f;
         }
-        fn[0][0] = read_frag(BK{}, rn, slot_b(0), IC<0>{}, IC<0>{});
-        fm[0] = read_frag(AK{}, rm, slot_a(0), IC<0>{}, IC<0>{});
-        fn[0][1] = read_frag(BK{}, rn, slot_b(0), IC<0>{}, IC<1>{});
-        fn[0][2] = read_frag(BK{}, rn, slot_b(0), IC<0>{}, IC<2>{});
-        fn[0][3] = read_frag(BK{}, rn, slot_b(0), IC<0>{}, IC<3>{});
-        fm[1] = read_frag(AK{}, rm, slot_a(0), IC<0>{}, IC<1>{});
-        fm[2] = read_frag(AK{}, rm, slot_a(0), IC<0>{}, IC<2>{});
-        fm[3] = read_frag(AK{}, rm, slot_a(0), IC<0>{}, IC<3>{});
+        const uint32_t first_m = GATED ? slot_b(0) : slot_a(0), first_n = GATED ? slot_a(0) : slot_b(0);
+        fn[0][0] = read_n(first_n, IC<0>{}, IC<0>{});
+        fm[0] = read_m(first_m, IC<0>{}, IC<0>{});
+        fn[0][1] = read_n(first_n, IC<0>{}, IC<1>{});
+        fn[0][2] = read_n(first_n, IC<0>{}, IC<2>{});
+        fn[0][3] = read_n(first_n, IC<0>{}, IC<3>{});
+        fm[1] = read_m(first_m, IC<0>{}, IC<1>{});
+        fm[2] = read_m(first_m, IC<0>{}, IC<2>{});
+        fm[3] = read_m(first_m, IC<0>{}, IC<3>{});
         // Step i, with X the deep operand (A) and Y the other one: copies of the second half of Y(i+1), then
         // X(i+2), then, behind the barrier that frees its slot, the first half of Y(i+2).
         uint32_t sa = slot_a(0), sb = slot_b(0), sa1 = slot_a(1), sb1 = slot_b(1), sx2 = slot_a(2);
         for (int i = 0; i < nk; i++) {
             const bool cb = i > 0 && i + 1 < nk, ca = i > 0 && i + 2 < nk, cn = i + 2 < nk;
+            const uint32_t cm = GATED ? sb : sa, cf = GATED ? sa : sb, nm = GATED ? sb1 : sa1, nf = GATED ? sa1 : sb1;
             colsum_step(sb);
-            slot(IC<0>{}, IC<0>{}, sa, sa, sb);
+            slot(IC<0>{}, IC<0>{}, cm, cm, cf);
             if (cb) copy(IC<2>{}, IC<3>{}, Y_{}, DEEP_B ? sa1 : sb1, i + 1);
-            slot(IC<0>{}, IC<1>{}, sa, sa, sb);
-            slot(IC<0>{}, IC<2>{}, sa, sa, sb);
+            slot(IC<0>{}, IC<1>{}, cm, cm, cf);
+            slot(IC<0>{}, IC<2>{}, cm, cm, cf);
             if (cb) copy(IC<3>{}, IC<4>{}, Y_{}, DEEP_B ? sa1 : sb1, i + 1);
-            slot(IC<0>{}, IC<3>{}, sa, sa, sb);
-            slot(IC<0>{}, IC<4>{}, sa, sa, sb);
+            slot(IC<0>{}, IC<3>{}, cm, cm, cf);
+            slot(IC<0>{}, IC<4>{}, cm, cm, cf);
             if (ca) copy(IC<0>{}, IC<1>{}, X_{}, sx2, i + 2);
-            slot(IC<0>{}, IC<5>{}, sa, sa, sb);
-            slot(IC<0>{}, IC<6>{}, sa, sa, sb);
+            slot(IC<0>{}, IC<5>{}, cm, cm, cf);
+            slot(IC<0>{}, IC<6>{}, cm, cm, cf);
             if (ca) copy(IC<1>{}, IC<2>{}, X_{}, sx2, i + 2);
-            slot(IC<0>{}, IC<7>{}, sa, sa, sb);
-            slot(IC<1>{}, IC<0>{}, sa, sa1, sb1);
+            slot(IC<0>{}, IC<7>{}, cm, cm, cf);
+            slot(IC<1>{}, IC<0>{}, cm, nm, nf);
             if (ca) copy(IC<2>{}, IC<3>{}, X_{}, sx2, i + 2);
-            slot(IC<1>{}, IC<1>{}, sa, sa1, sb1);
-            slot(IC<1>{}, IC<2>{}, sa, sa1, sb1);
+            slot(IC<1>{}, IC<1>{}, cm, nm, nf);
+            slot(IC<1>{}, IC<2>{}, cm, nm, nf);
             if (ca) copy(IC<3>{}, IC<4>{}, X_{}, sx2, i + 2);
-            slot(IC<1>{}, IC<3>{}, sa, sa1, sb1);
+            slot(IC<1>{}, IC<3>{}, cm, nm, nf);
             // stage i + 1 has landed; X(i+2) may still be in flight, in step 0 also the previous
             // tile's stores (and the class bias), which were issued between the copies of stage 1 and X(2)
             if (cn) {
@@ -418,12 +424,12 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
             lds_barrier_seen();                 // ... everywhere, and stage i is no longer read
             if (ragged && i + 2 == nk) zero_tail(sa1, sb1);
             // (after the last step the reads touch a slot that may be changing and are not used)
-            slot(IC<1>{}, IC<4>{}, sa, sa1, sb1);
-            slot(IC<1>{}, IC<5>{}, sa, sa1, sb1);
+            slot(IC<1>{}, IC<4>{}, cm, nm, nf);
+            slot(IC<1>{}, IC<5>{}, cm, nm, nf);
             if (cn) copy(IC<0>{}, IC<1>{}, Y_{}, DEEP_B ? sa : sb, i + 2);
-            slot(IC<1>{}, IC<6>{}, sa, sa1, sb1);
+            slot(IC<1>{}, IC<6>{}, cm, nm, nf);
             if (cn) copy(IC<1>{}, IC<2>{}, Y_{}, DEEP_B ? sa : sb, i + 2);
-            slot(IC<1>{}, IC<7>{}, sa, sa1, sb1);
+            slot(IC<1>{}, IC<7>{}, cm, nm, nf);
             const uint32_t t = sa, u = sb;
             sa = sa1;
             sb = sb1;
@@ -433,12 +439,13 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
         }
 
         // ---- epilogue.  acc[a][b] holds C of row m0 + 128 wm + 16 b + l % 16, columns
-        // n0 + 64 wn + 16 a + 4 (l / 16) + 0..3.  Each wave passes its part through 4 KB of its own
+        // n0 + 64 wn + 16 a + 4 (l / 16) + 0..3 (gated: row m0 + 64 wm + 16 a + l % 16, stage columns
+        // 128 wn + 16 b + 4 (l / 16) + 0..3).  Each wave passes its part through 4 KB of its own
         // in the fifth slot (no barrier), so that a store instruction writes whole 128-byte lines (or
         // 256-byte rows of fp32 partials), and the first stages of the workgroup's next tile are
         // copied meanwhile.
         const int el = once(lane), er = el & 15, eg = el >> 4;
-        const int em = m0 + 128 * wm, en = n0 + 64 * wn, hn = n0 + 32 * wn;
+        const int em = m0 + WAVE_M * wm, en = n0 + 64 * wn;
         const int tile_mb = mb, tile_nb = nb;          // (mb, nb, m0 and n0 move on to the next tile below)
         char* stg = sm + WSTAGING + 4096 * w;
         // fp32 rows of block b: 16-byte chunk c (of 16) of row r at chunk c ^ r
@@ -649,52 +656,37 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
                 wave_lds_fence();
             }
         } else if constexpr (GATED) {
-            // acc[0..1] hold gate columns hn + 16 a + 4 (l / 16) + 0..3, acc[2..3] the up columns of the
-            // same numbers.
-            if constexpr (EPI == GEMM_EPI_GATED_SAVE) {
-                // 32 rows at a time: chunks 0..3 of a row are gate columns, 4..7 up columns
+            // acc[a][0..3] hold gate columns en + 16 b + 4 (l / 16) + 0..3, acc[a][4..7] the up columns of the same
+            // numbers.  32 rows at a time: 16-byte chunk c (of 8) of row r at c ^ (r & 7)
+            auto rows_out = [&](int rd, uint16_t* base, long long ld, auto value) {
 #pragma unroll
-                for (int rd = 0; rd < WNM / 2; rd++) {
+                for (int aa = 0; aa < 2; aa++)
 #pragma unroll
-                    for (int bb = 0; bb < 2; bb++)
-#pragma unroll
-                        for (int a = 0; a < WNN; a++) {
-                            const floatx4 v = acc[a][2 * rd + bb];
-                            *(uint2*)(stg + 128 * (16 * bb + er) + 16 * ((2 * a + (eg >> 1)) ^ (er & 7)) + 8 * (eg & 1)) =
-                                make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-                        }
-                    wave_lds_fence();
-                    const int gm = em + 32 * rd + (el >> 3), gn = hn + 8 * (el & 3);
-                    uint16_t* dst = (uint16_t*)g.C + gm * g.ldc + gn + ((el & 4) ? N : 0);
-#pragma unroll
-                    for (int q = 0; q < 4; q++) {
-                        const uint4 v = *(const uint4*)(stg + 128 * (8 * q + (el >> 3)) + 16 * ((el & 7) ^ (el >> 3)));
-                        if (full || (gm + 8 * q < M && gn < N)) store_nt16(dst + 8 * q * g.ldc, &v);
-                    }
-                    wave_lds_fence();
-                }
-            }
-            // h, 64 rows at a time: 16-byte chunk c (of 4) of row r at c ^ (r / 2 & 3)
-#pragma unroll
-            for (int rd = 0; rd < WNM / 4; rd++) {
-#pragma unroll
-                for (int bb = 0; bb < 4; bb++)
-#pragma unroll
-                    for (int a = 0; a < WNN / 2; a++) {
-                        const floatx4 ga = acc[a][4 * rd + bb], up = acc[a + 2][4 * rd + bb];
-                        *(uint2*)(stg + 64 * (16 * bb + er) + 16 * ((2 * a + (eg >> 1)) ^ (er >> 1 & 3)) + 8 * (eg & 1)) =
-                            make_uint2(pack_bf16x2(silu(ga[0]) * up[0], silu(ga[1]) * up[1]),
-                                       pack_bf16x2(silu(ga[2]) * up[2], silu(ga[3]) * up[3]));
+                    for (int b = 0; b < 4; b++) {
+                        const floatx4 v = value(2 * rd + aa, b);
+                        *(uint2*)(stg + 128 * (16 * aa + er) + 16 * ((2 * b + (eg >> 1)) ^ (er & 7)) + 8 * (eg & 1)) =
+                            make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
                     }
                 wave_lds_fence();
-                const int gm = em + 64 * rd + (el >> 2), gn = hn + 8 * (el & 3);
-                uint16_t* dst = (uint16_t*)g.C2 + gm * g.ldc2 + gn;
+                const int gm = em + 32 * rd + (el >> 3), gn = en + 8 * (el & 7);
+                uint16_t* dst = base + gm * ld + gn;
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
-                    const uint4 v = *(const uint4*)(stg + 64 * (16 * q + (el >> 2)) + 16 * ((el & 3) ^ (el >> 3 & 3)));
-                    if (full || (gm + 16 * q < M && gn < N)) store_nt16(dst + 16 * q * g.ldc2, &v);
+                    const uint4 v = *(const uint4*)(stg + 128 * (8 * q + (el >> 3)) + 16 * ((el & 7) ^ (el >> 3)));
+                    if (full || (gm + 8 * q < M && gn < N)) store_nt16(dst + 8 * q * ld, &v);
                 }
                 wave_lds_fence();
+            };
+#pragma unroll
+            for (int rd = 0; rd < 2; rd++) {
+                if constexpr (EPI == GEMM_EPI_GATED_SAVE) {
+                    rows_out(rd, (uint16_t*)g.C, g.ldc, [&](int a, int b) { return acc[a][b]; });
+                    rows_out(rd, (uint16_t*)g.C + N, g.ldc, [&](int a, int b) { return acc[a][b + 4]; });
+                }
+                rows_out(rd, (uint16_t*)g.C2, g.ldc2, [&](int a, int b) {
+                    const floatx4 ga = acc[a][b], up = acc[a][b + 4];
+                    return floatx4{silu(ga[0]) * up[0], silu(ga[1]) * up[1], silu(ga[2]) * up[2], silu(ga[3]) * up[3]};
+                });
             }
         } else if constexpr (!RESIDUAL) {
             if constexpr (GRAD) {
