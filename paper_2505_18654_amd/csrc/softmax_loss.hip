@@ -34,6 +34,7 @@ struct SmPlan {
     int vpad;                 // V rounded up to whole tiles
     Tiles logits;             // of x W^T (forward and backward), dx and dW; which kernel
     Tiles dx, dw;
+    bool direct;              // dW without partials
     size_t rows /* their count, the largest |g| */, counts, tops, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
 };
 
@@ -75,10 +76,12 @@ SmPlan sm_plan(long long N, int V, int d, bool backward) {
     } else {
         p.info = take(sizeof(int4) * npad);
         p.dz = take((size_t)N * p.piece * 2);
-        // fp32 partials (of the wide dx kernel: one split, or as many as make at most 256 tiles)
+        // fp32 partials (of the wide dx kernel: one split, or as many as make at most 256 tiles; none of a dW that
+        // the wide kernel finishes in place)
         const size_t tiles = (size_t)mblocks * ((d + WBN - 1) / WBN);
-        p.dxp = take(std::max<size_t>(std::max<size_t>(tiles, 256) * WBM * WBN, (size_t)p.dx.splits * N * d) * sizeof(float));
-        p.dwp = take((size_t)p.dw.splits * p.piece * d * sizeof(float));
+        p.dxp = take((p.dx.mid ? (size_t)p.dx.splits * N * d : std::max<size_t>(tiles, 256) * WBM * WBN) * sizeof(float));
+        p.direct = p.dw.splits == 1 && !p.dw.mid;
+        p.dwp = take(p.direct ? 0 : (size_t)p.dw.splits * p.piece * d * sizeof(float));
         p.colp = take((size_t)(p.logits.mid ? 4 : 2) * mblocks * p.piece * sizeof(float));
     }
     p.total = at;
@@ -481,7 +484,7 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         w.mblocks = (nv + side - 1) / side;
         w.nblocks = (a.d + side - 1) / side;
         // (without a split the 256 x 256 tiles finish dW in place)
-        const bool direct = w.splits == 1 && !p.dw.mid, last = i == p.pieces - 1;
+        const bool last = i == p.pieces - 1;
         if (p.dx.mid) {
             x.mblocks = (int)((a.N + MBM - 1) / MBM);
             x.nblocks = (a.d + MBN - 1) / MBN;
@@ -504,7 +507,7 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
             }
             if (e != hipSuccess) break;
             e = p.dw.mid ? mid_launch<GEMM_TN, GEMM_EPI_ROWS>(w, s)
-                : direct ? wide_launch<GEMM_TN, GEMM_EPI_ROWS_DIRECT, false>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_ROWS, false>(w, s);
+                : p.direct ? wide_launch<GEMM_TN, GEMM_EPI_ROWS_DIRECT, false>(w, s) : wide_launch<GEMM_TN, GEMM_EPI_ROWS, false>(w, s);
         }
         if (e != hipSuccess) break;
         FinishArgs f{};
@@ -519,7 +522,7 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         f.nv = nv;
         f.ld_col = (int)g.N;
         f.mid = p.logits.mid;
-        f.dw_blocks = direct ? 0 : (int)std::min(((long long)nv * a.d / 4 + 255) / 256, 8192ll);
+        f.dw_blocks = p.direct ? 0 : (int)std::min(((long long)nv * a.d / 4 + 255) / 256, 8192ll);
         f.col_blocks = a.dbias ? (nv + 255) / 256 : 0;
         const int dx_blocks = last ? (int)std::min((a.N * (a.d / 8) + 255) / 256, 8192ll) : 0;
         if (f.dw_blocks + f.col_blocks + dx_blocks == 0) continue;
