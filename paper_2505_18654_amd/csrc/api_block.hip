@@ -4,7 +4,7 @@
 
 #include "../../include/mtgr_block.h"
 #include "api_util.h"
-#include "mtgr_internal.h"
+#include "block_internal.h"
 
 namespace {
 

@@ -9,6 +9,14 @@
 // columns of the same numbers, in the same lanes), and so are dh and dpre: neither the pre-activations
 // (in serving) nor dh go through memory.  Roundings to bf16: h and dpre, as operands of the next product;
 // pre, which the forward keeps for the backward (its tensors of the kind are bf16).
+//
+// Bound by the matrix cores (power) and, beside them, by what the epilogues read and write and compute.
+// Large products run on 256 x 256 tiles, fewer tiles than CUs on 128 x 128 ones (gemm_mid.h), deep ones of
+// them split over k; few tokens on a kernel of their own (ffn_rows.hip).  Measured:
+// - 75,132 tokens, 512 / 1408, training: first product 250 us (0.87 PFLOP/s; 635 MB written), second 120;
+// - 69,563 tokens, 1024 / 2816, training: 771 (1.04 PFLOP/s) and 380 us; backward: dpre 550 us (0.73; 1.6 GB of
+//   pre read and dpre written), dx 710 (1.13), the weight gradients 1,180 (1.02) with their splits' sums;
+// - 6,418 tokens, 256 / 704, backward: dpre 21.6 us, the three products behind it in one launch 28.4, the sums 7.2.
 #include "gemm_mid.h"
 
 namespace mtgr {
@@ -51,15 +59,15 @@ __global__ __launch_bounds__(256) void ffn_sum_kernel(SumArgs a, SumArgs b, SumA
     else sum_splits(c, blockIdx.x - second, gridDim.x - second);
 }
 
-SumArgs sum_of(const GemmArgs& g) {
+SumArgs sum_of(const TileArgs& g) {
     return {g.partial, g.splits, (int)g.N, g.M, (uint16_t*)g.C, g.ldc, (const uint16_t*)g.R, g.ldr};
 }
 
-int sum_grid(const GemmArgs& g) { return (int)std::min((g.M * (g.N / 4) + 255) / 256, 4096ll); }
+int sum_grid(const TileArgs& g) { return (int)std::min((g.M * (g.N / 4) + 255) / 256, 4096ll); }
 
-GemmArgs product(int layout, long long M, long long N, long long K, const void* A, long long lda, const void* B,
+TileArgs product(int layout, long long M, long long N, long long K, const void* A, long long lda, const void* B,
                  long long ldb, void* C, long long ldc) {
-    GemmArgs g{};
+    TileArgs g{};
     g.layout = layout;
     g.M = M;
     g.N = N;
@@ -77,7 +85,7 @@ GemmArgs product(int layout, long long M, long long N, long long K, const void* 
 
 // C = A B (NN) or A B^T (NT), plus the residual R where there is one; `partial` holds the K splits' sums.
 template <int LAYOUT>
-static hipError_t deep_product(GemmArgs g, const Tiles& t, float* partial, hipStream_t s) {
+static hipError_t deep_product(TileArgs g, const Tiles& t, float* partial, hipStream_t s) {
     if (!t.mid && (LAYOUT == GEMM_NT || !g.R)) {
         gemm_plan(&g);
         return launch_gemm_bf16(g, s);
@@ -123,7 +131,7 @@ hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
     if (ffn_rows_fit(a.T, a.f, FFN_HIDDEN_COLUMNS)) {
         e = launch_ffn_rows_hidden(a, s);
     } else {
-        GemmArgs g = product(GEMM_NN, a.T, a.f, a.d, a.x, a.ld_x, a.w_in, a.ld_win, a.pre, a.ld_pre);
+        TileArgs g = product(GEMM_NN, a.T, a.f, a.d, a.x, a.ld_x, a.w_in, a.ld_win, a.pre, a.ld_pre);
         g.C2 = a.h;
         g.ldc2 = a.ld_h;
         const Tiles t = plan(a.T, a.f, a.d, WBN / 2);
@@ -133,7 +141,7 @@ hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
     }
     if (e != hipSuccess) return e;
     if (rows_output(a.T, a.d, a.f)) return launch_ffn_rows_out(a, s);
-    GemmArgs g = product(GEMM_NN, a.T, a.d, a.f, a.h, a.ld_h, a.w_out, a.ld_wout, a.y, a.ld_y);
+    TileArgs g = product(GEMM_NN, a.T, a.d, a.f, a.h, a.ld_h, a.w_out, a.ld_wout, a.y, a.ld_y);
     g.R = a.residual;
     g.ldr = a.ld_r;
     return deep_product<GEMM_NN>(g, plan_deep(g.M, g.N, g.K), partial, s);
@@ -204,7 +212,7 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
     const long long f2 = 2ll * a.f;
     char* dpre = (char*)workspace;
     float* partial = (float*)(dpre + align256((size_t)a.T * f2 * 2));
-    GemmArgs g = product(GEMM_NT, a.T, a.f, a.d, a.dy, a.ld_y, a.w_out, a.ld_wout, dpre, f2);
+    TileArgs g = product(GEMM_NT, a.T, a.f, a.d, a.dy, a.ld_y, a.w_out, a.ld_wout, dpre, f2);
     g.R = a.pre;
     g.ldr = a.ld_pre;
     const Tiles t = plan(a.T, a.f, a.d);
@@ -212,9 +220,9 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
     hipError_t e = t.mid ? mid_launch<GEMM_NT, GEMM_EPI_GATED_BWD>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_GATED_BWD, false>(g, s);
     if (e != hipSuccess) return e;
     const BackwardPlan p = plan_backward(a.T, a.d, a.f);
-    GemmArgs x = product(GEMM_NT, a.T, a.d, f2, dpre, f2, a.w_in, a.ld_win, a.dx, a.ld_x);
-    GemmArgs wi = product(GEMM_TN, a.d, f2, a.T, a.x, a.ld_x, dpre, f2, a.dw_in, a.ld_win);
-    GemmArgs wo = product(GEMM_TN, a.f, a.d, a.T, a.h, a.ld_h, a.dy, a.ld_y, a.dw_out, a.ld_wout);
+    TileArgs x = product(GEMM_NT, a.T, a.d, f2, dpre, f2, a.w_in, a.ld_win, a.dx, a.ld_x);
+    TileArgs wi = product(GEMM_TN, a.d, f2, a.T, a.x, a.ld_x, dpre, f2, a.dw_in, a.ld_win);
+    TileArgs wo = product(GEMM_TN, a.f, a.d, a.T, a.h, a.ld_h, a.dy, a.ld_y, a.dw_out, a.ld_wout);
     set_tiles(&wi, p.in);
     set_tiles(&wo, p.out);
     if (p.together) {
@@ -230,7 +238,7 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
     }
     if ((e = deep_product<GEMM_NT>(x, p.dx, partial, s)) != hipSuccess) return e;
     wi.partial = wo.partial = partial;
-    auto gradient = [&](const GemmArgs& w) {
+    auto gradient = [&](const TileArgs& w) {
         const hipError_t r = w.wide ? wide_launch<GEMM_TN, GEMM_EPI_NONE, false>(w, s) : mid_launch<GEMM_TN, GEMM_EPI_PART>(w, s);
         return r != hipSuccess ? r : launch_split_reduce(w, s);
     };

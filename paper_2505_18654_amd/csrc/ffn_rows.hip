@@ -10,8 +10,11 @@
 // reads columns CPL (l % 16) .. + CPL - 1 of the rows 8 (l / 16) .. + 7 of a k block of 32, and v_perm
 // pairs the rows' 16-bit halves: fragment j then holds the columns CPL (l % 16) + j, a row order of the
 // (transposed) result that only the epilogue sees.
+//
+// Bound by latency: start, one chain of weight loads and the additions through LDS (one token, 512 / 1408: 4.3 and
+// 4.2 us for 2.9 and 1.4 MB; 1024 / 2816: 6.8 us for 11.5 MB, 1.7 TB/s, and 7.4 for 5.8 MB).
+#include "block_internal.h"
 #include "mtgr_device.h"
-#include "mtgr_internal.h"
 
 namespace mtgr {
 

@@ -33,8 +33,8 @@
 // Large products run on the 256 x 256 tiles of gemm_wide.hip (gemm_plan decides).
 #include <type_traits>
 
+#include "block_internal.h"
 #include "mtgr_device.h"
-#include "mtgr_internal.h"
 
 namespace mtgr {
 

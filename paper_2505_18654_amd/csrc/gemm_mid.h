@@ -31,7 +31,7 @@ constexpr int MID_WORKGROUPS = 512;
 
 // The tile of workgroup `block` of a product's own grid; sm: MID_LDS bytes.
 template <int LAYOUT, int EPI>
-__device__ __forceinline__ void mid_tile(const GemmArgs& g, int block, char* sm) {
+__device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm) {
     constexpr bool A_KR = LAYOUT == GEMM_TN, B_KR = LAYOUT != GEMM_NT;
     constexpr bool ACC = EPI == GEMM_EPI_ACC, SPLIT = LAYOUT == GEMM_TN || ACC || EPI == GEMM_EPI_PART;
     constexpr bool GATED = EPI == GEMM_EPI_GATED || EPI == GEMM_EPI_GATED_SAVE;
@@ -327,30 +327,30 @@ __device__ __forceinline__ void mid_tile(const GemmArgs& g, int block, char* sm)
 }
 
 template <int LAYOUT, int EPI>
-__global__ __launch_bounds__(256, 2) void gemm_mid_kernel(GemmArgs g) {
+__global__ __launch_bounds__(256, 2) void gemm_mid_kernel(TileArgs g) {
     __shared__ __align__(1024) char sm[MID_LDS];
     mid_tile<LAYOUT, EPI>(g, blockIdx.x, sm);
 }
 
 // Several products in one launch, each from a workgroup of its own on (a multiple of the XCDs).
 template <int LAYOUT0, int EPI0, int LAYOUT1, int EPI1>
-__global__ __launch_bounds__(256, 2) void gemm_mid_pair_kernel(GemmArgs g, GemmArgs h, int first) {
+__global__ __launch_bounds__(256, 2) void gemm_mid_pair_kernel(TileArgs g, TileArgs h, int first) {
     __shared__ __align__(1024) char sm[MID_LDS];
     if ((int)blockIdx.x < first) mid_tile<LAYOUT0, EPI0>(g, blockIdx.x, sm);
     else mid_tile<LAYOUT1, EPI1>(h, blockIdx.x - first, sm);
 }
 
 template <int LAYOUT0, int EPI0, int LAYOUT1, int EPI1>
-__global__ __launch_bounds__(256, 2) void gemm_mid_trio_kernel(GemmArgs g, GemmArgs h, GemmArgs k, int first, int second) {
+__global__ __launch_bounds__(256, 2) void gemm_mid_trio_kernel(TileArgs g, TileArgs h, TileArgs k, int first, int second) {
     __shared__ __align__(1024) char sm[MID_LDS];
     if ((int)blockIdx.x < first) mid_tile<LAYOUT0, EPI0>(g, blockIdx.x, sm);
     else mid_tile<LAYOUT1, EPI1>((int)blockIdx.x < second ? h : k, blockIdx.x - ((int)blockIdx.x < second ? first : second), sm);
 }
 
-static inline int mid_grid(const GemmArgs& g) { return XCDS * ((g.mblocks * g.nblocks * g.splits + XCDS - 1) / XCDS); }
+static inline int mid_grid(const TileArgs& g) { return XCDS * ((g.mblocks * g.nblocks * g.splits + XCDS - 1) / XCDS); }
 
 template <int LAYOUT, int EPI>
-static hipError_t mid_launch(const GemmArgs& g, hipStream_t s) {
+static hipError_t mid_launch(const TileArgs& g, hipStream_t s) {
     gemm_mid_kernel<LAYOUT, EPI><<<mid_grid(g), 256, 0, s>>>(g);
     return hipGetLastError();
 }
@@ -428,7 +428,7 @@ static inline size_t partial_bytes(const Tiles& t, long long M, long long N) {
     return t.splits > 1 ? (size_t)t.splits * M * N * sizeof(float) : 0;
 }
 
-static inline void set_tiles(GemmArgs* g, const Tiles& t) {
+static inline void set_tiles(TileArgs* g, const Tiles& t) {
     g->mblocks = t.mblocks;
     g->nblocks = t.nblocks;
     g->splits = t.splits;

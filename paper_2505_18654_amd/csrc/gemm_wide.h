@@ -1,5 +1,6 @@
-// The large dense products of the encoder layer (the same layouts and epilogues as gemm.hip):
-// a 256 x 256 tile of C per workgroup of 8 waves, one workgroup per CU.
+// The large dense products of the encoder layer (the same layouts and epilogues as gemm.hip), of the
+// feed-forward block (ffn.hip) and of the softmax loss (softmax_loss.hip): a 256 x 256 tile of C per
+// workgroup of 8 waves, one workgroup per CU.
 //
 // What bounds the 256 x 128 tiles of gemm.hip on large products is the path into LDS, not the
 // matrix cores: per 32 k a tile copies 24 KB for 512 cycles of MFMA work, and the path delivers
@@ -8,8 +9,9 @@
 // 256 x 256 tile copies a third less per MFMA, and k steps of 64 make every row 128 bytes:
 // 64 KB x 9.2 ns = 0.59 us of copies under 2048 cycles = 0.89 us of MFMAs.
 //
-// Wave w computes the 128 x 64 part (m half w % 2, n quarter w / 2) as 8 x 4 blocks of 16 x 16,
-// transposed (C^T = B^T A^T), with v_mfma_f32_16x16x32_bf16.  On random data the card is bound by
+// Wave w computes the 128 x 64 part (m half w % 2, n quarter w / 2; in the gated products 64 x 128, so that
+// its 64 gate and 64 up columns leave as whole 128-byte lines) as 8 x 4 blocks of 16 x 16, transposed
+// (C^T = B^T A^T), with v_mfma_f32_16x16x32_bf16.  On random data the card is bound by
 // its power, not by issue: the clock falls to 1.3 - 1.8 GHz, and a loop of nothing but MFMAs on
 // N(0, 1) operands in registers reaches 2.02 PFLOP/s with 16 x 16 x 32 and 1.82 with 32 x 32 x 16
 // (both 2.45 on zeros).
@@ -28,12 +30,20 @@
 // 1,045 -> 850 us, without 723 -> 615 us, its input gradient 702 -> 541 us (1.23 PFLOP/s; hipBLASLt
 // 616 us), its weight gradient 654 -> 612 us, the d x d products 193 -> 170, 173 -> 150 and
 // 190 -> 170 us.
+//
+// A k step takes about 1.27 us.  The epilogues of the gated product and of the softmax come on top: their
+// vector work (about 28 cycles per logit and 50 per hidden value, of which transcendentals 16 and 32) fills a
+// SIMD while its matrix cores rest, and both waves of a SIMD are in it at once (counters, loss of 1,900 rows,
+// 400,003 classes, d = 256: MFMA 35 % busy, VALU 46 %, both at once 2 %).  Starting the workgroups at
+// different times changed nothing (-1 to +2 %); two workgroups of 128 x 256 tiles per CU, which do overlap,
+// have room for k steps of 32 only, whose half lines make the copies as slow as that gained (statistics,
+// d = 256: 502 -> 430 us; d = 512: 1,124 -> 1,184).
 #pragma once
 
 #include <type_traits>
 
+#include "block_internal.h"
 #include "mtgr_device.h"
-#include "mtgr_internal.h"
 
 namespace mtgr {
 
@@ -86,7 +96,7 @@ __device__ __forceinline__ void wave_lds_fence() {
 }  // namespace
 
 template <int LAYOUT, int EPI, bool COLSUM>
-__global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
+__global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
     constexpr bool A_KR = LAYOUT == GEMM_TN;      // A stored [K][M]
     constexpr bool B_KR = LAYOUT != GEMM_NT;      // B stored [K][N]
     constexpr bool ACC = EPI == GEMM_EPI_ACC;     // fp32 partials added up over calls
@@ -801,7 +811,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(GemmArgs g) {
 }
 
 template <int LAYOUT, int EPI, bool COLSUM>
-static hipError_t wide_launch(const GemmArgs& g, hipStream_t s) {
+static hipError_t wide_launch(const TileArgs& g, hipStream_t s) {
     // NN / NT: one workgroup per CU (those without a tile end at once); TN: one per (split, tile)
     const int items = g.mblocks * g.nblocks * g.splits;
     const int gx = LAYOUT == GEMM_TN && EPI != GEMM_EPI_ROWS_DIRECT ? XCDS * ((items + XCDS - 1) / XCDS) : WIDE_WORKGROUPS;

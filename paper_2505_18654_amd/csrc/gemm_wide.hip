@@ -3,7 +3,9 @@
 
 namespace mtgr {
 
-hipError_t launch_gemm_wide(const GemmArgs& g, hipStream_t s) {
+hipError_t launch_gemm_wide(const GemmArgs& a, hipStream_t s) {
+    TileArgs g{};
+    (GemmArgs&)g = a;
     if (g.layout == GEMM_TN)
         return g.colsum ? wide_launch<GEMM_TN, GEMM_EPI_NONE, true>(g, s)
                         : wide_launch<GEMM_TN, GEMM_EPI_NONE, false>(g, s);

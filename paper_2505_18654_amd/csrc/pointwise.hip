@@ -3,7 +3,7 @@
 // (8 bf16 or 4 fp32) per thread and step.  Every byte is read or written once: the bf16 chunks
 // move with the non-temporal hint (measured on [69563, 4096]: bias + SiLU backward 0.303 ->
 // 0.291 ms, the residual add on [69563, 1024] 0.077 -> 0.071 ms).
-#include "mtgr_internal.h"
+#include "block_internal.h"
 #include "mtgr_device.h"
 
 namespace mtgr {
