@@ -82,9 +82,11 @@ mtgr_status_t mtgr_dropout(int64_t rows, int32_t cols, mtgr_dtype_t dtype, const
  *
  * The logits are never kept.  A row whose target lies outside 0 .. V-1 has no label: its loss, lse and
  * gradient are 0, its x may hold anything, and it costs next to nothing.  A bias of -inf takes a class
- * out (its row of w still has to be finite); a row for which no class is left has the loss 0, lse -inf
- * and no gradient; a label whose class is out has the loss +inf.  bias below +inf; d is a multiple of 32,
- * at most 2048; N below 2^24, V below 2^30. */
+ * out (its row of w still has to be finite), and so does one below -2.36e38, which is -inf in the units of
+ * log 2 that it is kept in; a row for which no class is left has the loss 0, lse -inf and no gradient; a
+ * label whose class is out has the loss +inf.  bias below 2.36e38; d is a multiple of 32, at most 2048; N
+ * below 2^24, V below 2^30.
+ */
 typedef struct {
     int64_t num_rows;         /* N */
     int64_t num_classes;      /* V */

@@ -88,6 +88,13 @@ __device__ __forceinline__ int stat_chunks(int mblocks, int nblocks) {
     return (nblocks + per_item - 1) / per_item;
 }
 
+// 16 bytes that are read once: they leave the operands of the next k steps in the L2 (backward of the gated
+// product, 69,563 tokens, 1024 / 2816: 551 -> 535 us).
+__device__ __forceinline__ uint4 load_nt16(const void* p) {
+    const u32x4_nt v = __builtin_nontemporal_load((const u32x4_nt*)p);
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 // LDS hand-off between the lanes of one wave (its LDS operations run in order).
 __device__ __forceinline__ void wave_lds_fence() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -518,8 +525,8 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
 #pragma unroll
             for (int q = 0; q < 2; q++) {
                 const uint16_t* r = R + min(em + 16 * b + 8 * q + (el >> 3), M - 1) * g.ldr;
-                pg[b & 3][q] = *(const uint4*)r;
-                pu[b & 3][q] = *(const uint4*)(r + N);
+                pg[b & 3][q] = load_nt16(r);
+                pu[b & 3][q] = load_nt16(r + N);
             }
         };
         if constexpr (EPI == GEMM_EPI_GATED_BWD) {

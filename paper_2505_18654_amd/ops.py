@@ -439,7 +439,7 @@ def softmax_loss_workspace(rows: int, classes: int, dim: int, device="cuda", bac
 def softmax_loss_fwd(x, w, targets, bias=None, scale: float = 1.0, workspace=None):
     """Softmax cross entropy of the rows of x [N, d] against the classes w [V, d] (bf16), with the logits
     z = scale x w^T + bias (bias [V] fp32), which are never kept: (loss [N], lse [N]) fp32.  A row whose target lies
-    outside 0 .. V-1 has no label: loss and lse 0.  A bias of -inf takes a class out."""
+    outside 0 .. V-1 has no label: loss and lse 0.  A bias of -inf (or below -2.36e38) takes a class out."""
     p = _softmax_loss_problem(x, w, targets, bias, scale)
     loss = torch.empty(p.num_rows, dtype=torch.float32, device=x.device)
     lse = torch.empty_like(loss)

@@ -112,6 +112,18 @@ def test_classes_taken_out():
     assert not any(v.any() for v in ops.softmax_loss_bwd(dloss, x, w, t, s4, bias=none))
 
 
+def test_lowest_numbers_take_classes_out():
+    """A bias below -2.36e38 is -inf in units of log 2; one that a mask of 16-bit logits would use is a number."""
+    x, w, t, b, dloss = make(300, 600, 64, 1.0, True)
+    out = torch.arange(600, device="cuda") % 3 == 1
+    t = torch.where(out[t], t - 1, t)
+    for lowest in (torch.finfo(torch.float32).min, torch.finfo(torch.bfloat16).min):
+        got, want = (ops.softmax_loss_fwd(x, w, t, bias=b.masked_fill(out, v)) for v in (lowest, float("-inf")))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    half = torch.full_like(b, -65504.0)                      # all classes: the softmax of what is left of them
+    check(x, w, t, half, dloss)
+
+
 def test_one_infinite_gradient_stays_in_its_row():
     x, w, t, b, dloss = make(300, 200, 64, 1.0, False)
     _, lse = ops.softmax_loss_fwd(x, w, t)
