@@ -20,8 +20,8 @@
 //
 // Bound by the matrix cores (power) and by the epilogues' vector work, which does not run beside them
 // (gemm_wide.h).  24,000 rows of 69,563, 50,021 classes, d = 512: statistics 1.08 ms (1.14 PFLOP/s); backward, of
-// 7 pieces, dz 1.45 ms (0.85; 2.4 GB written), dx 1.40 (0.88), dW 1.18 (1.04), sums 0.09.  1,900 rows, 400,003
-// classes, d = 256: 0.51; dz 0.70, dx 0.39, dW 0.47 ms.  Pieces of 256 or 512 MB of dz were slower.
+// 2 pieces, dz 1.35 ms (0.91; 2.4 GB written), dx 1.24 (0.99), dW 1.10 (1.12), sums 0.10.  1,900 rows, 400,003
+// classes, d = 256: 0.51; dz 0.70, dx 0.36, dW 0.41 ms.
 #include "gemm_mid.h"
 
 namespace mtgr {
@@ -46,12 +46,14 @@ struct SmPlan {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Pieces of the classes: the statistics (forward, 8 bytes per row and 64 classes) or dz (backward, 2 bytes
-// per row and class) of one piece take about half or one gigabyte.
+// per row and class) of one piece take about half or four gigabytes (backward of 24,000 of 69,563 rows, 50,021
+// classes, d = 512: 3.82 ms; with one gigabyte, 7 pieces instead of 2, 3.94; 1,900 of 2,048 rows, 400,003 classes,
+// d = 256, one piece instead of two: 1.50, 1.57).  At most 2^22 classes: 32-bit copy offsets over 256 rows of dz.
 SmPlan sm_plan(long long N, int V, int d, bool backward) {
     SmPlan p{};
     const long long mblocks = (N + WBM - 1) / WBM, npad = mblocks * WBM;
     const long long blocks = (V + WBN - 1ll) / WBN;
-    const long long budget = backward ? (1ll << 30) / (npad * 2 * WBN) : (512ll << 20) / (npad * 32);
+    const long long budget = backward ? std::min((4ll << 30) / (npad * 2 * WBN), (1ll << 22) / WBN) : (512ll << 20) / (npad * 32);
     long long per = std::max(1ll, std::min(budget, blocks));
     p.pieces = (int)((blocks + per - 1) / per);
     per = (blocks + p.pieces - 1) / p.pieces;     // pieces of equal size

@@ -163,6 +163,13 @@ def test_pieces():
     check(x, w, t, b, dloss)
 
 
+def test_more_classes_than_a_piece_may_have():
+    """2^22 classes are the most of a piece of the backward, whatever the rows."""
+    x, w, t, b, dloss = make(3, (1 << 22) + 5000, 32, 1.0, True, seed=33)
+    t[0], t[1] = w.shape[0] - 1, 1 << 22
+    check(x, w, t, b, dloss)
+
+
 def test_gradients_against_differences():
     """The 64-bit definition's gradients against differences of its losses."""
     x, w, t, b, dloss = make(9, 23, 32, 0.8, True)
