@@ -21,7 +21,8 @@ struct TileArgs : GemmArgs {
     int b_rows;               // rows of B (classes), where they are fewer than N or K
     int class0;               // first class of the piece
     int group_m;              // m blocks that an XCD's workgroups share
-    int accumulate;           // ACC: add to the partials of the calls before
+    int accumulate;           // ACC: add to the partials of the calls before; ks_per_split is the k steps of the first
+                              // call, by which all of them are split (256 x 256 tiles)
     float scale;              // z = scale acc + bias, in units of log 2; ROWS_DIRECT: C = scale max |g| acc
     float2* stats;            // SM_STATS: (reference, sum) per row and wave, [4 chunks][M] (128 x 128 tiles: [2 nblocks][M])
     const int4* row_info;     // SM_GRAD: per row (lse, gradient of its loss, label, factor 2^-low of lse), whole m blocks

@@ -52,6 +52,7 @@ namespace {
 constexpr int WBM = 256, WBN = 256, WBK = 64;
 constexpr int WNM = 8, WNN = 4;                 // 16 x 16 blocks per wave (m, n)
 constexpr uint32_t WSLOT = WBM * WBK * 2;       // bytes of one operand's stage
+constexpr int ACC_ROUNDS = 4, ACC_SPLITS = 64;  // see acc_splits
 constexpr int WQ = 4;                           // copy instructions per wave, operand and stage
 // Slots: A 0, A 1, B 0, B 1 and the third stage of the deep operand; the epilogue stages in the last one.
 constexpr uint32_t WSTAGING = 4 * WSLOT;
@@ -78,8 +79,25 @@ __device__ __forceinline__ float bf16_half(uint32_t w, int hi) {
     return __uint_as_float(hi ? w & 0xffff0000u : w << 16);
 }
 
-// K splits of a product with `tiles` tiles whose rows are counted on the device: the chip filled once.
-__device__ __forceinline__ int acc_splits(int tiles) { return max(1, min(256 / max(tiles, 1), 64)); }
+// K splits of a product of `tiles` tiles and `steps` k steps whose rows are counted on the device: the number that
+// fills one to four rounds of the chip and ends first, by the figures of tiles_of in gemm_mid.h in 64ths of a step,
+// in integers, because the kernel that adds the splits has to come to the same number (188 tiles, 391 steps: four
+// splits, 752 items in three rounds, 566 us; one, on 188 of the 256 CUs, 630; 130 tiles, 782 steps: 786 and 1,120).
+__device__ __forceinline__ int acc_splits(int tiles, int steps) {
+    constexpr int START = 346, STEP = 64, PARTIAL = 5;      // an item, its steps, its partials written and read
+    if (tiles > 256 * ACC_ROUNDS) return 1;
+    int best = 1, cost = (tiles + 255) / 256 * (START + STEP * steps) + PARTIAL * tiles;
+#pragma unroll
+    for (int k = 1; k <= ACC_ROUNDS; k++) {
+        const int s = max(min(min(256 * k / max(tiles, 1), ACC_SPLITS), steps), 1);
+        const int c = (s * tiles + 255) / 256 * (START + STEP * ((steps + s - 1) / s)) + PARTIAL * s * tiles;
+        if (c < cost) {
+            best = s;
+            cost = c;
+        }
+    }
+    return best;
+}
 
 // Columns of items of the softmax statistics: about 16 items per CU, so that the last round of them is short,
 // each of as many class tiles as that leaves (their statistics stay in registers in between).
@@ -138,7 +156,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
     // Items (split, m block, n block), an equal share of consecutive ones per XCD (workgroup % 8):
     // an XCD's 32 workgroups share a few m blocks' rows (NN / NT) or few k ranges (TN) in its L2.
     const int x = blockIdx.x % XCDS, tiles = mblocks * g.nblocks;
-    const int splits = ACC ? acc_splits(tiles) : g.splits;
+    const int splits = ACC ? acc_splits(tiles, g.ks_per_split) : g.splits;
     // SM_STATS: an item is an m block and every chunks-th n block
     const int chunks = STATS ? stat_chunks(mblocks, g.nblocks) : g.nblocks;
     const int items = STATS ? mblocks * chunks : tiles * splits;

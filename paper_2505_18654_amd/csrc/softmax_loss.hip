@@ -20,7 +20,7 @@
 //
 // Bound by the matrix cores (power) and by the epilogues' vector work, which does not run beside them
 // (gemm_wide.h).  24,000 rows of 69,563, 50,021 classes, d = 512: statistics 1.08 ms (1.14 PFLOP/s); backward, of
-// 2 pieces, dz 1.35 ms (0.91; 2.4 GB written), dx 1.24 (0.99), dW 1.10 (1.12), sums 0.10.  1,900 rows, 400,003
+// 2 pieces, dz 1.35 ms (0.91; 2.4 GB written), dx 1.13 (1.09), dW 1.10 (1.12), sums 0.13.  1,900 rows, 400,003
 // classes, d = 256: 0.51; dz 0.70, dx 0.36, dW 0.41 ms.
 #include "gemm_mid.h"
 
@@ -40,10 +40,17 @@ struct SmPlan {
     Tiles logits;             // of x W^T (forward and backward), dx and dW; which kernel
     Tiles dx, dw;
     bool direct;              // dW without partials
+    int items;                // most of the wide dx kernel
     size_t rows /* their count, the largest |g| */, counts, tops, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Most items of a product with accumulated partials, over all numbers of labels (acc_splits in gemm_wide.h).
+long long acc_items(long long N, int d) {
+    const long long tiles = (N + WBM - 1) / WBM * ((d + WBN - 1) / WBN);
+    return std::max(tiles, std::min(256ll * ACC_ROUNDS, tiles * ACC_SPLITS));
+}
 
 // Pieces of the classes: the statistics (forward, 8 bytes per row and 64 classes) or dz (backward, 2 bytes
 // per row and class) of one piece take about half or four gigabytes (backward of 24,000 of 69,563 rows, 50,021
@@ -83,10 +90,10 @@ SmPlan sm_plan(long long N, int V, int d, bool backward) {
     } else {
         p.info = take(sizeof(int4) * npad);
         p.dz = take((size_t)N * p.piece * 2);
-        // fp32 partials (of the wide dx kernel: one split, or as many as make at most 256 tiles; none of a dW that
-        // the wide kernel finishes in place)
-        const size_t tiles = (size_t)mblocks * ((d + WBN - 1) / WBN);
-        p.dxp = take((p.dx.mid ? (size_t)p.dx.splits * N * d : std::max<size_t>(tiles, 256) * WBM * WBN) * sizeof(float));
+        // fp32 partials (of the wide dx kernel: as many tiles as it may have items; none of a dW that the wide kernel
+        // finishes in place)
+        p.items = (int)acc_items(N, d);
+        p.dxp = take((p.dx.mid ? (size_t)p.dx.splits * N * d : (size_t)p.items * WBM * WBN) * sizeof(float));
         p.direct = p.dw.splits == 1 && !p.dw.mid;
         p.dwp = take(p.direct ? 0 : (size_t)p.dw.splits * p.piece * d * sizeof(float));
         p.colp = take((size_t)(p.logits.mid ? 4 : 2) * mblocks * p.piece * sizeof(float));
@@ -304,7 +311,8 @@ struct FinishArgs {
     const int* rows;
     const int* index;
     const float *dw_partial, *col_partial, *dx_partial;
-    int dw_splits, dx_splits; // dx_splits 0: those of the wide kernel
+    int dw_splits, dx_splits; // dx_splits 0: those of the wide kernel, of dx_steps k steps
+    int dx_steps;
     int v0, nv, ld_col;
     bool mid;                 // col_partial is that of 128-row tiles
     int dw_blocks, col_blocks;
@@ -342,7 +350,7 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SoftmaxLossArgs a, Finis
     }
     block -= f.col_blocks;
     const int blocks = gridDim.x - f.dw_blocks - f.col_blocks, ch = a.d / 8;
-    const int splits = f.dx_splits > 0 ? f.dx_splits : acc_splits((count + WBM - 1) / WBM * ((a.d + WBN - 1) / WBN));
+    const int splits = f.dx_splits > 0 ? f.dx_splits : acc_splits((count + WBM - 1) / WBM * ((a.d + WBN - 1) / WBN), f.dx_steps);
     const long long per = (long long)count * a.d;
     for (long long i = (long long)block * 256 + threadIdx.x; i < (long long)count * ch; i += (long long)blocks * 256) {
         const long long r = i / ch;
@@ -508,8 +516,8 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
             if (p.dx.mid) {
                 e = mid_launch<GEMM_NN, GEMM_EPI_ACC>(x, s);
             } else {
-                const int grid = XCDS * ((std::max(x.mblocks * x.nblocks, 256) + XCDS - 1) / XCDS);
-                gemm_wide_kernel<GEMM_NN, GEMM_EPI_ACC, false><<<grid, 512, 0, s>>>(x);
+                x.ks_per_split = p.piece / WBK;
+                gemm_wide_kernel<GEMM_NN, GEMM_EPI_ACC, false><<<XCDS * ((p.items + XCDS - 1) / XCDS), 512, 0, s>>>(x);
                 e = hipGetLastError();
             }
             if (e != hipSuccess) break;
@@ -525,6 +533,7 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         f.dx_partial = x.partial;
         f.dw_splits = w.splits;
         f.dx_splits = p.dx.mid ? p.dx.splits : 0;
+        f.dx_steps = p.piece / WBK;
         f.v0 = v0;
         f.nv = nv;
         f.ld_col = (int)g.N;
