@@ -23,6 +23,7 @@
 // 2 pieces, dz 1.35 ms (0.91; 2.4 GB written), dx 1.13 (1.09), dW 1.10 (1.12), sums 0.13.  1,900 rows, 400,003
 // classes, d = 256: 0.51; dz 0.70, dx 0.36, dW 0.41 ms.
 #include "gemm_mid.h"
+#include "softmax_tiles.h"
 
 namespace mtgr {
 
@@ -37,11 +38,12 @@ struct SmPlan {
     int piece;                // classes per piece, a multiple of 256
     int pieces;
     int vpad;                 // V rounded up to whole tiles
+    bool regs;                // x W^T on the tiles of softmax_tiles.h, otherwise on those of `logits`
     Tiles logits;             // of x W^T (forward and backward), dx and dW; which kernel
     Tiles dx, dw;
     bool direct;              // dW without partials
     int items;                // most of the wide dx kernel
-    size_t rows /* their count, the largest |g| */, counts, tops, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
+    size_t rows /* their count, the largest |g|, class tiles of an item */, counts, tops, index, xc, bias, info, stats, running, dz, dxp, dwp, colp, total;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -70,6 +72,9 @@ SmPlan sm_plan(long long N, int V, int d, bool backward) {
     const long long half = (N + 1) / 2;
     const Tiles lw = tiles_of(false, N, p.piece, d, WBN, 1, false), lm = tiles_of(true, N, p.piece, d, WBN, 1, false);
     p.logits = lm.us < lw.us ? lm : lw;
+    // (where both were measured: 2,900 rows, 20,011 classes, d = 256: 35 us, 48 on `logits`; 1,900, 400,003: 312, 513;
+    // 256, 100,003: 24, 27; 64, 100,003: 14, 11; 600, 20,011, d = 192: 14, 14; 2,007, 5,003, d = 128: 11, 10)
+    p.regs = d <= CT_MAX_D && sm_tiles_us(N, p.piece, d) < p.logits.us;
     p.dx = plan_split(half, d, p.piece, true);
     p.dw = plan_split(p.piece, d, half, false);
     size_t at = 0;
@@ -96,7 +101,7 @@ SmPlan sm_plan(long long N, int V, int d, bool backward) {
         p.dxp = take((p.dx.mid ? (size_t)p.dx.splits * N * d : (size_t)p.items * WBM * WBN) * sizeof(float));
         p.direct = p.dw.splits == 1 && !p.dw.mid;
         p.dwp = take(p.direct ? 0 : (size_t)p.dw.splits * p.piece * d * sizeof(float));
-        p.colp = take((size_t)(p.logits.mid ? 4 : 2) * mblocks * p.piece * sizeof(float));
+        p.colp = take((size_t)(p.regs || p.logits.mid ? 4 : 2) * mblocks * p.piece * sizeof(float));
     }
     p.total = at;
     return p;
@@ -152,7 +157,7 @@ constexpr int SCAN_ROWS = 8192;
 template <class T, bool BWD, bool SCAN>
 __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* rows, const int* block_counts,
                                                        const float* block_tops, int* index, uint16_t* xc, int4* info,
-                                                       float* bias2, int vpad, int row_blocks) {
+                                                       float* bias2, int vpad, int row_blocks, int class_tiles) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     if (SCAN && (int)blockIdx.x >= row_blocks)
         return padded_bias(a, bias2, vpad, ((int)blockIdx.x - row_blocks) * 1024 + tid);
@@ -195,6 +200,11 @@ __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* r
     for (int i = 0; i < 4; i++) {
         if (i < w) at += own[i];
         n += own[i];
+    }
+    // (by a wave that has no other part in this)
+    if (last && class_tiles > 0 && tid == 1023) {
+        int cost;
+        rows[2] = tile_run((before + n + CT_ROWS - 1) / CT_ROWS, class_tiles, &cost);
     }
     const int in_block = (int)min((long long)ROWS_PER_BLOCK, a.N - r0);
     if (tid < in_block) {
@@ -262,9 +272,9 @@ __device__ __forceinline__ float2 join(float2 p, float2 q) {
 template <class T>
 __global__ __launch_bounds__(1024) void sm_join_kernel(SoftmaxLossArgs a, const int* rows, const int* index,
                                                        const uint16_t* xc, const float* bias2, const float2* stats,
-                                                       bool mid, int nblocks, float2* running, bool first, bool last) {
+                                                       bool regs, bool mid, int nblocks, float2* running, bool first, bool last) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, count = *rows;
-    const int parts = mid ? 2 * nblocks : 4 * stat_chunks((count + WBM - 1) / WBM, nblocks);
+    const int parts = regs ? (nblocks + rows[2] - 1) / rows[2] : mid ? 2 * nblocks : 4 * stat_chunks((count + WBM - 1) / WBM, nblocks);
     const int r0 = (int)blockIdx.x * 16;
     if (r0 >= count) return;
     __shared__ float2 part[16][16];
@@ -314,7 +324,7 @@ struct FinishArgs {
     int dw_splits, dx_splits; // dx_splits 0: those of the wide kernel, of dx_steps k steps
     int dx_steps;
     int v0, nv, ld_col;
-    bool mid;                 // col_partial is that of 128-row tiles
+    bool mid;                 // col_partial has two parts per 128 rows, not per 256
     int dw_blocks, col_blocks;
 };
 
@@ -378,17 +388,19 @@ hipError_t launch_rows(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, hipS
     uint16_t* xc = (uint16_t*)(ws + p.xc);
     float* bias2 = (float*)(ws + p.bias);
     int4* info = (int4*)(ws + p.info);
+    const int class_tiles = p.regs ? std::min(p.piece, (a.V + CT_CLASSES - 1) / CT_CLASSES * CT_CLASSES) / CT_CLASSES : 0;
     auto launch = [&](auto type) {
         typedef decltype(type) T;
         if (a.N <= SCAN_ROWS) {
             sm_rows_kernel<T, BWD, true><<<rb + (p.vpad + 1023) / 1024, 1024, 0, s>>>(a, rows, counts, tops, index, xc, info,
-                                                                                   bias2, p.vpad, rb);
+                                                                                   bias2, p.vpad, rb, class_tiles);
             return hipGetLastError();
         }
         sm_count_kernel<T, BWD><<<rb + p.vpad / 256, 256, 0, s>>>(a, counts, tops, bias2, p.vpad, rb);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        sm_rows_kernel<T, BWD, false><<<rb, 1024, 0, s>>>(a, rows, counts, tops, index, xc, info, bias2, p.vpad, rb);
+        sm_rows_kernel<T, BWD, false><<<rb, 1024, 0, s>>>(a, rows, counts, tops, index, xc, info, bias2, p.vpad, rb,
+                                                                class_tiles);
         return hipGetLastError();
     };
     return a.targets64 ? launch(int64_t{}) : launch(int{});
@@ -411,9 +423,9 @@ TileArgs logits_product(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, int
     g.b_rows = std::min(p.piece, a.V - v0);
     g.class0 = v0;
     g.group_m = GROUP_M;
-    const int side = p.logits.mid ? MBM : WBM;
+    const int side = p.logits.mid ? MBM : WBM, cols = p.regs ? CT_CLASSES : side;
     g.mblocks = (int)((a.N + side - 1) / side);
-    g.nblocks = (g.b_rows + side - 1) / side;
+    g.nblocks = (g.b_rows + cols - 1) / cols;
     g.splits = 1;
     g.ks_per_split = (a.d + WBK - 1) / WBK;
     return g;
@@ -432,7 +444,8 @@ hipError_t launch_softmax_loss_fwd(const SoftmaxLossArgs& a, void* workspace, hi
     for (int i = 0; i < p.pieces && e == hipSuccess; i++) {
         TileArgs g = logits_product(a, p, ws, i * p.piece);
         g.stats = (float2*)(ws + p.stats);
-        e = p.logits.mid ? mid_launch<GEMM_NT, GEMM_EPI_SM_STATS>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_SM_STATS, false>(g, s);
+        e = p.regs ? sm_tile_launch<false>(g, s)
+            : p.logits.mid ? mid_launch<GEMM_NT, GEMM_EPI_SM_STATS>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_SM_STATS, false>(g, s);
         if (e != hipSuccess) break;
         const int blocks = (int)((a.N + 15) / 16);
         const bool first = i == 0, last = i == p.pieces - 1;
@@ -440,8 +453,8 @@ hipError_t launch_softmax_loss_fwd(const SoftmaxLossArgs& a, void* workspace, hi
         const uint16_t* xc = (const uint16_t*)(ws + p.xc);
         const float* bias2 = (const float*)(ws + p.bias);
         float2* running = (float2*)(ws + p.running);
-        if (a.targets64) sm_join_kernel<int64_t><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, p.logits.mid, g.nblocks, running, first, last);
-        else sm_join_kernel<int><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, p.logits.mid, g.nblocks, running, first, last);
+        if (a.targets64) sm_join_kernel<int64_t><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, p.regs, p.logits.mid, g.nblocks, running, first, last);
+        else sm_join_kernel<int><<<blocks, 1024, 0, s>>>(a, rows, index, xc, bias2, g.stats, p.regs, p.logits.mid, g.nblocks, running, first, last);
         e = hipGetLastError();
     }
     return e;
@@ -464,7 +477,8 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         g.ldc = p.piece;
         g.row_info = (const int4*)(ws + p.info);
         g.col_partial = a.dbias ? (float*)(ws + p.colp) : nullptr;
-        e = p.logits.mid ? mid_launch<GEMM_NT, GEMM_EPI_SM_GRAD>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_SM_GRAD, false>(g, s);
+        e = p.regs ? sm_tile_launch<true>(g, s)
+            : p.logits.mid ? mid_launch<GEMM_NT, GEMM_EPI_SM_GRAD>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_SM_GRAD, false>(g, s);
         if (e != hipSuccess) break;
 
         TileArgs x{};                                    // dx += dz W
@@ -537,7 +551,7 @@ hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hi
         f.v0 = v0;
         f.nv = nv;
         f.ld_col = (int)g.N;
-        f.mid = p.logits.mid;
+        f.mid = p.regs || p.logits.mid;
         f.dw_blocks = p.direct ? 0 : (int)std::min(((long long)nv * a.d / 4 + 255) / 256, 8192ll);
         f.col_blocks = a.dbias ? (nv + 255) / 256 : 0;
         const int dx_blocks = last ? (int)std::min((a.N * (a.d / 8) + 255) / 256, 8192ll) : 0;

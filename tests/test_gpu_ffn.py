@@ -96,6 +96,31 @@ def test_backward_strided():
         ops.gated_ffn_bwd(dy, x, pre, h, w_in, w_out, grads=(grads[0].contiguous(), grads[1], grads[2]))
 
 
+def test_offsets_past_32_bits():
+    """pre and its gradient hold 2.2e9 elements; the gradient of y is zero but for the last rows, so that the weights'
+    gradients follow from them alone (zeros add no rounding)."""
+    T, d, f, n = 1_000_003, 32, 1120, 400
+    x, dy = normal((T, d), 41), torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
+    dy[-n:] = normal((n, d), 42, 0.1)
+    w_in, w_out = weights(d, f)
+    y, pre, h = ops.gated_ffn_fwd(x, w_in, w_out, save=True)
+    s = ops.gated_ffn_fwd(x, w_in, w_out)
+    dx, dw_in, dw_out = ops.gated_ffn_bwd(dy, x, pre, h, w_in, w_out)
+    torch.cuda.synchronize()
+    W = w_out.double()
+    for rows in (slice(0, n), slice(T - n, T)):
+        want_pre, e_pre = ffn_pre(x[rows], w_in)
+        want_h, e_h = ffn_h(want_pre, e_pre)
+        within("pre", pre[rows], want_pre, half_step(pre[rows]) + e_pre)
+        within("h", h[rows], want_h, half_step(h[rows]) + e_h)
+        within("y", y[rows], h[rows].double() @ W, half_step(y[rows]) + (f + 5) * U * (h[rows].double().abs() @ W.abs()))
+        assert torch.equal(s[rows], y[rows])                 # (the same kernels, and h rounded alike)
+    assert not dx[:-n].any()
+    for name, got, (want, b) in zip(("dx", "dw_in", "dw_out"), (dx[-n:], dw_in, dw_out),
+                                    ffn_back(dy[-n:], x[-n:], pre[-n:], h[-n:], w_in, w_out).values()):
+        within(name, got, want, half_step(got) + b)
+
+
 def test_gradients_against_differences():
     """(y(w + e v) - y(w - e v)) . dy / 2e of the 64-bit definition, whose gradients ffn_back states."""
     T, d, f = 7, 32, 64

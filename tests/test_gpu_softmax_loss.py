@@ -48,6 +48,9 @@ def check(x, w, t, b, dloss, scale=0.9):
     (16, 256, 96, 1.0, False, 64), (17, 257, 544, 1.0, True, 32), (255, 33, 64, 0.5, True, 64), (256, 4099, 64, 1.0, False, 64),
     (257, 700, 160, 0.3, True, 32), (1000, 5003, 256, 0.6, True, 64), (5000, 301, 32, 0.2, True, 64),
     (2100, 1999, 1056, 0.9, False, 64), (40, 20011, 128, 1.0, True, 64), (300, 64, 2048, 0.5, True, 32),
+    (2500, 20000, 256, 0.9, True, 64), (3001, 16001, 224, 0.7, False, 32), (5000, 9999, 160, 0.6, True, 64),
+    (4000, 12345, 96, 1.0, True, 64), (9000, 7001, 32, 0.95, True, 64), (300, 70001, 256, 1.0, True, 64),
+    (8001, 9999, 128, 0.9, False, 64), (7000, 30011, 288, 1.0, True, 64),
 ])
 def test_loss_and_gradients(N, V, d, share, bias, bits):
     print(f"[loss] N={N} V={V} d={d} share={share} bias={bias} int{bits}", flush=True)
@@ -168,6 +171,36 @@ def test_more_classes_than_a_piece_may_have():
     x, w, t, b, dloss = make(3, (1 << 22) + 5000, 32, 1.0, True, seed=33)
     t[0], t[1] = w.shape[0] - 1, 1 << 22
     check(x, w, t, b, dloss)
+
+
+def test_offsets_past_32_bits():
+    """2.2e9 elements of x, then of w: labels among the last rows (and the first ones), then among the last classes."""
+    n, d = 1_100_003, 2048
+    few, w, t, b, dloss = make(40, 300, d, 1.0, True, seed=35)
+    x = torch.full((n, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    at = torch.cat([torch.arange(4), torch.arange(n - 36, n)]).cuda()
+    x[at] = few
+    labels, g = torch.full((n,), -1, device="cuda"), torch.ones(n, device="cuda")
+    labels[at], g[at] = t, dloss
+    loss, lse = ops.softmax_loss_fwd(x, w, labels, bias=b, scale=0.9)
+    dx, dw, db = ops.softmax_loss_bwd(g, x, w, labels, lse, bias=b, scale=0.9)
+    want, e = softmax_loss(few, w, t, b, 0.9, dloss)
+    for name, got in (("loss", loss[at]), ("lse", lse[at]), ("dx", dx[at]), ("dw", dw), ("dbias", db)):
+        within(name, got, want[name], e[name] + (half_step(got) if name in ("dx", "dw") else 0))
+    assert not dx[4:n - 36].any() and not loss[4:n - 36].any()
+    del x, dx, labels, g
+    w = torch.zeros(n, d, dtype=torch.bfloat16, device="cuda")
+    w[-600:] = normal((600, d), 36, 2.0 * d ** -0.5)
+    b = torch.full((n,), float("-inf"), device="cuda")
+    b[-600:] = 0.5
+    t = n - 1 - t
+    loss, lse, dx, dw, db = check(few, w[-600:], t - (n - 600), b[-600:], dloss)
+    loss2, lse2 = ops.softmax_loss_fwd(few, w, t, bias=b, scale=0.9)
+    dx2, dw2, db2 = ops.softmax_loss_bwd(dloss, few, w, t, lse2, bias=b, scale=0.9)
+    want, e = softmax_loss(few, w[-600:], t - (n - 600), b[-600:], 0.9, dloss)
+    for name, got in (("loss", loss2), ("lse", lse2), ("dx", dx2), ("dw", dw2[-600:]), ("dbias", db2[-600:])):
+        within(name, got, want[name], e[name] + (half_step(got) if name in ("dx", "dw") else 0))
+    assert not dw2[:-600].any() and not db2[:-600].any()
 
 
 def test_gradients_against_differences():
