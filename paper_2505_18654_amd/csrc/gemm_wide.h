@@ -37,7 +37,7 @@
 // 400,003 classes, d = 256: MFMA 35 % busy, VALU 46 %, both at once 2 %).  Starting the workgroups at
 // different times changed nothing (-1 to +2 %); two workgroups of 128 x 256 tiles per CU, which do overlap,
 // have room for k steps of 32 only, whose half lines make the copies as slow as that gained (statistics,
-// d = 256: 502 -> 430 us; d = 512: 1,124 -> 1,184).
+// d = 256: 502 -> 430 us; d = 512: 1,124 -> 1,184).  Up to 256 columns the loss has softmax_tiles.h instead.
 #pragma once
 
 #include <type_traits>

@@ -8,7 +8,8 @@
 // the products' cost follows their number, which stays on the device (no synchronisation): the grids are
 // laid out for N rows and the kernels stop at the count.
 //
-// Forward: x W^T on the matrix cores (gemm_wide.h).  A workgroup walks class tiles of its rows, and every lane
+// Forward: x W^T on the matrix cores (gemm_wide.h; up to 256 columns mostly softmax_tiles.h, small batches
+// gemm_mid.h).  A workgroup walks class tiles of its rows, and every lane
 // keeps a reference and a sum of exponentials for the columns that it saw of a row; a second kernel joins
 // them.  2 n V d operations; written are at most 8 bytes per row and 64 classes, a sixteenth of the logits in
 // bf16.
@@ -19,9 +20,9 @@
 // rounding error would be common to all labels' terms (-g), and a label's own term -1 is exact.
 //
 // Bound by the matrix cores (power) and by the epilogues' vector work, which does not run beside them
-// (gemm_wide.h).  24,000 rows of 69,563, 50,021 classes, d = 512: statistics 1.08 ms (1.14 PFLOP/s); backward, of
+// in gemm_wide.h.  24,000 rows of 69,563, 50,021 classes, d = 512: statistics 1.08 ms (1.14 PFLOP/s); backward, of
 // 2 pieces, dz 1.35 ms (0.91; 2.4 GB written), dx 1.13 (1.09), dW 1.10 (1.12), sums 0.13.  1,900 rows, 400,003
-// classes, d = 256: 0.51; dz 0.70, dx 0.36, dW 0.41 ms.
+// classes, d = 256: 0.31 (1.25); dz 0.56 (0.69; 1.5 GB written), dx 0.37 (1.05), dW 0.42 (0.93).
 #include "gemm_mid.h"
 #include "softmax_tiles.h"
 
@@ -73,8 +74,9 @@ SmPlan sm_plan(long long N, int V, int d, bool backward) {
     const Tiles lw = tiles_of(false, N, p.piece, d, WBN, 1, false), lm = tiles_of(true, N, p.piece, d, WBN, 1, false);
     p.logits = lm.us < lw.us ? lm : lw;
     // (where both were measured: 2,900 rows, 20,011 classes, d = 256: 35 us, 48 on `logits`; 1,900, 400,003: 312, 513;
-    // 256, 100,003: 24, 27; 64, 100,003: 14, 11; 600, 20,011, d = 192: 14, 14; 2,007, 5,003, d = 128: 11, 10)
-    p.regs = d <= CT_MAX_D && sm_tiles_us(N, p.piece, d) < p.logits.us;
+    // 300, 100,003: 32, 36; 64, 100,003: 14, 11; 600, 20,011, d = 192: 14, 14; 2,007 of 6,418, 5,003, d = 128: 11, 10.
+    // The margin is for rows without a label, whose tiles of 256 rows are the coarser ones.)
+    p.regs = d <= CT_MAX_D && sm_tiles_us(N, p.piece, d) < 0.86 * p.logits.us;
     p.dx = plan_split(half, d, p.piece, true);
     p.dw = plan_split(p.piece, d, half, false);
     size_t at = 0;
@@ -201,7 +203,7 @@ __global__ __launch_bounds__(1024) void sm_rows_kernel(SoftmaxLossArgs a, int* r
         if (i < w) at += own[i];
         n += own[i];
     }
-    // (by a wave that has no other part in this)
+    // (one thread, while the others gather)
     if (last && class_tiles > 0 && tid == 1023) {
         int cost;
         rows[2] = tile_run((before + n + CT_ROWS - 1) / CT_ROWS, class_tiles, &cost);
