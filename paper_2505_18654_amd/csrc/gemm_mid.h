@@ -161,16 +161,25 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
 
     // acc[a][b] will hold row em + 16 b, columns en + 16 a + 0..3; what the epilogue reads there is loaded first
     const int em = m0 + 64 * wm + lr, en = n0 + 64 * wn + 4 * lg;
-    constexpr bool READS = EPI == GEMM_EPI_RESIDUAL || EPI == GEMM_EPI_GATED_BWD;
-    uint2 r0[READS ? 4 : 1][4], r1[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][4];
-    if constexpr (READS) {
+    uint2 r0[EPI == GEMM_EPI_RESIDUAL ? 4 : 1][4];
+    if constexpr (EPI == GEMM_EPI_RESIDUAL) {
 #pragma unroll
         for (int b = 0; b < 4; b++)
 #pragma unroll
-            for (int a = 0; a < 4; a++) {
-                const uint16_t* r = (const uint16_t*)g.R + min(em + 16 * b, M - 1) * g.ldr + min(en + 16 * a, N - 4);
-                r0[a][b] = *(const uint2*)r;
-                if constexpr (EPI == GEMM_EPI_GATED_BWD) r1[a][b] = *(const uint2*)(r + N);
+            for (int a = 0; a < 4; a++)
+                r0[a][b] = *(const uint2*)((const uint16_t*)g.R + min(em + 16 * b, M - 1) * g.ldr + min(en + 16 * a, N - 4));
+    }
+    // gate and up values of row 8 q + l / 8 of block b, chunk l % 8 of the wave's 64 columns
+    uint4 pg[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][2], pu[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][2];
+    if constexpr (EPI == GEMM_EPI_GATED_BWD) {
+        const uint16_t* R = (const uint16_t*)g.R + min(n0 + 64 * wn + 8 * (lane & 7), N - 8);
+#pragma unroll
+        for (int b = 0; b < 4; b++)
+#pragma unroll
+            for (int q = 0; q < 2; q++) {
+                const uint16_t* r = R + min(m0 + 64 * wm + 16 * b + 8 * q + (lane >> 3), M - 1) * g.ldr;
+                pg[b][q] = load_nt16(r);
+                pu[b][q] = load_nt16(r + N);
             }
     }
     floatx4 acc[4][4];
@@ -297,6 +306,31 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
                 const floatx4 h = {silu(z[0]) * u[0], silu(z[1]) * u[1], silu(z[2]) * u[2], silu(z[3]) * u[3]};
                 *(uint2*)((uint16_t*)g.C2 + gm * g.ldc2 + gn) = pack(h);
             }
+    } else if constexpr (EPI == GEMM_EPI_GATED_BWD) {
+        // as in gemm_wide.h: dh passes through LDS in fp32, so that a lane has 8 columns of a row
+        lds_barrier();                                         // (the stages are no longer read)
+        char* stg = sm + 4096 * w;
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+#pragma unroll
+            for (int a = 0; a < 4; a++) *(floatx4*)(stg + 256 * lr + 16 * ((4 * a + lg) ^ lr)) = acc[a][b];
+            wave_lds_fence();
+#pragma unroll
+            for (int q = 0; q < 2; q++) {
+                const int row = 8 * q + (lane >> 3), ch = lane & 7;
+                const int gm = m0 + 64 * wm + 16 * b + row, gn = n0 + 64 * wn + 8 * ch;
+                const floatx4 x0 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch) ^ row));
+                const floatx4 x1 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch + 1) ^ row));
+                uint4 og, ou;
+                gated_gradient(x0, x1, pg[b][q], pu[b][q], &og, &ou);
+                if (gm < M && gn < N) {
+                    uint16_t* dst = (uint16_t*)g.C + gm * g.ldc + gn;
+                    *(uint4*)dst = og;
+                    *(uint4*)(dst + N) = ou;
+                }
+            }
+            wave_lds_fence();
+        }
     } else {
 #pragma unroll
         for (int b = 0; b < 4; b++)
@@ -305,23 +339,8 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
                 const int gm = em + 16 * b, gn = en + 16 * a;
                 if (gm >= M || gn >= N) continue;
                 floatx4 v = acc[a][b];
-                uint16_t* dst = (uint16_t*)g.C + gm * g.ldc + gn;
-                if constexpr (EPI == GEMM_EPI_GATED_BWD) {
-                    const floatx4 z = unpack(r0[a][b]), u = unpack(r1[a][b]);
-                    floatx4 dz, du;
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const float sg = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z[e]));
-                        const float s = v[e] * sg;
-                        du[e] = s * z[e];
-                        dz[e] = s * u[e] * (1.0f + z[e] * (1.0f - sg));
-                    }
-                    *(uint2*)dst = pack(dz);
-                    *(uint2*)(dst + N) = pack(du);
-                } else {
-                    if constexpr (EPI == GEMM_EPI_RESIDUAL) v += unpack(r0[a][b]);
-                    *(uint2*)dst = pack(v);
-                }
+                if constexpr (EPI == GEMM_EPI_RESIDUAL) v += unpack(r0[a][b]);
+                *(uint2*)((uint16_t*)g.C + gm * g.ldc + gn) = pack(v);
             }
     }
 }

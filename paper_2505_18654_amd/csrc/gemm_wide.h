@@ -125,6 +125,23 @@ __device__ __forceinline__ void store_plain16(void* p, const uint4& v) {
     asm volatile("" ::: "memory");
 }
 
+// dgate = dh up silu'(gate) and dup = dh silu(gate) of eight columns (dh: x0, x1), each rounded once.
+__device__ __forceinline__ void gated_gradient(const floatx4& x0, const floatx4& x1, const uint4& gate, const uint4& up,
+                                               uint4* dgate, uint4* dup) {
+    const uint32_t gw[4] = {gate.x, gate.y, gate.z, gate.w}, uw[4] = {up.x, up.y, up.z, up.w};
+    float dg[8], du[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        const float dh = e < 4 ? x0[e & 3] : x1[e & 3], z = bf16_half(gw[e >> 1], e & 1);
+        const float sg = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
+        const float s = dh * sg;
+        du[e] = s * z;
+        dg[e] = s * bf16_half(uw[e >> 1], e & 1) * (1.0f + z * (1.0f - sg));
+    }
+    *dgate = make_uint4(pack_bf16x2(dg[0], dg[1]), pack_bf16x2(dg[2], dg[3]), pack_bf16x2(dg[4], dg[5]), pack_bf16x2(dg[6], dg[7]));
+    *dup = make_uint4(pack_bf16x2(du[0], du[1]), pack_bf16x2(du[2], du[3]), pack_bf16x2(du[4], du[5]), pack_bf16x2(du[6], du[7]));
+}
+
 // LDS hand-off between the lanes of one wave (its LDS operations run in order).
 __device__ __forceinline__ void wave_lds_fence() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -678,21 +695,8 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
                     const int row = 8 * q + (el >> 3), ch = el & 7, gm = em + 16 * b + row, gn = en + 8 * ch;
                     const floatx4 x0 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch) ^ row));
                     const floatx4 x1 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch + 1) ^ row));
-                    const uint32_t gw[4] = {pg[b & 3][q].x, pg[b & 3][q].y, pg[b & 3][q].z, pg[b & 3][q].w};
-                    const uint32_t uw[4] = {pu[b & 3][q].x, pu[b & 3][q].y, pu[b & 3][q].z, pu[b & 3][q].w};
-                    float dg[8], du[8];
-#pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        const float dh = e < 4 ? x0[e & 3] : x1[e & 3], z = bf16_half(gw[e >> 1], e & 1);
-                        const float sg = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
-                        const float s = dh * sg;
-                        du[e] = s * z;
-                        dg[e] = s * bf16_half(uw[e >> 1], e & 1) * (1.0f + z * (1.0f - sg));
-                    }
-                    const uint4 og = make_uint4(pack_bf16x2(dg[0], dg[1]), pack_bf16x2(dg[2], dg[3]),
-                                                pack_bf16x2(dg[4], dg[5]), pack_bf16x2(dg[6], dg[7]));
-                    const uint4 ou = make_uint4(pack_bf16x2(du[0], du[1]), pack_bf16x2(du[2], du[3]),
-                                                pack_bf16x2(du[4], du[5]), pack_bf16x2(du[6], du[7]));
+                    uint4 og, ou;
+                    gated_gradient(x0, x1, pg[b & 3][q], pu[b & 3][q], &og, &ou);
                     if (full || (gm < M && gn < N)) {
                         uint16_t* dst = (uint16_t*)g.C + gm * g.ldc + gn;
                         store_nt16(dst, &og);
