@@ -10,7 +10,7 @@
 // 0.15 us shorter.  Four stages, operands read a half step ahead, eight waves, and copies spread between the matrix
 // instructions, 2 to 15 % slower, gained nothing, so products of few tiles are split over k instead.)  Epilogues
 // work on a lane's four consecutive columns of a row, without staging: at these sizes the results stay in the L2
-// caches, which join the 32-byte pieces.
+// caches, which join the pieces.
 #pragma once
 
 #include <type_traits>
@@ -215,6 +215,9 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
         return floatx4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                        __uint_as_float(u.y & 0xffff0000u)};
     };
+    // Where the results are bf16 they pass through LDS, 4 KB of its own per wave, so that a lane has 16 bytes of a row.
+    char* stg = sm + 4096 * w;
+    if constexpr (GRAD || GATED || EPI == GEMM_EPI_GATED_BWD) lds_barrier();      // (the stages are no longer read)
     if constexpr (SPLIT) {
 #pragma unroll
         for (int b = 0; b < 4; b++)
@@ -265,7 +268,7 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
         for (int b = 0; b < 4; b++) {
             const float lse = __int_as_float(ri[b].x), gr = __int_as_float(ri[b].y) / top;
             const float gp = gr * __int_as_float(ri[b].w);
-            const int label = ri[b].z - g.class0 - en, gm = em + 16 * b;
+            const int label = ri[b].z - g.class0 - en;
 #pragma unroll
             for (int a = 0; a < 4; a++) {
 #pragma unroll
@@ -274,8 +277,16 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
                     if (label == 16 * a + e) acc[a][b][e] -= gr;
                 }
                 cs[a] += acc[a][b];
-                if (gm < M) *(uint2*)((uint16_t*)g.C + gm * g.ldc + en + 16 * a) = pack(acc[a][b]);
+                *(uint2*)(stg + 128 * lr + 16 * ((2 * a + (lg >> 1)) ^ (lr & 7)) + 8 * (lg & 1)) = pack(acc[a][b]);
             }
+            wave_lds_fence();
+#pragma unroll
+            for (int q = 0; q < 2; q++) {
+                const int gm = m0 + 64 * wm + 16 * b + 8 * q + (lane >> 3);
+                const uint4 v = *(const uint4*)(stg + 128 * (8 * q + (lane >> 3)) + 16 * ((lane & 7) ^ (lane >> 3)));
+                if (gm < M) *(uint4*)((uint16_t*)g.C + gm * g.ldc + n0 + 64 * wn + 8 * (lane & 7)) = v;
+            }
+            wave_lds_fence();
         }
         if (g.col_partial != nullptr) {
 #pragma unroll
@@ -291,25 +302,45 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
             }
         }
     } else if constexpr (GATED) {
+        // 16 rows at a time, 16-byte chunks: 0..3 the gate columns of a row, 4..7 the up columns (chunk c of row r at
+        // c ^ (r & 7)); then h, 32 rows at a time, 4 chunks a row (at c ^ (r / 2 & 3))
+        if constexpr (EPI == GEMM_EPI_GATED_SAVE) {
 #pragma unroll
-        for (int b = 0; b < 4; b++)
+            for (int b = 0; b < 4; b++) {
 #pragma unroll
-            for (int a = 0; a < 2; a++) {
-                const int gm = em + 16 * b, gn = n0 + 32 * wn + 16 * a + 4 * lg;
-                if (gm >= M || gn >= N) continue;
-                const floatx4 z = acc[a][b], u = acc[a + 2][b];
-                if constexpr (EPI == GEMM_EPI_GATED_SAVE) {
-                    uint16_t* p = (uint16_t*)g.C + gm * g.ldc + gn;
-                    *(uint2*)p = pack(z);
-                    *(uint2*)(p + N) = pack(u);
+                for (int a = 0; a < 4; a++)
+                    *(uint2*)(stg + 128 * lr + 16 * ((2 * a + (lg >> 1)) ^ (lr & 7)) + 8 * (lg & 1)) = pack(acc[a][b]);
+                wave_lds_fence();
+#pragma unroll
+                for (int q = 0; q < 2; q++) {
+                    const int gm = m0 + 64 * wm + 16 * b + 8 * q + (lane >> 3), gn = n0 + 32 * wn + 8 * (lane & 3);
+                    const uint4 v = *(const uint4*)(stg + 128 * (8 * q + (lane >> 3)) + 16 * ((lane & 7) ^ (lane >> 3)));
+                    if (gm < M && gn < N) *(uint4*)((uint16_t*)g.C + gm * g.ldc + gn + ((lane & 4) ? N : 0)) = v;
                 }
-                const floatx4 h = {silu(z[0]) * u[0], silu(z[1]) * u[1], silu(z[2]) * u[2], silu(z[3]) * u[3]};
-                *(uint2*)((uint16_t*)g.C2 + gm * g.ldc2 + gn) = pack(h);
+                wave_lds_fence();
             }
+        }
+#pragma unroll
+        for (int b2 = 0; b2 < 2; b2++) {
+#pragma unroll
+            for (int bb = 0; bb < 2; bb++)
+#pragma unroll
+                for (int a = 0; a < 2; a++) {
+                    const floatx4 z = acc[a][2 * b2 + bb], u = acc[a + 2][2 * b2 + bb];
+                    *(uint2*)(stg + 64 * (16 * bb + lr) + 16 * ((2 * a + (lg >> 1)) ^ (lr >> 1 & 3)) + 8 * (lg & 1)) =
+                        pack(floatx4{silu(z[0]) * u[0], silu(z[1]) * u[1], silu(z[2]) * u[2], silu(z[3]) * u[3]});
+                }
+            wave_lds_fence();
+#pragma unroll
+            for (int q = 0; q < 2; q++) {
+                const int row = 16 * q + (lane >> 2), gm = m0 + 64 * wm + 32 * b2 + row, gn = n0 + 32 * wn + 8 * (lane & 3);
+                const uint4 v = *(const uint4*)(stg + 64 * row + 16 * ((lane & 3) ^ (row >> 1 & 3)));
+                if (gm < M && gn < N) *(uint4*)((uint16_t*)g.C2 + gm * g.ldc2 + gn) = v;
+            }
+            wave_lds_fence();
+        }
     } else if constexpr (EPI == GEMM_EPI_GATED_BWD) {
         // as in gemm_wide.h: dh passes through LDS in fp32, so that a lane has 8 columns of a row
-        lds_barrier();                                         // (the stages are no longer read)
-        char* stg = sm + 4096 * w;
 #pragma unroll
         for (int b = 0; b < 4; b++) {
 #pragma unroll
