@@ -8,9 +8,9 @@
 // (A workgroup alone on its CU takes 0.8 us per step, for 0.2 us of matrix work: a chain of the wait, the barrier,
 // the copies and the reads.  Without the matrix instructions or the reads it was as long, without the copies
 // 0.15 us shorter.  Four stages, operands read a half step ahead, eight waves, and copies spread between the matrix
-// instructions, 2 to 15 % slower, gained nothing, so products of few tiles are split over k instead.)  Epilogues
-// work on a lane's four consecutive columns of a row, without staging: at these sizes the results stay in the L2
-// caches, which join the pieces.
+// instructions, 2 to 15 % slower, gained nothing, so products of few tiles are split over k instead.)  bf16 results
+// pass through LDS, so that a lane stores 16 bytes and eight lanes a line: straight from the accumulators, 8 bytes and
+// 32 bytes of a row at a time, dpre of 6,418 tokens, 256 / 704, took 21.6 us, now 16.3.
 #pragma once
 
 #include <type_traits>
@@ -161,13 +161,15 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
 
     // acc[a][b] will hold row em + 16 b, columns en + 16 a + 0..3; what the epilogue reads there is loaded first
     const int em = m0 + 64 * wm + lr, en = n0 + 64 * wn + 4 * lg;
-    uint2 r0[EPI == GEMM_EPI_RESIDUAL ? 4 : 1][4];
+    // residual of row 8 q + l / 8 of block b, chunk l % 8 of the wave's 64 columns
+    uint4 rr[EPI == GEMM_EPI_RESIDUAL ? 4 : 1][2];
     if constexpr (EPI == GEMM_EPI_RESIDUAL) {
+        const uint16_t* R = (const uint16_t*)g.R + min(n0 + 64 * wn + 8 * (lane & 7), N - 8);
 #pragma unroll
         for (int b = 0; b < 4; b++)
 #pragma unroll
-            for (int a = 0; a < 4; a++)
-                r0[a][b] = *(const uint2*)((const uint16_t*)g.R + min(em + 16 * b, M - 1) * g.ldr + min(en + 16 * a, N - 4));
+            for (int q = 0; q < 2; q++)
+                rr[b][q] = *(const uint4*)(R + min(m0 + 64 * wm + 16 * b + 8 * q + (lane >> 3), M - 1) * g.ldr);
     }
     // gate and up values of row 8 q + l / 8 of block b, chunk l % 8 of the wave's 64 columns
     uint4 pg[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][2], pu[EPI == GEMM_EPI_GATED_BWD ? 4 : 1][2];
@@ -217,7 +219,7 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
     };
     // Where the results are bf16 they pass through LDS, 4 KB of its own per wave, so that a lane has 16 bytes of a row.
     char* stg = sm + 4096 * w;
-    if constexpr (GRAD || GATED || EPI == GEMM_EPI_GATED_BWD) lds_barrier();      // (the stages are no longer read)
+    if constexpr (!SPLIT && !STATS) lds_barrier();             // (the stages are no longer read)
     if constexpr (SPLIT) {
 #pragma unroll
         for (int b = 0; b < 4; b++)
@@ -339,8 +341,8 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
             }
             wave_lds_fence();
         }
-    } else if constexpr (EPI == GEMM_EPI_GATED_BWD) {
-        // as in gemm_wide.h: dh passes through LDS in fp32, so that a lane has 8 columns of a row
+    } else {
+        // through LDS in fp32, so that dh and the residual are met unrounded
 #pragma unroll
         for (int b = 0; b < 4; b++) {
 #pragma unroll
@@ -350,29 +352,28 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
             for (int q = 0; q < 2; q++) {
                 const int row = 8 * q + (lane >> 3), ch = lane & 7;
                 const int gm = m0 + 64 * wm + 16 * b + row, gn = n0 + 64 * wn + 8 * ch;
-                const floatx4 x0 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch) ^ row));
-                const floatx4 x1 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch + 1) ^ row));
-                uint4 og, ou;
-                gated_gradient(x0, x1, pg[b][q], pu[b][q], &og, &ou);
-                if (gm < M && gn < N) {
-                    uint16_t* dst = (uint16_t*)g.C + gm * g.ldc + gn;
-                    *(uint4*)dst = og;
-                    *(uint4*)(dst + N) = ou;
+                floatx4 x0 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch) ^ row));
+                floatx4 x1 = *(const floatx4*)(stg + 256 * row + 16 * ((2 * ch + 1) ^ row));
+                uint16_t* dst = (uint16_t*)g.C + gm * g.ldc + gn;
+                const bool in = gm < M && gn < N;
+                if constexpr (EPI == GEMM_EPI_GATED_BWD) {
+                    uint4 og, ou;
+                    gated_gradient(x0, x1, pg[b][q], pu[b][q], &og, &ou);
+                    if (in) {
+                        *(uint4*)dst = og;
+                        *(uint4*)(dst + N) = ou;
+                    }
+                } else {
+                    if constexpr (EPI == GEMM_EPI_RESIDUAL) {
+                        x0 += unpack(make_uint2(rr[b][q].x, rr[b][q].y));
+                        x1 += unpack(make_uint2(rr[b][q].z, rr[b][q].w));
+                    }
+                    const uint2 lo = pack(x0), hi = pack(x1);
+                    if (in) *(uint4*)dst = make_uint4(lo.x, lo.y, hi.x, hi.y);
                 }
             }
             wave_lds_fence();
         }
-    } else {
-#pragma unroll
-        for (int b = 0; b < 4; b++)
-#pragma unroll
-            for (int a = 0; a < 4; a++) {
-                const int gm = em + 16 * b, gn = en + 16 * a;
-                if (gm >= M || gn >= N) continue;
-                floatx4 v = acc[a][b];
-                if constexpr (EPI == GEMM_EPI_RESIDUAL) v += unpack(r0[a][b]);
-                *(uint2*)((uint16_t*)g.C + gm * g.ldc + gn) = pack(v);
-            }
     }
 }
 
