@@ -16,7 +16,7 @@
 // - 75,132 tokens, 512 / 1408, training: first product 250 us (0.87 PFLOP/s; 635 MB written), second 120;
 // - 69,563 tokens, 1024 / 2816, training: 771 (1.04 PFLOP/s) and 380 us; backward: dpre 535 us (0.75; 1.6 GB of
 //   pre read and dpre written), dx 710 (1.13), the weight gradients 1,180 (1.02) with their splits' sums;
-// - 6,418 tokens, 256 / 704, backward: dpre 21.6 us, the three products behind it in one launch 28.4, the sums 7.2.
+// - 6,418 tokens, 256 / 704, backward: dpre 16.3 us, the three products behind it in one launch 26.9, the sums 7.2.
 #include "gemm_mid.h"
 
 namespace mtgr {

@@ -8,8 +8,8 @@
 // (A workgroup alone on its CU takes 0.8 us per step, for 0.2 us of matrix work: a chain of the wait, the barrier,
 // the copies and the reads.  Without the matrix instructions or the reads it was as long, without the copies
 // 0.15 us shorter.  Four stages, operands read a half step ahead, eight waves, and copies spread between the matrix
-// instructions, 2 to 15 % slower, gained nothing, so products of few tiles are split over k instead.)  bf16 results
-// pass through LDS, so that a lane stores 16 bytes and eight lanes a line: straight from the accumulators, 8 bytes and
+// instructions, 2 to 15 % slower, gained nothing, so products of few tiles are split over k instead.)  Results pass
+// through LDS, so that a lane stores 16 bytes and its neighbours the rest of the line: straight from the accumulators, 8 bytes and
 // 32 bytes of a row at a time, dpre of 6,418 tokens, 256 / 704, took 21.6 us, now 16.3.
 #pragma once
 
@@ -217,19 +217,25 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
         return floatx4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                        __uint_as_float(u.y & 0xffff0000u)};
     };
-    // Where the results are bf16 they pass through LDS, 4 KB of its own per wave, so that a lane has 16 bytes of a row.
+    // The results pass through LDS, 4 KB of its own per wave, so that a lane has 16 bytes of a row and a line is whole.
     char* stg = sm + 4096 * w;
-    if constexpr (!SPLIT && !STATS) lds_barrier();             // (the stages are no longer read)
+    if constexpr (!STATS) lds_barrier();                       // (the stages are no longer read)
     if constexpr (SPLIT) {
 #pragma unroll
-        for (int b = 0; b < 4; b++)
+        for (int b = 0; b < 4; b++) {
 #pragma unroll
-            for (int a = 0; a < 4; a++) {
-                const int gm = em + 16 * b, gn = en + 16 * a;
+            for (int a = 0; a < 4; a++) *(floatx4*)(stg + 256 * lr + 16 * ((4 * a + lg) ^ lr)) = acc[a][b];
+            wave_lds_fence();
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const int row = 4 * q + lg, gm = m0 + 64 * wm + 16 * b + row, gn = n0 + 64 * wn + 4 * lr;
+                const floatx4 v = *(const floatx4*)(stg + 256 * row + 16 * (lr ^ row));
                 if (gm >= M || gn >= N) continue;
                 floatx4* dst = (floatx4*)(g.partial + ((long long)split * M + gm) * N + gn);
-                *dst = ACC && g.accumulate ? *dst + acc[a][b] : acc[a][b];
+                *dst = ACC && g.accumulate ? *dst + v : v;
             }
+            wave_lds_fence();
+        }
     } else if constexpr (STATS) {
         floatx4 bias[4];
 #pragma unroll
