@@ -431,7 +431,8 @@ constexpr double WIDE_START = 7.0, WIDE_STEP = 1.3;
 static inline double partials_us(double elements) { return 4.0 + elements * 8 / 8e6; }
 
 // n_cols: columns of the result per 256 columns of B (128 for the gated products).
-static inline Tiles tiles_of(bool mid, long long M, long long N, long long K, int n_cols, int splits, bool partials) {
+// end: an epilogue's own time per round.
+static inline Tiles tiles_of(bool mid, long long M, long long N, long long K, int n_cols, int splits, bool partials, double end = 0.0) {
     Tiles t{};
     t.mid = mid;
     const int side = mid ? MBM : WBM, cols = mid ? n_cols / 2 : n_cols;
@@ -441,14 +442,14 @@ static inline Tiles tiles_of(bool mid, long long M, long long N, long long K, in
     const unsigned all = (unsigned)((K + WBK - 1) / WBK), steps = (all + splits - 1) / (unsigned)splits;
     const long long items = (long long)t.mblocks * t.nblocks * splits;
     if (mid) t.us = (double)((items + MID_WORKGROUPS - 1) / MID_WORKGROUPS) *
-                    (MID_START + (items > WIDE_WORKGROUPS ? MID_STEP : MID_STEP_ALONE) * steps);
-    else t.us = (double)((items + WIDE_WORKGROUPS - 1) / WIDE_WORKGROUPS) * (WIDE_START + WIDE_STEP * steps);
+                    (MID_START + end + (items > WIDE_WORKGROUPS ? MID_STEP : MID_STEP_ALONE) * steps);
+    else t.us = (double)((items + WIDE_WORKGROUPS - 1) / WIDE_WORKGROUPS) * (WIDE_START + end + WIDE_STEP * steps);
     if (partials) t.us += partials_us((double)splits * M * N);
     return t;
 }
 
-static inline Tiles plan(long long M, long long N, long long K, int n_cols = WBN) {
-    const Tiles wide = tiles_of(false, M, N, K, n_cols, 1, false), mid = tiles_of(true, M, N, K, n_cols, 1, false);
+static inline Tiles plan(long long M, long long N, long long K, int n_cols = WBN, double wide_end = 0.0, double mid_end = 0.0) {
+    const Tiles wide = tiles_of(false, M, N, K, n_cols, 1, false, wide_end), mid = tiles_of(true, M, N, K, n_cols, 1, false, mid_end);
     return mid.us < wide.us ? mid : wide;
 }
 

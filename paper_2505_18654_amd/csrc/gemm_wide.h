@@ -113,10 +113,12 @@ __device__ __forceinline__ uint4 load_nt16(const void* p) {
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// Whether dz (`rows` of `ld` bf16) stays in the last-level cache of 256 MB until the next two products have read it
-// (2,900 rows, 20,011 classes, 120 MB, backward with stores past the caches 186 us, with plain ones 171; 8,000 rows,
-// 320 MB: 247 and 266).
-__device__ __forceinline__ bool dz_stays(long long rows, long long ld) { return rows * ld * 2 <= 192ll << 20; }
+// Whether a result of so many bytes is left in the last-level cache of 256 MB for the next product, or stored past
+// the caches.  dz, up to 192 MB: 2,900 rows, 20,011 classes, 120 MB, backward with stores past the caches 186 us, with
+// plain ones 171; 8,000 rows, 320 MB: 247 and 266.  h, 64 MB: 8,000 tokens, 512 / 1408, 22 MB, second product 23 and
+// 19 us; 75,132, 212 MB, forward 371 and 422.  dpre, 128 MB: 6,418 tokens, 1024 / 2816, 72 MB, dx 99 and 78 us.
+__device__ __forceinline__ bool stays(long long bytes, long long most) { return bytes <= most; }
+__device__ __forceinline__ bool dz_stays(long long rows, long long ld) { return stays(rows * ld * 2, 192ll << 20); }
 
 // A plain store beside a non-temporal one of the same value: merged by the compiler, both would be plain.
 __device__ __forceinline__ void store_plain16(void* p, const uint4& v) {
@@ -685,6 +687,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
                 }
             }
         } else if constexpr (EPI == GEMM_EPI_GATED_BWD) {
+            const bool dpre_stays = stays((long long)M * N * 4, 128ll << 20);
             // dh passes through LDS in fp32, one block at a time, so that a lane has 8 columns of a row:
             // dgate = dh up silu'(gate), dup = dh silu(gate), rounded once
 #pragma unroll
@@ -699,17 +702,23 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
                     gated_gradient(x0, x1, pg[b & 3][q], pu[b & 3][q], &og, &ou);
                     if (full || (gm < M && gn < N)) {
                         uint16_t* dst = (uint16_t*)g.C + gm * g.ldc + gn;
-                        store_nt16(dst, &og);
-                        store_nt16(dst + N, &ou);
+                        if (dpre_stays) {
+                            store_plain16(dst, og);
+                            store_plain16(dst + N, ou);
+                        } else {
+                            store_nt16(dst, &og);
+                            store_nt16(dst + N, &ou);
+                        }
                     }
                 }
                 if (b < 4) load_pre(b + 4);
                 wave_lds_fence();
             }
         } else if constexpr (GATED) {
+            const bool h_stays = stays((long long)M * N * 2, 64ll << 20);
             // acc[a][0..3] hold gate columns en + 16 b + 4 (l / 16) + 0..3, acc[a][4..7] the up columns of the same
             // numbers.  32 rows at a time: 16-byte chunk c (of 8) of row r at c ^ (r & 7)
-            auto rows_out = [&](int rd, uint16_t* base, long long ld, auto value) {
+            auto rows_out = [&](int rd, uint16_t* base, long long ld, bool keep, auto value) {
 #pragma unroll
                 for (int aa = 0; aa < 2; aa++)
 #pragma unroll
@@ -724,17 +733,20 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
                     const uint4 v = *(const uint4*)(stg + 128 * (8 * q + (el >> 3)) + 16 * ((el & 7) ^ (el >> 3)));
-                    if (full || (gm + 8 * q < M && gn < N)) store_nt16(dst + 8 * q * ld, &v);
+                    if (full || (gm + 8 * q < M && gn < N)) {
+                        if (keep) store_plain16(dst + 8 * q * ld, v);
+                        else store_nt16(dst + 8 * q * ld, &v);
+                    }
                 }
                 wave_lds_fence();
             };
 #pragma unroll
             for (int rd = 0; rd < 2; rd++) {
                 if constexpr (EPI == GEMM_EPI_GATED_SAVE) {
-                    rows_out(rd, (uint16_t*)g.C, g.ldc, [&](int a, int b) { return acc[a][b]; });
-                    rows_out(rd, (uint16_t*)g.C + N, g.ldc, [&](int a, int b) { return acc[a][b + 4]; });
+                    rows_out(rd, (uint16_t*)g.C, g.ldc, false, [&](int a, int b) { return acc[a][b]; });
+                    rows_out(rd, (uint16_t*)g.C + N, g.ldc, false, [&](int a, int b) { return acc[a][b + 4]; });
                 }
-                rows_out(rd, (uint16_t*)g.C2, g.ldc2, [&](int a, int b) {
+                rows_out(rd, (uint16_t*)g.C2, g.ldc2, h_stays, [&](int a, int b) {
                     const floatx4 ga = acc[a][b], up = acc[a][b + 4];
                     return floatx4{silu(ga[0]) * up[0], silu(ga[1]) * up[1], silu(ga[2]) * up[2], silu(ga[3]) * up[3]};
                 });
