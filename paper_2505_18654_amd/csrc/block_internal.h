@@ -16,8 +16,8 @@ constexpr int GEMM_EPI_RESIDUAL = 3, GEMM_EPI_GATED = 4, GEMM_EPI_GATED_SAVE = 5
               GEMM_EPI_PART = 12;
 struct TileArgs : GemmArgs {
     // The products of the softmax loss:
-    const int* rows;          // number of token rows on the device (at most M, or K of TN); SM_GRAD: a float
-                              // behind it, the largest gradient of a row's loss
+    const int* rows;          // number of token rows on the device (at most M, or K of TN); behind it a float, the
+                              // largest gradient of a row's loss (SM_GRAD), and tile_run's number (softmax_tiles.h)
     int b_rows;               // rows of B (classes), where they are fewer than N or K
     int class0;               // first class of the piece
     int group_m;              // m blocks that an XCD's workgroups share
