@@ -5,7 +5,7 @@
  * The conventions are those of include/mtgr_hstu.h: caller-owned device memory, calls asynchronous on
  * `stream`, no allocation, no synchronisation, outputs overwritten, arguments checked on the host before
  * any launch.  Matrices are row-major with a row stride (ld, in elements) of at least their columns, a
- * multiple of 16 bytes; their base is 16-byte aligned.  Outputs do not overlap inputs unless stated.  A
+ * multiple of 16 bytes, below 2^22; their base is 16-byte aligned.  Outputs do not overlap inputs unless stated.  A
  * workspace may hold anything before a call and belongs to it until it has ended on its stream: calls
  * that can run at the same time (captured graphs too) take one each.
  */
@@ -24,7 +24,7 @@ extern "C" {
  *   h   = silu(gate) * up      [T, f]
  *   y   = h W_out (+ r)        W_out [f, d], r [T, d]
  *
- * d and f are multiples of 32.  Sums are fp32; h, pre and the gradients of pre are rounded to bf16. */
+ * d and f are multiples of 32, below 2^20; ceil(T / 256) ceil(2 max(d, f) / 128) is below 2^24.  Sums are fp32; h, pre and the gradients of pre are rounded to bf16. */
 typedef struct {
     int64_t num_tokens;       /* T, 0 .. 2^31 - 1 */
     int32_t dim;              /* d */
@@ -69,7 +69,7 @@ mtgr_status_t mtgr_gated_ffn_bwd(const mtgr_gated_ffn_problem_t* p, const void* 
  * captured graph.  site numbers the places of a model that drop, so that their masks differ; the step
  * counts modulo 2^32.  Element e is kept when word e % 4 of Philox4x32-7 with the key seed and the counter
  * (e / 4 low, e / 4 high, site, step) is at least floor(prob 2^32).  0 <= prob < 1.  cols is a multiple of
- * 16 bytes, rows * cols below 2^50.  A dropped element counts as 0 whatever x holds.  out may be x or the residual. */
+ * 16 bytes, rows * cols below 2^50; dense rows (ld = cols) may be of any width.  A dropped element counts as 0 whatever x holds.  out may be x or the residual. */
 mtgr_status_t mtgr_dropout(int64_t rows, int32_t cols, mtgr_dtype_t dtype, const void* x, int64_t ld_x, double prob,
                            const uint64_t* rng, uint32_t site, const void* residual, int64_t ld_residual, void* out,
                            int64_t ld_out, mtgr_stream_t stream);

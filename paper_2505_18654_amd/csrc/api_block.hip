@@ -12,14 +12,14 @@ using namespace mtgr_api;
 
 constexpr long long MAX_LD = 1ll << 22;        // 32-bit copy offsets over 256 rows
 
-// A matrix of `cols` columns of `esize` bytes per element.
-mtgr_status_t check_matrix(const void* p, const char* name, int64_t ld, int64_t cols, int esize = 2) {
+// A matrix of `cols` columns of `esize` bytes per element; dense_any: of any width where its rows are dense.
+mtgr_status_t check_matrix(const void* p, const char* name, int64_t ld, int64_t cols, int esize = 2, bool dense_any = false) {
     if (!p) return fail(MTGR_ERROR_NULL_POINTER, "%s is NULL", name);
     if (!aligned16(p)) return fail(MTGR_ERROR_INVALID_ARGUMENT, "%s is not 16-byte aligned", name);
     if (ld < cols || ld % (16 / esize) != 0)
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "row stride of %s = %lld (needs at least %lld and 16-byte rows)", name,
                     (long long)ld, (long long)cols);
-    if (ld >= MAX_LD)
+    if (ld >= MAX_LD && !(dense_any && ld == cols))
         return fail(MTGR_ERROR_UNSUPPORTED, "row stride of %s = %lld is not below %lld", name, (long long)ld, MAX_LD);
     return MTGR_SUCCESS;
 }
@@ -223,9 +223,9 @@ mtgr_status_t mtgr_dropout(int64_t rows, int32_t cols, mtgr_dtype_t dtype, const
     if (cols % per != 0) return fail(MTGR_ERROR_INVALID_ARGUMENT, "cols = %d is not a multiple of %d", cols, per);
     if (!(prob >= 0.0 && prob < 1.0)) return fail(MTGR_ERROR_INVALID_ARGUMENT, "prob = %g outside [0, 1)", prob);
     if (rows == 0) return ok();
-    CHECK(check_matrix(x, "x", ld_x, cols, esize));
-    CHECK(check_matrix(out, "out", ld_out, cols, esize));
-    if (residual) CHECK(check_matrix(residual, "residual", ld_residual, cols, esize));
+    CHECK(check_matrix(x, "x", ld_x, cols, esize, true));
+    CHECK(check_matrix(out, "out", ld_out, cols, esize, true));
+    if (residual) CHECK(check_matrix(residual, "residual", ld_residual, cols, esize, true));
     if (!rng) return fail(MTGR_ERROR_NULL_POINTER, "rng is NULL");
     if (!aligned(rng, 8)) return fail(MTGR_ERROR_INVALID_ARGUMENT, "rng is not 8-byte aligned");
     mtgr::DropoutArgs a{};
