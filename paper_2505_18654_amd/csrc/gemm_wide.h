@@ -795,7 +795,8 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
                     }
                 }
             }
-            const float factor = DIRECT ? g.scale * ((const float*)g.rows)[1] : 0.f;
+            // (scale and the largest |g| one after the other: their product alone may leave the float range)
+            const float largest = DIRECT ? ((const float*)g.rows)[1] : 0.f;
             const bool plain = GRAD && dz_stays(M, g.ldc);
             // bf16, 32 rows (two blocks) at a time: 16-byte chunk c (of 8) of row r at c ^ (r & 7)
 #pragma unroll
@@ -807,7 +808,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
 #pragma unroll
                         for (int a = 0; a < WNN; a++) {
                             floatx4 v = acc[a][2 * rd + bb];
-                            if constexpr (DIRECT) v *= factor;
+                            if constexpr (DIRECT) v = v * g.scale * largest;
                             if (out == 1) {
 #pragma unroll
                                 for (int e = 0; e < 4; e++) v[e] = silu(v[e] + bi[a][e]);

@@ -331,7 +331,8 @@ struct FinishArgs {
 };
 
 __global__ __launch_bounds__(256) void sm_finish_kernel(SoftmaxLossArgs a, FinishArgs f) {
-    const float top = ((const float*)f.rows)[1], factor = a.scale * top;
+    // (scale and the largest |g| one after the other: their product alone may leave the float range)
+    const float top = ((const float*)f.rows)[1], scale = a.scale;
     int block = blockIdx.x;
     if (block < f.dw_blocks) {
         const int ch = a.d / 4;
@@ -342,7 +343,7 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SoftmaxLossArgs a, Finis
             const float* p = f.dw_partial + r * a.d + c;
             floatx4 s = *(const floatx4*)p;
             for (int k = 1; k < f.dw_splits; k++) s += *(const floatx4*)(p + k * per);
-            s *= factor;
+            s = s * scale * top;
             *(uint2*)((uint16_t*)a.dw + (f.v0 + r) * a.ld_w + c) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
         }
         return;
@@ -374,8 +375,8 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SoftmaxLossArgs a, Finis
             lo += *(const floatx4*)(p + k * per);
             hi += *(const floatx4*)(p + k * per + 4);
         }
-        lo *= factor;
-        hi *= factor;
+        lo = lo * scale * top;
+        hi = hi * scale * top;
         *(uint4*)((uint16_t*)a.dx + f.index[r] * a.ld_x + c) =
             make_uint4(pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3]));
     }
