@@ -92,7 +92,7 @@ typedef struct {
     int64_t num_classes;      /* V */
     int32_t dim;              /* d */
     int32_t target_bits;      /* targets are int32 (32) or int64 (64) */
-    float scale;              /* finite */
+    float scale;              /* absolute value below 2.358e38 (finite in units of log 2) */
     int64_t ld_x;             /* x and dx */
     int64_t ld_w;             /* w and dw */
 } mtgr_softmax_loss_problem_t;

@@ -70,7 +70,9 @@ mtgr_status_t check_loss(const mtgr_softmax_loss_problem_t* p) {
         return fail(MTGR_ERROR_UNSUPPORTED, "dim = %d is not a multiple of 32 up to 2048", p->dim);
     if (p->target_bits != 32 && p->target_bits != 64)
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "target_bits = %d is not 32 or 64", p->target_bits);
-    if (!std::isfinite(p->scale)) return fail(MTGR_ERROR_INVALID_ARGUMENT, "scale is not finite");
+    // (the logits are formed in units of log 2)
+    if (!std::isfinite(p->scale * 1.4426950408889634f))
+        return fail(MTGR_ERROR_INVALID_ARGUMENT, "scale = %g is not below 2.358e38", p->scale);
     if (p->num_rows > 0 && p->num_classes == 0)
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "num_classes is 0 with rows present");
     // tiles of a piece's products in one launch
