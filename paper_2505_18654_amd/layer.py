@@ -115,6 +115,12 @@ class FfnParams:
     w_out: torch.Tensor      # [f, d] bf16
 
 
+def _drops(p_drop: float) -> bool:
+    if not 0.0 <= p_drop < 1.0:
+        raise ValueError(f"p_drop = {p_drop} is outside [0, 1)")
+    return p_drop > 0.0
+
+
 def ffn_fwd(x: torch.Tensor, jag: ops.Jagged, P: FfnParams, rng=None, p_drop: float = 0.0, site: int = 0,
             eps: float = 1e-5, save: bool = True):
     """The feed-forward block that may follow an encoder layer, with its residual branch:
@@ -123,8 +129,8 @@ def ffn_fwd(x: torch.Tensor, jag: ops.Jagged, P: FfnParams, rng=None, p_drop: fl
 
     Returns (x_out [T, d], ctx for ffn_bwd), with save=False (serving) (x_out, None).  `rng` (device int64 [2]:
     seed, step) and `site` fix the dropped elements and have to be the same in ffn_bwd (ops.dropout)."""
+    drops = _drops(p_drop)
     xt, m, r = ops.gln_fwd(x, None, jag.seg, P.gamma, P.beta, eps)
-    drops = p_drop > 0.0
     out = ops.gated_ffn_fwd(xt, P.w_in, P.w_out, residual=None if drops else x, save=save)
     y, pre, h = out if save else (out, None, None)
     if drops:
@@ -135,7 +141,7 @@ def ffn_fwd(x: torch.Tensor, jag: ops.Jagged, P: FfnParams, rng=None, p_drop: fl
 def ffn_bwd(dx_out: torch.Tensor, ctx: dict, jag: ops.Jagged, P: FfnParams, rng=None, p_drop: float = 0.0,
             site: int = 0, eps: float = 1e-5) -> dict:
     """Gradients of ffn_fwd: dict with x and every FfnParams field."""
-    dy = ops.dropout(dx_out, p_drop, rng, site) if p_drop > 0.0 else dx_out
+    dy = ops.dropout(dx_out, p_drop, rng, site) if _drops(p_drop) else dx_out
     g = {}
     dxt, g["w_in"], g["w_out"] = ops.gated_ffn_bwd(dy, ctx["xt"], ctx["pre"], ctx["h"], P.w_in, P.w_out)
     # (one pass adds the residual branch's gradient, unless X is a view with gaps between its rows)
