@@ -59,6 +59,13 @@ mtgr_status_t mtgr_gated_ffn_bwd(const mtgr_gated_ffn_problem_t* p, const void* 
                                  const void* h, const void* w_in, const void* w_out, void* dx, void* dw_in,
                                  void* dw_out, void* workspace, size_t workspace_bytes, mtgr_stream_t stream);
 
+/* Debugging aid (host only): the kernels that a pass of these sizes runs on, as "name=kernel" pairs separated by
+ * blanks, for profiles and for tests that mean to reach a certain kernel; the names may change.  Forward: hidden
+ * (rows, or tiles with their K splits), h (cached or streamed stores), out; residual: whether there is one.
+ * Backward: dpre, store, together (one launch behind dpre), dx, dw_in, dw_out.  128 bytes are enough. */
+mtgr_status_t mtgr_debug_gated_ffn_kernels(const mtgr_gated_ffn_problem_t* p, mtgr_ffn_pass_t pass, int residual, char* text,
+                                           size_t text_bytes);
+
 /* ---------------------------------------------------------------- dropout
  *
  *   out = [residual +] (keep ? x / (1 - prob) : 0)         [rows, cols] of bf16 or fp32
@@ -109,6 +116,11 @@ mtgr_status_t mtgr_softmax_loss_bwd(const mtgr_softmax_loss_problem_t* p, const 
                                     const void* w, const void* targets, const float* bias, const float* lse, void* dx,
                                     void* dw, float* dbias, void* workspace, size_t workspace_bytes,
                                     mtgr_stream_t stream);
+
+/* Debugging aid (host only), as mtgr_debug_gated_ffn_kernels, for `labels` rows with a label: logits, run (class tiles
+ * that an item goes through), pieces and piece (of classes), and for the backward dz (cached or streamed stores), dx, dw. */
+mtgr_status_t mtgr_debug_softmax_loss_kernels(const mtgr_softmax_loss_problem_t* p, int backward, int64_t labels, char* text,
+                                              size_t text_bytes);
 
 #ifdef __cplusplus
 }

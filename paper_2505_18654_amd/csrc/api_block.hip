@@ -114,6 +114,13 @@ mtgr::SoftmaxLossArgs loss_args(const mtgr_softmax_loss_problem_t* p, const void
     return a;
 }
 
+// What snprintf returned for a caller's buffer.
+mtgr_status_t text_fits(int length, size_t bytes) {
+    if (length < 0 || (size_t)length >= bytes)
+        return fail(MTGR_ERROR_INVALID_ARGUMENT, "text of %d bytes does not fit into %zu", length + 1, bytes);
+    return ok();
+}
+
 size_t loss_workspace(const mtgr_softmax_loss_problem_t* p, bool backward) {
     return mtgr::softmax_loss_workspace_bytes(p->num_rows, (int)p->num_classes, p->dim, backward);
 }
@@ -215,6 +222,20 @@ mtgr_status_t mtgr_gated_ffn_bwd(const mtgr_gated_ffn_problem_t* p, const void* 
     return ok();
 }
 
+mtgr_status_t mtgr_debug_gated_ffn_kernels(const mtgr_gated_ffn_problem_t* p, mtgr_ffn_pass_t pass, int residual, char* text,
+                                           size_t text_bytes) {
+    if (!text) return fail(MTGR_ERROR_NULL_POINTER, "text is NULL");
+    CHECK(check_ffn(p));
+    if (pass != MTGR_FFN_SERVING && pass != MTGR_FFN_BACKWARD && pass != MTGR_FFN_TRAINING)
+        return fail(MTGR_ERROR_INVALID_ARGUMENT, "pass %d unknown", (int)pass);
+    if (p->num_tokens == 0) return fail(MTGR_ERROR_INVALID_ARGUMENT, "no tokens, no kernels");
+    const long long T = p->num_tokens;
+    return text_fits(pass == MTGR_FFN_BACKWARD
+                         ? mtgr::ffn_bwd_kernels(T, p->dim, p->hidden, text, text_bytes)
+                         : mtgr::ffn_fwd_kernels(T, p->dim, p->hidden, pass == MTGR_FFN_TRAINING, residual != 0, text, text_bytes),
+                     text_bytes);
+}
+
 mtgr_status_t mtgr_dropout(int64_t rows, int32_t cols, mtgr_dtype_t dtype, const void* x, int64_t ld_x, double prob,
                            const uint64_t* rng, uint32_t site, const void* residual, int64_t ld_residual, void* out,
                            int64_t ld_out, mtgr_stream_t stream) {
@@ -253,6 +274,17 @@ mtgr_status_t mtgr_softmax_loss_workspace_size(const mtgr_softmax_loss_problem_t
     CHECK(check_loss(p));
     *bytes = loss_workspace(p, backward != 0);
     return ok();
+}
+
+mtgr_status_t mtgr_debug_softmax_loss_kernels(const mtgr_softmax_loss_problem_t* p, int backward, int64_t labels, char* text,
+                                              size_t text_bytes) {
+    if (!text) return fail(MTGR_ERROR_NULL_POINTER, "text is NULL");
+    CHECK(check_loss(p));
+    if (labels < 0 || labels > p->num_rows)
+        return fail(MTGR_ERROR_INVALID_ARGUMENT, "labels = %lld of %lld rows", (long long)labels, (long long)p->num_rows);
+    if (p->num_rows == 0) return fail(MTGR_ERROR_INVALID_ARGUMENT, "no rows, no kernels");
+    return text_fits(mtgr::softmax_loss_kernels(p->num_rows, (int)p->num_classes, p->dim, backward != 0, labels, text, text_bytes),
+                     text_bytes);
 }
 
 mtgr_status_t mtgr_softmax_loss_fwd(const mtgr_softmax_loss_problem_t* p, const void* x, const void* w,

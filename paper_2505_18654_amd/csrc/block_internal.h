@@ -68,6 +68,9 @@ hipError_t launch_ffn_rows_hidden(const FfnArgs& a, hipStream_t s);
 hipError_t launch_ffn_rows_out(const FfnArgs& a, hipStream_t s);
 size_t ffn_bwd_workspace_bytes(long long T, int d, int f);
 hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s);
+// The kernels that a pass runs on, as text (snprintf's result).
+int ffn_fwd_kernels(long long T, int d, int f, bool save, bool residual, char* text, size_t n);
+int ffn_bwd_kernels(long long T, int d, int f, char* text, size_t n);
 
 // Softmax loss over a class set (softmax_loss.hip).
 struct SoftmaxLossArgs {
@@ -87,5 +90,6 @@ struct SoftmaxLossArgs {
 size_t softmax_loss_workspace_bytes(long long N, int V, int d, bool backward);
 hipError_t launch_softmax_loss_fwd(const SoftmaxLossArgs& a, void* workspace, hipStream_t s);
 hipError_t launch_softmax_loss_bwd(const SoftmaxLossArgs& a, void* workspace, hipStream_t s);
+int softmax_loss_kernels(long long N, int V, int d, bool backward, long long labels, char* text, size_t n);
 
 }  // namespace mtgr

@@ -17,6 +17,8 @@
 // - 69,563 tokens, 1024 / 2816, training: 771 (1.04 PFLOP/s) and 380 us; backward: dpre 535 us (0.75; 1.6 GB of
 //   pre read and dpre written), dx 710 (1.13), the weight gradients 1,180 (1.02) with their splits' sums;
 // - 6,418 tokens, 256 / 704, backward: dpre 16.3 us, the three products behind it in one launch 26.9, the sums 7.2.
+#include <stdio.h>
+
 #include "gemm_mid.h"
 
 namespace mtgr {
@@ -110,18 +112,33 @@ static hipError_t deep_product(TileArgs g, const Tiles& t, float* partial, hipSt
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Whether the second product is done by the kernel for few rows.  Its waves go through k alone (no launch adds
-// partials), so that a deep k favours the tiles split over k: 64 .. 128 tokens, f = 1408: 8.7 us, 11.2 there; f = 2816:
-// 15, 11.3; up to 32 tokens, f = 2816: 7.5 .. 10.8, 9.6 .. 10.1; 312 tokens, f = 2048: 11.5, 14.4.
-static bool rows_output(long long T, int d, int f) {
-    if (!ffn_rows_fit(T, d, FFN_OUT_COLUMNS)) return false;
+namespace {
+
+// The kernels of the forward's two products: the one for few rows, or tiles.
+struct ForwardPlan {
+    bool rows_hidden, rows_out;
+    Tiles hidden, out;
+};
+
+// The second product on the kernel for few rows: its waves go through k alone (no launch adds partials), so that a
+// deep k favours the tiles split over k: 64 .. 128 tokens, f = 1408: 8.7 us, 11.2 there; f = 2816: 15, 11.3; up to
+// 32 tokens, f = 2816: 7.5 .. 10.8, 9.6 .. 10.1; 312 tokens, f = 2048: 11.5, 14.4.
+ForwardPlan plan_forward(long long T, int d, int f, bool save) {
+    ForwardPlan p{};
+    p.rows_hidden = ffn_rows_fit(T, f, FFN_HIDDEN_COLUMNS);
+    if (!p.rows_hidden) p.hidden = plan(T, f, d, WBN / 2, save ? WIDE_SAVE : 0.0);
+    p.out = plan_deep(T, d, f);
     const double us = T <= 16 ? 1.0 + 1.4 * f / 512 : 1.5 + (T <= 32 ? 0.85 : 1.25) * f / 256;
-    return us < plan_deep(T, d, f).us;
+    p.rows_out = ffn_rows_fit(T, d, FFN_OUT_COLUMNS) && us < p.out.us;
+    return p;
 }
+
+}  // namespace
 
 // Workspace of the forward: h, where the caller does not keep it, and the second product's partials.
 size_t ffn_fwd_workspace_bytes(long long T, int d, int f, bool save) {
-    return (save ? 0 : align256((size_t)T * f * 2)) + (rows_output(T, d, f) ? 0 : partial_bytes(plan_deep(T, d, f), T, d));
+    const ForwardPlan p = plan_forward(T, d, f, save);
+    return (save ? 0 : align256((size_t)T * f * 2)) + (p.rows_out ? 0 : partial_bytes(p.out, T, d));
 }
 
 hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
@@ -132,38 +149,40 @@ hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
         a.ld_h = a.f;
         partial = (float*)((char*)workspace + align256((size_t)a.T * a.f * 2));
     }
+    const ForwardPlan p = plan_forward(a.T, a.d, a.f, a.pre != nullptr);
     hipError_t e;
-    if (ffn_rows_fit(a.T, a.f, FFN_HIDDEN_COLUMNS)) {
+    if (p.rows_hidden) {
         e = launch_ffn_rows_hidden(a, s);
     } else {
         TileArgs g = product(GEMM_NN, a.T, a.f, a.d, a.x, a.ld_x, a.w_in, a.ld_win, a.pre, a.ld_pre);
         g.C2 = a.h;
         g.ldc2 = a.ld_h;
-        const Tiles t = plan(a.T, a.f, a.d, WBN / 2, a.pre ? WIDE_SAVE : 0.0);
-        set_tiles(&g, t);
-        if (t.mid) e = a.pre ? mid_launch<GEMM_NN, GEMM_EPI_GATED_SAVE>(g, s) : mid_launch<GEMM_NN, GEMM_EPI_GATED>(g, s);
+        set_tiles(&g, p.hidden);
+        if (p.hidden.mid) e = a.pre ? mid_launch<GEMM_NN, GEMM_EPI_GATED_SAVE>(g, s) : mid_launch<GEMM_NN, GEMM_EPI_GATED>(g, s);
         else e = a.pre ? wide_launch<GEMM_NN, GEMM_EPI_GATED_SAVE, false>(g, s) : wide_launch<GEMM_NN, GEMM_EPI_GATED, false>(g, s);
     }
     if (e != hipSuccess) return e;
-    if (rows_output(a.T, a.d, a.f)) return launch_ffn_rows_out(a, s);
+    if (p.rows_out) return launch_ffn_rows_out(a, s);
     TileArgs g = product(GEMM_NN, a.T, a.d, a.f, a.h, a.ld_h, a.w_out, a.ld_wout, a.y, a.ld_y);
     g.R = a.residual;
     g.ldr = a.ld_r;
-    return deep_product<GEMM_NN>(g, plan_deep(g.M, g.N, g.K), partial, s);
+    return deep_product<GEMM_NN>(g, p.out, partial, s);
 }
 
 namespace {
 
-// The three products behind dpre: dx, dW_in and dW_out, one after the other, or in one launch on 128 x 128 tiles,
+// The backward's products: dpre, and the three behind it: dx, dW_in and dW_out, one after the other, or in one launch on 128 x 128 tiles,
 // their k cut into about equal numbers of steps, and one launch that adds up all partials.
 struct BackwardPlan {
     bool together;
+    Tiles dpre;               // of dh = dy W_out^T with the gradient of the activation
     Tiles dx, in, out;
     size_t bytes;             // of the partials
 };
 
 BackwardPlan plan_backward(long long T, int d, int f) {
     BackwardPlan p{};
+    p.dpre = plan(T, f, d, WBN, WIDE_BWD, MID_BWD);
     p.dx = plan_deep(T, d, 2ll * f);
     p.in = plan_split(d, 2ll * f, T, true);
     p.out = plan_split(f, d, T, true);
@@ -220,11 +239,10 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
     TileArgs g = product(GEMM_NT, a.T, a.f, a.d, a.dy, a.ld_y, a.w_out, a.ld_wout, dpre, f2);
     g.R = a.pre;
     g.ldr = a.ld_pre;
-    const Tiles t = plan(a.T, a.f, a.d, WBN, WIDE_BWD, MID_BWD);
-    set_tiles(&g, t);
-    hipError_t e = t.mid ? mid_launch<GEMM_NT, GEMM_EPI_GATED_BWD>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_GATED_BWD, false>(g, s);
-    if (e != hipSuccess) return e;
     const BackwardPlan p = plan_backward(a.T, a.d, a.f);
+    set_tiles(&g, p.dpre);
+    hipError_t e = p.dpre.mid ? mid_launch<GEMM_NT, GEMM_EPI_GATED_BWD>(g, s) : wide_launch<GEMM_NT, GEMM_EPI_GATED_BWD, false>(g, s);
+    if (e != hipSuccess) return e;
     TileArgs x = product(GEMM_NT, a.T, a.d, f2, dpre, f2, a.w_in, a.ld_win, a.dx, a.ld_x);
     TileArgs wi = product(GEMM_TN, a.d, f2, a.T, a.x, a.ld_x, dpre, f2, a.dw_in, a.ld_win);
     TileArgs wo = product(GEMM_TN, a.f, a.d, a.T, a.h, a.ld_h, a.dy, a.ld_y, a.dw_out, a.ld_wout);
@@ -249,6 +267,29 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
     };
     e = gradient(wi);
     return e != hipSuccess ? e : gradient(wo);
+}
+
+// As deep_product chooses, for the text below.
+static TilesName deep_name(int layout, const Tiles& t, bool residual, long long M, long long N, long long K) {
+    if (t.mid || (layout == GEMM_NN && residual)) return tiles_name(t);
+    TileArgs g = product(layout, M, N, K, nullptr, K, nullptr, N, nullptr, N);
+    gemm_plan(&g);
+    return tiles_name(g.wide ? "256x256" : "256x128", 1);
+}
+
+int ffn_fwd_kernels(long long T, int d, int f, bool save, bool residual, char* text, size_t n) {
+    const ForwardPlan p = plan_forward(T, d, f, save);
+    return snprintf(text, n, "hidden=%s h=%s out=%s", p.rows_hidden ? "rows" : tiles_name(p.hidden).text,
+                    p.rows_hidden || p.hidden.mid || h_stays(T, f) ? "cached" : "streamed",
+                    p.rows_out ? "rows" : deep_name(GEMM_NN, p.out, residual, T, d, f).text);
+}
+
+int ffn_bwd_kernels(long long T, int d, int f, char* text, size_t n) {
+    const BackwardPlan p = plan_backward(T, d, f);
+    return snprintf(text, n, "dpre=%s store=%s together=%d dx=%s dw_in=%s dw_out=%s", tiles_name(p.dpre).text,
+                    p.dpre.mid || dpre_stays(T, f) ? "cached" : "streamed", p.together,
+                    p.together ? tiles_name(p.dx).text : deep_name(GEMM_NT, p.dx, false, T, d, 2ll * f).text,
+                    tiles_name(p.in).text, tiles_name(p.out).text);
 }
 
 }  // namespace mtgr

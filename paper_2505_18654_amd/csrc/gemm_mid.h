@@ -13,6 +13,8 @@
 // 32 bytes of a row at a time, dpre of 6,418 tokens, 256 / 704, took 21.6 us, now 16.3.
 #pragma once
 
+#include <stdio.h>
+
 #include <type_traits>
 
 #include "gemm_wide.h"
@@ -481,6 +483,17 @@ static inline Tiles plan_split(long long M, long long N, long long K, bool alway
     }
     return best;
 }
+
+// "128x128/3": the tiles and, beyond one, their K splits.
+struct TilesName {
+    char text[24];
+};
+static inline TilesName tiles_name(const char* tiles, int splits) {
+    TilesName n;
+    snprintf(n.text, sizeof(n.text), splits > 1 ? "%s/%d" : "%s", tiles, splits);
+    return n;
+}
+static inline TilesName tiles_name(const Tiles& t) { return tiles_name(t.mid ? "128x128" : "256x256", t.splits); }
 
 static inline size_t partial_bytes(const Tiles& t, long long M, long long N) {
     return t.splits > 1 ? (size_t)t.splits * M * N * sizeof(float) : 0;

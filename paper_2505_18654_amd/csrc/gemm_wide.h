@@ -83,7 +83,7 @@ __device__ __forceinline__ float bf16_half(uint32_t w, int hi) {
 // fills one to four rounds of the chip and ends first, by the figures of tiles_of in gemm_mid.h in 64ths of a step,
 // in integers, because the kernel that adds the splits has to come to the same number (188 tiles, 391 steps: four
 // splits, 752 items in three rounds, 566 us; one, on 188 of the 256 CUs, 630; 130 tiles, 782 steps: 786 and 1,120).
-__device__ __forceinline__ int acc_splits(int tiles, int steps) {
+__host__ __device__ __forceinline__ int acc_splits(int tiles, int steps) {
     constexpr int START = 346, STEP = 64, PARTIAL = 5;      // an item, its steps, its partials written and read
     if (tiles > 256 * ACC_ROUNDS) return 1;
     int best = 1, cost = (tiles + 255) / 256 * (START + STEP * steps) + PARTIAL * tiles;
@@ -101,7 +101,7 @@ __device__ __forceinline__ int acc_splits(int tiles, int steps) {
 
 // Columns of items of the softmax statistics: about 16 items per CU, so that the last round of them is short,
 // each of as many class tiles as that leaves (their statistics stay in registers in between).
-__device__ __forceinline__ int stat_chunks(int mblocks, int nblocks) {
+__host__ __device__ __forceinline__ int stat_chunks(int mblocks, int nblocks) {
     const int per_item = min(max(mblocks * nblocks / 4096, 1), 32);
     return (nblocks + per_item - 1) / per_item;
 }
@@ -117,8 +117,9 @@ __device__ __forceinline__ uint4 load_nt16(const void* p) {
 // the caches.  dz, up to 192 MB: 2,900 rows, 20,011 classes, 120 MB, backward with stores past the caches 186 us, with
 // plain ones 171; 8,000 rows, 320 MB: 247 and 266.  h, 64 MB: 8,000 tokens, 512 / 1408, 22 MB, second product 23 and
 // 19 us; 75,132, 212 MB, forward 371 and 422.  dpre, 128 MB: 6,418 tokens, 1024 / 2816, 72 MB, dx 99 and 78 us.
-__device__ __forceinline__ bool stays(long long bytes, long long most) { return bytes <= most; }
-__device__ __forceinline__ bool dz_stays(long long rows, long long ld) { return stays(rows * ld * 2, 192ll << 20); }
+__host__ __device__ __forceinline__ bool dz_stays(long long rows, long long ld) { return rows * ld * 2 <= 192ll << 20; }
+__host__ __device__ __forceinline__ bool h_stays(long long rows, long long hidden) { return rows * hidden * 2 <= 64ll << 20; }
+__host__ __device__ __forceinline__ bool dpre_stays(long long rows, long long hidden) { return rows * hidden * 4 <= 128ll << 20; }
 
 // A plain store beside a non-temporal one of the same value: merged by the compiler, both would be plain.
 __device__ __forceinline__ void store_plain16(void* p, const uint4& v) {
@@ -687,7 +688,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
                 }
             }
         } else if constexpr (EPI == GEMM_EPI_GATED_BWD) {
-            const bool dpre_stays = stays((long long)M * N * 4, 128ll << 20);
+            const bool keep = dpre_stays(M, N);
             // dh passes through LDS in fp32, one block at a time, so that a lane has 8 columns of a row:
             // dgate = dh up silu'(gate), dup = dh silu(gate), rounded once
 #pragma unroll
@@ -702,7 +703,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
                     gated_gradient(x0, x1, pg[b & 3][q], pu[b & 3][q], &og, &ou);
                     if (full || (gm < M && gn < N)) {
                         uint16_t* dst = (uint16_t*)g.C + gm * g.ldc + gn;
-                        if (dpre_stays) {
+                        if (keep) {
                             store_plain16(dst, og);
                             store_plain16(dst + N, ou);
                         } else {
@@ -715,7 +716,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
                 wave_lds_fence();
             }
         } else if constexpr (GATED) {
-            const bool h_stays = stays((long long)M * N * 2, 64ll << 20);
+            const bool keep_h = h_stays(M, N);
             // acc[a][0..3] hold gate columns en + 16 b + 4 (l / 16) + 0..3, acc[a][4..7] the up columns of the same
             // numbers.  32 rows at a time: 16-byte chunk c (of 8) of row r at c ^ (r & 7)
             auto rows_out = [&](int rd, uint16_t* base, long long ld, bool keep, auto value) {
@@ -746,7 +747,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
                     rows_out(rd, (uint16_t*)g.C, g.ldc, false, [&](int a, int b) { return acc[a][b]; });
                     rows_out(rd, (uint16_t*)g.C + N, g.ldc, false, [&](int a, int b) { return acc[a][b + 4]; });
                 }
-                rows_out(rd, (uint16_t*)g.C2, g.ldc2, h_stays, [&](int a, int b) {
+                rows_out(rd, (uint16_t*)g.C2, g.ldc2, keep_h, [&](int a, int b) {
                     const floatx4 ga = acc[a][b], up = acc[a][b + 4];
                     return floatx4{silu(ga[0]) * up[0], silu(ga[1]) * up[1], silu(ga[2]) * up[2], silu(ga[3]) * up[3]};
                 });

@@ -23,6 +23,8 @@
 // in gemm_wide.h.  24,000 rows of 69,563, 50,021 classes, d = 512: statistics 1.08 ms (1.14 PFLOP/s); backward, of
 // 2 pieces, dz 1.35 ms (0.91; 2.4 GB written), dx 1.13 (1.09), dW 1.10 (1.12), sums 0.13.  1,900 rows, 400,003
 // classes, d = 256: 0.31 (1.25); dz 0.56 (0.69; 1.5 GB written), dx 0.37 (1.05), dW 0.42 (0.93).
+#include <stdio.h>
+
 #include "gemm_mid.h"
 #include "softmax_tiles.h"
 
@@ -382,6 +384,9 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SoftmaxLossArgs a, Finis
     }
 }
 
+// Class tiles of the first piece on the tiles of softmax_tiles.h.
+int register_tiles(const SmPlan& p, int V) { return std::min(p.piece / CT_CLASSES, (V + CT_CLASSES - 1) / CT_CLASSES); }
+
 template <bool BWD>
 hipError_t launch_rows(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, hipStream_t s) {
     const int rb = (int)((a.N + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK);
@@ -391,7 +396,7 @@ hipError_t launch_rows(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, hipS
     uint16_t* xc = (uint16_t*)(ws + p.xc);
     float* bias2 = (float*)(ws + p.bias);
     int4* info = (int4*)(ws + p.info);
-    const int class_tiles = p.regs ? std::min(p.piece, (a.V + CT_CLASSES - 1) / CT_CLASSES * CT_CLASSES) / CT_CLASSES : 0;
+    const int class_tiles = p.regs ? register_tiles(p, a.V) : 0;
     auto launch = [&](auto type) {
         typedef decltype(type) T;
         if (a.N <= SCAN_ROWS) {
@@ -438,6 +443,22 @@ TileArgs logits_product(const SoftmaxLossArgs& a, const SmPlan& p, char* ws, int
 
 size_t softmax_loss_workspace_bytes(long long N, int V, int d, bool backward) {
     return N > 0 && V > 0 ? sm_plan(N, V, d, backward).total : 0;
+}
+
+// run: class tiles that an item (256 rows, or a tile's) goes through, of the first piece.
+int softmax_loss_kernels(long long N, int V, int d, bool backward, long long labels, char* text, size_t n) {
+    const SmPlan p = sm_plan(N, V, d, backward);
+    const int mblocks = (int)((labels + WBM - 1) / WBM), nblocks = (std::min(p.piece, V) + WBN - 1) / WBN;
+    int cost, run = 1;
+    if (p.regs) run = tile_run(mblocks, register_tiles(p, V), &cost);
+    else if (!p.logits.mid && !backward) run = (nblocks + stat_chunks(mblocks, nblocks) - 1) / stat_chunks(mblocks, nblocks);
+    const char* logits = p.regs ? "registers" : p.logits.mid ? "128x128" : "256x256";
+    if (!backward) return snprintf(text, n, "logits=%s run=%d pieces=%d piece=%d", logits, run, p.pieces, p.piece);
+    Tiles dx = p.dx;
+    if (!dx.mid) dx.splits = acc_splits(mblocks * ((d + WBN - 1) / WBN), p.piece / WBK);
+    return snprintf(text, n, "logits=%s run=%d pieces=%d piece=%d dz=%s dx=%s dw=%s%s", logits, run, p.pieces, p.piece,
+                    (!p.regs && p.logits.mid) || dz_stays(labels, p.piece) ? "cached" : "streamed", tiles_name(dx).text,
+                    tiles_name(p.dw).text, p.direct ? "/direct" : "");
 }
 
 hipError_t launch_softmax_loss_fwd(const SoftmaxLossArgs& a, void* workspace, hipStream_t s) {

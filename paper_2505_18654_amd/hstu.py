@@ -57,6 +57,7 @@ EXPORTED = (
     "mtgr_embedding_rehash",
     "mtgr_gated_ffn_workspace_size", "mtgr_gated_ffn_fwd", "mtgr_gated_ffn_bwd", "mtgr_dropout",
     "mtgr_softmax_loss_workspace_size", "mtgr_softmax_loss_fwd", "mtgr_softmax_loss_bwd",
+    "mtgr_debug_gated_ffn_kernels", "mtgr_debug_softmax_loss_kernels",
 )
 
 
@@ -168,6 +169,8 @@ def lib() -> ctypes.CDLL:
         L.mtgr_softmax_loss_workspace_size.argtypes = [S, ctypes.c_int, ctypes.POINTER(sz)]
         L.mtgr_softmax_loss_fwd.argtypes = [S, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.mtgr_softmax_loss_bwd.argtypes = [S, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mtgr_debug_gated_ffn_kernels.argtypes = [F, ctypes.c_int, ctypes.c_int, ctypes.c_char_p, sz]
+        L.mtgr_debug_softmax_loss_kernels.argtypes = [S, ctypes.c_int, i64, ctypes.c_char_p, sz]
         for name in EXPORTED:
             if name not in ("mtgr_status_string", "mtgr_last_error_message", "mtgr_version"):
                 getattr(L, name).restype = ctypes.c_int
@@ -479,3 +482,19 @@ def mtgr_softmax_loss_bwd(problem, dloss, x, w, targets, bias, lse, dx, dw, dbia
     _check(lib().mtgr_softmax_loss_bwd(ctypes.byref(problem), _ptr(dloss), _ptr(x), _ptr(w), _ptr(targets), _ptr(bias),
                                        _ptr(lse), _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(workspace),
                                        int(workspace_bytes), _stream(stream)))
+
+
+def _pairs(call, *args) -> dict:
+    text = ctypes.create_string_buffer(256)
+    _check(call(*args, text, len(text)))
+    return dict(p.split("=") for p in text.value.decode().split())
+
+
+def mtgr_debug_gated_ffn_kernels(problem, which: int, residual: bool = False) -> dict:
+    return _pairs(lib().mtgr_debug_gated_ffn_kernels, ctypes.byref(problem), int(which), int(residual))
+
+
+def mtgr_debug_softmax_loss_kernels(problem, backward: bool, labels: Optional[int] = None) -> dict:
+    """labels: the number of rows with a label; all of them if None."""
+    return _pairs(lib().mtgr_debug_softmax_loss_kernels, ctypes.byref(problem), int(backward),
+                  problem.num_rows if labels is None else int(labels))
