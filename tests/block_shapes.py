@@ -9,15 +9,15 @@ FFN = {
     (127, 1024, 2848): (dict(hidden="rows", out="128x128/10"), dict(hidden="rows", out="128x128/10"), dict(together="1")),
     (12001, 480, 1376): (dict(hidden="256x256", out="128x128"), dict(hidden="128x128", out="128x128"),
                          dict(dpre="128x128", together="0", dx="128x128", dw_in="256x256/10", dw_out="128x128/10")),
-    # all on 256 x 256 tiles: h (55 MB) and dpre (110 MB) left in the caches, then (83 and 165 MB) stored past them
+    # all on 256 x 256 tiles: h (55 MB) and dpre (110 MB) left in the caches
     (20001, 480, 1376): (dict(hidden="256x256", h="cached", out="256x256"), dict(hidden="256x256", h="cached", out="256x256"),
                          dict(dpre="256x256", store="cached", dx="256x256", dw_in="256x256/10", dw_out="256x256/20")),
-    (30001, 480, 1376): (dict(hidden="256x256", h="streamed", out="256x256"),
-                         dict(hidden="256x256", h="streamed", out="256x256"),
-                         dict(dpre="256x256", store="streamed", dx="256x256", dw_in="256x256/10", dw_out="256x256/20")),
     # products without a residual on 256 x 128 tiles
-    (40001, 512, 1408): (dict(hidden="256x256", out="256x256"), dict(hidden="256x256", h="streamed", out="256x128"),
-                         dict(dpre="256x256", store="streamed", dx="256x128")),
+    (40001, 512, 1408): (dict(hidden="256x256", h="cached", out="256x256"), dict(hidden="256x256", h="cached", out="256x128"),
+                         dict(dpre="256x256", store="cached", dx="256x128")),
+    # h (206 MB) and dpre (413 MB) stored past the caches
+    (75001, 480, 1376): (dict(hidden="256x256", h="streamed", out="256x256"), dict(hidden="256x256", h="streamed"),
+                         dict(dpre="256x256", store="streamed", dx="256x256", dw_in="256x256/10", dw_out="256x256/20")),
 }
 # pre and dpre of 2.25e9 elements on 256 x 256 tiles
 FFN_LONG = (800_003, 512, 1408)
