@@ -91,15 +91,22 @@ TileArgs product(int layout, long long M, long long N, long long K, const void* 
 constexpr double WIDE_SAVE = 3.0, WIDE_BWD = 14.0, MID_BWD = 6.0;
 
 // C = A B (NN) or A B^T (NT), plus the residual R where there is one; `partial` holds the K splits' sums.
+// Where 256 x 256 tiles are estimated to end before 128 x 128 ones, an NN product without a residual goes by gemm_plan,
+// which may take 256 x 128 tiles (us on 256 x 128, 256 x 256 and 128 x 128 tiles: 33,001 tokens, 512 / 1408: 67, 76, 71;
+// 40,001: 73, 76, 81; 75,132: 120, 120, 133; 17,001, 1024 / 2816: 122, 136, 126; 20,001: 132, 138, 138); those have no
+// epilogue for a residual.  NT products stay on 256 x 256 tiles (33,001, 512 / 1408: 126, 128, 117; 40,001: 148, 136,
+// 152; 45,001: 150, 134, 166; 17,001, 1024 / 2816: 259, 250, 262; 22,001: 283, 257, 286; 70,001, 256 / 704: 78, 74, 76).
 template <int LAYOUT>
 static hipError_t deep_product(TileArgs g, const Tiles& t, float* partial, hipStream_t s) {
-    if (!t.mid && (LAYOUT == GEMM_NT || !g.R)) {
-        gemm_plan(&g);
-        return launch_gemm_bf16(g, s);
+    if constexpr (LAYOUT == GEMM_NN) {
+        if (!t.mid && !g.R) {
+            gemm_plan(&g);
+            return launch_gemm_bf16(g, s);
+        }
     }
     set_tiles(&g, t);
+    if (!t.mid) return wide_launch<LAYOUT, LAYOUT == GEMM_NN ? GEMM_EPI_RESIDUAL : GEMM_EPI_NONE, false>(g, s);
     if constexpr (LAYOUT == GEMM_NN) {
-        if (!t.mid) return wide_launch<GEMM_NN, GEMM_EPI_RESIDUAL, false>(g, s);
         if (t.splits == 1 && g.R) return mid_launch<GEMM_NN, GEMM_EPI_RESIDUAL>(g, s);
     }
     if (t.splits == 1) return mid_launch<LAYOUT, GEMM_EPI_NONE>(g, s);
@@ -271,7 +278,7 @@ hipError_t launch_ffn_bwd(const FfnArgs& a, void* workspace, hipStream_t s) {
 
 // As deep_product chooses, for the text below.
 static TilesName deep_name(int layout, const Tiles& t, bool residual, long long M, long long N, long long K) {
-    if (t.mid || (layout == GEMM_NN && residual)) return tiles_name(t);
+    if (t.mid || layout == GEMM_NT || residual) return tiles_name(t);
     TileArgs g = product(layout, M, N, K, nullptr, K, nullptr, N, nullptr, N);
     gemm_plan(&g);
     return tiles_name(g.wide ? "256x256" : "256x128", 1);

@@ -116,9 +116,9 @@ __device__ __forceinline__ uint4 load_nt16(const void* p) {
 // Whether a result is left in the last-level cache of 256 MB for the next product, or stored past the caches, by its
 // bytes.  Measured with plain stores and with stores past the caches, us (products that write and read it, in turn):
 // dz, up to 192 MiB: 2,900 rows, 20,011 classes, 120 MB, backward 171 and 186; 8,000 rows, 320 MB: 266 and 247.
-// h, up to 176 MiB (training forward, 512 / 1408): 56 MB 109 and 114; 85 MB 147 and 152; 113 MB 190 and 204; 155 MB 263
-// and 273; 189 MB 317 and 329, 335 and 331 on another card; 203 MB 367 and 349; 212 MB 386 and 371.  1024 / 2816: 141 MB 406 and 417, 169 MB 476
-// and 486, 197 MB 590 and 595, 225 MB 654 and 657, 392 MB 1,210 and 1,204.
+// h, up to 176 MiB (training forward, 512 / 1408): 56 MB 109 and 114; 85 MB 147 and 152; 113 MB 190 and 204; 155 MB
+// 263 and 273; 189 MB 317 and 329, 335 and 331 on another card; 203 MB 367 and 349; 212 MB 386 and 371.  1024 / 2816:
+// 141 MB 406 and 417, 169 MB 476 and 486, 197 MB 590 and 595, 225 MB 654 and 657, 392 MB 1,210 and 1,204.
 // dpre, up to 256 MiB (backward, 512 / 1408): 113 MB 243 and 250; 169 MB 317 and 323; 225 MB 448 and 467; 282 MB 553 and
 // 555; 338 MB 605 and 606.  1024 / 2816: 135 MB 473 and 483, 191 MB 725 and 735, 225 MB 801 and 822, 248 MB 884 and 896.
 __host__ __device__ __forceinline__ bool dz_stays(long long rows, long long ld) { return rows * ld * 2 <= 192ll << 20; }

@@ -12,9 +12,9 @@ FFN = {
     # all on 256 x 256 tiles: h (55 MB) and dpre (110 MB) left in the caches
     (20001, 480, 1376): (dict(hidden="256x256", h="cached", out="256x256"), dict(hidden="256x256", h="cached", out="256x256"),
                          dict(dpre="256x256", store="cached", dx="256x256", dw_in="256x256/10", dw_out="256x256/20")),
-    # products without a residual on 256 x 128 tiles
+    # the second product of a training forward on 256 x 128 tiles
     (40001, 512, 1408): (dict(hidden="256x256", h="cached", out="256x256"), dict(hidden="256x256", h="cached", out="256x128"),
-                         dict(dpre="256x256", store="cached", dx="256x128")),
+                         dict(dpre="256x256", store="cached", dx="256x256")),
     # h (206 MB) and dpre (413 MB) stored past the caches
     (75001, 480, 1376): (dict(hidden="256x256", h="streamed", out="256x256"), dict(hidden="256x256", h="streamed"),
                          dict(dpre="256x256", store="streamed", dx="256x256", dw_in="256x256/10", dw_out="256x256/20")),

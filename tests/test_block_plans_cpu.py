@@ -40,7 +40,7 @@ def test_ffn_shapes_reach_every_kernel():
     assert {g[2]["dpre"] for g in got} == {"128x128", "256x256"} and {g[2]["together"] for g in got} == {"0", "1"}
     assert {g[2]["store"] for g in got if g[2]["dpre"] == "256x256"} == {"cached", "streamed"}
     apart = [g[2] for g in got if g[2]["together"] == "0"]
-    assert {tiles(g["dx"]) for g in apart} == {"128x128", "256x128", "256x256"}
+    assert {tiles(g["dx"]) for g in apart} == {"128x128", "256x256"}
     assert {tiles(g["dw_out"]) for g in apart} == {"128x128", "256x256"}
 
 
