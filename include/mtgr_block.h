@@ -24,7 +24,8 @@ extern "C" {
  *   h   = silu(gate) * up      [T, f]
  *   y   = h W_out (+ r)        W_out [f, d], r [T, d]
  *
- * d and f are multiples of 32, below 2^20; ceil(T / 256) ceil(2 max(d, f) / 128) is below 2^24.  Sums are fp32; h, pre and the gradients of pre are rounded to bf16. */
+ * d and f are multiples of 32, below 2^20; ceil(T / 256) ceil(2 max(d, f) / 128) is below 2^24.  Sums are fp32; h, pre
+ * and the gradients of pre are rounded to bf16. */
 typedef struct {
     int64_t num_tokens;       /* T, 0 .. 2^31 - 1 */
     int32_t dim;              /* d */
@@ -76,7 +77,8 @@ mtgr_status_t mtgr_debug_gated_ffn_kernels(const mtgr_gated_ffn_problem_t* p, mt
  * captured graph.  site numbers the places of a model that drop, so that their masks differ; the step
  * counts modulo 2^32.  Element e is kept when word e % 4 of Philox4x32-7 with the key seed and the counter
  * (e / 4 low, e / 4 high, site, step) is at least floor(prob 2^32).  0 <= prob < 1.  cols is a multiple of
- * 16 bytes, rows * cols below 2^50; dense rows (ld = cols) may be of any width.  A dropped element counts as 0 whatever x holds.  out may be x or the residual. */
+ * 16 bytes, rows * cols below 2^50; dense rows (ld = cols) may be of any width.  A dropped element counts as 0
+ * whatever x holds.  out may be x or the residual. */
 mtgr_status_t mtgr_dropout(int64_t rows, int32_t cols, mtgr_dtype_t dtype, const void* x, int64_t ld_x, double prob,
                            const uint64_t* rng, uint32_t site, const void* residual, int64_t ld_residual, void* out,
                            int64_t ld_out, mtgr_stream_t stream);
@@ -111,7 +113,10 @@ mtgr_status_t mtgr_softmax_loss_fwd(const mtgr_softmax_loss_problem_t* p, const 
                                     size_t workspace_bytes, mtgr_stream_t stream);
 
 /* Gradients for dloss [N] fp32 (that of a mean: 1 / count), with lse of the forward pass on the same
- * inputs: dx [N, d] bf16, dw [V, d] bf16, dbias [V] fp32 or NULL.  N = 0: dw and dbias are zero-filled. */
+ * inputs: dx [N, d] bf16, dw [V, d] bf16, dbias [V] fp32 or NULL.  N = 0: dw and dbias are zero-filled.  The gradient of
+ * the logits, dz, is rounded to bf16 relative to the largest |dloss| of a row with a label, as operand of the products
+ * that form dx and dw; their sums are fp32, dbias is summed from unrounded dz.  The workspace holds dz of a piece of the
+ * classes: 2 N V bytes (all rows count, with a label or not) up to 4 GB, beyond which there are more pieces. */
 mtgr_status_t mtgr_softmax_loss_bwd(const mtgr_softmax_loss_problem_t* p, const float* dloss, const void* x,
                                     const void* w, const void* targets, const float* bias, const float* lse, void* dx,
                                     void* dw, float* dbias, void* workspace, size_t workspace_bytes,

@@ -10,13 +10,18 @@
 // (in serving) nor dh go through memory.  Roundings to bf16: h and dpre, as operands of the next product;
 // pre, which the forward keeps for the backward (its tensors of the kind are bf16).
 //
+// h and dpre are rounded to bf16 because the next product's matrix instructions take bf16 operands (split into two bf16
+// numbers each they would double that product); every sum is fp32, and h and dpre are formed from unrounded sums.
+//
 // Bound by the matrix cores (power) and, beside them, by what the epilogues read and write and compute.
-// Large products run on 256 x 256 tiles, fewer tiles than CUs on 128 x 128 ones (gemm_mid.h), deep ones of
-// them split over k; few tokens on a kernel of their own (ffn_rows.hip).  Measured:
-// - 75,132 tokens, 512 / 1408, training: first product 250 us (0.87 PFLOP/s; 635 MB written), second 120;
-// - 69,563 tokens, 1024 / 2816, training: 771 (1.04 PFLOP/s) and 380 us; backward: dpre 535 us (0.75; 1.6 GB of
-//   pre read and dpre written), dx 710 (1.13), the weight gradients 1,180 (1.02) with their splits' sums;
-// - 6,418 tokens, 256 / 704, backward: dpre 16.3 us, the three products behind it in one launch 26.9, the sums 7.2.
+// Large products run on 256 x 256 tiles (the second one of a training forward partly on the 256 x 128 tiles of gemm.hip),
+// fewer tiles than CUs on 128 x 128 ones (gemm_mid.h), deep ones of them split over k; few tokens on a kernel of their
+// own (ffn_rows.hip).  Measured in a kernel trace of ten calls in a row (in short bursts, as the rules' figures below were
+// taken, the clock is up to a fifth higher):
+// - 75,132 tokens, 512 / 1408, training: first product 292 us (0.74 PFLOP/s; 635 MB written), second 132 (0.82);
+// - 69,563 tokens, 1024 / 2816, training: 915 (0.88) and 449 us (0.89); backward: dpre 555 us (0.72; 1.6 GB of
+//   pre read and dpre written), dx 734 (1.09), the weight gradients 763 and 401 (1.05, 1.00), their splits' sums 43;
+// - 6,418 tokens, 256 / 704, backward: dpre 16.7 us, the three products behind it in one launch 27.1, the sums 7.1.
 #include <stdio.h>
 
 #include "gemm_mid.h"

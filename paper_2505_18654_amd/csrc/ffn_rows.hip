@@ -11,8 +11,9 @@
 // pairs the rows' 16-bit halves: fragment j then holds the columns CPL (l % 16) + j, a row order of the
 // (transposed) result that only the epilogue sees.
 //
-// Bound by latency: start, one chain of weight loads and the additions through LDS (one token, 512 / 1408: 4.3 and
-// 4.2 us for 2.9 and 1.4 MB; 1024 / 2816: 6.8 us for 11.5 MB, 1.7 TB/s, and 7.4 for 5.8 MB).
+// Bound by latency (start, one chain of weight loads, the additions through LDS) and, the larger the weights, by what
+// the few workgroups can load: one token, 512 / 1408, 44 and 16 workgroups: 4.3 and 3.9 us for 2.9 and 1.4 MB; 1024 /
+// 2816, 88 and 32 workgroups: 8.2 us for 11.5 MB, 1.4 TB/s, and 7.9 for 5.8 MB, 0.7 TB/s.
 #include "block_internal.h"
 #include "mtgr_device.h"
 
@@ -134,7 +135,7 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_rows_kernel(RowsArgs a) {
                 *(uint2*)(p + a.N) = make_uint2(pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3]));
             }
 #pragma unroll
-            for (int e = 0; e < 4; e++)
+            for (int e = 0; e < 4; e++)       // (rounded below: an operand of the second product)
                 s[e] = s[e] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * s[e])) * u[e];
         }
         *(uint2*)(a.out + gm * a.ld_out + gn) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));

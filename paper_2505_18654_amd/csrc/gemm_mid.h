@@ -10,7 +10,7 @@
 // 0.15 us shorter.  Four stages, operands read a half step ahead, eight waves, and copies spread between the matrix
 // instructions, 2 to 15 % slower, gained nothing, so products of few tiles are split over k instead.)  Results pass
 // through LDS, so that a lane stores 16 bytes and its neighbours the rest of the line: straight from the accumulators, 8 bytes and
-// 32 bytes of a row at a time, dpre of 6,418 tokens, 256 / 704, took 21.6 us, now 16.3.
+// 32 bytes of a row at a time, dpre of 6,418 tokens, 256 / 704, took 21.6 us, like this 16.3.
 #pragma once
 
 #include <stdio.h>
@@ -286,6 +286,7 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
                     acc[a][b][e] = gp * __builtin_amdgcn_exp2f(fmaf(acc[a][b][e], g.scale, bias[a][e]) - lse);
                     if (label == 16 * a + e) acc[a][b][e] -= gr;
                 }
+                // (dz is rounded as an operand of the next two products; its column sums take it unrounded)
                 cs[a] += acc[a][b];
                 *(uint2*)(stg + 128 * lr + 16 * ((2 * a + (lg >> 1)) ^ (lr & 7)) + 8 * (lg & 1)) = pack(acc[a][b]);
             }
@@ -312,6 +313,7 @@ __device__ __forceinline__ void mid_tile(const TileArgs& g, int block, char* sm)
             }
         }
     } else if constexpr (GATED) {
+        // h is rounded as an operand of the second product, from unrounded gate and up values.
         // 16 rows at a time, 16-byte chunks: 0..3 the gate columns of a row, 4..7 the up columns (chunk c of row r at
         // c ^ (r & 7)); then h, 32 rows at a time, 4 chunks a row (at c ^ (r / 2 & 3))
         if constexpr (EPI == GEMM_EPI_GATED_SAVE) {

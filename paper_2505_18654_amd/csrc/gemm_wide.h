@@ -132,7 +132,8 @@ __device__ __forceinline__ void store_plain16(void* p, const uint4& v) {
     asm volatile("" ::: "memory");
 }
 
-// dgate = dh up silu'(gate) and dup = dh silu(gate) of eight columns (dh: x0, x1), each rounded once.
+// dgate = dh up silu'(gate) and dup = dh silu(gate) of eight columns (dh: x0, x1), each rounded once: dpre is an operand of
+// the next products.
 __device__ __forceinline__ void gated_gradient(const floatx4& x0, const floatx4& x1, const uint4& gate, const uint4& up,
                                                uint4* dgate, uint4* dup) {
     const uint32_t gw[4] = {gate.x, gate.y, gate.z, gate.w}, uw[4] = {up.x, up.y, up.z, up.w};
@@ -722,7 +723,8 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
         } else if constexpr (GATED) {
             const bool keep_h = h_stays(M, N);
             // acc[a][0..3] hold gate columns en + 16 b + 4 (l / 16) + 0..3, acc[a][4..7] the up columns of the same
-            // numbers.  32 rows at a time: 16-byte chunk c (of 8) of row r at c ^ (r & 7)
+            // numbers; h is rounded as an operand of the second product, from unrounded values.  32 rows at a time:
+            // 16-byte chunk c (of 8) of row r at c ^ (r & 7)
             auto rows_out = [&](int rd, uint16_t* base, long long ld, bool keep, auto value) {
 #pragma unroll
                 for (int aa = 0; aa < 2; aa++)
@@ -803,7 +805,8 @@ __global__ __launch_bounds__(512, 2) void gemm_wide_kernel(TileArgs g) {
             // (scale and the largest |g| one after the other: their product alone may leave the float range)
             const float largest = DIRECT ? ((const float*)g.rows)[1] : 0.f;
             const bool plain = GRAD && dz_stays(M, g.ldc);
-            // bf16, 32 rows (two blocks) at a time: 16-byte chunk c (of 8) of row r at c ^ (r & 7)
+            // bf16 (dz: an operand of the next two products; its column sums above take it unrounded), 32 rows (two blocks) at
+            // a time: 16-byte chunk c (of 8) of row r at c ^ (r & 7)
 #pragma unroll
             for (int rd = 0; rd < WNM / 2; rd++)
 #pragma unroll

@@ -14,15 +14,16 @@
 // them.  2 n V d operations; written are at most 8 bytes per row and 64 classes, a sixteenth of the logits in
 // bf16.
 // Backward, per piece of classes: x W^T again, its epilogue turning the products into dz (rounded to bf16
-// as operand of the next two products; the bias gradient is summed from dz before that rounding), then
-// dx += dz W (fp32, over the pieces) and the piece's dW = dz^T x.  6 n V d operations.  dz is kept divided by
+// as operand of the next two products' matrix instructions; the bias gradient is summed from dz before that rounding),
+// then dx += dz W (fp32, over the pieces) and the piece's dW = dz^T x.  6 n V d operations.  dz is kept divided by
 // the largest |g| of the rows, which multiplies the finished sums: under a mean the g are one number, whose
 // rounding error would be common to all labels' terms (-g), and a label's own term -1 is exact.
 //
 // Bound by the matrix cores (power) and by the epilogues' vector work, which does not run beside them
-// in gemm_wide.h.  24,000 rows of 69,563, 50,021 classes, d = 512: statistics 1.08 ms (1.14 PFLOP/s); backward, of
-// 2 pieces, dz 1.35 ms (0.91; 2.4 GB written), dx 1.13 (1.09), dW 1.10 (1.12), sums 0.13.  1,900 rows, 400,003
-// classes, d = 256: 0.31 (1.25); dz 0.56 (0.69; 1.5 GB written), dx 0.37 (1.05), dW 0.42 (0.93).
+// in gemm_wide.h.  Kernel traces of ten calls in a row: 24,000 rows of 69,563, 50,021 classes, d = 512: statistics 1.23 ms
+// (1.00 PFLOP/s); backward, of 2 pieces, dz 1.48 ms (0.83; 2.4 GB written), dx 1.14 (1.08), dW 1.14 (1.08), sums 0.15.
+// 1,900 rows, 400,003 classes, d = 256: 0.38 (1.04); dz 0.57 (0.68; 1.5 GB written), dx 0.40 (0.98), dW 0.46 (0.84).
+// (The rules' and the tiles' figures are of short bursts, in which the clock is up to a fifth higher.)
 #include <stdio.h>
 
 #include "gemm_mid.h"

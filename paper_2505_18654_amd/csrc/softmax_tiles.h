@@ -5,8 +5,8 @@
 // tile.  Per matrix instruction that is half the LDS reads and a quarter of the copies of 128 x 128 tiles with
 // both operands in LDS, and 80 KB at the most, so that two workgroups share a CU: the epilogue of one (the
 // exponentials of a tile take about as long as its products) runs beside the matrix instructions of the other.
-// 1,900 rows, 400,003 classes, d = 256: statistics 513 us on 256 x 256 tiles, 312 here (1.25 PFLOP/s: power); dz
-// 700 and 560 (1.5 GB written).  7,900 rows, 50,021 classes, d = 128: 190 and 109, 237 and 204.  4,800, d = 64: 98
+// In turn, in short bursts: 1,900 rows, 400,003 classes, d = 256: statistics 513 us on 256 x 256 tiles, 312 here (1.25
+// PFLOP/s: power); dz 700 and 560 (1.5 GB written).  7,900 rows, 50,021 classes, d = 128: 190 and 109, 237 and 204.  4,800, d = 64: 98
 // and 60, 118 and 118 (writes).  Wave priorities and a later start of every other workgroup changed nothing.
 // Transposed as in gemm_wide.h: a lane holds rows l % 16 of each block of 16, four consecutive classes each.
 #pragma once
@@ -211,7 +211,8 @@ __global__ __launch_bounds__(256, 2) void sm_tile_kernel(TileArgs g) {
                         for (int e = 0; e < 4; e++)
                             if (label == 16 * a + 4 * lg + e) v[a][e] -= __int_as_float(ri.y);
                 }
-                // 16-byte chunk c (of 8) of row r at c ^ (r & 7), so that a store writes whole lines
+                // rounded (an operand of the next two products; the column sums above take it unrounded); 16-byte chunk c
+                // (of 8) of row r at c ^ (r & 7), so that a store writes whole lines
 #pragma unroll
                 for (int a = 0; a < 4; a++) {
                     cs[a] += v[a];

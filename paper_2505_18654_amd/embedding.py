@@ -2,8 +2,9 @@
 Lookup"), driven through the C ABI of include/mtgr_embedding.h.
 
 Torch provides the device buffers and the stream; every step (de-duplication, probing,
-insertion, gather, the sparse SGD step, eviction, rebuilding the key store) runs in the
-library's HIP kernels.  IDs are int64 tensors holding the bit patterns of uint64 IDs.
+insertion, gather, the sparse SGD step, eviction, rebuilding the key store, the item loss's
+products and softmax) runs in the library's HIP kernels; torch forms the item loss's labels and
+bias and lays out its gradient.  IDs are int64 tensors holding the bit patterns of uint64 IDs.
 
     table = DynamicEmbedding(row_capacity=1 << 20, dim=64)
     out, batch = table.lookup(ids, now=t)        # dedup + lookup/insert + gather
@@ -145,7 +146,9 @@ class DynamicEmbedding:
         """Softmax cross entropy of the rows of x [N, dim] against the batch's distinct items, each item's logit
         corrected by the log of its share of the batch (popular items would be pushed down as classes for being
         there more often).  labels [N] int64: the position in the batch's IDs of the row's label, outside 0 .. n-1 for
-        a row without one; a label whose ID the table does not hold counts as none.  Nothing synchronises.
+        a row without one; a label whose ID the table does not hold counts as none.  Nothing synchronises, and the
+        number of distinct items is on the device only, so that time and workspace follow the n IDs of the batch (items
+        past the distinct ones are classes that are taken out).
         Returns (loss [N], saved for item_loss_bwd)."""
         at = torch.arange(batch.n_max, device=self.device)
         known = (at < batch.num_unique) & (batch.rows >= 0)
