@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2505_18654_amd import ops
+from paper_2505_18654_amd.layer import FfnParams, ffn_bwd, ffn_fwd
 from tests.block_ref import keep_mask, normal
 
 pytestmark = pytest.mark.gpu
@@ -51,3 +52,18 @@ def test_loss_gradients_when_scale_times_dloss_leaves_the_float_range(N, V, d, a
         on = (q == 0) | ((q.abs() > 2.0 ** -120) & (q.abs() < 2.0 ** 126))
         assert on.float().mean() > 0.9, name
         assert torch.equal(p.double()[on], q[on]), name
+
+
+@pytest.mark.parametrize("p", [0.0, 0.4])
+def test_layers_feed_forward_block_without_tokens(p):
+    """A batch without a token: empty outputs, gradients of zero for every parameter."""
+    d, f = 64, 96
+    P = FfnParams(torch.ones(4, d, device="cuda"), torch.zeros(4, d, device="cuda"), normal((d, 2 * f), 1), normal((f, d), 2))
+    jag = ops.Jagged.from_host([0, 0, 0], [], [])
+    x = torch.empty(0, d, dtype=torch.bfloat16, device="cuda")
+    rng = torch.zeros(2, dtype=torch.int64, device="cuda")
+    out, ctx = ffn_fwd(x, jag, P, rng, p)
+    g = ffn_bwd(out, ctx, jag, P, rng, p)
+    torch.cuda.synchronize()
+    assert out.shape == g["x"].shape == (0, d)
+    assert not any(g[n].any() for n in ("w_in", "w_out", "gamma", "beta"))

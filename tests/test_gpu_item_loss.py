@@ -57,3 +57,32 @@ def test_a_hot_item_and_an_empty_batch():
     loss, saved = table.item_loss(x, batch, labels)
     dx, grad_out = table.item_loss_bwd(torch.ones(50, device="cuda"), saved)
     assert not loss.any() and not dx.any() and grad_out.shape == (0, 32)
+
+
+def test_captured_and_replayed():
+    """lookup's batch held, x and labels changed between replays; the eager program runs in between."""
+    ids = torch.randint(0, 90, (700,), generator=torch.Generator().manual_seed(4))
+    table, batch = batch_of(ids)
+    x, labels = normal((80, 32), 3), torch.randint(-100, 700, (80,), generator=torch.Generator().manual_seed(5)).cuda()
+    dloss = torch.full((80,), 1.0 / 80, device="cuda")
+
+    def step():
+        loss, saved = table.item_loss(x, batch, labels, scale=0.7)
+        return loss, *table.item_loss_bwd(dloss, saved)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for k in range(4):
+        x.copy_(normal((80, 32), 30 + k))
+        labels.copy_(torch.randint(-100, 700, (80,), generator=torch.Generator().manual_seed(50 + k)))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, eager)), k
