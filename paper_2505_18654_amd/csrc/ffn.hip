@@ -183,8 +183,8 @@ hipError_t launch_ffn_fwd(const FfnArgs& f, void* workspace, hipStream_t s) {
 
 namespace {
 
-// The backward's products: dpre, and the three behind it: dx, dW_in and dW_out, one after the other, or in one launch on 128 x 128 tiles,
-// their k cut into about equal numbers of steps, and one launch that adds up all partials.
+// The backward's products: dpre, and the three behind it: dx, dW_in and dW_out, one after the other, or in one launch on
+// 128 x 128 tiles, their k cut into about equal numbers of steps, and one launch that adds up all partials.
 struct BackwardPlan {
     bool together;
     Tiles dpre;               // of dh = dy W_out^T with the gradient of the activation
