@@ -1,0 +1,243 @@
+// One query token of each sequence against its paged cache.
+//
+// A workgroup takes a chunk of a sequence's keys for one key head and up to 32 of the query heads that share it, a query
+// head per column of the 32 x 32 products; its 4 waves take the chunk's tiles of 32 keys in turn, each with its own
+// maximum, sum and outputs, and its own LDS tiles, so that no wave waits for another.  They are joined through LDS, and the chunks of
+// a sequence, where there are several, by a second kernel.  Bound by the read of the cache.
+#include "causal_device.h"
+
+namespace mtgr {
+namespace {
+
+using namespace causal;
+constexpr int BN = 32, WAVES = 4, QT = 32;
+
+// A wave's copy of 32 rows of a head's pages into a swizzled tile, page0 and page1 those of its halves (16 rows, the
+// smallest page).  Rows outside lo .. hi are copies of row lo or hi, so that every row of the tile is one of the sequence's own.
+template <int DH>
+__device__ __forceinline__ void page_dma(uint16_t* tile, const uint16_t* base, long long page_stride, int in_page, int page0,
+                                         int page1, int row0, int lo, int hi, int lane) {
+    constexpr int CPR = DH / 8, RPI = 64 / CPR;
+    const int rl = lane / CPR;
+    const uint32_t dst = lds_address(tile);
+#pragma unroll
+    for (int i = 0; i < BN / RPI; i++) {
+        const int page = min(max(i * RPI, lo), hi) >= 16 ? page1 : page0;
+        const int r = min(max(i * RPI + rl, lo), hi);
+        const int c = (lane % CPR) ^ swz<CPR>(i * RPI + rl);
+        lds_dma16(dst + i * 1024u, uniform_ptr(base + page * page_stride), (uint32_t)(((row0 + r) & in_page) * DH + c * 8) * 2u);
+    }
+}
+
+template <int DH>
+__global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
+    constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, TILE = BN * DH;
+    __shared__ __align__(16) uint16_t sT[WAVES][4][TILE];        // K 0, K 1, V 0, V 1 of each wave; then its outputs
+    __shared__ float sML[WAVES][2][QT];
+    static_assert(4 * TILE * 2 >= QT * DH * 4, "a wave's outputs fit its tiles");
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, hh = lane >> 5;
+    const int b = blockIdx.z, split = blockIdx.x;
+    const int qtiles = (a.group + QT - 1) / QT, hk = blockIdx.y / qtiles;
+    const int g0 = QT * (blockIdx.y % qtiles), heads = min(QT, a.group - g0), h0 = hk * a.group + g0;
+    const int len = min(max(a.lens[b], 0), a.max_len);
+    const int c0 = split * a.chunk, c1 = min(c0 + a.chunk, len);
+    if (c0 >= len && split > 0) return;
+    const CacheArgs& cache = a.cache;
+    const int* table = cache.table + b * cache.ld_table;
+    const long long head_ofs = (long long)hk << cache.page_shift, page_stride = ((long long)cache.kv_heads << cache.page_shift) * DH;
+    const uint16_t* Kb = (const uint16_t*)cache.keys + head_ofs * DH;
+    const uint16_t* Vb = (const uint16_t*)cache.values + head_ofs * DH;
+    const int in_page = (1 << cache.page_shift) - 1;
+    bf16x8 qreg[KSTEPS];
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk++)
+        qreg[kk] = col < heads ? as_bf16x8(*(const uint4*)((const uint16_t*)a.q + b * a.ld_q + (h0 + col) * DH + 16 * kk + 8 * hh))
+                               : bf16x8{};
+    floatx16 oacc[DBLK];
+#pragma unroll
+    for (int d = 0; d < DBLK; d++) oacc[d] = floatx16{};
+    float m = -3.0e38f, l = 0.f;
+    wait_vmcnt_seen<0>();
+    for (int k0 = c0 + BN * w; k0 < c1; k0 += BN * WAVES) {
+        const int last = min(c1 - k0, BN) - 1;
+        // pages of the tile's halves (the same one where pages are larger); the last half may have none of its keys
+        const int page0 = __builtin_amdgcn_readfirstlane(table[k0 >> cache.page_shift]);
+        const int page1 = __builtin_amdgcn_readfirstlane(table[(k0 + min(16, last)) >> cache.page_shift]);
+        const bool has0 = page0 >= 0 && page0 < cache.num_pages, has1 = last >= 16 && page1 >= 0 && page1 < cache.num_pages;
+        if (!has0 && !has1) continue;
+        const int lo = has0 ? 0 : 16, hi = has1 ? last : min(last, 15);
+        wait_vmcnt_seen<0>();
+        page_dma<DH>(sT[w][0], Kb, page_stride, in_page, page0, page1, k0 & in_page, lo, hi, lane);
+        page_dma<DH>(sT[w][2], Vb, page_stride, in_page, page0, page1, k0 & in_page, lo, hi, lane);
+        wait_vmem();
+        const uint16_t* sK = sT[w][0];
+        const uint16_t* sV = sT[w][2];
+        floatx16 s{};
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; kk++)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sK, col, 2 * kk + hh), qreg[kk], s, 0, 0, 0);
+        if (lo > 0 || hi < BN - 1) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+                const int key = 8 * (e >> 2) + 4 * hh + (e & 3);
+                s[e] = key >= lo && key <= hi ? s[e] : neg_inf();
+            }
+        }
+        float top = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; e++) top = fmaxf(top, s[e]);
+        top = fmaxf(max_halves(top), m);
+        if (__any(top > m)) {
+            const float f = __builtin_amdgcn_exp2f((m - top) * a.c);
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DBLK; d++) oacc[d] *= f;
+            m = top;
+        }
+        const float mc = m * a.c;
+        uint32_t pk[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, -mc));
+            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], a.c, -mc));
+            l += p0 + p1;
+            pk[e >> 1] = pack_bf16x2(p0, p1);
+        }
+#pragma unroll
+        for (int kq = 0; kq < 2; kq++) {
+            const bf16x8 pb = as_bf16x8(make_uint4(pk[4 * kq], pk[4 * kq + 1], pk[4 * kq + 2], pk[4 * kq + 3]));
+#pragma unroll
+            for (int d = 0; d < DBLK; d++)
+                oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read_tr<CPR>(sV, 16 * kq, 32 * d, lane), pb, oacc[d], 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the tile is read before the next one's copies
+    }
+    l = sum_halves(l);
+    if (hh == 0) {
+        sML[w][0][col] = m;
+        sML[w][1][col] = l;
+    }
+    // the wave's outputs, [query][feature] fp32
+    float* sO = (float*)sT[w];
+#pragma unroll
+    for (int d = 0; d < DBLK; d++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+            *(float4*)&sO[col * DH + 32 * d + 8 * g + 4 * hh] =
+                make_float4(oacc[d][4 * g], oacc[d][4 * g + 1], oacc[d][4 * g + 2], oacc[d][4 * g + 3]);
+    __syncthreads();
+    for (int i = tid; i < heads * (DH / 4); i += 256) {
+        const int q = i / (DH / 4), f = 4 * (i % (DH / 4));
+        float top = sML[0][0][q];
+#pragma unroll
+        for (int j = 1; j < WAVES; j++) top = fmaxf(top, sML[j][0][q]);
+        float total = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < WAVES; j++) {
+            const float e = __builtin_amdgcn_exp2f((sML[j][0][q] - top) * a.c);
+            const float4 v = *(const float4*)&((const float*)sT[j])[q * DH + f];
+            total = __builtin_fmaf(e, sML[j][1][q], total);
+            o.x = __builtin_fmaf(e, v.x, o.x);
+            o.y = __builtin_fmaf(e, v.y, o.y);
+            o.z = __builtin_fmaf(e, v.z, o.z);
+            o.w = __builtin_fmaf(e, v.w, o.w);
+        }
+        const long long row = (long long)b * a.H + h0 + q;
+        if (a.splits > 1) {
+            *(float4*)&a.part[(row * a.splits + split) * DH + f] = o;
+            if (f == 0) a.part_ml[row * a.splits + split] = make_float2(top, total);
+        } else {
+            const float inv = total != 0.f ? 1.0f / total : 0.f;      // no key: zeros
+            *(uint2*)((uint16_t*)a.out + b * a.ld_o + (h0 + q) * DH + f) =
+                make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+            if (f == 0 && a.lse) a.lse[row] = total != 0.f ? top * a.scale + logf(total) : neg_inf();
+        }
+    }
+}
+
+// Joins the chunks of a (sequence, head): lanes over features, groups of lanes over chunks.
+template <int DH>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
+    constexpr int L = DH / 4, G = 256 / L;
+    __shared__ float sTop[4], sTotal[G];
+    __shared__ float4 sO[256];
+    const int tid = threadIdx.x, h = blockIdx.x, b = blockIdx.y;
+    const long long row = (long long)b * a.H + h;
+    const int len = min(max(a.lens[b], 0), a.max_len), n = max(1, (len + a.chunk - 1) / a.chunk);
+    const float2* ml = a.part_ml + row * a.splits;
+    float top = -3.0e38f;
+    for (int i = tid; i < n; i += 256) top = fmaxf(top, ml[i].x);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    if ((tid & 63) == 0) sTop[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(sTop[0], sTop[1]), fmaxf(sTop[2], sTop[3]));
+    const int g = tid / L, f = 4 * (tid % L);
+    float total = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = g; i < n; i += G) {
+        const float2 x = ml[i];
+        const float e = __builtin_amdgcn_exp2f((x.x - top) * a.c);
+        const float4 v = *(const float4*)&a.part[(row * a.splits + i) * DH + f];
+        total = __builtin_fmaf(e, x.y, total);
+        o.x = __builtin_fmaf(e, v.x, o.x);
+        o.y = __builtin_fmaf(e, v.y, o.y);
+        o.z = __builtin_fmaf(e, v.z, o.z);
+        o.w = __builtin_fmaf(e, v.w, o.w);
+    }
+    sO[tid] = o;
+    if (f == 0) sTotal[g] = total;
+    __syncthreads();
+    if (g > 0) return;
+    for (int j = 1; j < G; j++) {
+        const float4 v = sO[j * L + tid];
+        total += sTotal[j];
+        o.x += v.x;
+        o.y += v.y;
+        o.z += v.z;
+        o.w += v.w;
+    }
+    const float inv = total != 0.f ? 1.0f / total : 0.f;
+    *(uint2*)((uint16_t*)a.out + b * a.ld_o + h * DH + f) =
+        make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    if (f == 0 && a.lse) a.lse[row] = total != 0.f ? top * a.scale + logf(total) : neg_inf();
+}
+
+}  // namespace
+
+CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_len) {
+    CacheAttnPlan p{};
+    const int group = H / Hk;
+    const long long units = (long long)B * Hk * ((group + QT - 1) / QT);
+    const long long want = (512 + units - 1) / units;             // chunks of a sequence that fill the chip
+    long long chunk = (max_len + want - 1) / want;
+    chunk = std::min<long long>(std::max<long long>((chunk + 127) / 128 * 128, 128), 2048);
+    p.chunk = (int)chunk;
+    p.splits = (int)std::max<long long>(1, (max_len + chunk - 1) / chunk);
+    if (p.splits > 1) {
+        p.part_bytes = ((size_t)B * H * p.splits * head_dim * 4 + 255) & ~(size_t)255;
+        p.bytes = p.part_bytes + (((size_t)B * H * p.splits * 8 + 255) & ~(size_t)255);
+    }
+    return p;
+}
+
+template <int DH>
+static hipError_t cache_attn_dh(const CacheAttnArgs& a, hipStream_t s) {
+    const int Hk = a.H / a.group;
+    cache_attn_kernel<DH><<<dim3(a.splits, Hk * ((a.group + QT - 1) / QT), a.B), 256, 0, s>>>(a);
+    if (a.splits > 1) cache_join_kernel<DH><<<dim3(a.H, a.B), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_attn(const CacheAttnArgs& a, int head_dim, hipStream_t s) {
+    switch (head_dim) {
+        case 32: return cache_attn_dh<32>(a, s);
+        case 64: return cache_attn_dh<64>(a, s);
+        case 128: return cache_attn_dh<128>(a, s);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+}  // namespace mtgr

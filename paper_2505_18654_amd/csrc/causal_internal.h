@@ -1,0 +1,87 @@
+// Host-side argument structs and launch entry points behind include/mtgr_causal.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+namespace mtgr {
+
+// Rotary positions, and the append that applies them (rope.hip).
+struct RopeArgs {
+    long long T;
+    int B;
+    int heads;                // heads of x; append: of q
+    int dh, rot;
+    bool interleaved, inverse;
+    float amplitude;
+    const double* freqs;
+    const void* x;            // append: q or NULL
+    void* out;                // append: q_out
+    long long ld_x, ld_out;
+    const int* positions;     // or NULL
+    const int* offsets;       // or NULL
+};
+hipError_t launch_rope(const RopeArgs& a, bool bf16, hipStream_t s);
+
+struct CacheArgs {
+    void *keys, *values;
+    long long num_pages;
+    int page_shift, kv_heads;
+    const int* table;
+    long long ld_table;
+    int max_pages;
+};
+struct AppendArgs {
+    RopeArgs rope;            // of q and k; rot 0: none
+    CacheArgs cache;
+    const int* past;
+    const void *k, *v;
+    long long ld_k, ld_v;
+};
+hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s);
+
+// Causal attention (causal_fwd.hip, causal_bwd_dkdv.hip, causal_bwd_dq.hip).
+struct CausalArgs {
+    int B, H, Hk, group;      // group: query heads of a key head
+    long long T;
+    int slots;                // tiles of 128 rows, at most
+    float scale, c;           // c = scale / ln 2
+    const int* offsets;
+    const void *q, *k, *v, *dout;
+    void* out;                // backward: read
+    float* lse;               // [H, T], or NULL in the forward
+    const float* delta;       // [H, T] of the backward
+    void *dq, *dk, *dv;
+    long long ld_q, ld_k, ld_v, ld_o, ld_do;
+};
+hipError_t launch_causal_fwd(const CausalArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_causal_delta(const CausalArgs& a, int head_dim, float* delta, hipStream_t s);
+hipError_t launch_causal_dkdv(const CausalArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_causal_dq(const CausalArgs& a, int head_dim, hipStream_t s);
+
+// Single tokens against the cache (cache_attn.hip).
+struct CacheAttnArgs {
+    CacheArgs cache;
+    int B, H, group;
+    int chunk, splits;        // keys of a workgroup, and how many of them a sequence has at most
+    int max_len;
+    float scale, c;
+    const int* lens;
+    const void* q;
+    long long ld_q, ld_o;
+    void* out;
+    float* lse;               // or NULL
+    float* part;              // [B H][splits][dh] sums, splits > 1
+    float2* part_ml;          // [B H][splits] their maxima and totals
+};
+struct CacheAttnPlan {
+    int chunk, splits;
+    size_t part_bytes, bytes;
+};
+CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_len);
+hipError_t launch_cache_attn(const CacheAttnArgs& a, int head_dim, hipStream_t s);
+
+}  // namespace mtgr

@@ -38,6 +38,8 @@ MTGR_NOALLOC_SCRATCH_BYTES = 16 * 1024 * 1024
 MTGR_GEMM_NN, MTGR_GEMM_NT, MTGR_GEMM_TN = 0, 1, 2
 MTGR_GEMM_EPI_NONE, MTGR_GEMM_EPI_BIAS_SILU, MTGR_GEMM_EPI_BIAS_RESIDUAL = 0, 1, 2
 MTGR_FFN_SERVING, MTGR_FFN_BACKWARD, MTGR_FFN_TRAINING = 0, 1, 2
+MTGR_ROPE_HALF, MTGR_ROPE_INTERLEAVED = 0, 1
+MTGR_ROPE_NONE, MTGR_ROPE_LINEAR, MTGR_ROPE_BASE, MTGR_ROPE_PARTS = 0, 1, 2, 3
 MTGR_EMB_KEY_EMPTY = 0xFFFFFFFFFFFFFFFF
 MTGR_EMB_KEY_DELETED = 0xFFFFFFFFFFFFFFFE
 MTGR_EMB_STATE_WORDS = 8
@@ -58,6 +60,8 @@ EXPORTED = (
     "mtgr_gated_ffn_workspace_size", "mtgr_gated_ffn_fwd", "mtgr_gated_ffn_bwd", "mtgr_dropout",
     "mtgr_softmax_loss_workspace_size", "mtgr_softmax_loss_fwd", "mtgr_softmax_loss_bwd",
     "mtgr_debug_gated_ffn_kernels", "mtgr_debug_softmax_loss_kernels",
+    "mtgr_rope_frequencies", "mtgr_rope", "mtgr_causal_attn_workspace_size", "mtgr_causal_attn_fwd", "mtgr_causal_attn_bwd",
+    "mtgr_kv_append", "mtgr_cache_attn_workspace_size", "mtgr_cache_attn",
 )
 
 
@@ -102,6 +106,46 @@ class SoftmaxLossProblem(ctypes.Structure):
     _fields_ = [
         ("num_rows", ctypes.c_int64), ("num_classes", ctypes.c_int64), ("dim", ctypes.c_int32),
         ("target_bits", ctypes.c_int32), ("scale", ctypes.c_float), ("ld_x", ctypes.c_int64), ("ld_w", ctypes.c_int64),
+    ]
+
+
+class RopeProblem(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int64), ("num_seqs", ctypes.c_int32), ("heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("inverse", ctypes.c_int32), ("amplitude", ctypes.c_float), ("ld_x", ctypes.c_int64), ("ld_out", ctypes.c_int64),
+    ]
+
+
+class CausalProblem(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("total_tokens", ctypes.c_int64), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+        ("ld_q", ctypes.c_int64), ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64), ("ld_o", ctypes.c_int64),
+        ("ld_do", ctypes.c_int64),
+    ]
+
+
+class KvCachePages(ctypes.Structure):
+    _fields_ = [
+        ("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32), ("keys", ctypes.c_void_p), ("values", ctypes.c_void_p),
+    ]
+
+
+class KvAppendProblem(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int64), ("num_seqs", ctypes.c_int32), ("heads", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("amplitude", ctypes.c_float),
+        ("ld_table", ctypes.c_int64), ("ld_q", ctypes.c_int64), ("ld_q_out", ctypes.c_int64), ("ld_k", ctypes.c_int64),
+        ("ld_v", ctypes.c_int64),
+    ]
+
+
+class CacheAttnProblem(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("heads", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("max_len", ctypes.c_int64), ("ld_table", ctypes.c_int64), ("ld_q", ctypes.c_int64), ("ld_o", ctypes.c_int64),
     ]
 
 
@@ -171,6 +215,16 @@ def lib() -> ctypes.CDLL:
         L.mtgr_softmax_loss_bwd.argtypes = [S, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.mtgr_debug_gated_ffn_kernels.argtypes = [F, ctypes.c_int, ctypes.c_int, ctypes.c_char_p, sz]
         L.mtgr_debug_softmax_loss_kernels.argtypes = [S, ctypes.c_int, i64, ctypes.c_char_p, sz]
+        R, C, A, D, K = (ctypes.POINTER(t) for t in (RopeProblem, CausalProblem, KvAppendProblem, CacheAttnProblem, KvCachePages))
+        L.mtgr_rope_frequencies.argtypes = [i32, ctypes.c_double, ctypes.c_int, ctypes.c_double, i64, ctypes.c_double,
+                                            ctypes.c_double, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)]
+        L.mtgr_rope.argtypes = [R, vp, vp, vp, vp, vp, vp]
+        L.mtgr_causal_attn_workspace_size.argtypes = [C, ctypes.c_int, ctypes.POINTER(sz)]
+        L.mtgr_causal_attn_fwd.argtypes = [C, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mtgr_causal_attn_bwd.argtypes = [C, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mtgr_kv_append.argtypes = [A, K, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.mtgr_cache_attn_workspace_size.argtypes = [D, K, ctypes.POINTER(sz)]
+        L.mtgr_cache_attn.argtypes = [D, K, vp, vp, vp, vp, vp, vp, sz, vp]
         for name in EXPORTED:
             if name not in ("mtgr_status_string", "mtgr_last_error_message", "mtgr_version"):
                 getattr(L, name).restype = ctypes.c_int
@@ -498,3 +552,57 @@ def mtgr_debug_softmax_loss_kernels(problem, backward: bool, labels: Optional[in
     """labels: the number of rows with a label; all of them if None."""
     return _pairs(lib().mtgr_debug_softmax_loss_kernels, ctypes.byref(problem), int(backward),
                   problem.num_rows if labels is None else int(labels))
+
+
+# ------------------------------------------------------------------ rotary positions, causal attention, paged cache
+
+def mtgr_rope_frequencies(rot_dim: int, base: float, scaling: int = MTGR_ROPE_NONE, factor: float = 1.0, trained_len: int = 0,
+                          slow: float = 1.0, fast: float = 32.0):
+    """(list of rot_dim / 2 frequencies, amplitude), on the host."""
+    freqs, amplitude = (ctypes.c_double * max(int(rot_dim) // 2, 1))(), ctypes.c_float(0.0)
+    _check(lib().mtgr_rope_frequencies(int(rot_dim), float(base), int(scaling), float(factor), int(trained_len), float(slow),
+                                       float(fast), freqs, ctypes.byref(amplitude)))
+    return list(freqs), amplitude.value
+
+
+def mtgr_rope(problem, x, positions, offsets, freqs, out, stream=None) -> None:
+    _check(lib().mtgr_rope(ctypes.byref(problem), _ptr(x), _ptr(positions), _ptr(offsets), _ptr(freqs), _ptr(out),
+                           _stream(stream)))
+
+
+def mtgr_causal_attn_workspace_size(problem: CausalProblem, backward: bool = False) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().mtgr_causal_attn_workspace_size(ctypes.byref(problem), int(backward), ctypes.byref(out)))
+    return int(out.value)
+
+
+def mtgr_causal_attn_fwd(problem, offsets, q, k, v, out, lse, workspace, workspace_bytes, stream=None) -> None:
+    _check(lib().mtgr_causal_attn_fwd(ctypes.byref(problem), _ptr(offsets), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
+                                      _ptr(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def mtgr_causal_attn_bwd(problem, offsets, q, k, v, out, lse, dout, dq, dk, dv, workspace, workspace_bytes,
+                         stream=None) -> None:
+    _check(lib().mtgr_causal_attn_bwd(ctypes.byref(problem), _ptr(offsets), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
+                                      _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace), int(workspace_bytes),
+                                      _stream(stream)))
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def mtgr_kv_append(problem, cache, page_table, past, offsets, q, k, v, freqs, q_out, stream=None) -> None:
+    _check(lib().mtgr_kv_append(_ref(problem), _ref(cache), _ptr(page_table), _ptr(past), _ptr(offsets), _ptr(q), _ptr(k),
+                                _ptr(v), _ptr(freqs), _ptr(q_out), _stream(stream)))
+
+
+def mtgr_cache_attn_workspace_size(problem: CacheAttnProblem, cache: KvCachePages) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().mtgr_cache_attn_workspace_size(_ref(problem), _ref(cache), ctypes.byref(out)))
+    return int(out.value)
+
+
+def mtgr_cache_attn(problem, cache, page_table, lens, q, out, lse, workspace, workspace_bytes, stream=None) -> None:
+    _check(lib().mtgr_cache_attn(_ref(problem), _ref(cache), _ptr(page_table), _ptr(lens), _ptr(q), _ptr(out), _ptr(lse),
+                                 _ptr(workspace), int(workspace_bytes), _stream(stream)))

@@ -465,3 +465,249 @@ def softmax_loss_bwd(dloss, x, w, targets, lse, bias=None, scale: float = 1.0, g
     workspace = _scratch(workspace, hstu.mtgr_softmax_loss_workspace_size(p, True), x)
     hstu.mtgr_softmax_loss_bwd(p, dloss, x, w, targets, bias, lse, dx, dw, dbias, workspace, workspace.numel())
     return dx, dw, dbias
+
+
+# ------------------------------------------------------------------ rotary positions, causal attention, paged cache
+
+def _heads(name: str, t, tokens: Optional[int], heads: Optional[int], dh: Optional[int], dtype, dev: int,
+           like: Optional[int] = None) -> int:
+    """Checks a [tokens, heads, head_dim] operand (shape, type, device, dense heads, token rows that do not overlap) and
+    returns its token stride; `like`: the stride that a gradient shares with its primal."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype is not dtype:
+        got = f"{list(t.shape)} {t.dtype}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise ValueError(f"{name} is [tokens, heads, head_dim] of {dtype}, got {got}")
+    shape = t.shape
+    if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or \
+            (dh is not None and shape[2] != dh):
+        raise ValueError(f"{name} is [{tokens}, {heads}, {dh}], got {list(shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    ld, sh, se = t.stride()
+    row = shape[1] * shape[2]
+    if (se != 1 and shape[2] > 1) or (sh != shape[2] and shape[1] > 1):
+        raise ValueError(f"the heads of {name} are not dense")
+    if shape[0] <= 1:
+        ld = row
+    elif ld < row:
+        raise ValueError(f"the rows of {name} overlap")
+    if like is not None and ld != like:
+        raise ValueError(f"{name} must share the token stride of its primal")
+    return ld
+
+
+@dataclass
+class Rotary:
+    """Rotary positions: pair i of a head turns by freqs[i] (radians, device float64 [rot_dim / 2]) per position, and is
+    multiplied by `amplitude`.  layout "half" pairs feature i with i + rot_dim / 2, "interleaved" 2 i with 2 i + 1; features
+    behind rot_dim are kept."""
+    freqs: torch.Tensor
+    layout: str = "half"
+    amplitude: float = 1.0
+
+    def code(self, dev: int) -> int:
+        if self.layout not in ("half", "interleaved"):
+            raise ValueError(f"layout {self.layout!r} is neither 'half' nor 'interleaved'")
+        _vector("freqs", self.freqs, self.freqs.numel(), (torch.float64,), dev)
+        return hstu.MTGR_ROPE_HALF if self.layout == "half" else hstu.MTGR_ROPE_INTERLEAVED
+
+
+_ROPE_SCALINGS = {"none": hstu.MTGR_ROPE_NONE, "linear": hstu.MTGR_ROPE_LINEAR, "base": hstu.MTGR_ROPE_BASE,
+                  "parts": hstu.MTGR_ROPE_PARTS}
+
+
+def rotary(rot_dim: int, base: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+           trained_len: int = 0, slow: float = 1.0, fast: float = 32.0, device="cuda") -> Rotary:
+    """Rotary positions of the first rot_dim features (a multiple of 16) with frequencies base^(-2 i / rot_dim), stretched
+    for contexts `factor` times the trained ones by `scaling`: "linear", "base" or "parts" (mtgr_rope_frequencies)."""
+    if scaling not in _ROPE_SCALINGS:
+        raise ValueError(f"scaling {scaling!r} is none of {', '.join(_ROPE_SCALINGS)}")
+    freqs, amplitude = hstu.mtgr_rope_frequencies(rot_dim, base, _ROPE_SCALINGS[scaling], factor, trained_len, slow, fast)
+    return Rotary(torch.tensor(freqs, dtype=torch.float64, device=device), layout, amplitude)
+
+
+def rope(x, rotary: Rotary, positions=None, offsets=None, inverse: bool = False, out=None):
+    """x [T, heads, head_dim] (bf16 or fp32) with its heads rotated by their tokens' positions: `positions` [T] int32, or
+    those inside each sequence of `offsets` [B + 1] int32 (rows behind the last are left).  inverse=True turns back: the
+    gradient of x.  out may be x."""
+    code, dev = _dtype_code(x), _device()
+    ld_x = _heads("x", x, None, None, None, x.dtype, dev)
+    T, H, dh = x.shape
+    if out is None:
+        out = torch.empty((T, H, dh), dtype=x.dtype, device=x.device)
+    ld_out = _heads("out", out, T, H, dh, x.dtype, dev)
+    layout = rotary.code(dev)
+    if (positions is None) == (offsets is None):
+        raise ValueError("either positions or offsets is given")
+    B = 0
+    if positions is not None:
+        _vector("positions", positions, T, (torch.int32,), dev)
+    else:
+        B = _sequences(offsets, dev)
+    p = hstu.RopeProblem(T, B, H, dh, 2 * rotary.freqs.numel(), layout, code, int(inverse), rotary.amplitude, ld_x, ld_out)
+    hstu.mtgr_rope(p, x, positions, offsets, rotary.freqs, out)
+    return out
+
+
+def _sequences(offsets, dev: int) -> int:
+    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.numel() < 1:
+        raise ValueError("offsets is [B + 1] int32")
+    _vector("offsets", offsets, offsets.numel(), (torch.int32,), dev)
+    return offsets.numel() - 1
+
+
+def _causal_problem(q, k, v, offsets, scale, ld_o: int, ld_do: int) -> hstu.CausalProblem:
+    bf, dev = torch.bfloat16, _device()
+    ld_q = _heads("q", q, None, None, None, bf, dev)
+    T, H, dh = q.shape
+    ld_k = _heads("k", k, T, None, dh, bf, dev)
+    ld_v = _heads("v", v, T, k.shape[1], dh, bf, dev)
+    return hstu.CausalProblem(_sequences(offsets, dev), H, k.shape[1], dh, T, dh ** -0.5 if scale is None else scale, 0, ld_q, ld_k,
+                              ld_v, ld_o, ld_do)
+
+
+def causal_attn_workspace(q, k, offsets, backward: bool = False) -> torch.Tensor:
+    """A workspace for causal_attn_fwd or causal_attn_bwd of these sizes."""
+    p = _causal_problem(q, k, k, offsets, None, 0, 0)
+    n = hstu.mtgr_causal_attn_workspace_size(p, backward)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
+
+
+def causal_attn_fwd(q, k, v, offsets, scale: Optional[float] = None, save: bool = False, out=None, lse=None, workspace=None):
+    """Causal softmax attention of packed sequences (bf16): q [T, heads, head_dim], k and v [T, kv_heads, head_dim], heads a
+    multiple of kv_heads, offsets [B + 1] int32 (a Jagged's offsets); scale: 1 / sqrt(head_dim) by default.  Returns out
+    [T, heads, head_dim], or with save=True (out, lse [heads, T] fp32) for causal_attn_bwd.  Rows behind the last sequence are
+    left as they were."""
+    p = _causal_problem(q, k, v, offsets, scale, 0, 0)
+    dev = q.get_device()
+    T, H, dh = q.shape
+    if out is None:
+        out = torch.empty((T, H, dh), dtype=torch.bfloat16, device=q.device)
+    p.ld_o = _heads("out", out, T, H, dh, torch.bfloat16, dev)
+    if save and lse is None:
+        lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _lse(lse, H, T, dev)
+    workspace = _scratch(workspace, hstu.mtgr_causal_attn_workspace_size(p), q)
+    hstu.mtgr_causal_attn_fwd(p, offsets, q, k, v, out, lse, workspace, workspace.numel())
+    return (out, lse) if save else out
+
+
+def _lse(t, rows: int, cols: int, dev: int) -> None:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (rows, cols) or not t.is_contiguous():
+        raise ValueError(f"lse is a dense [{rows}, {cols}] of fp32")
+    if t.get_device() != dev:
+        raise ValueError(f"lse is on {t.device}, not on the current device")
+
+
+def causal_attn_bwd(dout, q, k, v, out, lse, offsets, scale: Optional[float] = None, grads=None, workspace=None):
+    """Gradients of causal_attn_fwd for dout, with its out and lse: (dq, dk, dv), in the layouts of q, k and v (`grads`: the
+    tensors to write).  Rows behind the last sequence are left as they were."""
+    p = _causal_problem(q, k, v, offsets, scale, 0, 0)
+    bf, dev = torch.bfloat16, q.get_device()
+    p.ld_o, p.ld_do = _heads("out", out, *q.shape, bf, dev), _heads("dout", dout, *q.shape, bf, dev)
+    _lse(lse, q.shape[1], q.shape[0], dev)
+    dq, dk, dv = grads if grads is not None else (_like_layout(t) for t in (q, k, v))
+    _heads("dq", dq, *q.shape, bf, dev, p.ld_q)
+    _heads("dk", dk, *k.shape, bf, dev, p.ld_k)
+    _heads("dv", dv, *v.shape, bf, dev, p.ld_v)
+    workspace = _scratch(workspace, hstu.mtgr_causal_attn_workspace_size(p, True), q)
+    hstu.mtgr_causal_attn_bwd(p, offsets, q, k, v, out, lse, dout, dq, dk, dv, workspace, workspace.numel())
+    return dq, dk, dv
+
+
+@dataclass
+class KvCache:
+    """A paged cache of keys and values, bf16 [num_pages, kv_heads, page_size, head_dim] each: token p of a sequence lies in
+    row p % page_size of page page_table[sequence, p // page_size]."""
+    keys: torch.Tensor
+    values: torch.Tensor
+
+    @staticmethod
+    def empty(num_pages: int, kv_heads: int, page_size: int, head_dim: int, device="cuda") -> "KvCache":
+        keys = torch.empty((num_pages, kv_heads, page_size, head_dim), dtype=torch.bfloat16, device=device)
+        return KvCache(keys, torch.empty_like(keys))
+
+    def struct(self, dev: int) -> hstu.KvCachePages:
+        k, v = self.keys, self.values
+        for name, t in (("keys", k), ("values", v)):
+            if not isinstance(t, torch.Tensor) or t.dim() != 4 or t.dtype is not torch.bfloat16 or not t.is_contiguous():
+                raise ValueError(f"the cache's {name} are a dense [num_pages, kv_heads, page_size, head_dim] of bf16")
+            if t.get_device() != dev:
+                raise ValueError(f"the cache's {name} are on {t.device}, not on the current device")
+        if k.shape != v.shape:
+            raise ValueError(f"keys {list(k.shape)} and values {list(v.shape)} of the cache differ")
+        return hstu.KvCachePages(k.shape[0], k.shape[2], k.shape[1], k.shape[3], 0, k.data_ptr(), v.data_ptr())
+
+
+def _page_table(t, dev: int):
+    """(num_seqs, max_pages, row stride) of a page table."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype is not torch.int32 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("page_table is [num_seqs, max_pages] of int32 with dense rows")
+    if t.get_device() != dev:
+        raise ValueError(f"page_table is on {t.device}, not on the current device")
+    B, n = t.shape
+    ld = t.stride(0) if B > 1 else n
+    if ld < n:
+        raise ValueError("the rows of page_table overlap")
+    return B, n, ld
+
+
+def kv_append(cache: KvCache, page_table, past, k, v, offsets=None, q=None, rotary: Optional[Rotary] = None, q_out=None):
+    """Appends new tokens to a paged cache: rows offsets[b] .. offsets[b + 1] - 1 of k and v [N, kv_heads, head_dim] (without
+    offsets: row b) become tokens past[b], past[b] + 1, .. of sequence b.  With `rotary`, k is rotated on the way by its
+    position in the sequence, and q [N, heads, head_dim] by the same; returns the rotated q (q_out, which may be q), or None
+    without q.  past [B] int32; a sequence whose past is negative is left alone, with its rows of q_out."""
+    bf, dev = torch.bfloat16, _device()
+    c = cache.struct(dev)
+    B, pages, ld_table = _page_table(page_table, dev)
+    _vector("past", past, B, (torch.int32,), dev)
+    ld_k = _heads("k", k, None, c.kv_heads, c.head_dim, bf, dev)
+    N = k.shape[0]
+    ld_v = _heads("v", v, N, c.kv_heads, c.head_dim, bf, dev)
+    if offsets is not None and _sequences(offsets, dev) != B:
+        raise ValueError(f"offsets are those of {offsets.numel() - 1} sequences, page_table of {B}")
+    H = ld_q = ld_q_out = 0
+    if q is not None:
+        ld_q = _heads("q", q, N, None, c.head_dim, bf, dev)
+        H = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty((N, H, c.head_dim), dtype=bf, device=q.device)
+        ld_q_out = _heads("q_out", q_out, N, H, c.head_dim, bf, dev)
+    elif q_out is not None:
+        raise ValueError("q_out goes with q")
+    rot, layout, amplitude, freqs = 0, 0, 1.0, None
+    if rotary is not None:
+        rot, layout, amplitude, freqs = 2 * rotary.freqs.numel(), rotary.code(dev), rotary.amplitude, rotary.freqs
+    p = hstu.KvAppendProblem(N, B, H, pages, rot, layout, amplitude, ld_table, ld_q, ld_q_out, ld_k, ld_v)
+    hstu.mtgr_kv_append(p, c, page_table, past, offsets, q, k, v, freqs, q_out)
+    return q_out
+
+
+def cache_attn_workspace(cache: KvCache, num_seqs: int, heads: int, max_len: int) -> torch.Tensor:
+    """A workspace for cache_attn of these sizes."""
+    c = cache.struct(_device())
+    p = hstu.CacheAttnProblem(num_seqs, heads, -(-max(max_len, 1) // c.page_size), 1.0, max_len, 0, 0, 0)
+    n = hstu.mtgr_cache_attn_workspace_size(p, c)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=cache.keys.device)
+
+
+def cache_attn(q, cache: KvCache, page_table, lens, scale: Optional[float] = None, max_len: Optional[int] = None,
+               save: bool = False, out=None, workspace=None):
+    """One query token of each sequence, q [B, heads, head_dim] (bf16), against tokens 0 .. lens[b] - 1 of its cache: out
+    [B, heads, head_dim], or with save=True (out, lse [B, heads] fp32).  lens [B] int32 on the device; max_len, their bound,
+    should be tight (by default what the page table holds).  A sequence without tokens gets zeros and an lse of -inf."""
+    bf, dev = torch.bfloat16, _device()
+    c = cache.struct(dev)
+    B, pages, ld_table = _page_table(page_table, dev)
+    ld_q = _heads("q", q, B, None, c.head_dim, bf, dev)
+    H = q.shape[1]
+    _vector("lens", lens, B, (torch.int32,), dev)
+    if out is None:
+        out = torch.empty((B, H, c.head_dim), dtype=bf, device=q.device)
+    lse = torch.empty((B, H), dtype=torch.float32, device=q.device) if save else None
+    p = hstu.CacheAttnProblem(B, H, pages, c.head_dim ** -0.5 if scale is None else scale,
+                              pages * c.page_size if max_len is None else max_len, ld_table, ld_q,
+                              _heads("out", out, B, H, c.head_dim, bf, dev))
+    workspace = _scratch(workspace, hstu.mtgr_cache_attn_workspace_size(p, c), q)
+    hstu.mtgr_cache_attn(p, c, page_table, lens, q, out, lse, workspace, workspace.numel())
+    return (out, lse) if save else out

@@ -1,0 +1,275 @@
+"""Refusals of the entry points of include/mtgr_causal.h on the CPU (every bad argument is a status before any device call;
+pointers are fake addresses that nothing reads), the rotary frequencies, and the 64-bit definitions that the GPU tests
+compare with, against differences."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2505_18654_amd import hstu, ops
+from tests.causal_ref import causal, causal_back, rotate
+
+FAKE = 0x7f0000000000
+BIG = 1 << 40
+NULL, INVALID, UNSUPPORTED, SMALL = (hstu.MTGR_ERROR_NULL_POINTER, hstu.MTGR_ERROR_INVALID_ARGUMENT,
+                                     hstu.MTGR_ERROR_UNSUPPORTED, hstu.MTGR_ERROR_WORKSPACE_TOO_SMALL)
+INF, NAN = float("inf"), float("nan")
+
+
+def status_of(call, *args, **kw):
+    with pytest.raises(hstu.MtgrError) as e:
+        call(*args, **kw)
+    assert hstu.mtgr_last_error_message()
+    return e.value.status
+
+
+def test_struct_layouts():
+    for t, size, field, offset in ((hstu.RopeProblem, 56, "ld_x", 40), (hstu.CausalProblem, 72, "ld_q", 32),
+                                   (hstu.KvCachePages, 40, "keys", 24), (hstu.KvAppendProblem, 72, "ld_table", 32),
+                                   (hstu.CacheAttnProblem, 48, "max_len", 16)):
+        assert ctypes.sizeof(t) == size and getattr(t, field).offset == offset, t
+
+
+# ------------------------------------------------------------------ rotary positions
+
+def rope(**kw):
+    a = dict(x=FAKE, positions=FAKE, offsets=None, freqs=FAKE, out=FAKE, stream=0)
+    args = {n: kw.pop(n) for n in list(kw) if n in a}
+    a.update(args)
+    p = dict(num_tokens=10, num_seqs=2, heads=4, head_dim=64, rot_dim=64, layout=0, dtype=0, inverse=0, amplitude=1.0, ld_x=256,
+             ld_out=256)
+    p.update(kw)
+    hstu.mtgr_rope(hstu.RopeProblem(**p), **a)
+
+
+@pytest.mark.parametrize("kw, status", [
+    (dict(num_tokens=-1), INVALID), (dict(num_tokens=1 << 31), INVALID), (dict(num_seqs=-1), INVALID),
+    (dict(heads=0), INVALID), (dict(heads=65536), INVALID), (dict(head_dim=60), UNSUPPORTED), (dict(head_dim=0), UNSUPPORTED),
+    (dict(head_dim=1032), UNSUPPORTED), (dict(rot_dim=0), UNSUPPORTED), (dict(rot_dim=24), UNSUPPORTED),
+    (dict(rot_dim=80), UNSUPPORTED), (dict(rot_dim=-16), UNSUPPORTED), (dict(layout=2), INVALID), (dict(dtype=7), UNSUPPORTED),
+    (dict(amplitude=INF), INVALID), (dict(amplitude=NAN), INVALID), (dict(ld_x=255), INVALID), (dict(ld_x=260), INVALID),
+    (dict(ld_x=1 << 22), UNSUPPORTED), (dict(ld_out=128), INVALID), (dict(x=None), NULL), (dict(out=None), NULL),
+    (dict(x=FAKE + 8), INVALID), (dict(positions=None), NULL), (dict(offsets=FAKE), INVALID),
+    (dict(positions=FAKE + 2), INVALID), (dict(positions=None, offsets=FAKE + 1), INVALID), (dict(freqs=None), NULL),
+    (dict(freqs=FAKE + 4), INVALID),
+])
+def test_rope_refused(kw, status):
+    assert status_of(rope, **kw) == status
+
+
+def test_rope_of_nothing():
+    rope(num_tokens=0, x=None, out=None, positions=None)
+    rope(num_seqs=0, positions=None, offsets=FAKE)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rot_dim=8), dict(rot_dim=1040), dict(base=1.0), dict(base=INF), dict(base=NAN), dict(scaling=4), dict(scaling=-1),
+    dict(scaling=1, factor=0.5), dict(scaling=2, factor=INF), dict(scaling=3, factor=NAN), dict(scaling=3, factor=2.0),
+    dict(scaling=3, factor=2.0, trained_len=100, slow=-1.0), dict(scaling=3, factor=2.0, trained_len=100, slow=2.0, fast=2.0),
+    dict(scaling=3, factor=2.0, trained_len=100, fast=INF),
+])
+def test_frequencies_refused(kw):
+    a = dict(rot_dim=64, base=1e4)
+    a.update(kw)
+    assert status_of(hstu.mtgr_rope_frequencies, **a) in (INVALID, UNSUPPORTED)
+
+
+def test_frequencies():
+    r, base, s, L = 64, 10000.0, 8.0, 1024
+    plain = [base ** (-2 * i / r) for i in range(r // 2)]
+    near = lambda got, want: all(abs(g - w) <= 1e-14 * w for g, w in zip(got, want, strict=True))  # noqa: E731
+    f, a = hstu.mtgr_rope_frequencies(r, base)
+    assert near(f, plain) and a == 1.0
+    f, a = hstu.mtgr_rope_frequencies(r, base, hstu.MTGR_ROPE_LINEAR, s)
+    assert near(f, [x / s for x in plain]) and a == 1.0
+    f, a = hstu.mtgr_rope_frequencies(r, base, hstu.MTGR_ROPE_BASE, s)
+    assert f[0] == 1.0 and abs(f[-1] * s / plain[-1] - 1) < 1e-12 and a == 1.0
+    f, a = hstu.mtgr_rope_frequencies(r, base, hstu.MTGR_ROPE_PARTS, s, L, 1.0, 32.0)
+    for got, x in zip(f, plain):
+        turns = L * x / (2 * math.pi)
+        keep = 0.0 if turns <= 1 else 1.0 if turns >= 32 else (turns - 1) / 31
+        assert abs(got - x * (keep + (1 - keep) / s)) <= 1e-13 * x
+    assert abs(a - (0.1 * math.log(s) + 1)) < 1e-7 and f[0] == plain[0] and abs(f[-1] * s / plain[-1] - 1) < 1e-12
+    assert ops.rotary(16, device="cpu").freqs.dtype == torch.float64
+    with pytest.raises(ValueError):
+        ops.rotary(16, scaling="longer", device="cpu")
+
+
+# ------------------------------------------------------------------ causal attention
+
+def causal_problem(**kw):
+    p = dict(num_seqs=3, heads=4, kv_heads=2, head_dim=64, total_tokens=100, scale=0.125, reserved=0, ld_q=256, ld_k=128,
+             ld_v=128, ld_o=256, ld_do=256)
+    p.update(kw)
+    return hstu.CausalProblem(**p)
+
+
+FWD = dict(offsets=FAKE, q=FAKE, k=FAKE, v=FAKE, out=FAKE, lse=FAKE, workspace=FAKE, workspace_bytes=BIG, stream=0)
+BWD = dict(FWD, dout=FAKE, dq=FAKE, dk=FAKE, dv=FAKE)
+
+
+def split(base, kw):
+    a = {n: kw.get(n, v) for n, v in base.items()}
+    return {n: v for n, v in kw.items() if n not in base}, a
+
+
+def causal_fwd(**kw):
+    p, a = split(FWD, kw)
+    hstu.mtgr_causal_attn_fwd(causal_problem(**p), **a)
+
+
+def causal_bwd(**kw):
+    p, a = split(BWD, kw)
+    hstu.mtgr_causal_attn_bwd(causal_problem(**p), **a)
+
+
+@pytest.mark.parametrize("call", [causal_fwd, causal_bwd])
+@pytest.mark.parametrize("kw, status", [
+    (dict(num_seqs=-1), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID), (dict(kv_heads=3), INVALID),
+    (dict(kv_heads=8), INVALID), (dict(head_dim=96), UNSUPPORTED), (dict(head_dim=16), UNSUPPORTED),
+    (dict(head_dim=256), UNSUPPORTED), (dict(total_tokens=-1), INVALID), (dict(total_tokens=1 << 31), INVALID),
+    (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID),
+    (dict(scale=3e38), INVALID), (dict(reserved=1), INVALID), (dict(num_seqs=2 ** 31 - 1), UNSUPPORTED),
+    (dict(ld_q=255), INVALID), (dict(ld_q=260), INVALID), (dict(ld_k=127), INVALID), (dict(ld_v=1 << 22), UNSUPPORTED),
+    (dict(ld_o=248), INVALID), (dict(offsets=None), NULL), (dict(offsets=FAKE + 2), INVALID), (dict(q=None), NULL),
+    (dict(k=None), NULL), (dict(v=FAKE + 2), INVALID), (dict(out=None), NULL), (dict(lse=FAKE + 2), INVALID),
+])
+def test_causal_refused(call, kw, status):
+    assert status_of(call, **kw) == status
+
+
+@pytest.mark.parametrize("kw, status", [
+    (dict(lse=None), NULL), (dict(dout=None), NULL), (dict(ld_do=128), INVALID), (dict(dq=None), NULL), (dict(dk=None), NULL),
+    (dict(dv=FAKE + 8), INVALID), (dict(workspace=None), NULL), (dict(workspace=FAKE + 64), INVALID),
+    (dict(workspace_bytes=1599), SMALL),
+])
+def test_causal_backward_refused(kw, status):
+    assert status_of(causal_bwd, **kw) == status
+
+
+def test_causal_of_nothing():
+    for call in (causal_fwd, causal_bwd):
+        call(total_tokens=0, q=None, k=None, v=None, out=None, offsets=None)
+        call(num_seqs=0, q=None, offsets=None)
+
+
+# ------------------------------------------------------------------ paged cache
+
+def pages(**kw):
+    c = dict(num_pages=9, page_size=32, kv_heads=2, head_dim=64, reserved=0, keys=FAKE, values=FAKE)
+    c.update(kw)
+    return hstu.KvCachePages(**c)
+
+
+APPEND = dict(page_table=FAKE, past=FAKE, offsets=FAKE, q=FAKE, k=FAKE, v=FAKE, freqs=FAKE, q_out=FAKE, stream=0)
+
+
+def append(cache=None, **kw):
+    p, a = split(APPEND, kw)
+    base = dict(num_tokens=10, num_seqs=3, heads=4, max_pages=5, rot_dim=64, layout=0, amplitude=1.0, ld_table=5, ld_q=256,
+                ld_q_out=256, ld_k=128, ld_v=128)
+    base.update(p)
+    hstu.mtgr_kv_append(hstu.KvAppendProblem(**base), cache or pages(), **a)
+
+
+BAD_CACHE = [(dict(num_pages=0), INVALID), (dict(num_pages=1 << 31), INVALID), (dict(page_size=8), UNSUPPORTED),
+             (dict(page_size=48), UNSUPPORTED), (dict(page_size=8192), UNSUPPORTED), (dict(page_size=-32), UNSUPPORTED),
+             (dict(kv_heads=0), INVALID), (dict(reserved=1), INVALID), (dict(keys=None), NULL), (dict(values=None), NULL),
+             (dict(values=FAKE + 8), INVALID)]
+
+
+@pytest.mark.parametrize("kw, status", BAD_CACHE + [(dict(head_dim=60), UNSUPPORTED), (dict(head_dim=1032), UNSUPPORTED)])
+def test_append_cache_refused(kw, status):
+    assert status_of(append, cache=pages(**kw)) == status
+
+
+@pytest.mark.parametrize("kw, status", [
+    (dict(num_tokens=-1), INVALID), (dict(num_tokens=1 << 31), INVALID), (dict(num_seqs=-1), INVALID), (dict(heads=-1), INVALID),
+    (dict(max_pages=0), INVALID), (dict(rot_dim=24), UNSUPPORTED), (dict(rot_dim=80), UNSUPPORTED), (dict(layout=5), INVALID),
+    (dict(amplitude=NAN), INVALID), (dict(ld_table=4), INVALID), (dict(ld_q=252), INVALID), (dict(ld_q_out=1 << 22), UNSUPPORTED),
+    (dict(ld_k=64), INVALID), (dict(ld_v=132), INVALID), (dict(offsets=None), INVALID), (dict(offsets=FAKE + 2), INVALID),
+    (dict(page_table=None), NULL), (dict(past=None), NULL), (dict(past=FAKE + 1), INVALID), (dict(k=None), NULL),
+    (dict(v=None), NULL), (dict(q=None), NULL), (dict(q_out=None), NULL), (dict(heads=0), INVALID), (dict(freqs=None), NULL),
+])
+def test_append_refused(kw, status):
+    assert status_of(append, **kw) == status
+
+
+def test_append_of_nothing():
+    append(num_tokens=0, page_table=None)
+    append(num_seqs=0, page_table=None)
+
+
+def cache_attn(cache=None, **kw):
+    p, a = split(dict(page_table=FAKE, lens=FAKE, q=FAKE, out=FAKE, lse=FAKE, workspace=FAKE, workspace_bytes=BIG, stream=0), kw)
+    base = dict(num_seqs=3, heads=4, max_pages=5, scale=0.125, max_len=160, ld_table=5, ld_q=256, ld_o=256)
+    base.update(p)
+    hstu.mtgr_cache_attn(hstu.CacheAttnProblem(**base), cache or pages(), **a)
+
+
+@pytest.mark.parametrize("kw, status", BAD_CACHE + [(dict(head_dim=96), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED)])
+def test_cache_attn_cache_refused(kw, status):
+    assert status_of(cache_attn, cache=pages(**kw)) == status
+
+
+@pytest.mark.parametrize("kw, status", [
+    (dict(num_seqs=-1), INVALID), (dict(num_seqs=65536), INVALID), (dict(heads=0), INVALID), (dict(heads=3), INVALID),
+    (dict(max_pages=0), INVALID), (dict(scale=0.0), INVALID), (dict(scale=NAN), INVALID), (dict(max_len=-1), INVALID),
+    (dict(max_len=161), INVALID), (dict(max_pages=1 << 30, ld_table=1 << 30, max_len=1 << 31), INVALID), (dict(ld_table=4), INVALID),
+    (dict(ld_q=128), INVALID), (dict(ld_o=252), INVALID), (dict(page_table=None), NULL), (dict(page_table=FAKE + 2), INVALID),
+    (dict(lens=None), NULL), (dict(q=None), NULL), (dict(out=FAKE + 2), INVALID), (dict(lse=FAKE + 2), INVALID),
+    (dict(workspace=None, max_pages=5000, ld_table=5000, max_len=150000), NULL),
+    (dict(workspace_bytes=256, max_pages=5000, ld_table=5000, max_len=150000), SMALL),
+    (dict(workspace=FAKE + 16, max_pages=5000, ld_table=5000, max_len=150000), INVALID),
+])
+def test_cache_attn_refused(kw, status):
+    assert status_of(cache_attn, **kw) == status
+
+
+def test_cache_attn_of_nothing():
+    cache_attn(num_seqs=0, page_table=None, q=None)
+
+
+# ------------------------------------------------------------------ the definitions
+
+def random(*shape, seed=1):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+
+
+def test_gradients_of_the_definition():
+    """causal_back against autograd and against central differences of causal."""
+    lengths, H, Hk, dh, scale = [5, 1, 0, 7], 4, 2, 8, 0.4
+    T = sum(lengths)
+    q, k, v, g = random(T, H, dh), random(T, Hk, dh, seed=2), random(T, Hk, dh, seed=3), random(T, H, dh, seed=4)
+    out, lse = causal(q, k, v, lengths, scale)[:2]
+    grads = causal_back(g, q, k, v, out, lse, lengths, scale)
+    for i, (name, t) in enumerate((("dq", q), ("dk", k), ("dv", v))):
+        d = random(*t.shape, seed=7 + i)
+        h = 1e-6
+        up, down = ([x + s * h * d if x is t else x for x in (q, k, v)] for s in (1, -1))
+        slope = ((causal(*up, lengths, scale)[0] - causal(*down, lengths, scale)[0]) * g).sum() / (2 * h)
+        assert abs(slope - (grads[name][0] * d).sum()) < 1e-7 * (grads[name][0].abs() * d.abs()).sum()
+    a = 0
+    for n in lengths:
+        if n == 0:
+            continue
+        x = [t[a:a + n].clone().requires_grad_() for t in (q, k, v)]
+        kk, vv = (t.repeat_interleave(H // Hk, 1) for t in x[1:])
+        z = torch.einsum("ihd,jhd->hij", x[0], kk) * scale
+        p = torch.softmax(z.masked_fill(torch.ones(n, n, dtype=torch.bool).triu(1), -INF), -1)
+        (torch.einsum("hij,jhd->ihd", p, vv) * g[a:a + n]).sum().backward()
+        for t, name in zip(x, ("dq", "dk", "dv")):
+            assert torch.allclose(t.grad, grads[name][0][a:a + n], atol=1e-12)
+        a += n
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rotation_of_the_definition(layout):
+    """Scores of rotated queries and keys depend on the distance alone, lengths are kept, and turning back undoes it."""
+    f = torch.tensor(hstu.mtgr_rope_frequencies(16, 100.0)[0], dtype=torch.float64)
+    x, y = random(1, 1, 24, seed=5), random(1, 1, 24, seed=6)
+    at = lambda t, p: rotate(t, f, torch.tensor([p]), 1.0, layout)[0]  # noqa: E731
+    assert torch.allclose((at(x, 9) * at(y, 4)).sum(), (at(x, 105) * at(y, 100)).sum())
+    assert torch.allclose(at(x, 77).norm(), x.norm()) and torch.allclose(at(at(x, 31), -31), x)
+    assert torch.equal(at(x, 5)[..., 16:], x[..., 16:])

@@ -1,0 +1,187 @@
+"""Causal attention of packed sequences against its 64-bit definition, element by element (bounds: tests/causal_ref.py)."""
+import pytest
+import torch
+
+from paper_2505_18654_amd import ops
+from tests.block_ref import half_step, within
+from tests.causal_ref import causal, causal_back, heads, offsets_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def batch(lengths, H, Hk, dh, seed=1, wide=0, more=0, size=1.0):
+    T = sum(lengths) + more
+    return (heads((T, H, dh), seed, size, wide), heads((T, Hk, dh), seed + 1, size, wide), heads((T, Hk, dh), seed + 2, 1.0, wide),
+            heads((T, H, dh), seed + 3, 1.0, wide))
+
+
+def check(lengths, H, Hk, dh, wide=0, more=0, scale=None, size=1.0, seed=1):
+    print(f"[causal] lengths={lengths[:8]}.. {len(lengths)} H={H} Hk={Hk} dh={dh} wide={wide} more={more}", flush=True)
+    q, k, v, dout = batch(lengths, H, Hk, dh, seed, wide, more, size)
+    o, n, s = offsets_of(lengths), sum(lengths), dh ** -0.5 if scale is None else scale
+    out, lse = ops.causal_attn_fwd(q, k, v, o, scale=scale, save=True)
+    torch.cuda.synchronize()
+    want, wl, eo, el = causal(q[:n], k[:n], v[:n], lengths, s)
+    within("out", out[:n], want, half_step(out[:n]) + eo * (1 + 2.0 ** -7))
+    within("lse", lse[:, :n], wl, el)
+    assert torch.equal(ops.causal_attn_fwd(q, k, v, o, scale=scale)[:n], out[:n])
+    print("[causal] backward", flush=True)
+    got = dict(zip(("dq", "dk", "dv"), ops.causal_attn_bwd(dout, q, k, v, out, lse, o, scale=scale)))
+    torch.cuda.synchronize()
+    for x, (g, b) in causal_back(dout[:n], q[:n], k[:n], v[:n], out[:n], lse[:, :n], lengths, s).items():
+        within(x, got[x][:n], g, half_step(got[x][:n]) + b * (1 + 2.0 ** -7))
+    for x, (g, b) in causal_back(dout[:n], q[:n], k[:n], v[:n], want, wl, lengths, s, exact_out=True).items():
+        within(x + " of the definition", got[x][:n], g, half_step(got[x][:n]) + b * (1 + 2.0 ** -7))
+    again = ops.causal_attn_bwd(dout, q, k, v, out, lse, o, scale=scale)
+    assert all(torch.equal(a[:n], got[x][:n]) for a, x in zip(again, got))      # the same order of sums each time
+
+
+LENGTHS = [[1], [2], [31], [32], [33], [63, 64, 65], [127, 128, 129], [1, 1, 1, 0, 5, 0], [300, 1, 77], [513]]
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+def test_lengths(lengths, dh):
+    check(lengths, 2, 1, dh)
+
+
+@pytest.mark.parametrize("H, Hk, dh", [(1, 1, 128), (4, 4, 64), (6, 2, 128), (3, 3, 32), (8, 1, 64), (24, 8, 32), (10, 2, 128)])
+def test_head_layouts(H, Hk, dh):
+    check([150, 40], H, Hk, dh)
+
+
+def test_columns_of_a_projection_and_rows_behind():
+    check([100, 31, 200], 4, 2, 64, wide=3, more=37)
+    check([257], 2, 2, 128, wide=1, more=1)
+
+
+def test_long():
+    check([3001, 2], 2, 1, 128)
+    check([5000], 1, 1, 64)
+
+
+def test_many_sequences():
+    check([3, 1, 0, 7, 2] * 40, 2, 1, 32)
+    check([1, 0, 2] * 1700, 1, 1, 32)                    # the search for a tile's sequence takes three steps
+
+
+@pytest.mark.parametrize("size, scale", [(1.0, 0.5), (4.0, 0.3), (0.0, 1.0), (1.0, 1e-30)])
+def test_scales(size, scale):
+    check([130, 5], 2, 1, 64, scale=scale, size=size)
+
+
+def test_falling_and_rising_scores():
+    """Keys whose scores grow or shrink along the sequence, so that the running maximum moves at every tile or never."""
+    for up in (True, False):
+        n, dh = 700, 64
+        q, k, v, _ = batch([n], 1, 1, dh)
+        ramp = torch.linspace(0, 40, n).cuda()
+        q = torch.zeros_like(q)
+        q[..., 0] = 8.0
+        k[..., 0] = (ramp if up else ramp.flip(0))[:, None].bfloat16()
+        o = offsets_of([n])
+        out, lse = ops.causal_attn_fwd(q, k, v, o, save=True)
+        want, wl, eo, el = causal(q, k, v, [n], dh ** -0.5)
+        within("out", out, want, half_step(out) + eo * (1 + 2.0 ** -7))
+        within("lse", lse, wl, el)
+
+
+def test_rows_behind_are_left():
+    lengths = [40, 0, 90]
+    q, k, v, dout = batch(lengths, 2, 1, 64, more=50)
+    n, o = sum(lengths), offsets_of(lengths)
+    for t in (q, k, v, dout):
+        t[n:] = float("nan")
+    out, lse = torch.full_like(q, 7.0), torch.full((2, n + 50), 7.0, device="cuda")
+    ops.causal_attn_fwd(q, k, v, o, save=True, out=out, lse=lse)
+    assert (out[n:] == 7).all() and (lse[:, n:] == 7).all() and torch.isfinite(out.float()).all()
+    grads = [torch.full_like(t, 7.0) for t in (q, k, v)]
+    ops.causal_attn_bwd(dout, q, k, v, out, lse, o, grads=grads)
+    assert all((g[n:] == 7).all() and torch.isfinite(g.float()).all() for g in grads)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_other_sequences_do_not_matter(bad):
+    lengths = [70, 33, 129]
+    q, k, v, dout = batch(lengths, 2, 1, 64)
+    o = offsets_of(lengths)
+    out, lse = ops.causal_attn_fwd(q, k, v, o, save=True)
+    grads = ops.causal_attn_bwd(dout, q, k, v, out, lse, o)
+    q2, k2, v2, g2 = (t.clone() for t in (q, k, v, dout))
+    for t in (q2, k2, v2, g2):
+        t[70:103] = bad
+    out2, lse2 = ops.causal_attn_fwd(q2, k2, v2, o, save=True)
+    grads2 = ops.causal_attn_bwd(g2, q2, k2, v2, out2, lse2, o)
+    for a, b in [(out, out2), *zip(grads, grads2)]:
+        assert torch.equal(a[:70], b[:70]) and torch.equal(a[103:], b[103:])
+    assert torch.equal(lse[:, :70], lse2[:, :70]) and torch.equal(lse[:, 103:], lse2[:, 103:])
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("n, at", [(1, 0), (90, 89), (200, 150), (300, 64), (129, 128), (128, 127)])
+def test_later_tokens_do_not_matter(n, at, dh):
+    """Infinities and NaN in the keys and values of a token reach its own and later outputs alone."""
+    q, k, v, _ = batch([n], 2, 1, dh)
+    o = offsets_of([n])
+    lse = ops.causal_attn_fwd(q, k, v, o, save=True)[1]
+    want, _, eo, _ = causal(q, k, v, [n], dh ** -0.5)
+    for t, bad in ((v, float("nan")), (v, float("inf")), (k, float("nan"))):
+        keep = t[at].clone()
+        t[at, :, 5] = bad
+        out2, lse2 = ops.causal_attn_fwd(q, k, v, o, save=True)
+        t[at] = keep
+        assert torch.isfinite(out2[:at].float()).all()
+        within("before", out2[:at], want[:at], half_step(out2[:at]) + eo[:at] * (1 + 2.0 ** -7))
+        assert torch.equal(lse2[:, :at], lse[:, :at])
+        if t is v:
+            assert not torch.isfinite(out2[at:, :, 5].float()).any()
+            rest = [c for c in range(dh) if c != 5]
+            assert torch.isfinite(out2[at:][..., rest].float()).all()
+        else:
+            assert torch.isnan(out2[at:].float()).all()
+
+
+def test_nothing():
+    q, k, v, dout = batch([], 2, 1, 64)
+    out, lse = ops.causal_attn_fwd(q, k, v, offsets_of([]), save=True)
+    assert out.shape == (0, 2, 64) and lse.shape == (2, 0)
+    assert [g.shape[0] for g in ops.causal_attn_bwd(dout, q, k, v, out, lse, offsets_of([0, 0]))] == [0, 0, 0]
+    q, k, v, _ = batch([5], 2, 1, 64)
+    out = torch.full_like(q, 3.0)
+    ops.causal_attn_fwd(q, k, v, offsets_of([0, 0]), out=out)
+    assert (out == 3).all()
+
+
+def test_streams_and_graph():
+    lengths = [100, 31]
+    q, k, v, dout = batch(lengths, 4, 2, 64)
+    o = offsets_of(lengths)
+
+    def step(out, lse, grads, ws):
+        ops.causal_attn_fwd(q, k, v, o, save=True, out=out, lse=lse)
+        ops.causal_attn_bwd(dout, q, k, v, out, lse, o, grads=grads, workspace=ws)
+
+    out, lse = torch.zeros_like(q), torch.zeros(4, 131, device="cuda")
+    grads, ws = [torch.zeros_like(t) for t in (q, k, v)], ops.causal_attn_workspace(q, k, o, backward=True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(out, lse, grads, ws)
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(out, lse, grads, ws)
+    for i in range(3):
+        q.copy_(heads(q.shape, 50 + i))
+        ws.fill_(255)                                    # a workspace may hold anything
+        g.replay()
+        torch.cuda.synchronize()
+        o2, l2 = ops.causal_attn_fwd(q, k, v, o, save=True)
+        g2 = ops.causal_attn_bwd(dout, q, k, v, o2, l2, o)
+        assert torch.equal(out, o2) and torch.equal(lse, l2) and all(torch.equal(a, b) for a, b in zip(grads, g2))
