@@ -83,13 +83,23 @@ mtgr_status_t check_causal(const mtgr_causal_problem_t* p) {
     CHECK(check_tokens(p->total_tokens, "total_tokens"));
     CHECK(check_attn(p->heads, p->kv_heads, p->head_dim, p->scale));
     if ((p->total_tokens / 128 + p->num_seqs) * p->heads >= (1ll << 31) ||
-        p->total_tokens * p->heads * (p->head_dim / 8) >= (1ll << 39))
+        p->total_tokens * p->heads >= (1ll << 35))
         return fail(MTGR_ERROR_UNSUPPORTED, "problem too large for one launch");
     return MTGR_SUCCESS;
 }
 
+long long causal_slots(const mtgr_causal_problem_t* p) { return p->total_tokens / 128 + p->num_seqs; }
+
+// The backward's workspace: - lse / ln 2 and - delta, then the plan with its sums.
+size_t rows_bytes(const mtgr_causal_problem_t* p) { return align256((size_t)p->heads * (size_t)p->total_tokens * 4); }
+
+mtgr::CausalPlan plan_of(const mtgr_causal_problem_t* p) {
+    return mtgr::causal_plan(p->total_tokens, p->num_seqs, p->heads, p->kv_heads, p->head_dim);
+}
+
 size_t causal_workspace(const mtgr_causal_problem_t* p, bool backward) {
-    return backward ? align256((size_t)p->heads * (size_t)p->total_tokens * 4) : 0;      // delta
+    if (!backward || p->total_tokens == 0 || p->num_seqs == 0) return 0;
+    return 2 * rows_bytes(p) + plan_of(p).bytes;
 }
 
 mtgr::CausalArgs causal_args(const mtgr_causal_problem_t* p, const int32_t* offsets, const void* q, const void* k, const void* v) {
@@ -99,7 +109,7 @@ mtgr::CausalArgs causal_args(const mtgr_causal_problem_t* p, const int32_t* offs
     a.Hk = p->kv_heads;
     a.group = p->heads / p->kv_heads;
     a.T = p->total_tokens;
-    a.slots = (int)(p->total_tokens / 128 + p->num_seqs);
+    a.slots = (int)causal_slots(p);
     a.scale = p->scale;
     a.c = p->scale * 1.4426950408889634f;
     a.offsets = offsets;
@@ -289,14 +299,19 @@ mtgr_status_t mtgr_causal_attn_bwd(const mtgr_causal_problem_t* p, const int32_t
     a.out = (void*)out;
     a.lse = (float*)lse;
     a.dout = dout;
-    a.delta = (const float*)workspace;
     a.dq = dq;
     a.dk = dk;
     a.dv = dv;
+    char* ws = (char*)workspace;
+    a.rows_l = (float*)ws;
+    a.rows_d = (float*)(ws + rows_bytes(p));
+    ws += 2 * rows_bytes(p);
+    const mtgr::CausalPlan plan = plan_of(p);
+    mtgr::CausalItem *items = (mtgr::CausalItem*)ws, *joins = (mtgr::CausalItem*)(ws + plan.joins_ofs);
     const hipStream_t s = (hipStream_t)stream;
-    hipError_t e = mtgr::launch_causal_delta(a, p->head_dim, (float*)workspace, s);
-    if (e == hipSuccess) e = mtgr::launch_causal_dkdv(a, p->head_dim, s);
+    hipError_t e = mtgr::launch_causal_plan(a, plan, items, joins, s);
     if (e == hipSuccess) e = mtgr::launch_causal_dq(a, p->head_dim, s);
+    if (e == hipSuccess) e = mtgr::launch_causal_dkdv(a, plan, items, joins, (float*)(ws + plan.parts_ofs), p->head_dim, s);
     if (e != hipSuccess) return device_fail(e, "causal attention backward");
     return ok();
 }

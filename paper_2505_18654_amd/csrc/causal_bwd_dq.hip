@@ -1,6 +1,11 @@
-// dQ of the causal softmax attention: dQ = scale dS K with dS = P (dP - delta) recomputed.  As the forward, a workgroup
-// takes 128 query rows of one (sequence, head), 32 per wave, over the 64-key tiles up to its last row; a lane holds one
-// query's scores, so its lse and delta are one value each.
+// dQ of the causal softmax attention: dQ = scale dS K with dS = P (dP - delta) recomputed, delta = sum_d dO O.
+//
+// As the forward, a workgroup takes 128 query rows of one (sequence, head), 32 per wave, over the 64-key tiles up to its last
+// row; a lane holds one query's scores, so its lse and delta are one value each.  It forms delta from the rows of dO that it
+// holds anyway and leaves it, and the lse in units of log 2, both negative, for the dK / dV kernel behind it: a kernel of
+// its own read dO and O once more (50 us for 68,000 tokens, 8 heads of 128).
+#include <type_traits>
+
 #include "causal_device.h"
 
 namespace mtgr {
@@ -12,6 +17,7 @@ constexpr int BN = 64;
 template <int DH>
 __global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a) {
     constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, TILE = BN * DH;
+    constexpr int NM = 2 * KSTEPS + 2 * DBLK, PF = 3;            // products of a step; how far ahead operands are read
     __shared__ __align__(16) uint16_t sKV[4][TILE];              // K 0, K 1, V 0, V 1
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, hh = lane >> 5;
@@ -21,64 +27,140 @@ __global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a) {
     const int h = hk * a.group + id % a.group;
     const Tile at = tile_of_slot(a.offsets, a.B, a.T, a.slots - 1 - id / a.group);
     const int q0 = at.tile * BM, n = at.n;
-    if (at.tile < 0 || q0 >= n) return;
+    if (at.tile < 0) return;
     const uint16_t* Kb = (const uint16_t*)a.k + (long long)at.o * a.ld_k;
     const uint16_t* Vb = (const uint16_t*)a.v + (long long)at.o * a.ld_v;
     const int qw = q0 + 32 * w, qr = min(qw + col, n - 1);
+    const int nh = qw < n ? qw / 32 + 1 : 0;                     // halves that this wave's rows see, the last on the diagonal
+    const int ntk = (min(q0 + BM, n) + BN - 1) / BN;
+    auto issue_k = [&](int t, int buf) { tile_dma<DH>(sKV[buf], Kb, a.ld_k, t * BN, n, hk * DH, tid); };
+    auto issue_v = [&](int t, int buf) { tile_dma<DH>(sKV[2 + buf], Vb, a.ld_v, t * BN, n, hk * DH, tid); };
+    issue_k(0, 0);
+    issue_v(0, 0);
+    if (ntk > 1) issue_v(1, 1);
     bf16x8 qreg[KSTEPS], greg[KSTEPS];
+    float nl, nd;                                                // - lse / ln 2 and - delta of the lane's query
     {
         const uint16_t* Q = (const uint16_t*)a.q + (long long)(at.o + qr) * a.ld_q + h * DH + 8 * hh;
         const uint16_t* G = (const uint16_t*)a.dout + (long long)(at.o + qr) * a.ld_do + h * DH + 8 * hh;
+        const uint16_t* O = (const uint16_t*)a.out + (long long)(at.o + qr) * a.ld_o + h * DH + 8 * hh;
+        nl = a.lse[h * a.T + at.o + qr] * NEG_LOG2E;
+        float d = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KSTEPS; kk++) {
             qreg[kk] = as_bf16x8(*(const uint4*)(Q + 16 * kk));
-            greg[kk] = as_bf16x8(*(const uint4*)(G + 16 * kk));
+            const uint4 g = *(const uint4*)(G + 16 * kk), o = *(const uint4*)(O + 16 * kk);
+            greg[kk] = as_bf16x8(g);
+            const uint32_t gw[4] = {g.x, g.y, g.z, g.w}, ow[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                d = __builtin_fmaf(__uint_as_float(gw[i] << 16), __uint_as_float(ow[i] << 16), d);
+                d = __builtin_fmaf(__uint_as_float(gw[i] & 0xffff0000u), __uint_as_float(ow[i] & 0xffff0000u), d);
+            }
+        }
+        nd = -sum_halves(d);
+        if (hh == 0 && qw + col < n) {
+            a.rows_l[h * a.T + at.o + qr] = nl;
+            a.rows_d[h * a.T + at.o + qr] = nd;
         }
     }
-    const float lse = a.lse[h * a.T + at.o + qr] * NEG_LOG2E, delta = a.delta[h * a.T + at.o + qr];
     floatx16 dq[DBLK];
 #pragma unroll
     for (int d = 0; d < DBLK; d++) dq[d] = floatx16{};
-    const int ntk = (min(q0 + BM, n) + BN - 1) / BN;
-    auto issue = [&](int t, int buf) {
-        tile_dma<DH>(sKV[buf], Kb, a.ld_k, t * BN, n, hk * DH, tid);
-        tile_dma<DH>(sKV[2 + buf], Vb, a.ld_v, t * BN, n, hk * DH, tid);
+    const uint32_t kofs0 = tile_ofs<CPR>(col, hh);
+    uint32_t tofs0, tofs1;
+    tile_ofs_tr<CPR>(0, lane, tofs0, tofs1);
+    constexpr uint32_t ROW16 = 16u * CPR * 16u;                  // bytes of 16 tile rows
+
+    auto mask = [&](floatx16& s) {                               // on the diagonal: element e is key 8 (e / 4) + 4 hh + e % 4
+#pragma unroll
+        for (int e = 0; e < 16; e++) s[e] = 8 * (e >> 2) + 4 * hh + (e & 3) > col ? neg_inf() : s[e];
     };
-    wait_vmcnt_seen<0>();
-    issue(0, 0);
-    for (int t = 0; t < ntk; t++) {
-        wait_vmem();
-        lds_barrier();
-        if (t + 1 < ntk) issue(t + 1, (t + 1) & 1);
-        const uint16_t* sK = sKV[t & 1];
-        const uint16_t* sV = sKV[2 + (t & 1)];
+    // A step: dS and its product with K for half HC of the tile in buffer KB, whose scores and dP - delta are s and p; beside
+    // them those of the next half, half HN of the tile in buffers NB, product by product between the elements' arithmetic.
+    auto step = [&](auto kb_tag, auto hc_tag, auto nb_tag, auto hn_tag, const floatx16& s, const floatx16& p, floatx16& sn,
+                    floatx16& pn, int j) {
+        constexpr int KB = decltype(kb_tag)::value, HC = decltype(hc_tag)::value, NB = decltype(nb_tag)::value,
+                      HN = decltype(hn_tag)::value;
+        // (the transposed reads' offsets afresh in each step: kept in registers, at 256 of them, one fragment of Q spilled,
+        // whose reload waits for the copies under way)
+        uint32_t t0 = tofs0, t1 = tofs1;
+        if constexpr (DH == 128) asm volatile("" : "+v"(t0), "+v"(t1));
+        auto operand = [&](int i) {
+            if (i < 2 * KSTEPS) return lds_read16(sKV[NB + 2 * (i & 1)], (kofs0 ^ (32u * (i >> 1))) + 2 * HN * ROW16);
+            const uint32_t d = (i - 2 * KSTEPS) % DBLK, kq = (i - 2 * KSTEPS) / DBLK;
+            return lds_read_tr(sKV[KB], (t0 ^ (64u * d)) + (2 * HC + kq) * ROW16, (t1 ^ (64u * d)) + (2 * HC + kq) * ROW16);
+        };
+        bf16x8 op[NM];
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            const int k0 = t * BN + 32 * half;
-            if (k0 > qw) continue;
-            floatx16 s{}, dp{};
-#pragma unroll
-            for (int kk = 0; kk < KSTEPS; kk++) {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sK, 32 * half + col, 2 * kk + hh), qreg[kk], s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sV, 32 * half + col, 2 * kk + hh), greg[kk], dp, 0, 0, 0);
+        for (int i = 0; i < PF; i++) op[i] = operand(i);
+        uint32_t pk[8];
+        float ds[16];
+        auto element = [&](int e) {
+            ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, nl)) * p[e];
+            if (e & 1) {
+                pk[e >> 1] = pack_bf16x2(ds[e - 1], ds[e]);
+                asm volatile("" : "+v"(pk[e >> 1]));
             }
-            float ds[16];
+        };
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, lse)) * (dp[e] - delta);
-                if (k0 == qw && 8 * (e >> 2) + 4 * hh + (e & 3) > col) ds[e] = 0.f;
+        for (int i = 0; i < NM; i++) {
+            if (i + PF < NM) op[i + PF] = operand(i + PF);
+            if (i < 2 * KSTEPS) {
+                const int kk = i >> 1;
+                if ((i & 1) == 0) {
+                    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i], qreg[kk], kk == 0 ? floatx16{} : sn, 0, 0, 0);
+                } else {
+                    if (kk == 0) {
+#pragma unroll
+                        for (int e = 0; e < 16; e++) pn[e] = nd;
+                    }
+                    pn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i], greg[kk], pn, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 16 * i / (2 * KSTEPS); e < 16 * (i + 1) / (2 * KSTEPS); e++) element(e);
+            } else {
+                const int d = (i - 2 * KSTEPS) % DBLK, kq = (i - 2 * KSTEPS) / DBLK;
+                const bf16x8 b = as_bf16x8(make_uint4(pk[4 * kq], pk[4 * kq + 1], pk[4 * kq + 2], pk[4 * kq + 3]));
+                dq[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i], b, dq[d], 0, 0, 0);
             }
-#pragma unroll
-            for (int kq = 0; kq < 2; kq++) {
-                const float* x = ds + 8 * kq;
-                const bf16x8 db = as_bf16x8(make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                                                       pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])));
-#pragma unroll
-                for (int d = 0; d < DBLK; d++)
-                    dq[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        tile_read_tr<CPR>(sK, 32 * half + 16 * kq, 32 * d, lane), db, dq[d], 0, 0, 0);
-            }
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if (j + 2 == nh) mask(sn);
+    };
+    using C0 = std::integral_constant<int, 0>;
+    using C1 = std::integral_constant<int, 1>;
+
+    floatx16 sA{}, pA, sB, pB;                                   // of the tile's halves 0 and 1
+#pragma unroll
+    for (int e = 0; e < 16; e++) pA[e] = nd;
+    wait_vmcnt_seen<0>();
+    lds_barrier();
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk++) {
+        sA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(sKV[0], kofs0 ^ (32u * kk)), qreg[kk], sA, 0, 0, 0);
+        pA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(sKV[2], kofs0 ^ (32u * kk)), greg[kk], pA, 0, 0, 0);
+    }
+    if (nh == 1) mask(sA);
+    // Tile t in buffers P; its first half's scores are formed.  V(t + 1) is on its way or here.
+    auto tile = [&](auto par, int t) {
+        constexpr int P = decltype(par)::value;
+        using CP = std::integral_constant<int, P>;
+        using CQ = std::integral_constant<int, P ^ 1>;
+        const bool more = t + 1 < ntk;
+        if (t > 0) lds_barrier();                                // K(t - 1) is no longer read
+        if (more) issue_k(t + 1, P ^ 1);
+        if (2 * t < nh) step(CP{}, C0{}, CP{}, C1{}, sA, pA, sB, pB, 2 * t);
+        if (more) {
+            wait_vmem();                                         // K(t + 1), V(t + 1)
+            lds_barrier();                                       // everywhere, and V(t) is no longer read
+            if (t + 2 < ntk) issue_v(t + 2, P);
+        }
+        if (2 * t + 1 < nh) step(CP{}, C1{}, CQ{}, C0{}, sB, pB, sA, pA, 2 * t + 1);
+    };
+    for (int t = 0; t < ntk; t += 2) {
+        tile(C0{}, t);
+        if (t + 1 < ntk) tile(C1{}, t + 1);
     }
     __syncthreads();                                             // the tiles' LDS is reused below
     store_rows<DH>(dq, a.scale, sKV[0] + w * 32 * DH, (uint16_t*)a.dq + (long long)at.o * a.ld_q + h * DH, a.ld_q, qw, n, lane);

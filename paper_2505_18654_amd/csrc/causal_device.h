@@ -16,8 +16,18 @@ __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 // without a plan, and T / 128 + B slots hold every tile.  The search takes the first entries of 64 ranges at once, a range per
 // lane: two loads one after another for 4,096 sequences.  All lanes get the same result.
 struct Tile {
-    int o, n, tile;           // the sequence's first row and length, the tile inside it
+    int o, n, tile;           // the sequence's first row and length, the tile inside it; no tile: tile < 0
 };
+__device__ __forceinline__ Tile tile_at(const int* offsets, long long T, int b, int slot) {
+    // rows outside 0 .. T-1 are never touched, whatever the offsets hold
+    const int o = (int)min(max((long long)offsets[b], 0ll), T), e = (int)min((long long)offsets[b + 1], T);
+    Tile t;
+    t.o = o;
+    t.n = max(e - o, 0);
+    t.tile = slot - (offsets[b] >> 7) - b;
+    if (t.tile >= (t.n + BM - 1) / BM) t.tile = -1;
+    return t;
+}
 __device__ __forceinline__ Tile tile_of_slot(const int* offsets, int B, long long T, int slot) {
     const int lane = threadIdx.x & 63;
     int lo = 0, hi = B;
@@ -29,14 +39,7 @@ __device__ __forceinline__ Tile tile_of_slot(const int* offsets, int B, long lon
         lo = min(lo + k * step, hi - 1);
         hi = min(lo + step, hi);
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    // rows outside 0 .. T-1 are never touched, whatever the offsets hold
-    const int o = (int)min(max((long long)offsets[lo], 0ll), T), e = (int)min((long long)offsets[lo + 1], T);
-    Tile t;
-    t.o = o;
-    t.n = max(e - o, 0);
-    t.tile = slot - (offsets[lo] >> 7) - lo;
-    return t;
+    return tile_at(offsets, T, __builtin_amdgcn_readfirstlane(lo), slot);
 }
 
 // Larger (sum) of this lane's value and that of lane ^ 32, in both.
