@@ -396,6 +396,7 @@ mtgr_status_t mtgr_cache_attn(const mtgr_cache_attn_problem_t* p, const mtgr_kv_
     a.group = p->heads / cache->kv_heads;
     a.chunk = plan.chunk;
     a.splits = plan.splits;
+    a.waves = plan.waves;
     a.max_len = (int)p->max_len;
     a.scale = p->scale;
     a.c = p->scale * 1.4426950408889634f;

@@ -1,16 +1,18 @@
 // One query token of each sequence against its paged cache.
 //
 // A workgroup takes a chunk of a sequence's keys for one key head and up to 32 of the query heads that share it, a query
-// head per column of the 32 x 32 products; its 4 waves take the chunk's tiles of 32 keys in turn, each with its own
-// maximum, sum and outputs, and its own LDS tiles, so that no wave waits for another.  They are joined through LDS, and the chunks of
-// a sequence, where there are several, by a second kernel.  Bound by the read of the cache.
+// head per column of the 32 x 32 products; its waves take the chunk's tiles of 32 keys in turn, each with its own maximum,
+// sum and outputs, and its own LDS tiles, so that no wave waits for another.  A wave copies the next tile's keys while it
+// works on this one's probabilities, and the next values once this one's are used, so that half of its 32 DH bytes of LDS at least
+// are under way at any time.  The waves are joined through LDS, and the chunks of a sequence, where there are several, by a
+// second kernel.  Bound by the read of the cache.
 #include "causal_device.h"
 
 namespace mtgr {
 namespace {
 
 using namespace causal;
-constexpr int BN = 32, WAVES = 4, QT = 32;
+constexpr int BN = 32, QT = 32, CHUNKS = 512;
 
 // A wave's copy of 32 rows of a head's pages into a swizzled tile, page0 and page1 those of its halves (16 rows, the
 // smallest page).  Rows outside lo .. hi are copies of row lo or hi, so that every row of the tile is one of the sequence's own.
@@ -29,12 +31,12 @@ __device__ __forceinline__ void page_dma(uint16_t* tile, const uint16_t* base, l
     }
 }
 
-template <int DH>
-__global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
-    constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, TILE = BN * DH;
-    __shared__ __align__(16) uint16_t sT[WAVES][4][TILE];        // K 0, K 1, V 0, V 1 of each wave; then its outputs
+template <int DH, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(CacheAttnArgs a) {
+    constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, TILE = BN * DH, NI = CPR / 2;
+    __shared__ __align__(16) uint16_t sT[WAVES][2][TILE];        // K and V of each wave; then its outputs
     __shared__ float sML[WAVES][2][QT];
-    static_assert(4 * TILE * 2 >= QT * DH * 4, "a wave's outputs fit its tiles");
+    static_assert(2 * TILE * 2 >= QT * DH * 4, "a wave's outputs fit its tiles");
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, hh = lane >> 5;
     const int b = blockIdx.z, split = blockIdx.x;
@@ -49,39 +51,61 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
     const uint16_t* Kb = (const uint16_t*)cache.keys + head_ofs * DH;
     const uint16_t* Vb = (const uint16_t*)cache.values + head_ofs * DH;
     const int in_page = (1 << cache.page_shift) - 1;
+    // A tile: its first key, the pages of its halves (the same one where pages are larger) and the rows lo .. hi that have one.
+    struct Keys {
+        int k0, page0, page1, lo, hi;
+    };
+    // The wave's next tile with a page from k0 on; k0 >= c1: none.
+    auto find = [&](int k0) {
+        Keys t{};
+        for (; k0 < c1; k0 += BN * WAVES) {
+            const int last = min(c1 - k0, BN) - 1;
+            t.page0 = __builtin_amdgcn_readfirstlane(table[k0 >> cache.page_shift]);
+            t.page1 = __builtin_amdgcn_readfirstlane(table[(k0 + min(16, last)) >> cache.page_shift]);
+            const bool has0 = t.page0 >= 0 && t.page0 < cache.num_pages;
+            const bool has1 = last >= 16 && t.page1 >= 0 && t.page1 < cache.num_pages;
+            t.lo = has0 ? 0 : 16;
+            t.hi = has1 ? last : min(last, 15);
+            if (has0 || has1) break;
+        }
+        t.k0 = k0;
+        return t;
+    };
+    auto issue = [&](const Keys& t, int which) {
+        page_dma<DH>(sT[w][which], which ? Vb : Kb, page_stride, in_page, t.page0, t.page1, t.k0 & in_page, t.lo, t.hi, lane);
+    };
+    Keys t = find(c0 + BN * w);
     bf16x8 qreg[KSTEPS];
 #pragma unroll
     for (int kk = 0; kk < KSTEPS; kk++)
         qreg[kk] = col < heads ? as_bf16x8(*(const uint4*)((const uint16_t*)a.q + b * a.ld_q + (h0 + col) * DH + 16 * kk + 8 * hh))
                                : bf16x8{};
+    wait_vmcnt_seen<0>();
+    if (t.k0 < c1) {
+        issue(t, 0);
+        issue(t, 1);
+    }
     floatx16 oacc[DBLK];
 #pragma unroll
     for (int d = 0; d < DBLK; d++) oacc[d] = floatx16{};
     float m = -3.0e38f, l = 0.f;
-    wait_vmcnt_seen<0>();
-    for (int k0 = c0 + BN * w; k0 < c1; k0 += BN * WAVES) {
-        const int last = min(c1 - k0, BN) - 1;
-        // pages of the tile's halves (the same one where pages are larger); the last half may have none of its keys
-        const int page0 = __builtin_amdgcn_readfirstlane(table[k0 >> cache.page_shift]);
-        const int page1 = __builtin_amdgcn_readfirstlane(table[(k0 + min(16, last)) >> cache.page_shift]);
-        const bool has0 = page0 >= 0 && page0 < cache.num_pages, has1 = last >= 16 && page1 >= 0 && page1 < cache.num_pages;
-        if (!has0 && !has1) continue;
-        const int lo = has0 ? 0 : 16, hi = has1 ? last : min(last, 15);
-        wait_vmcnt_seen<0>();
-        page_dma<DH>(sT[w][0], Kb, page_stride, in_page, page0, page1, k0 & in_page, lo, hi, lane);
-        page_dma<DH>(sT[w][2], Vb, page_stride, in_page, page0, page1, k0 & in_page, lo, hi, lane);
-        wait_vmem();
+    while (t.k0 < c1) {
+        const Keys next = find(t.k0 + BN * WAVES);
+        const bool more = next.k0 < c1;
         const uint16_t* sK = sT[w][0];
-        const uint16_t* sV = sT[w][2];
+        const uint16_t* sV = sT[w][1];
+        wait_vmcnt<NI>();                                        // this tile's keys
         floatx16 s{};
 #pragma unroll
         for (int kk = 0; kk < KSTEPS; kk++)
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sK, col, 2 * kk + hh), qreg[kk], s, 0, 0, 0);
-        if (lo > 0 || hi < BN - 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // they are read
+        if (more) issue(next, 0);
+        if (t.lo > 0 || t.hi < BN - 1) {
 #pragma unroll
             for (int e = 0; e < 16; e++) {
                 const int key = 8 * (e >> 2) + 4 * hh + (e & 3);
-                s[e] = key >= lo && key <= hi ? s[e] : neg_inf();
+                s[e] = key >= t.lo && key <= t.hi ? s[e] : neg_inf();
             }
         }
         float top = s[0];
@@ -104,6 +128,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
             l += p0 + p1;
             pk[e >> 1] = pack_bf16x2(p0, p1);
         }
+        if (more) wait_vmcnt<NI>(); else wait_vmem();            // this tile's values
 #pragma unroll
         for (int kq = 0; kq < 2; kq++) {
             const bf16x8 pb = as_bf16x8(make_uint4(pk[4 * kq], pk[4 * kq + 1], pk[4 * kq + 2], pk[4 * kq + 3]));
@@ -111,7 +136,9 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
             for (int d = 0; d < DBLK; d++)
                 oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read_tr<CPR>(sV, 16 * kq, 32 * d, lane), pb, oacc[d], 0, 0, 0);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the tile is read before the next one's copies
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) issue(next, 1);
+        t = next;
     }
     l = sum_halves(l);
     if (hh == 0) {
@@ -127,7 +154,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
             *(float4*)&sO[col * DH + 32 * d + 8 * g + 4 * hh] =
                 make_float4(oacc[d][4 * g], oacc[d][4 * g + 1], oacc[d][4 * g + 2], oacc[d][4 * g + 3]);
     __syncthreads();
-    for (int i = tid; i < heads * (DH / 4); i += 256) {
+    for (int i = tid; i < heads * (DH / 4); i += 64 * WAVES) {
         const int q = i / (DH / 4), f = 4 * (i % (DH / 4));
         float top = sML[0][0][q];
 #pragma unroll
@@ -157,13 +184,13 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
     }
 }
 
-// Joins the chunks of a (sequence, head): lanes over features, groups of lanes over chunks.
+// Joins the chunks of a (sequence, head): 32 features of it per workgroup, 8 lanes for them and 32 groups of lanes over the chunks.
 template <int DH>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
-    constexpr int L = DH / 4, G = 256 / L;
+    constexpr int L = 8, G = 256 / L;
     __shared__ float sTop[4], sTotal[G];
     __shared__ float4 sO[256];
-    const int tid = threadIdx.x, h = blockIdx.x, b = blockIdx.y;
+    const int tid = threadIdx.x, h = blockIdx.x / (DH / 32), f = 32 * (blockIdx.x % (DH / 32)) + 4 * (tid % L), g = tid / L, b = blockIdx.y;
     const long long row = (long long)b * a.H + h;
     const int len = min(max(a.lens[b], 0), a.max_len), n = max(1, (len + a.chunk - 1) / a.chunk);
     const float2* ml = a.part_ml + row * a.splits;
@@ -174,13 +201,12 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
     if ((tid & 63) == 0) sTop[tid >> 6] = top;
     __syncthreads();
     top = fmaxf(fmaxf(sTop[0], sTop[1]), fmaxf(sTop[2], sTop[3]));
-    const int g = tid / L, f = 4 * (tid % L);
     float total = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i = g; i < n; i += G) {
         const float2 x = ml[i];
-        const float e = __builtin_amdgcn_exp2f((x.x - top) * a.c);
         const float4 v = *(const float4*)&a.part[(row * a.splits + i) * DH + f];
+        const float e = __builtin_amdgcn_exp2f((x.x - top) * a.c);
         total = __builtin_fmaf(e, x.y, total);
         o.x = __builtin_fmaf(e, v.x, o.x);
         o.y = __builtin_fmaf(e, v.y, o.y);
@@ -188,10 +214,11 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
         o.w = __builtin_fmaf(e, v.w, o.w);
     }
     sO[tid] = o;
-    if (f == 0) sTotal[g] = total;
+    if (tid % L == 0) sTotal[g] = total;
     __syncthreads();
     if (g > 0) return;
-    for (int j = 1; j < G; j++) {
+    const int groups = min(n, G);
+    for (int j = 1; j < groups; j++) {
         const float4 v = sO[j * L + tid];
         total += sTotal[j];
         o.x += v.x;
@@ -207,15 +234,19 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
 
 }  // namespace
 
+// Chunks as long as they leave each CU two workgroups of 4 waves; up to 1,024 keys, where the workgroups of one chunk do
+// not fill the chip, 8 waves and no second kernel.
 CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_len) {
     CacheAttnPlan p{};
     const int group = H / Hk;
     const long long units = (long long)B * Hk * ((group + QT - 1) / QT);
-    const long long want = (512 + units - 1) / units;             // chunks of a sequence that fill the chip
+    const long long want = (CHUNKS + units - 1) / units;          // chunks of a sequence that fill the chip
     long long chunk = (max_len + want - 1) / want;
     chunk = std::min<long long>(std::max<long long>((chunk + 127) / 128 * 128, 128), 2048);
+    if (max_len <= 1024) chunk = 1024;
     p.chunk = (int)chunk;
     p.splits = (int)std::max<long long>(1, (max_len + chunk - 1) / chunk);
+    p.waves = p.splits == 1 && units <= 256 ? 8 : 4;
     if (p.splits > 1) {
         p.part_bytes = ((size_t)B * H * p.splits * head_dim * 4 + 255) & ~(size_t)255;
         p.bytes = p.part_bytes + (((size_t)B * H * p.splits * 8 + 255) & ~(size_t)255);
@@ -225,9 +256,10 @@ CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_
 
 template <int DH>
 static hipError_t cache_attn_dh(const CacheAttnArgs& a, hipStream_t s) {
-    const int Hk = a.H / a.group;
-    cache_attn_kernel<DH><<<dim3(a.splits, Hk * ((a.group + QT - 1) / QT), a.B), 256, 0, s>>>(a);
-    if (a.splits > 1) cache_join_kernel<DH><<<dim3(a.H, a.B), 256, 0, s>>>(a);
+    const dim3 grid(a.splits, a.H / a.group * ((a.group + QT - 1) / QT), a.B);
+    if (a.waves == 8) cache_attn_kernel<DH, 8><<<grid, 512, 0, s>>>(a);
+    else cache_attn_kernel<DH, 4><<<grid, 256, 0, s>>>(a);
+    if (a.splits > 1) cache_join_kernel<DH><<<dim3(a.H * (DH / 32), a.B), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

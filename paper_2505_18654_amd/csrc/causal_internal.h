@@ -82,6 +82,7 @@ struct CacheAttnArgs {
     CacheArgs cache;
     int B, H, group;
     int chunk, splits;        // keys of a workgroup, and how many of them a sequence has at most
+    int waves;                // of a workgroup: 4 or 8
     int max_len;
     float scale, c;
     const int* lens;
@@ -93,7 +94,7 @@ struct CacheAttnArgs {
     float2* part_ml;          // [B H][splits] their maxima and totals
 };
 struct CacheAttnPlan {
-    int chunk, splits;
+    int chunk, splits, waves;
     size_t part_bytes, bytes;
 };
 CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_len);
