@@ -106,7 +106,7 @@ mtgr_status_t mtgr_causal_attn_bwd(const mtgr_causal_problem_t* p, const int32_t
  *
  * keys, values [num_pages, kv_heads, page_size, head_dim], dense: token p of a sequence lies in row p % page_size of page
  * page_table[sequence][p / page_size].  page_size is a power of two, 16 .. 4096.  The page table is int32
- * [num_seqs, max_pages] with a row stride ld_table; entries past a sequence's length are not read, and an entry outside
+ * [num_seqs, max_pages] with a row stride ld_table; entries past a sequence's length are not used, and an entry outside
  * 0 .. num_pages-1 is no page: nothing is written through it, and its tokens count as absent. */
 typedef struct {
     int64_t num_pages;        /* 1 .. 2^31 - 1 */

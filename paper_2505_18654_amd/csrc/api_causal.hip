@@ -175,6 +175,7 @@ mtgr_status_t check_cache_attn(const mtgr_cache_attn_problem_t* p, const mtgr_kv
     if (p->num_seqs < 0 || p->num_seqs > 65535)
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "num_seqs = %d outside [0, 65535]", p->num_seqs);
     CHECK(check_attn(p->heads, cache->kv_heads, cache->head_dim, p->scale));
+    if ((int64_t)p->num_seqs * p->heads >= (1ll << 27)) return fail(MTGR_ERROR_UNSUPPORTED, "num_seqs heads is not below 2^27");
     if (p->max_pages < 1) return fail(MTGR_ERROR_INVALID_ARGUMENT, "max_pages = %d", p->max_pages);
     if (p->max_len < 0 || p->max_len > (int64_t)p->max_pages * cache->page_size || p->max_len >= (1ll << 31) - 4096)
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "max_len = %lld outside [0, max_pages page_size = %lld] or not below 2^31 - 4096",

@@ -32,36 +32,57 @@ __device__ __forceinline__ void page_dma(uint16_t* tile, const uint16_t* base, l
 }
 
 template <int DH, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(CacheAttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES, DH == 64 ? 4 : 2) void cache_attn_kernel(CacheAttnArgs a) {
     constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, TILE = BN * DH, NI = CPR / 2;
     __shared__ __align__(16) uint16_t sT[WAVES][2][TILE];        // K and V of each wave; then its outputs
     __shared__ float sML[WAVES][2][QT];
     static_assert(2 * TILE * 2 >= QT * DH * 4, "a wave's outputs fit its tiles");
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, hh = lane >> 5;
-    const int b = blockIdx.z, split = blockIdx.x;
-    const int qtiles = (a.group + QT - 1) / QT, hk = blockIdx.y / qtiles;
-    const int g0 = QT * (blockIdx.y % qtiles), heads = min(QT, a.group - g0), h0 = hk * a.group + g0;
-    const int len = min(max(a.lens[b], 0), a.max_len);
-    const int c0 = split * a.chunk, c1 = min(c0 + a.chunk, len);
-    if (c0 >= len && split > 0) return;
+    // Chunks slowest: workgroup i runs on XCD i % 8, and with the chunks of a sequence beside each other, where there are 4 or 8
+    // of them, some XCDs got the first chunks, which every sequence has, and others the last, which most have not (37 sequences
+    // of up to 2,113 tokens, 16 / 8 heads of 128: 30 us, with 4 chunks side by side 41).
+    const int qtiles = (a.group + QT - 1) / QT, units = a.cache.kv_heads * qtiles;
+    const int unit = blockIdx.x % units, b = blockIdx.x / units % a.B, split = blockIdx.x / units / a.B;
+    const int hk = unit / qtiles;
+    const int g0 = QT * (unit % qtiles), heads = min(QT, a.group - g0), h0 = hk * a.group + g0;
     const CacheArgs& cache = a.cache;
     const int* table = cache.table + b * cache.ld_table;
     const long long head_ofs = (long long)hk << cache.page_shift, page_stride = ((long long)cache.kv_heads << cache.page_shift) * DH;
     const uint16_t* Kb = (const uint16_t*)cache.keys + head_ofs * DH;
     const uint16_t* Vb = (const uint16_t*)cache.values + head_ofs * DH;
     const int in_page = (1 << cache.page_shift) - 1;
+    const int c0 = split * a.chunk;
+    // The query rows (columns of the products; those past `heads` are copies) come in through the wave's V tile, the first
+    // tile's pages and the sequence's length beside them: one latency for the three.
+    {
+        const uint16_t* Q = (const uint16_t*)a.q + b * a.ld_q + h0 * DH;
+#pragma unroll
+        for (int i = 0; i < NI; i++) {
+            const int row = i * (64 / CPR) + lane / CPR;
+            lds_dma16(lds_address(sT[w][1]) + i * 1024u, uniform_ptr(Q),
+                      (uint32_t)(min(row, heads - 1) * DH + ((lane % CPR) ^ swz<CPR>(row)) * 8) * 2u);
+        }
+    }
     // A tile: its first key, the pages of its halves (the same one where pages are larger) and the rows lo .. hi that have one.
     struct Keys {
         int k0, page0, page1, lo, hi;
     };
+    auto entry = [&](int key) { return __builtin_amdgcn_readfirstlane(table[min(key >> cache.page_shift, cache.max_pages - 1)]); };
+    const int first = c0 + BN * w;
+    const int entry0 = entry(first), entry1 = entry(first + 16);
+    const int len = min(max(a.lens[b], 0), a.max_len), c1 = min(c0 + a.chunk, len);
+    if (c0 >= len && split > 0) {
+        wait_vmem();
+        return;
+    }
     // The wave's next tile with a page from k0 on; k0 >= c1: none.
-    auto find = [&](int k0) {
+    auto find = [&](int k0, bool known) {
         Keys t{};
-        for (; k0 < c1; k0 += BN * WAVES) {
+        for (; k0 < c1; k0 += BN * WAVES, known = false) {
             const int last = min(c1 - k0, BN) - 1;
-            t.page0 = __builtin_amdgcn_readfirstlane(table[k0 >> cache.page_shift]);
-            t.page1 = __builtin_amdgcn_readfirstlane(table[(k0 + min(16, last)) >> cache.page_shift]);
+            t.page0 = known ? entry0 : entry(k0);
+            t.page1 = known ? entry1 : entry(k0 + 16);
             const bool has0 = t.page0 >= 0 && t.page0 < cache.num_pages;
             const bool has1 = last >= 16 && t.page1 >= 0 && t.page1 < cache.num_pages;
             t.lo = has0 ? 0 : 16;
@@ -74,23 +95,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(CacheAttnArgs
     auto issue = [&](const Keys& t, int which) {
         page_dma<DH>(sT[w][which], which ? Vb : Kb, page_stride, in_page, t.page0, t.page1, t.k0 & in_page, t.lo, t.hi, lane);
     };
-    Keys t = find(c0 + BN * w);
+    Keys t = find(first, true);
+    const bool any = t.k0 < c1;
+    if (any) issue(t, 0);
+    if (any) wait_vmcnt<NI>(); else wait_vmem();
     bf16x8 qreg[KSTEPS];
 #pragma unroll
-    for (int kk = 0; kk < KSTEPS; kk++)
-        qreg[kk] = col < heads ? as_bf16x8(*(const uint4*)((const uint16_t*)a.q + b * a.ld_q + (h0 + col) * DH + 16 * kk + 8 * hh))
-                               : bf16x8{};
-    wait_vmcnt_seen<0>();
-    if (t.k0 < c1) {
-        issue(t, 0);
-        issue(t, 1);
-    }
+    for (int kk = 0; kk < KSTEPS; kk++) qreg[kk] = tile_read8<CPR>(sT[w][1], col, 2 * kk + hh);
+    wait_lgkm_seen();
+    if (any) issue(t, 1);
     floatx16 oacc[DBLK];
 #pragma unroll
     for (int d = 0; d < DBLK; d++) oacc[d] = floatx16{};
     float m = -3.0e38f, l = 0.f;
     while (t.k0 < c1) {
-        const Keys next = find(t.k0 + BN * WAVES);
+        const Keys next = find(t.k0 + BN * WAVES, false);
         const bool more = next.k0 < c1;
         const uint16_t* sK = sT[w][0];
         const uint16_t* sV = sT[w][1];
@@ -151,7 +170,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_kernel(CacheAttnArgs
     for (int d = 0; d < DBLK; d++)
 #pragma unroll
         for (int g = 0; g < 4; g++)
-            *(float4*)&sO[col * DH + 32 * d + 8 * g + 4 * hh] =
+            if (col < heads) *(float4*)&sO[col * DH + 32 * d + 8 * g + 4 * hh] =
                 make_float4(oacc[d][4 * g], oacc[d][4 * g + 1], oacc[d][4 * g + 2], oacc[d][4 * g + 3]);
     __syncthreads();
     for (int i = tid; i < heads * (DH / 4); i += 64 * WAVES) {
@@ -234,16 +253,19 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
 
 }  // namespace
 
-// Chunks as long as they leave each CU two workgroups of 4 waves; up to 1,024 keys, where the workgroups of one chunk do
-// not fill the chip, 8 waves and no second kernel.
+// Chunks as long as they leave each CU two workgroups of 4 waves.  Of three sequences and more, most are shorter than max_len,
+// and half as long chunks balance better (4 sequences of up to 67,056 tokens, 6 / 3 heads of 128: 47 -> 43 us; 13 of up to 27,795,
+// 12 / 3: 53 -> 43; one of 100,003, 6 / 2, the other way: 27, with half the length 32).  Up to 1,024 keys, one workgroup per
+// (sequence, key head) without a second kernel, of 8 waves where they leave CUs idle.
 CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_len) {
     CacheAttnPlan p{};
     const int group = H / Hk;
     const long long units = (long long)B * Hk * ((group + QT - 1) / QT);
-    const long long want = (CHUNKS + units - 1) / units;          // chunks of a sequence that fill the chip
+    const long long want = ((B > 2 ? 2 * CHUNKS : CHUNKS) + units - 1) / units;      // chunks of a sequence that fill the chip
     long long chunk = (max_len + want - 1) / want;
     chunk = std::min<long long>(std::max<long long>((chunk + 127) / 128 * 128, 128), 2048);
     if (max_len <= 1024) chunk = 1024;
+    while (units * ((max_len + chunk - 1) / chunk) >= (1ll << 31)) chunk *= 2;
     p.chunk = (int)chunk;
     p.splits = (int)std::max<long long>(1, (max_len + chunk - 1) / chunk);
     p.waves = p.splits == 1 && units <= 256 ? 8 : 4;
@@ -256,7 +278,7 @@ CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_
 
 template <int DH>
 static hipError_t cache_attn_dh(const CacheAttnArgs& a, hipStream_t s) {
-    const dim3 grid(a.splits, a.H / a.group * ((a.group + QT - 1) / QT), a.B);
+    const int grid = a.H / a.group * ((a.group + QT - 1) / QT) * a.B * a.splits;
     if (a.waves == 8) cache_attn_kernel<DH, 8><<<grid, 512, 0, s>>>(a);
     else cache_attn_kernel<DH, 4><<<grid, 256, 0, s>>>(a);
     if (a.splits > 1) cache_join_kernel<DH><<<dim3(a.H * (DH / 32), a.B), 256, 0, s>>>(a);
