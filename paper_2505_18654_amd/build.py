@@ -23,7 +23,7 @@ SOURCES = ["api.hip", "schedule.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_bwd_
            "attn_bwd_dkdv.hip", "attn_bwd_dqds.hip", "group_ln.hip", "validate.hip",
            "pointwise.hip", "embedding.hip", "gemm.hip", "gemm_wide.hip", "clock.hip",
            "dropout.hip", "ffn.hip", "ffn_rows.hip", "softmax_loss.hip", "api_block.hip",
-           "rope.hip", "causal_plan.hip", "causal_fwd.hip",
+           "rope.hip", "causal_fwd.hip",
            "causal_bwd_dkdv.hip", "causal_bwd_dq.hip", "cache_attn.hip", "api_causal.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -308,11 +308,12 @@ mtgr_status_t mtgr_causal_attn_bwd(const mtgr_causal_problem_t* p, const int32_t
     a.rows_d = (float*)(ws + rows_bytes(p));
     ws += 2 * rows_bytes(p);
     const mtgr::CausalPlan plan = plan_of(p);
-    mtgr::CausalItem *items = (mtgr::CausalItem*)ws, *joins = (mtgr::CausalItem*)(ws + plan.joins_ofs);
+    a.items = (mtgr::CausalItem*)ws;
+    a.joins = (mtgr::CausalItem*)(ws + plan.joins_ofs);
+    a.parts = (float*)(ws + plan.parts_ofs);
     const hipStream_t s = (hipStream_t)stream;
-    hipError_t e = mtgr::launch_causal_plan(a, plan, items, joins, s);
-    if (e == hipSuccess) e = mtgr::launch_causal_dq(a, p->head_dim, s);
-    if (e == hipSuccess) e = mtgr::launch_causal_dkdv(a, plan, items, joins, (float*)(ws + plan.parts_ofs), p->head_dim, s);
+    hipError_t e = mtgr::launch_causal_dq(a, plan, p->head_dim, s);
+    if (e == hipSuccess) e = mtgr::launch_causal_dkdv(a, plan, p->head_dim, s);
     if (e != hipSuccess) return device_fail(e, "causal attention backward");
     return ok();
 }

@@ -18,7 +18,7 @@ __device__ __forceinline__ float4* part_of(float* parts, long long part, int whi
 }
 
 template <int DH>
-__global__ __launch_bounds__(256, 2) void causal_dkdv_kernel(CausalArgs a, const CausalItem* items, float* parts) {
+__global__ __launch_bounds__(256, 2) void causal_dkdv_kernel(CausalArgs a) {
     constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, UNIT = 32 * DH;
     __shared__ __align__(16) uint16_t sK[BM * DH];
     __shared__ __align__(16) uint16_t sQG[2][2 * UNIT];          // Q, then dO, of a unit
@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256, 2) void causal_dkdv_kernel(CausalArgs a, const
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, hh = lane >> 5;
     const int hk = blockIdx.x % a.Hk;
-    const CausalItem it = items[blockIdx.x / a.Hk];
+    const CausalItem it = a.items[blockIdx.x / a.Hk];
     if (it.tile < 0) return;
     const int k0 = it.tile * BM, n = it.n, kw = k0 + 32 * w;
     bf16x8 vreg[KSTEPS];
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void causal_dkdv_kernel(CausalArgs a, const
     if (it.part >= 0) {
 #pragma unroll
         for (int which = 0; which < 2; which++) {
-            float4* dst = part_of<DBLK>(parts, (long long)it.part * a.Hk + hk, which, w, lane);
+            float4* dst = part_of<DBLK>(a.parts, (long long)it.part * a.Hk + hk, which, w, lane);
             const floatx16* x = which ? dv : dk;
 #pragma unroll
             for (int d = 0; d < DBLK; d++)
@@ -156,18 +156,18 @@ __global__ __launch_bounds__(256, 2) void causal_dkdv_kernel(CausalArgs a, const
 
 // The sums of a tile's items, added in their order.
 template <int DH>
-__global__ __launch_bounds__(256) void causal_dkdv_join_kernel(CausalArgs a, const CausalItem* joins, float* parts) {
+__global__ __launch_bounds__(256) void causal_dkdv_join_kernel(CausalArgs a) {
     constexpr int DBLK = DH / 32;
     __shared__ __align__(16) uint16_t sO[4][32 * DH];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int which = blockIdx.x & 1, hk = (blockIdx.x >> 1) % a.Hk;
-    const CausalItem it = joins[(blockIdx.x >> 1) / a.Hk];
+    const CausalItem it = a.joins[(blockIdx.x >> 1) / a.Hk];
     if (it.tile < 0) return;
     floatx16 x[DBLK];
 #pragma unroll
     for (int d = 0; d < DBLK; d++) x[d] = floatx16{};
     for (int i = 0; i < it.parts; i++) {
-        const float4* src = part_of<DBLK>(parts, (long long)(it.part + i) * a.Hk + hk, which, w, lane);
+        const float4* src = part_of<DBLK>(a.parts, (long long)(it.part + i) * a.Hk + hk, which, w, lane);
 #pragma unroll
         for (int d = 0; d < DBLK; d++)
 #pragma unroll
@@ -185,21 +185,19 @@ __global__ __launch_bounds__(256) void causal_dkdv_join_kernel(CausalArgs a, con
 }
 
 template <int DH>
-hipError_t dkdv(const CausalArgs& a, const CausalPlan& p, const CausalItem* items, const CausalItem* joins, float* parts,
-                hipStream_t s) {
-    causal_dkdv_kernel<DH><<<p.items * a.Hk, 256, 0, s>>>(a, items, parts);
-    if (p.joins > 0) causal_dkdv_join_kernel<DH><<<2 * p.joins * a.Hk, 256, 0, s>>>(a, joins, parts);
+hipError_t dkdv(const CausalArgs& a, const CausalPlan& p, hipStream_t s) {
+    causal_dkdv_kernel<DH><<<p.items * a.Hk, 256, 0, s>>>(a);
+    if (p.joins > 0) causal_dkdv_join_kernel<DH><<<2 * p.joins * a.Hk, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_causal_dkdv(const CausalArgs& a, const CausalPlan& p, const CausalItem* items, const CausalItem* joins,
-                              float* parts, int head_dim, hipStream_t s) {
+hipError_t launch_causal_dkdv(const CausalArgs& a, const CausalPlan& p, int head_dim, hipStream_t s) {
     switch (head_dim) {
-        case 32: return dkdv<32>(a, p, items, joins, parts, s);
-        case 64: return dkdv<64>(a, p, items, joins, parts, s);
-        case 128: return dkdv<128>(a, p, items, joins, parts, s);
+        case 32: return dkdv<32>(a, p, s);
+        case 64: return dkdv<64>(a, p, s);
+        case 128: return dkdv<128>(a, p, s);
         default: return hipErrorInvalidValue;
     }
 }

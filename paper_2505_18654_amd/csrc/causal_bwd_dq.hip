@@ -6,7 +6,7 @@
 // its own read dO and O once more (50 us for 68,000 tokens, 8 heads of 128).
 #include <type_traits>
 
-#include "causal_device.h"
+#include "causal_plan.h"
 
 namespace mtgr {
 namespace {
@@ -15,13 +15,18 @@ using namespace causal;
 constexpr int BN = 64;
 
 template <int DH>
-__global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a) {
+__global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a, CausalPlan p) {
     constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, TILE = BN * DH;
     constexpr int NM = 2 * KSTEPS + 2 * DBLK, PF = 3;            // products of a step; how far ahead operands are read
     __shared__ __align__(16) uint16_t sKV[4][TILE];              // K 0, K 1, V 0, V 1
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, hh = lane >> 5;
-    int id = blockIdx.x;
+    if (blockIdx.x == 0) {
+        static_assert(PLAN_LDS * 4 <= 4 * TILE * 2, "the plan fits the tiles");
+        make_plan(a, p, (int*)sKV);
+        return;
+    }
+    int id = blockIdx.x - 1;
     const int hk = id % a.Hk;
     id /= a.Hk;
     const int h = hk * a.group + id % a.group;
@@ -33,8 +38,15 @@ __global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a) {
     const int qw = q0 + 32 * w, qr = min(qw + col, n - 1);
     const int nh = qw < n ? qw / 32 + 1 : 0;                     // halves that this wave's rows see, the last on the diagonal
     const int ntk = (min(q0 + BM, n) + BN - 1) / BN;
-    auto issue_k = [&](int t, int buf) { tile_dma<DH>(sKV[buf], Kb, a.ld_k, t * BN, n, hk * DH, tid); };
-    auto issue_v = [&](int t, int buf) { tile_dma<DH>(sKV[2 + buf], Vb, a.ld_v, t * BN, n, hk * DH, tid); };
+    // The thread's number, counted afresh for each copy: kept in a register it spilled, and its reload waits for the copies
+    // under way.
+    auto thread = [&] {
+        uint32_t none = 0;
+        asm volatile("" : "+v"(none));
+        return 64 * w + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
+    };
+    auto issue_k = [&](int t, int buf) { tile_dma<DH>(sKV[buf], Kb, a.ld_k, t * BN, n, hk * DH, thread()); };
+    auto issue_v = [&](int t, int buf) { tile_dma<DH>(sKV[2 + buf], Vb, a.ld_v, t * BN, n, hk * DH, thread()); };
     issue_k(0, 0);
     issue_v(0, 0);
     if (ntk > 1) issue_v(1, 1);
@@ -76,10 +88,10 @@ __global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; e++) s[e] = 8 * (e >> 2) + 4 * hh + (e & 3) > col ? neg_inf() : s[e];
     };
-    // A step: dS and its product with K for half HC of the tile in buffer KB, whose scores and dP - delta are s and p; beside
+    // A step: dS and its product with K for half HC of the tile in buffer KB, whose scores and dP - delta are s and g; beside
     // them those of the next half, half HN of the tile in buffers NB, product by product between the elements' arithmetic.
-    auto step = [&](auto kb_tag, auto hc_tag, auto nb_tag, auto hn_tag, const floatx16& s, const floatx16& p, floatx16& sn,
-                    floatx16& pn, int j) {
+    auto step = [&](auto kb_tag, auto hc_tag, auto nb_tag, auto hn_tag, const floatx16& s, const floatx16& g, floatx16& sn,
+                    floatx16& gn, int j) {
         constexpr int KB = decltype(kb_tag)::value, HC = decltype(hc_tag)::value, NB = decltype(nb_tag)::value,
                       HN = decltype(hn_tag)::value;
         // (the transposed reads' offsets afresh in each step: kept in registers, at 256 of them, one fragment of Q spilled,
@@ -97,7 +109,7 @@ __global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a) {
         uint32_t pk[8];
         float ds[16];
         auto element = [&](int e) {
-            ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, nl)) * p[e];
+            ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, nl)) * g[e];
             if (e & 1) {
                 pk[e >> 1] = pack_bf16x2(ds[e - 1], ds[e]);
                 asm volatile("" : "+v"(pk[e >> 1]));
@@ -113,9 +125,9 @@ __global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a) {
                 } else {
                     if (kk == 0) {
 #pragma unroll
-                        for (int e = 0; e < 16; e++) pn[e] = nd;
+                        for (int e = 0; e < 16; e++) gn[e] = nd;
                     }
-                    pn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i], greg[kk], pn, 0, 0, 0);
+                    gn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i], greg[kk], gn, 0, 0, 0);
                 }
 #pragma unroll
                 for (int e = 16 * i / (2 * KSTEPS); e < 16 * (i + 1) / (2 * KSTEPS); e++) element(e);
@@ -168,12 +180,14 @@ __global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a) {
 
 }  // namespace
 
-hipError_t launch_causal_dq(const CausalArgs& a, int head_dim, hipStream_t s) {
-    const int grid = a.slots * a.H;
+CausalPlan causal_plan(long long T, int B, int H, int Hk, int head_dim) { return make_causal_plan(T, B, H, Hk, head_dim); }
+
+hipError_t launch_causal_dq(const CausalArgs& a, const CausalPlan& p, int head_dim, hipStream_t s) {
+    const int grid = 1 + a.slots * a.H;
     switch (head_dim) {
-        case 32: causal_dq_kernel<32><<<grid, 256, 0, s>>>(a); break;
-        case 64: causal_dq_kernel<64><<<grid, 256, 0, s>>>(a); break;
-        case 128: causal_dq_kernel<128><<<grid, 256, 0, s>>>(a); break;
+        case 32: causal_dq_kernel<32><<<grid, 256, 0, s>>>(a, p); break;
+        case 64: causal_dq_kernel<64><<<grid, 256, 0, s>>>(a, p); break;
+        case 128: causal_dq_kernel<128><<<grid, 256, 0, s>>>(a, p); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();

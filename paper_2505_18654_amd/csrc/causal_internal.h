@@ -43,6 +43,14 @@ struct AppendArgs {
 };
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s);
 
+// Work of the dK / dV kernel (causal_plan.h).  An item is a range of the 32-query units that read a tile of 128 keys; a
+// tile of many units is cut into several, which leave fp32 sums that a second kernel adds up.
+struct CausalItem {
+    int o, n, tile;           // the sequence's first row and length, the tile in it; tile < 0: no item
+    int first, last;          // units first .. last-1 of group ceil((n - 128 tile) / 32)
+    int part;                 // where the sums go; < 0: the tile is whole
+    int parts, pad;           // of a tile to join: its sums are part .. part + parts - 1
+};
 // Causal attention (causal_fwd.hip, causal_bwd_dq.hip, causal_bwd_dkdv.hip).
 struct CausalArgs {
     int B, H, Hk, group;      // group: query heads of a key head
@@ -55,27 +63,19 @@ struct CausalArgs {
     float* lse;               // [H, T], or NULL in the forward
     float *rows_l, *rows_d;   // [H, T] each: - lse / ln 2 and - delta, from the dQ kernel to the dK / dV kernel
     void *dq, *dk, *dv;
+    CausalItem *items, *joins;       // the dK / dV kernel's plan, from the dQ kernel
+    float* parts;
     long long ld_q, ld_k, ld_v, ld_o, ld_do;
 };
-hipError_t launch_causal_fwd(const CausalArgs& a, int head_dim, hipStream_t s);
-hipError_t launch_causal_dq(const CausalArgs& a, int head_dim, hipStream_t s);
 
-// Work of the dK / dV kernel (causal_plan.hip).  An item is a range of the 32-query units that read a tile of 128 keys; a
-// tile of many units is cut into several, which leave fp32 sums that a second kernel adds up.
-struct CausalItem {
-    int o, n, tile;           // the sequence's first row and length, the tile in it; tile < 0: no item
-    int first, last;          // units first .. last-1 of group ceil((n - 128 tile) / 32)
-    int part;                 // where the sums go; < 0: the tile is whole
-    int parts, pad;           // of a tile to join: its sums are part .. part + parts - 1
-};
 struct CausalPlan {
     int items, joins, parts;  // bounds of the items, the tiles to join and the sums of each key head
     size_t joins_ofs, parts_ofs, bytes;
 };
 CausalPlan causal_plan(long long T, int B, int H, int Hk, int head_dim);
-hipError_t launch_causal_plan(const CausalArgs& a, const CausalPlan& p, CausalItem* items, CausalItem* joins, hipStream_t s);
-hipError_t launch_causal_dkdv(const CausalArgs& a, const CausalPlan& p, const CausalItem* items, const CausalItem* joins,
-                              float* parts, int head_dim, hipStream_t s);
+hipError_t launch_causal_fwd(const CausalArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_causal_dq(const CausalArgs& a, const CausalPlan& p, int head_dim, hipStream_t s);
+hipError_t launch_causal_dkdv(const CausalArgs& a, const CausalPlan& p, int head_dim, hipStream_t s);
 
 // Single tokens against the cache (cache_attn.hip).
 struct CacheAttnArgs {
