@@ -88,12 +88,12 @@ typedef struct {
     int64_t ld_do;            /* dout (backward) */
 } mtgr_causal_problem_t;
 
-mtgr_status_t mtgr_causal_attn_workspace_size(const mtgr_causal_problem_t* p, int backward, size_t* bytes);
-
 /* lse may be NULL (serving). */
 mtgr_status_t mtgr_causal_attn_fwd(const mtgr_causal_problem_t* p, const int32_t* offsets, const void* q, const void* k,
-                                   const void* v, void* out, float* lse, void* workspace, size_t workspace_bytes,
-                                   mtgr_stream_t stream);
+                                   const void* v, void* out, float* lse, mtgr_stream_t stream);
+
+/* Workspace bytes of the backward pass. */
+mtgr_status_t mtgr_causal_attn_workspace_size(const mtgr_causal_problem_t* p, size_t* bytes);
 
 /* Gradients for dout [T, heads, head_dim], with out and lse of the forward pass on the same inputs.  The gradients of
  * shared key and value heads are summed in fp32 over their query heads, in a fixed order.  Infinities and NaN in a sequence

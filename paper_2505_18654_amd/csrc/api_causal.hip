@@ -97,8 +97,8 @@ mtgr::CausalPlan plan_of(const mtgr_causal_problem_t* p) {
     return mtgr::causal_plan(p->total_tokens, p->num_seqs, p->heads, p->kv_heads, p->head_dim);
 }
 
-size_t causal_workspace(const mtgr_causal_problem_t* p, bool backward) {
-    if (!backward || p->total_tokens == 0 || p->num_seqs == 0) return 0;
+size_t causal_workspace(const mtgr_causal_problem_t* p) {
+    if (p->total_tokens == 0 || p->num_seqs == 0) return 0;
     return 2 * rows_bytes(p) + plan_of(p).bytes;
 }
 
@@ -259,22 +259,20 @@ mtgr_status_t mtgr_rope(const mtgr_rope_problem_t* p, const void* x, const int32
     return ok();
 }
 
-mtgr_status_t mtgr_causal_attn_workspace_size(const mtgr_causal_problem_t* p, int backward, size_t* bytes) {
+mtgr_status_t mtgr_causal_attn_workspace_size(const mtgr_causal_problem_t* p, size_t* bytes) {
     if (!bytes) return fail(MTGR_ERROR_NULL_POINTER, "bytes is NULL");
     CHECK(check_causal(p));
-    *bytes = causal_workspace(p, backward != 0);
+    *bytes = causal_workspace(p);
     return ok();
 }
 
 mtgr_status_t mtgr_causal_attn_fwd(const mtgr_causal_problem_t* p, const int32_t* offsets, const void* q, const void* k,
-                                   const void* v, void* out, float* lse, void* workspace, size_t workspace_bytes,
-                                   mtgr_stream_t stream) {
+                                   const void* v, void* out, float* lse, mtgr_stream_t stream) {
     CHECK(check_causal(p));
     if (p->total_tokens == 0 || p->num_seqs == 0) return ok();
     CHECK(check_qkv(p, offsets, q, k, v));
     CHECK(check_heads(out, "out", p->ld_o, p->heads, p->head_dim));
     if (lse) CHECK(check_array(lse, "lse", 4));
-    CHECK(check_workspace(workspace, workspace_bytes, causal_workspace(p, false)));
     mtgr::CausalArgs a = causal_args(p, offsets, q, k, v);
     a.out = out;
     a.lse = lse;
@@ -295,7 +293,7 @@ mtgr_status_t mtgr_causal_attn_bwd(const mtgr_causal_problem_t* p, const int32_t
     CHECK(check_heads(dq, "dq", p->ld_q, p->heads, p->head_dim));
     CHECK(check_heads(dk, "dk", p->ld_k, p->kv_heads, p->head_dim));
     CHECK(check_heads(dv, "dv", p->ld_v, p->kv_heads, p->head_dim));
-    CHECK(check_workspace(workspace, workspace_bytes, causal_workspace(p, true)));
+    CHECK(check_workspace(workspace, workspace_bytes, causal_workspace(p)));
     mtgr::CausalArgs a = causal_args(p, offsets, q, k, v);
     a.out = (void*)out;
     a.lse = (float*)lse;

@@ -219,8 +219,8 @@ def lib() -> ctypes.CDLL:
         L.mtgr_rope_frequencies.argtypes = [i32, ctypes.c_double, ctypes.c_int, ctypes.c_double, i64, ctypes.c_double,
                                             ctypes.c_double, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)]
         L.mtgr_rope.argtypes = [R, vp, vp, vp, vp, vp, vp]
-        L.mtgr_causal_attn_workspace_size.argtypes = [C, ctypes.c_int, ctypes.POINTER(sz)]
-        L.mtgr_causal_attn_fwd.argtypes = [C, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mtgr_causal_attn_workspace_size.argtypes = [C, ctypes.POINTER(sz)]
+        L.mtgr_causal_attn_fwd.argtypes = [C, vp, vp, vp, vp, vp, vp, vp]
         L.mtgr_causal_attn_bwd.argtypes = [C, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.mtgr_kv_append.argtypes = [A, K, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.mtgr_cache_attn_workspace_size.argtypes = [D, K, ctypes.POINTER(sz)]
@@ -570,15 +570,15 @@ def mtgr_rope(problem, x, positions, offsets, freqs, out, stream=None) -> None:
                            _stream(stream)))
 
 
-def mtgr_causal_attn_workspace_size(problem: CausalProblem, backward: bool = False) -> int:
+def mtgr_causal_attn_workspace_size(problem: CausalProblem) -> int:
     out = ctypes.c_size_t(0)
-    _check(lib().mtgr_causal_attn_workspace_size(ctypes.byref(problem), int(backward), ctypes.byref(out)))
-    return int(out.value)
+    _check(lib().mtgr_causal_attn_workspace_size(ctypes.byref(problem), ctypes.byref(out)))
+    return out.value
 
 
-def mtgr_causal_attn_fwd(problem, offsets, q, k, v, out, lse, workspace, workspace_bytes, stream=None) -> None:
+def mtgr_causal_attn_fwd(problem, offsets, q, k, v, out, lse, stream=None) -> None:
     _check(lib().mtgr_causal_attn_fwd(ctypes.byref(problem), _ptr(offsets), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
-                                      _ptr(workspace), int(workspace_bytes), _stream(stream)))
+                                      _stream(stream)))
 
 
 def mtgr_causal_attn_bwd(problem, offsets, q, k, v, out, lse, dout, dq, dk, dv, workspace, workspace_bytes,

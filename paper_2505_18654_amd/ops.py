@@ -472,27 +472,46 @@ def softmax_loss_bwd(dloss, x, w, targets, lse, bias=None, scale: float = 1.0, g
 def _heads(name: str, t, tokens: Optional[int], heads: Optional[int], dh: Optional[int], dtype, dev: int,
            like: Optional[int] = None) -> int:
     """Checks a [tokens, heads, head_dim] operand (shape, type, device, dense heads, token rows that do not overlap) and
-    returns its token stride; `like`: the stride that a gradient shares with its primal."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype is not dtype:
+    returns its token stride; None: any size; `like`: the stride that a gradient shares with its primal."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 3:
         got = f"{list(t.shape)} {t.dtype}" if isinstance(t, torch.Tensor) else type(t).__name__
         raise ValueError(f"{name} is [tokens, heads, head_dim] of {dtype}, got {got}")
-    shape = t.shape
-    if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or \
-            (dh is not None and shape[2] != dh):
-        raise ValueError(f"{name} is [{tokens}, {heads}, {dh}], got {list(shape)}")
+    n, h, d = t.shape
+    if (tokens is not None and n != tokens) or (heads is not None and h != heads) or (dh is not None and d != dh):
+        raise ValueError(f"{name} is [{tokens}, {heads}, {dh}], got {[n, h, d]}")
     if t.get_device() != dev:
         raise ValueError(f"{name} is on {t.device}, not on the current device")
     ld, sh, se = t.stride()
-    row = shape[1] * shape[2]
-    if (se != 1 and shape[2] > 1) or (sh != shape[2] and shape[1] > 1):
+    if (se != 1 and d > 1) or (sh != d and h > 1):
         raise ValueError(f"the heads of {name} are not dense")
-    if shape[0] <= 1:
-        ld = row
-    elif ld < row:
+    if n <= 1:
+        ld = h * d
+    elif ld < h * d:
         raise ValueError(f"the rows of {name} overlap")
     if like is not None and ld != like:
         raise ValueError(f"{name} must share the token stride of its primal")
     return ld
+
+
+def _int32(name: str, t, n: int, dev: int) -> None:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} is a dense [{n}] of int32")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+
+
+def _sequences(offsets, dev: int) -> int:
+    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.numel() < 1:
+        raise ValueError("offsets is [B + 1] int32")
+    _int32("offsets", offsets, offsets.numel(), dev)
+    return offsets.numel() - 1
+
+
+def _lse(t, rows: int, cols: int, dev: int) -> None:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (rows, cols) or not t.is_contiguous():
+        raise ValueError(f"lse is a dense [{rows}, {cols}] of fp32")
+    if t.get_device() != dev:
+        raise ValueError(f"lse is on {t.device}, not on the current device")
 
 
 @dataclass
@@ -505,10 +524,16 @@ class Rotary:
     amplitude: float = 1.0
 
     def code(self, dev: int) -> int:
-        if self.layout not in ("half", "interleaved"):
-            raise ValueError(f"layout {self.layout!r} is neither 'half' nor 'interleaved'")
-        _vector("freqs", self.freqs, self.freqs.numel(), (torch.float64,), dev)
-        return hstu.MTGR_ROPE_HALF if self.layout == "half" else hstu.MTGR_ROPE_INTERLEAVED
+        f = self.freqs
+        if not isinstance(f, torch.Tensor) or f.dtype is not torch.float64 or f.dim() != 1 or not f.is_contiguous():
+            raise ValueError("freqs is a dense [rot_dim / 2] of float64")
+        if f.get_device() != dev:
+            raise ValueError(f"freqs is on {f.device}, not on the current device")
+        if self.layout == "half":
+            return hstu.MTGR_ROPE_HALF
+        if self.layout == "interleaved":
+            return hstu.MTGR_ROPE_INTERLEAVED
+        raise ValueError(f"layout {self.layout!r} is neither 'half' nor 'interleaved'")
 
 
 _ROPE_SCALINGS = {"none": hstu.MTGR_ROPE_NONE, "linear": hstu.MTGR_ROPE_LINEAR, "base": hstu.MTGR_ROPE_BASE,
@@ -530,87 +555,75 @@ def rope(x, rotary: Rotary, positions=None, offsets=None, inverse: bool = False,
     those inside each sequence of `offsets` [B + 1] int32 (rows behind the last are left).  inverse=True turns back: the
     gradient of x.  out may be x."""
     code, dev = _dtype_code(x), _device()
-    ld_x = _heads("x", x, None, None, None, x.dtype, dev)
+    dtype = x.dtype
+    ld_x = _heads("x", x, None, None, None, dtype, dev)
     T, H, dh = x.shape
     if out is None:
-        out = torch.empty((T, H, dh), dtype=x.dtype, device=x.device)
-    ld_out = _heads("out", out, T, H, dh, x.dtype, dev)
+        out, ld_out = x.new_empty((T, H, dh)), H * dh
+    else:
+        ld_out = _heads("out", out, T, H, dh, dtype, dev)
     layout = rotary.code(dev)
     if (positions is None) == (offsets is None):
         raise ValueError("either positions or offsets is given")
     B = 0
     if positions is not None:
-        _vector("positions", positions, T, (torch.int32,), dev)
+        _int32("positions", positions, T, dev)
     else:
         B = _sequences(offsets, dev)
-    p = hstu.RopeProblem(T, B, H, dh, 2 * rotary.freqs.numel(), layout, code, int(inverse), rotary.amplitude, ld_x, ld_out)
+    p = hstu.RopeProblem(T, B, H, dh, 2 * rotary.freqs.numel(), layout, code, inverse, rotary.amplitude, ld_x, ld_out)
     hstu.mtgr_rope(p, x, positions, offsets, rotary.freqs, out)
     return out
 
 
-def _sequences(offsets, dev: int) -> int:
-    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.numel() < 1:
-        raise ValueError("offsets is [B + 1] int32")
-    _vector("offsets", offsets, offsets.numel(), (torch.int32,), dev)
-    return offsets.numel() - 1
-
-
-def _causal_problem(q, k, v, offsets, scale, ld_o: int, ld_do: int) -> hstu.CausalProblem:
-    bf, dev = torch.bfloat16, _device()
+def _causal_problem(q, k, v, offsets, scale, dev: int) -> hstu.CausalProblem:
+    bf = torch.bfloat16
     ld_q = _heads("q", q, None, None, None, bf, dev)
     T, H, dh = q.shape
     ld_k = _heads("k", k, T, None, dh, bf, dev)
-    ld_v = _heads("v", v, T, k.shape[1], dh, bf, dev)
-    return hstu.CausalProblem(_sequences(offsets, dev), H, k.shape[1], dh, T, dh ** -0.5 if scale is None else scale, 0, ld_q, ld_k,
-                              ld_v, ld_o, ld_do)
+    Hk = k.shape[1]
+    ld_v = _heads("v", v, T, Hk, dh, bf, dev)
+    return hstu.CausalProblem(_sequences(offsets, dev), H, Hk, dh, T, dh ** -0.5 if scale is None else scale, 0, ld_q, ld_k,
+                              ld_v, H * dh, H * dh)
 
 
-def causal_attn_workspace(q, k, offsets, backward: bool = False) -> torch.Tensor:
-    """A workspace for causal_attn_fwd or causal_attn_bwd of these sizes."""
-    p = _causal_problem(q, k, k, offsets, None, 0, 0)
-    n = hstu.mtgr_causal_attn_workspace_size(p, backward)
-    return torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
-
-
-def causal_attn_fwd(q, k, v, offsets, scale: Optional[float] = None, save: bool = False, out=None, lse=None, workspace=None):
+def causal_attn_fwd(q, k, v, offsets, scale: Optional[float] = None, save: bool = False, out=None, lse=None):
     """Causal softmax attention of packed sequences (bf16): q [T, heads, head_dim], k and v [T, kv_heads, head_dim], heads a
     multiple of kv_heads, offsets [B + 1] int32 (a Jagged's offsets); scale: 1 / sqrt(head_dim) by default.  Returns out
     [T, heads, head_dim], or with save=True (out, lse [heads, T] fp32) for causal_attn_bwd.  Rows behind the last sequence are
     left as they were."""
-    p = _causal_problem(q, k, v, offsets, scale, 0, 0)
-    dev = q.get_device()
+    dev = _device()
+    p = _causal_problem(q, k, v, offsets, scale, dev)
     T, H, dh = q.shape
     if out is None:
-        out = torch.empty((T, H, dh), dtype=torch.bfloat16, device=q.device)
-    p.ld_o = _heads("out", out, T, H, dh, torch.bfloat16, dev)
-    if save and lse is None:
-        lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+        out = q.new_empty((T, H, dh))
+    else:
+        p.ld_o = _heads("out", out, T, H, dh, torch.bfloat16, dev)
     if lse is not None:
         _lse(lse, H, T, dev)
-    workspace = _scratch(workspace, hstu.mtgr_causal_attn_workspace_size(p), q)
-    hstu.mtgr_causal_attn_fwd(p, offsets, q, k, v, out, lse, workspace, workspace.numel())
+    elif save:
+        lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+    hstu.mtgr_causal_attn_fwd(p, offsets, q, k, v, out, lse)
     return (out, lse) if save else out
 
 
-def _lse(t, rows: int, cols: int, dev: int) -> None:
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (rows, cols) or not t.is_contiguous():
-        raise ValueError(f"lse is a dense [{rows}, {cols}] of fp32")
-    if t.get_device() != dev:
-        raise ValueError(f"lse is on {t.device}, not on the current device")
+def causal_attn_workspace(q, k, offsets) -> torch.Tensor:
+    """A workspace for causal_attn_bwd of these sizes."""
+    n = hstu.mtgr_causal_attn_workspace_size(_causal_problem(q, k, k, offsets, None, _device()))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
 
 
 def causal_attn_bwd(dout, q, k, v, out, lse, offsets, scale: Optional[float] = None, grads=None, workspace=None):
     """Gradients of causal_attn_fwd for dout, with its out and lse: (dq, dk, dv), in the layouts of q, k and v (`grads`: the
     tensors to write).  Rows behind the last sequence are left as they were."""
-    p = _causal_problem(q, k, v, offsets, scale, 0, 0)
-    bf, dev = torch.bfloat16, q.get_device()
+    bf, dev = torch.bfloat16, _device()
+    p = _causal_problem(q, k, v, offsets, scale, dev)
     p.ld_o, p.ld_do = _heads("out", out, *q.shape, bf, dev), _heads("dout", dout, *q.shape, bf, dev)
     _lse(lse, q.shape[1], q.shape[0], dev)
     dq, dk, dv = grads if grads is not None else (_like_layout(t) for t in (q, k, v))
     _heads("dq", dq, *q.shape, bf, dev, p.ld_q)
     _heads("dk", dk, *k.shape, bf, dev, p.ld_k)
     _heads("dv", dv, *v.shape, bf, dev, p.ld_v)
-    workspace = _scratch(workspace, hstu.mtgr_causal_attn_workspace_size(p, True), q)
+    workspace = _scratch(workspace, hstu.mtgr_causal_attn_workspace_size(p), q)
     hstu.mtgr_causal_attn_bwd(p, offsets, q, k, v, out, lse, dout, dq, dk, dv, workspace, workspace.numel())
     return dq, dk, dv
 
@@ -629,25 +642,30 @@ class KvCache:
 
     def struct(self, dev: int) -> hstu.KvCachePages:
         k, v = self.keys, self.values
-        for name, t in (("keys", k), ("values", v)):
-            if not isinstance(t, torch.Tensor) or t.dim() != 4 or t.dtype is not torch.bfloat16 or not t.is_contiguous():
-                raise ValueError(f"the cache's {name} are a dense [num_pages, kv_heads, page_size, head_dim] of bf16")
+        for t in (k, v):
+            if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.dim() != 4 or not t.is_contiguous():
+                raise ValueError("a cache's keys and values are dense [num_pages, kv_heads, page_size, head_dim] of bf16")
             if t.get_device() != dev:
-                raise ValueError(f"the cache's {name} are on {t.device}, not on the current device")
-        if k.shape != v.shape:
+                raise ValueError(f"the cache is on {t.device}, not on the current device")
+        n, h, size, dh = k.shape
+        if v.shape != (n, h, size, dh):
             raise ValueError(f"keys {list(k.shape)} and values {list(v.shape)} of the cache differ")
-        return hstu.KvCachePages(k.shape[0], k.shape[2], k.shape[1], k.shape[3], 0, k.data_ptr(), v.data_ptr())
+        return hstu.KvCachePages(n, size, h, dh, 0, k.data_ptr(), v.data_ptr())
 
 
 def _page_table(t, dev: int):
     """(num_seqs, max_pages, row stride) of a page table."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype is not torch.int32 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.dim() != 2:
         raise ValueError("page_table is [num_seqs, max_pages] of int32 with dense rows")
     if t.get_device() != dev:
         raise ValueError(f"page_table is on {t.device}, not on the current device")
     B, n = t.shape
-    ld = t.stride(0) if B > 1 else n
-    if ld < n:
+    ld, inner = t.stride()
+    if inner != 1 and n > 1:
+        raise ValueError("page_table is [num_seqs, max_pages] of int32 with dense rows")
+    if B <= 1:
+        ld = n
+    elif ld < n:
         raise ValueError("the rows of page_table overlap")
     return B, n, ld
 
@@ -660,24 +678,27 @@ def kv_append(cache: KvCache, page_table, past, k, v, offsets=None, q=None, rota
     bf, dev = torch.bfloat16, _device()
     c = cache.struct(dev)
     B, pages, ld_table = _page_table(page_table, dev)
-    _vector("past", past, B, (torch.int32,), dev)
-    ld_k = _heads("k", k, None, c.kv_heads, c.head_dim, bf, dev)
+    _int32("past", past, B, dev)
+    Hk, dh = c.kv_heads, c.head_dim
+    ld_k = _heads("k", k, None, Hk, dh, bf, dev)
     N = k.shape[0]
-    ld_v = _heads("v", v, N, c.kv_heads, c.head_dim, bf, dev)
+    ld_v = _heads("v", v, N, Hk, dh, bf, dev)
     if offsets is not None and _sequences(offsets, dev) != B:
         raise ValueError(f"offsets are those of {offsets.numel() - 1} sequences, page_table of {B}")
     H = ld_q = ld_q_out = 0
     if q is not None:
-        ld_q = _heads("q", q, N, None, c.head_dim, bf, dev)
+        ld_q = _heads("q", q, N, None, dh, bf, dev)
         H = q.shape[1]
         if q_out is None:
-            q_out = torch.empty((N, H, c.head_dim), dtype=bf, device=q.device)
-        ld_q_out = _heads("q_out", q_out, N, H, c.head_dim, bf, dev)
+            q_out, ld_q_out = q.new_empty((N, H, dh)), H * dh
+        else:
+            ld_q_out = _heads("q_out", q_out, N, H, dh, bf, dev)
     elif q_out is not None:
         raise ValueError("q_out goes with q")
     rot, layout, amplitude, freqs = 0, 0, 1.0, None
     if rotary is not None:
-        rot, layout, amplitude, freqs = 2 * rotary.freqs.numel(), rotary.code(dev), rotary.amplitude, rotary.freqs
+        freqs = rotary.freqs
+        layout, rot, amplitude = rotary.code(dev), 2 * freqs.numel(), rotary.amplitude
     p = hstu.KvAppendProblem(N, B, H, pages, rot, layout, amplitude, ld_table, ld_q, ld_q_out, ld_k, ld_v)
     hstu.mtgr_kv_append(p, c, page_table, past, offsets, q, k, v, freqs, q_out)
     return q_out
@@ -699,15 +720,20 @@ def cache_attn(q, cache: KvCache, page_table, lens, scale: Optional[float] = Non
     bf, dev = torch.bfloat16, _device()
     c = cache.struct(dev)
     B, pages, ld_table = _page_table(page_table, dev)
-    ld_q = _heads("q", q, B, None, c.head_dim, bf, dev)
+    dh = c.head_dim
+    ld_q = _heads("q", q, B, None, dh, bf, dev)
     H = q.shape[1]
-    _vector("lens", lens, B, (torch.int32,), dev)
+    _int32("lens", lens, B, dev)
     if out is None:
-        out = torch.empty((B, H, c.head_dim), dtype=bf, device=q.device)
+        out, ld_o = q.new_empty((B, H, dh)), H * dh
+    else:
+        ld_o = _heads("out", out, B, H, dh, bf, dev)
     lse = torch.empty((B, H), dtype=torch.float32, device=q.device) if save else None
-    p = hstu.CacheAttnProblem(B, H, pages, c.head_dim ** -0.5 if scale is None else scale,
-                              pages * c.page_size if max_len is None else max_len, ld_table, ld_q,
-                              _heads("out", out, B, H, c.head_dim, bf, dev))
-    workspace = _scratch(workspace, hstu.mtgr_cache_attn_workspace_size(p, c), q)
-    hstu.mtgr_cache_attn(p, c, page_table, lens, q, out, lse, workspace, workspace.numel())
+    p = hstu.CacheAttnProblem(B, H, pages, dh ** -0.5 if scale is None else scale,
+                              pages * c.page_size if max_len is None else max_len, ld_table, ld_q, ld_o)
+    need = hstu.mtgr_cache_attn_workspace_size(p, c)
+    if need or workspace is not None:
+        workspace = _scratch(workspace, need, q)
+        need = workspace.numel()
+    hstu.mtgr_cache_attn(p, c, page_table, lens, q, out, lse, workspace, need)
     return (out, lse) if save else out

@@ -105,8 +105,8 @@ def causal_problem(**kw):
     return hstu.CausalProblem(**p)
 
 
-FWD = dict(offsets=FAKE, q=FAKE, k=FAKE, v=FAKE, out=FAKE, lse=FAKE, workspace=FAKE, workspace_bytes=BIG, stream=0)
-BWD = dict(FWD, dout=FAKE, dq=FAKE, dk=FAKE, dv=FAKE)
+FWD = dict(offsets=FAKE, q=FAKE, k=FAKE, v=FAKE, out=FAKE, lse=FAKE, stream=0)
+BWD = dict(FWD, workspace=FAKE, workspace_bytes=BIG, dout=FAKE, dq=FAKE, dk=FAKE, dv=FAKE)
 
 
 def split(base, kw):

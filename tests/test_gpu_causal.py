@@ -168,7 +168,7 @@ def test_streams_and_graph():
         ops.causal_attn_bwd(dout, q, k, v, out, lse, o, grads=grads, workspace=ws)
 
     out, lse = torch.zeros_like(q), torch.zeros(4, 131, device="cuda")
-    grads, ws = [torch.zeros_like(t) for t in (q, k, v)], ops.causal_attn_workspace(q, k, o, backward=True)
+    grads, ws = [torch.zeros_like(t) for t in (q, k, v)], ops.causal_attn_workspace(q, k, o)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
