@@ -164,32 +164,12 @@ __global__ __launch_bounds__(64 * WAVES, DH == 64 ? 4 : 2) void cache_attn_kerne
         sML[w][0][col] = m;
         sML[w][1][col] = l;
     }
-    // the wave's outputs, [query][feature] fp32
-    float* sO = (float*)sT[w];
-#pragma unroll
-    for (int d = 0; d < DBLK; d++)
-#pragma unroll
-        for (int g = 0; g < 4; g++)
-            if (col < heads) *(float4*)&sO[col * DH + 32 * d + 8 * g + 4 * hh] =
-                make_float4(oacc[d][4 * g], oacc[d][4 * g + 1], oacc[d][4 * g + 2], oacc[d][4 * g + 3]);
+    write_part<DH>(oacc, (float*)sT[w], lane, heads);
     __syncthreads();
     for (int i = tid; i < heads * (DH / 4); i += 64 * WAVES) {
         const int q = i / (DH / 4), f = 4 * (i % (DH / 4));
-        float top = sML[0][0][q];
-#pragma unroll
-        for (int j = 1; j < WAVES; j++) top = fmaxf(top, sML[j][0][q]);
-        float total = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int j = 0; j < WAVES; j++) {
-            const float e = __builtin_amdgcn_exp2f((sML[j][0][q] - top) * a.c);
-            const float4 v = *(const float4*)&((const float*)sT[j])[q * DH + f];
-            total = __builtin_fmaf(e, sML[j][1][q], total);
-            o.x = __builtin_fmaf(e, v.x, o.x);
-            o.y = __builtin_fmaf(e, v.y, o.y);
-            o.z = __builtin_fmaf(e, v.z, o.z);
-            o.w = __builtin_fmaf(e, v.w, o.w);
-        }
+        float top, total;
+        const float4 o = join_parts<DH, WAVES>(sT, sML, q, f / 4, a.c, top, total);
         const long long row = (long long)b * a.H + h0 + q;
         if (a.splits > 1) {
             *(float4*)&a.part[(row * a.splits + split) * DH + f] = o;

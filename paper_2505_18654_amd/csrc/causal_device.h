@@ -11,35 +11,37 @@ constexpr int BM = 128;       // query rows (dK, dV: keys) of a workgroup
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 
-// Sequence of a slot.  The tiles of sequence b take slots floor(o_b / 128) + b on (o: the offsets): at least
-// ceil(n_b / 128) of them lie before those of sequence b + 1, so that a tile's sequence follows from the offsets alone,
-// without a plan, and T / 128 + B slots hold every tile.  The search takes the first entries of 64 ranges at once, a range per
+// Sequence of a slot.  The tiles (of R rows) of sequence b take slots floor(o_b / R) + b on (o: the offsets): at least
+// ceil(n_b / R) of them lie before those of sequence b + 1, so that a tile's sequence follows from the offsets alone,
+// without a plan, and T / R + B slots hold every tile.  The search takes the first entries of 64 ranges at once, a range per
 // lane: two loads one after another for 4,096 sequences.  All lanes get the same result.
 struct Tile {
     int o, n, tile;           // the sequence's first row and length, the tile inside it; no tile: tile < 0
 };
+template <int R = BM>
 __device__ __forceinline__ Tile tile_at(const int* offsets, long long T, int b, int slot) {
     // rows outside 0 .. T-1 are never touched, whatever the offsets hold
     const int o = (int)min(max((long long)offsets[b], 0ll), T), e = (int)min((long long)offsets[b + 1], T);
     Tile t;
     t.o = o;
     t.n = max(e - o, 0);
-    t.tile = slot - (offsets[b] >> 7) - b;
-    if (t.tile >= (t.n + BM - 1) / BM) t.tile = -1;
+    t.tile = slot - offsets[b] / R - b;
+    if (t.tile >= (t.n + R - 1) / R) t.tile = -1;
     return t;
 }
+template <int R = BM>
 __device__ __forceinline__ Tile tile_of_slot(const int* offsets, int B, long long T, int slot) {
     const int lane = threadIdx.x & 63;
     int lo = 0, hi = B;
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-        const bool before = i < hi && (offsets[min(i, B)] >> 7) + i <= slot;
+        const bool before = i < hi && offsets[min(i, B)] / R + i <= slot;
         // (offsets that do not ascend leave the range too, as does a slot before the first sequence's)
         const int k = max(__builtin_popcountll(__ballot(before)), 1) - 1;
         lo = min(lo + k * step, hi - 1);
         hi = min(lo + step, hi);
     }
-    return tile_at(offsets, T, __builtin_amdgcn_readfirstlane(lo), slot);
+    return tile_at<R>(offsets, T, __builtin_amdgcn_readfirstlane(lo), slot);
 }
 
 // Larger (sum) of this lane's value and that of lane ^ 32, in both.
@@ -50,6 +52,43 @@ __device__ __forceinline__ float max_halves(float v) {
 __device__ __forceinline__ float sum_halves(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A wave's transposed outputs (as in store_rows) as [query][feature] fp32 into its LDS tiles, 16-byte pieces swizzled by the
+// query, of the first `queries` alone.
+template <int DH>
+__device__ __forceinline__ int part_chunk(int q, int chunk) { return q * (DH / 4) + (chunk ^ (q & (DH / 4 - 1))); }
+template <int DH>
+__device__ __forceinline__ void write_part(const floatx16 (&acc)[DH / 32], float* part, int lane, int queries) {
+    const int col = lane & 31, hh = lane >> 5;
+    if (col >= queries) return;
+#pragma unroll
+    for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+            *(float4*)&part[4 * part_chunk<DH>(col, 8 * d + 2 * g + hh)] =
+                make_float4(acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2], acc[d][4 * g + 3]);
+}
+// Features 4 f .. 4 f + 3 of query q over the waves' parts, relative to their largest reference score `top`, and their sum.
+template <int DH, int WAVES>
+__device__ __forceinline__ float4 join_parts(const uint16_t (*tiles)[2][32 * DH], const float (*ml)[2][32], int q, int f, float c,
+                                             float& top, float& total) {
+    top = ml[0][0][q];
+#pragma unroll
+    for (int j = 1; j < WAVES; j++) top = fmaxf(top, ml[j][0][q]);
+    total = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < WAVES; j++) {
+        const float e = __builtin_amdgcn_exp2f((ml[j][0][q] - top) * c);
+        const float4 v = *(const float4*)&((const float*)tiles[j])[4 * part_chunk<DH>(q, f)];
+        total = __builtin_fmaf(e, ml[j][1][q], total);
+        o.x = __builtin_fmaf(e, v.x, o.x);
+        o.y = __builtin_fmaf(e, v.y, o.y);
+        o.z = __builtin_fmaf(e, v.z, o.z);
+        o.w = __builtin_fmaf(e, v.w, o.w);
+    }
+    return o;
 }
 
 // A wave's 32 x DH results, transposed in the accumulators (lane: row lane % 32; element 4 g + e of block d: feature

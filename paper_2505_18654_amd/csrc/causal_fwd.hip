@@ -14,21 +14,22 @@ namespace {
 using namespace causal;
 constexpr int BN = 64;        // keys of a tile
 
-// Output rows with infinities or NaN once more, a key after the other: P = 0 of the keys behind a query, times an infinite or
-// NaN value there, is NaN in the products.  Such rows are rare, so that this path is slow (about 0.2 us per row and
-// thousand keys) and costs the others one look at their results.  A lane holds features lane, lane + 64 of the row; finite
-// ones keep what the products gave.
-template <int DH>
-__device__ void redo_rows(const CausalArgs& a, const Tile& at, const uint16_t* sO, int qw, int h, int hk, float m, float inv,
-                          unsigned long long rows, int lane) {
-    constexpr int CPR = DH / 8, F = (DH + 63) / 64;
+// Output rows (a bit each, from row qw on) with infinities or NaN once more, a key after the other: P = 0 of the keys behind a
+// query, times an infinite or NaN value there, is NaN in the products.  Such rows are rare, so that this path is slow (about
+// 0.2 us per row and thousand keys) and costs the others one look at their results.  A lane holds features lane, lane + 64 of
+// the row; elements that are finite keep what the products gave.  stat(r, m, inv): a row's reference score and the
+// reciprocal of its sum.  The rows have been written.
+template <int DH, class Stat>
+__device__ void redo_rows(const CausalArgs& a, const Tile& at, int qw, int h, int hk, uint32_t rows, int lane, Stat stat) {
+    constexpr int F = (DH + 63) / 64;
     const bool has = lane < DH;
-    wait_vmem();                                                 // the rows as they are have been written
     while (rows) {
-        const int r = __builtin_ctzll(rows), i = qw + r;
+        const int r = __builtin_ctz(rows), i = qw + r;
         rows &= rows - 1;
-        const float mc = __shfl(m, r, 64) * a.c, scale = __shfl(inv, r, 64);
+        float m, inv;
+        stat(r, m, inv);
         const uint16_t* Q = (const uint16_t*)a.q + (long long)(at.o + i) * a.ld_q + h * DH;
+        uint16_t* out = (uint16_t*)a.out + (long long)(at.o + i) * a.ld_o + h * DH;
         float q[F], o[F];
 #pragma unroll
         for (int f = 0; f < F; f++) {
@@ -41,16 +42,13 @@ __device__ void redo_rows(const CausalArgs& a, const Tile& at, const uint16_t* s
             float s = 0.f;
 #pragma unroll
             for (int f = 0; f < F; f++) s = __builtin_fmaf(q[f], has ? bf16_to_f32(K[lane + 64 * f]) : 0.f, s);
-            const float p = bf16_to_f32((uint16_t)f32_to_bf16_bits(__builtin_amdgcn_exp2f(__builtin_fmaf(wave_sum(s), a.c, -mc))));
+            const float p = bf16_to_f32((uint16_t)f32_to_bf16_bits(__builtin_amdgcn_exp2f((wave_sum(s) - m) * a.c)));
 #pragma unroll
             for (int f = 0; f < F; f++) o[f] = __builtin_fmaf(p, has ? bf16_to_f32(V[lane + 64 * f]) : 0.f, o[f]);
         }
 #pragma unroll
-        for (int f = 0; f < F; f++) {
-            const int d = lane + 64 * f;
-            if (has && (sO[8 * tile_chunk<CPR>(r, d >> 3) + (d & 7)] & 0x7f80) == 0x7f80)
-                ((uint16_t*)a.out)[(long long)(at.o + i) * a.ld_o + h * DH + d] = (uint16_t)f32_to_bf16_bits(o[f] * scale);
-        }
+        for (int f = 0; f < F; f++)
+            if (has && (out[lane + 64 * f] & 0x7f80) == 0x7f80) out[lane + 64 * f] = (uint16_t)f32_to_bf16_bits(o[f] * inv);
     }
 }
 
@@ -226,20 +224,158 @@ __global__ __launch_bounds__(256, 2) void causal_fwd_kernel(CausalArgs a) {
     const float inv = 1.0f / l;
     uint16_t* sO = sKV[0] + w * 32 * DH;
     store_rows<DH>(oacc, inv, sO, (uint16_t*)a.out + (long long)at.o * a.ld_o + h * DH, a.ld_o, qw, n, lane);
-    if (bad) redo_rows<DH>(a, at, sO, qw, h, hk, m, inv, (bad | (bad >> 32)) & 0xffffffffull, lane);
+    if (bad) {
+        wait_vmem();                                             // the rows as they are have been written
+        redo_rows<DH>(a, at, qw, h, hk, (uint32_t)(bad | (bad >> 32)), lane, [&](int r, float& rm, float& ri) {
+            rm = __shfl(m, r, 64);
+            ri = __shfl(inv, r, 64);
+        });
+    }
+}
+
+// Few query tiles: a workgroup takes 32 query rows of one (sequence, head), and its 8 waves take their halves of 32 keys in
+// turn, each with its own maximum, sum and outputs and its own LDS tiles, joined at the end.  A lone prompt of 700 tokens, 6
+// heads, is 36 workgroups of the kernel above, the last of them 11 tiles one after another.
+template <int DH>
+__global__ __launch_bounds__(512, 2) void causal_fwd_few_kernel(CausalArgs a) {
+    constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, TILE = 32 * DH, NI = CPR / 2, WAVES = 8;
+    __shared__ __align__(16) uint16_t sT[WAVES][2][TILE];        // K and V of each wave; then its outputs
+    __shared__ float sML[WAVES][2][32];
+    __shared__ uint32_t sBad;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, hh = lane >> 5;
+    int id = blockIdx.x;
+    const int hk = id % a.Hk;
+    id /= a.Hk;
+    const int h = hk * a.group + id % a.group;
+    const Tile at = tile_of_slot<32>(a.offsets, a.B, a.T, a.slots - 1 - id / a.group);
+    if (at.tile < 0) return;
+    const int q0 = 32 * at.tile, n = at.n;
+    // 32 rows from row0 on of columns of a matrix; rows behind the sequence are copies of its last one
+    auto copy = [&](const void* src, long long ld, int col0, int row0, int which) {
+        const uint16_t* base = (const uint16_t*)src + (long long)(at.o + row0) * ld + col0;
+        const int last = n - 1 - row0;
+#pragma unroll
+        for (int i = 0; i < NI; i++) {
+            const int row = i * (64 / CPR) + lane / CPR;
+            lds_dma16(lds_address(sT[w][which]) + i * 1024u, uniform_ptr(base),
+                      (uint32_t)(min(row, last) * ld + ((lane % CPR) ^ swz<CPR>(row)) * 8) * 2u);
+        }
+    };
+    auto issue_k = [&](int j) { copy(a.k, a.ld_k, hk * DH, 32 * j, 0); };
+    auto issue_v = [&](int j) { copy(a.v, a.ld_v, hk * DH, 32 * j, 1); };
+    const bool any = w <= at.tile;
+    if (tid == 0) sBad = 0;
+    copy(a.q, a.ld_q, h * DH, q0, 1);
+    if (any) issue_k(w);
+    if (any) wait_vmcnt<NI>(); else wait_vmem();
+    bf16x8 qreg[KSTEPS];
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk++) qreg[kk] = tile_read8<CPR>(sT[w][1], col, 2 * kk + hh);
+    wait_lgkm_seen();
+    if (any) issue_v(w);
+    floatx16 oacc[DBLK];
+#pragma unroll
+    for (int d = 0; d < DBLK; d++) oacc[d] = floatx16{};
+    float m = -3.0e38f, l = 0.f;
+    for (int j = w; j <= at.tile; j += WAVES) {
+        const bool more = j + WAVES <= at.tile;
+        wait_vmcnt<NI>();                                        // K(j)
+        floatx16 s{};
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; kk++)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sT[w][0], col, 2 * kk + hh), qreg[kk], s, 0, 0, 0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // it is read
+        if (more) issue_k(j + WAVES);
+        if (j == at.tile) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) s[e] = 8 * (e >> 2) + 4 * hh + (e & 3) > col ? neg_inf() : s[e];
+        }
+        float top = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; e++) top = fmaxf(top, s[e]);
+        top = fmaxf(max_halves(top), m);
+        if (__any(top > m)) {
+            const float f = __builtin_amdgcn_exp2f((m - top) * a.c);
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DBLK; d++) oacc[d] *= f;
+            m = top;
+        }
+        const float mc = m * a.c;
+        uint32_t pk[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, -mc));
+            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], a.c, -mc));
+            l += p0 + p1;
+            pk[e >> 1] = pack_bf16x2(p0, p1);
+        }
+        if (more) wait_vmcnt<NI>(); else wait_vmem();            // V(j)
+#pragma unroll
+        for (int kq = 0; kq < 2; kq++) {
+            const bf16x8 pb = as_bf16x8(make_uint4(pk[4 * kq], pk[4 * kq + 1], pk[4 * kq + 2], pk[4 * kq + 3]));
+#pragma unroll
+            for (int d = 0; d < DBLK; d++)
+                oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read_tr<CPR>(sT[w][1], 16 * kq, 32 * d, lane), pb, oacc[d], 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) issue_v(j + WAVES);
+    }
+    l = sum_halves(l);
+    if (hh == 0) {
+        sML[w][0][col] = m;
+        sML[w][1][col] = l;
+    }
+    write_part<DH>(oacc, (float*)sT[w], lane, 32);
+    __syncthreads();
+    for (int i = tid; i < 32 * (DH / 4); i += 64 * WAVES) {
+        const int r = i / (DH / 4), f = i % (DH / 4), qi = q0 + r;
+        if (qi >= n) continue;
+        float top, total;
+        const float4 o = join_parts<DH, WAVES>(sT, sML, r, f, a.c, top, total);
+        const float inv = 1.0f / total;
+        *(uint2*)((uint16_t*)a.out + (long long)(at.o + qi) * a.ld_o + h * DH + 4 * f) =
+            make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+        if (f == 0 && a.lse) a.lse[h * a.T + at.o + qi] = top * a.scale + logf(total);
+        if (o.x * 0.f + o.y * 0.f + o.z * 0.f + o.w * 0.f != 0.f) atomicOr(&sBad, 1u << r);
+    }
+    __syncthreads();
+    if (sBad != 0 && w == 0)
+        redo_rows<DH>(a, at, q0, h, hk, __builtin_amdgcn_readfirstlane(sBad), lane, [&](int r, float& rm, float& ri) {
+            float total;
+            join_parts<DH, WAVES>(sT, sML, r, 0, a.c, rm, total);
+            ri = 1.0f / total;
+        });
+}
+
+// Up to so many 32-row tiles (of all heads) the kernel for few is the faster one wherever sequences are long, and as fast where
+// they are short: one of 700 tokens, 6 / 2 heads of 128, 9.9 us, the other kernel 17.8; one of 3,000, 8 heads of 128 (752 tiles),
+// 41 and 59; three of 1,000, 8 / 2 heads of 64, 17.6 and 19.5; eight of 500, 4 / 2 of 128 (532), 15.5 and 15.0.  Above: 32 of 320,
+// 4 heads of 64 (1,408), 21.7 and 10.3.
+constexpr long long FEW_TILES = 1024;
+
+template <int DH>
+hipError_t fwd(CausalArgs a, hipStream_t s) {
+    const long long few = (a.T / 32 + a.B) * a.H;
+    if (few <= FEW_TILES) {
+        a.slots = (int)(a.T / 32 + a.B);
+        causal_fwd_few_kernel<DH><<<(int)few, 512, 0, s>>>(a);
+    } else {
+        causal_fwd_kernel<DH><<<a.slots * a.H, 256, 0, s>>>(a);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_causal_fwd(const CausalArgs& a, int head_dim, hipStream_t s) {
-    const int grid = a.slots * a.H;
     switch (head_dim) {
-        case 32: causal_fwd_kernel<32><<<grid, 256, 0, s>>>(a); break;
-        case 64: causal_fwd_kernel<64><<<grid, 256, 0, s>>>(a); break;
-        case 128: causal_fwd_kernel<128><<<grid, 256, 0, s>>>(a); break;
+        case 32: return fwd<32>(a, s);
+        case 64: return fwd<64>(a, s);
+        case 128: return fwd<128>(a, s);
         default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
 
 }  // namespace mtgr

@@ -25,7 +25,7 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
     unsigned long long* sum64 = (unsigned long long*)(wave_sum + 8);         // 4
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int step = (a.B + PLAN_STARTS - 1) / PLAN_STARTS, starts = (a.B + step - 1) / step;
-    for (int i = tid; i < starts; i += 256) start[i] = (a.offsets[i * step] >> 7) + i * step;
+    for (int i = tid; i < starts; i += 256) start[i] = a.offsets[i * step] / BM + i * step;
     for (int i = tid; i < PLAN_CLASSES; i += 256) count[i] = 0;
     if (tid == 0) *joined = *parted = 0;
     __syncthreads();
@@ -44,7 +44,7 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
         hi = min(lo + step, a.B);
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if ((a.offsets[mid] >> 7) + mid <= slot) lo = mid;
+            if (a.offsets[mid] / BM + mid <= slot) lo = mid;
             else hi = mid;
         }
         return tile_at(a.offsets, a.T, lo, slot);
