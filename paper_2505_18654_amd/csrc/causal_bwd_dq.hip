@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a, CausalP
     const int col = lane & 31, hh = lane >> 5;
     if (blockIdx.x == 0) {
         static_assert(PLAN_LDS * 4 <= 4 * TILE * 2, "the plan fits the tiles");
-        make_plan(a, p, (int*)sKV);
+        make_plan<256>(a, p, (int*)sKV);
         return;
     }
     int id = blockIdx.x - 1;
@@ -178,19 +178,145 @@ __global__ __launch_bounds__(256, 2) void causal_dq_kernel(CausalArgs a, CausalP
     store_rows<DH>(dq, a.scale, sKV[0] + w * 32 * DH, (uint16_t*)a.dq + (long long)at.o * a.ld_q + h * DH, a.ld_q, qw, n, lane);
 }
 
+// Few query tiles, as in the forward: a workgroup takes 32 query rows of one (sequence, head), and its 8 waves their halves
+// of 32 keys in turn, each with its own LDS tiles; their sums are added at the end, in the order of the waves.
+template <int DH>
+__global__ __launch_bounds__(512, 2) void causal_dq_few_kernel(CausalArgs a, CausalPlan p) {
+    constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, TILE = 32 * DH, NI = CPR / 2, WAVES = 8;
+    __shared__ __align__(16) uint16_t sT[WAVES][2][TILE];        // K and V of each wave; then its sums
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, hh = lane >> 5;
+    if (blockIdx.x == 0) {
+        static_assert(PLAN_LDS * 4 <= WAVES * 2 * TILE * 2, "the plan fits the tiles");
+        make_plan<512>(a, p, (int*)sT);
+        return;
+    }
+    int id = blockIdx.x - 1;
+    const int hk = id % a.Hk;
+    id /= a.Hk;
+    const int h = hk * a.group + id % a.group;
+    const Tile at = tile_of_slot<32>(a.offsets, a.B, a.T, (int)(a.T / 32) + a.B - 1 - id / a.group);
+    if (at.tile < 0) return;
+    const int q0 = 32 * at.tile, n = at.n, qr = min(q0 + col, n - 1);
+    // 32 rows from row0 on of columns of a matrix; rows behind the sequence are copies of its last one
+    auto copy = [&](const void* src, long long ld, int col0, int row0, int which) {
+        const uint16_t* base = (const uint16_t*)src + (long long)(at.o + row0) * ld + col0;
+        const int last = n - 1 - row0;
+#pragma unroll
+        for (int i = 0; i < NI; i++) {
+            const int row = i * (64 / CPR) + lane / CPR;
+            lds_dma16(lds_address(sT[w][which]) + i * 1024u, uniform_ptr(base),
+                      (uint32_t)(min(row, last) * ld + ((lane % CPR) ^ swz<CPR>(row)) * 8) * 2u);
+        }
+    };
+    auto issue_k = [&](int j) { copy(a.k, a.ld_k, hk * DH, 32 * j, 0); };
+    auto issue_v = [&](int j) { copy(a.v, a.ld_v, hk * DH, 32 * j, 1); };
+    copy(a.q, a.ld_q, h * DH, q0, 0);
+    copy(a.dout, a.ld_do, h * DH, q0, 1);
+    uint4 o[KSTEPS];
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk++)
+        o[kk] = *(const uint4*)((const uint16_t*)a.out + (long long)(at.o + qr) * a.ld_o + h * DH + 16 * kk + 8 * hh);
+    const float nl = a.lse[h * a.T + at.o + qr] * NEG_LOG2E;
+    wait_vmcnt_seen<0>();
+    bf16x8 qreg[KSTEPS], greg[KSTEPS];
+    float d = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk++) {
+        qreg[kk] = tile_read8<CPR>(sT[w][0], col, 2 * kk + hh);
+        greg[kk] = tile_read8<CPR>(sT[w][1], col, 2 * kk + hh);
+        const uint4 g = __builtin_bit_cast(uint4, greg[kk]);
+        const uint32_t gw[4] = {g.x, g.y, g.z, g.w}, ow[4] = {o[kk].x, o[kk].y, o[kk].z, o[kk].w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            d = __builtin_fmaf(__uint_as_float(gw[i] << 16), __uint_as_float(ow[i] << 16), d);
+            d = __builtin_fmaf(__uint_as_float(gw[i] & 0xffff0000u), __uint_as_float(ow[i] & 0xffff0000u), d);
+        }
+    }
+    wait_lgkm_seen();
+    const bool any = w <= at.tile;
+    if (any) {
+        issue_k(w);
+        issue_v(w);
+    }
+    const float nd = -sum_halves(d);
+    floatx16 dq[DBLK];
+#pragma unroll
+    for (int i = 0; i < DBLK; i++) dq[i] = floatx16{};
+    for (int j = w; j <= at.tile; j += WAVES) {
+        const bool more = j + WAVES <= at.tile;
+        wait_vmem();                                             // K(j), V(j)
+        floatx16 s{}, g;
+#pragma unroll
+        for (int e = 0; e < 16; e++) g[e] = nd;
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; kk++) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sT[w][0], col, 2 * kk + hh), qreg[kk], s, 0, 0, 0);
+            g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sT[w][1], col, 2 * kk + hh), greg[kk], g, 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // V(j) is read
+        if (more) issue_v(j + WAVES);
+        if (j == at.tile) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) s[e] = 8 * (e >> 2) + 4 * hh + (e & 3) > col ? neg_inf() : s[e];
+        }
+        uint32_t pk[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2)
+            pk[e >> 1] = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, nl)) * g[e],
+                                     __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], a.c, nl)) * g[e + 1]);
+#pragma unroll
+        for (int kq = 0; kq < 2; kq++) {
+            const bf16x8 b = as_bf16x8(make_uint4(pk[4 * kq], pk[4 * kq + 1], pk[4 * kq + 2], pk[4 * kq + 3]));
+#pragma unroll
+            for (int i = 0; i < DBLK; i++)
+                dq[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read_tr<CPR>(sT[w][0], 16 * kq, 32 * i, lane), b, dq[i], 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) issue_k(j + WAVES);
+    }
+    if (w == 0 && hh == 0 && q0 + col < n) {
+        a.rows_l[h * a.T + at.o + qr] = nl;
+        a.rows_d[h * a.T + at.o + qr] = nd;
+    }
+    write_part<DH>(dq, (float*)sT[w], lane, 32);
+    __syncthreads();
+    for (int i = tid; i < 32 * (DH / 4); i += 64 * WAVES) {
+        const int r = i / (DH / 4), f = i % (DH / 4);
+        if (q0 + r >= n) continue;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < WAVES; j++) {
+            const float4 v = *(const float4*)&((const float*)sT[j])[4 * part_chunk<DH>(r, f)];
+            x.x += v.x;
+            x.y += v.y;
+            x.z += v.z;
+            x.w += v.w;
+        }
+        *(uint2*)((uint16_t*)a.dq + (long long)(at.o + q0 + r) * a.ld_q + h * DH + 4 * f) =
+            make_uint2(pack_bf16x2(x.x * a.scale, x.y * a.scale), pack_bf16x2(x.z * a.scale, x.w * a.scale));
+    }
+}
+
+template <int DH>
+hipError_t dq(const CausalArgs& a, const CausalPlan& p, hipStream_t s) {
+    const long long few = (a.T / 32 + a.B) * a.H;
+    if (few <= FEW_TILES) causal_dq_few_kernel<DH><<<(int)few + 1, 512, 0, s>>>(a, p);
+    else causal_dq_kernel<DH><<<a.slots * a.H + 1, 256, 0, s>>>(a, p);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 CausalPlan causal_plan(long long T, int B, int H, int Hk, int head_dim) { return make_causal_plan(T, B, H, Hk, head_dim); }
 
 hipError_t launch_causal_dq(const CausalArgs& a, const CausalPlan& p, int head_dim, hipStream_t s) {
-    const int grid = 1 + a.slots * a.H;
     switch (head_dim) {
-        case 32: causal_dq_kernel<32><<<grid, 256, 0, s>>>(a, p); break;
-        case 64: causal_dq_kernel<64><<<grid, 256, 0, s>>>(a, p); break;
-        case 128: causal_dq_kernel<128><<<grid, 256, 0, s>>>(a, p); break;
+        case 32: return dq<32>(a, p, s);
+        case 64: return dq<64>(a, p, s);
+        case 128: return dq<128>(a, p, s);
         default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
 
 }  // namespace mtgr

@@ -9,6 +9,12 @@ namespace causal {
 
 constexpr int BM = 128;       // query rows (dK, dV: keys) of a workgroup
 
+// Up to so many 32-row tiles (of all heads) the kernel for few is the faster one wherever sequences are long, and as fast where
+// they are short: one of 700 tokens, 6 / 2 heads of 128, 9.9 us, the other kernel 17.8; one of 3,000, 8 heads of 128 (752 tiles),
+// 41 and 59; three of 1,000, 8 / 2 heads of 64, 17.6 and 19.5; eight of 500, 4 / 2 of 128 (532), 15.5 and 15.0.  Above: 32 of 320,
+// 4 heads of 64 (1,408), 21.7 and 10.3.
+constexpr long long FEW_TILES = 1024;
+
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 
 // Sequence of a slot.  The tiles (of R rows) of sequence b take slots floor(o_b / R) + b on (o: the offsets): at least

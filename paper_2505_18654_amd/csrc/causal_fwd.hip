@@ -349,12 +349,6 @@ __global__ __launch_bounds__(512, 2) void causal_fwd_few_kernel(CausalArgs a) {
         });
 }
 
-// Up to so many 32-row tiles (of all heads) the kernel for few is the faster one wherever sequences are long, and as fast where
-// they are short: one of 700 tokens, 6 / 2 heads of 128, 9.9 us, the other kernel 17.8; one of 3,000, 8 heads of 128 (752 tiles),
-// 41 and 59; three of 1,000, 8 / 2 heads of 64, 17.6 and 19.5; eight of 500, 4 / 2 of 128 (532), 15.5 and 15.0.  Above: 32 of 320,
-// 4 heads of 64 (1,408), 21.7 and 10.3.
-constexpr long long FEW_TILES = 1024;
-
 template <int DH>
 hipError_t fwd(CausalArgs a, hipStream_t s) {
     const long long few = (a.T / 32 + a.B) * a.H;

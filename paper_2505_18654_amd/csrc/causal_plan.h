@@ -1,7 +1,7 @@
 // The dK / dV kernel's work: items of at most about a thousandth of all units, costliest first.
 //
 // A tile of keys is read by all queries from it to its sequence's end, of every query head that shares its key head, so the
-// first tiles of a long sequence are most of the work of a few workgroups.  Cut into items of at most U = max(64, all units
+// first tiles of a long sequence are most of the work of a few workgroups.  Cut into items of at most U = max(16, all units
 // / 1024) units, and started costliest first (a counting sort), the workgroups end together: 64 sequences with 68,000 tokens,
 // 8 query heads on 2 of 128, PLAN_FIGURES.  One workgroup of the dQ kernel, which runs before, makes
 // the plan.  Which of two items of equal size comes first may differ from run to run; results do not depend on it.
@@ -12,21 +12,23 @@
 namespace mtgr {
 namespace causal {
 
-constexpr int PLAN_CLASSES = 1024, MOST_ITEMS = 1024, LEAST_UNITS = 64, PLAN_STARTS = 2048;
+constexpr int PLAN_CLASSES = 1024, MOST_ITEMS = 1024, LEAST_UNITS = 16, PLAN_STARTS = 2048;
 
-// The workgroup's 256 threads; lds: PLAN_LDS ints.
-constexpr int PLAN_LDS = PLAN_CLASSES + PLAN_STARTS + 16;
+// The workgroup's THREADS threads; lds: PLAN_LDS ints, 8-byte aligned.
+constexpr int PLAN_LDS = PLAN_CLASSES + PLAN_STARTS + 32;
+template <int THREADS>
 __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan& p, int* lds) {
     int* count = lds;                                            // of a class, then its next position
     int* start = lds + PLAN_CLASSES;                             // first slots of every step-th sequence
-    int* wave_sum = start + PLAN_STARTS;                         // 4
-    int* joined = wave_sum + 4;
-    int* parted = wave_sum + 5;
-    unsigned long long* sum64 = (unsigned long long*)(wave_sum + 8);         // 4
+    constexpr int WAVES = THREADS / 64, OWN = PLAN_CLASSES / THREADS;
+    int* wave_sum = start + PLAN_STARTS;                         // 8
+    int* joined = wave_sum + 8;
+    int* parted = wave_sum + 9;
+    unsigned long long* sum64 = (unsigned long long*)(wave_sum + 16);        // 8
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int step = (a.B + PLAN_STARTS - 1) / PLAN_STARTS, starts = (a.B + step - 1) / step;
-    for (int i = tid; i < starts; i += 256) start[i] = a.offsets[i * step] / BM + i * step;
-    for (int i = tid; i < PLAN_CLASSES; i += 256) count[i] = 0;
+    for (int i = tid; i < starts; i += THREADS) start[i] = a.offsets[i * step] / BM + i * step;
+    for (int i = tid; i < PLAN_CLASSES; i += THREADS) count[i] = 0;
     if (tid == 0) *joined = *parted = 0;
     __syncthreads();
     struct Work {
@@ -51,12 +53,14 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
     };
     auto units_of = [&](const Tile& t) { return t.tile < 0 ? 0 : (t.n - t.tile * BM + 31) / 32 * a.group; };
     unsigned long long units = 0;
-    for (int slot = tid; slot < a.slots; slot += 256) units += units_of(tile(slot));
+    for (int slot = tid; slot < a.slots; slot += THREADS) units += units_of(tile(slot));
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) units += __shfl_xor(units, off, 64);
     if (lane == 0) sum64[w] = units;
     __syncthreads();
-    const long long all = (long long)(sum64[0] + sum64[1] + sum64[2] + sum64[3]);
+    long long all = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; i++) all += (long long)sum64[i];
     const int U = (int)max((all * a.Hk + MOST_ITEMS - 1) / MOST_ITEMS, (long long)LEAST_UNITS);
     auto work = [&](int slot) {
         Work x;
@@ -67,15 +71,15 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
         return x;
     };
     auto class_of = [&](const Work& x) { return PLAN_CLASSES - 1 - (int)((long long)(x.size - 1) * PLAN_CLASSES / U); };
-    for (int slot = tid; slot < a.slots; slot += 256) {
+    for (int slot = tid; slot < a.slots; slot += THREADS) {
         const Work x = work(slot);
         if (x.n > 0) atomicAdd(&count[class_of(x)], x.n);
     }
     __syncthreads();
-    // first positions: four classes of a thread, sums over a wave, then over the waves before it
-    int own[4], sum = 0;
+    // first positions: a thread's classes, sums over a wave, then over the waves before it
+    int own[OWN], sum = 0;
 #pragma unroll
-    for (int i = 0; i < 4; i++) sum += own[i] = count[4 * tid + i];
+    for (int i = 0; i < OWN; i++) sum += own[i] = count[OWN * tid + i];
     const int mine = sum;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -86,17 +90,17 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
     __syncthreads();
     int at = sum - mine, total = 0;
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
+    for (int i = 0; i < WAVES; i++) {
         if (i < w) at += wave_sum[i];
         total += wave_sum[i];
     }
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        count[4 * tid + i] = at;
+    for (int i = 0; i < OWN; i++) {
+        count[OWN * tid + i] = at;
         at += own[i];
     }
     __syncthreads();
-    for (int slot = tid; slot < a.slots; slot += 256) {
+    for (int slot = tid; slot < a.slots; slot += THREADS) {
         const Work x = work(slot);
         if (x.n == 0) continue;
         const int first = atomicAdd(&count[class_of(x)], x.n), part = x.n > 1 ? atomicAdd(parted, x.n) : -1;
@@ -121,13 +125,13 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
     __syncthreads();
     CausalItem none{};
     none.tile = -1;
-    for (int i = total + tid; i < p.items; i += 256) a.items[i] = none;
-    for (int i = *joined + tid; i < p.joins; i += 256) a.joins[i] = none;
+    for (int i = total + tid; i < p.items; i += THREADS) a.items[i] = none;
+    for (int i = *joined + tid; i < p.joins; i += THREADS) a.joins[i] = none;
 }
 
 }  // namespace causal
 
-// With u units of a key head in all and U = max(64, u Hk / 1024): tiles of more than U units are at most u / U, their items at
+// With u units of a key head in all and U = max(16, u Hk / 1024): tiles of more than U units are at most u / U, their items at
 // most 2 u / U, all items at most slots + u / U.  A sequence of n tokens has at most (n / 32 + 1) (n / 128 + 1) units per
 // query head.
 inline CausalPlan make_causal_plan(long long T, int B, int H, int Hk, int head_dim) {
