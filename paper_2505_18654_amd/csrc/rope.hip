@@ -1,8 +1,8 @@
 // Rotary positions, alone and on the way into a paged cache.
 //
-// A thread takes one item of a token's heads: 16 bytes of pairs (two 16-byte vectors: features i .. and i + rot / 2 .. in
-// the half layout, neighbours in the interleaved one), or two vectors of features behind rot, which are copied.  It forms the
-// sines and cosines once and applies them to its heads.  Bound by memory: each head is read and written once.
+// A thread takes one item of a token's heads: two 16-byte vectors, features i .. and i + rot / 2 .., which hold whole pairs in
+// both layouts, or two of features behind rot, which are copied.  It forms the sines and cosines once and applies them to its
+// heads.  Bound by memory: each head is read and written once.
 #include "causal_device.h"
 
 namespace mtgr {
@@ -47,27 +47,28 @@ __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
     return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
 }
 
-// Features of an item, and its pairs' sines and cosines.
+// Features of an item, and its pairs' sines and cosines.  Items beside each other take vectors beside each other.
 template <class E>
 struct Item {
     static constexpr int N = Vec<E>::N;
     int e0, e1;               // first features of the two vectors; e1 < 0: only one
     bool turns;
-    float s[N], c[N];
+    float s[N], c[N];         // half layout: of the pairs (e0 + i, e1 + i); interleaved: of e0's N / 2 pairs, then of e1's
     __device__ __forceinline__ Item(const RopeArgs& a, int item, long long position) {
-        const int nrot = a.rot / (2 * N);
+        const int nrot = a.rot / (2 * N), ncopy = (a.dh - a.rot + 2 * N - 1) / (2 * N);
         turns = item < nrot;
         if (!turns) {
-            e0 = a.rot + 2 * N * (item - nrot);
-            e1 = e0 + N < a.dh ? e0 + N : -1;
+            e0 = a.rot + N * (item - nrot);
+            e1 = e0 + N * ncopy < a.dh ? e0 + N * ncopy : -1;
             return;
         }
-        e0 = (a.interleaved ? 2 : 1) * N * item;
-        e1 = e0 + (a.interleaved ? N : a.rot / 2);
+        e0 = N * item;
+        e1 = e0 + a.rot / 2;
         const double p = (double)(a.inverse ? -position : position) * 0.15915494309189533577;   // 1 / 2 pi
 #pragma unroll
         for (int i = 0; i < N; i++) {
-            sincos_turns(p * a.freqs[N * item + i], s[i], c[i]);
+            const int pair = !a.interleaved ? e0 + i : i < N / 2 ? e0 / 2 + i : e1 / 2 + i - N / 2;
+            sincos_turns(p * a.freqs[pair], s[i], c[i]);
             s[i] *= a.amplitude;
             c[i] *= a.amplitude;
         }
@@ -97,10 +98,6 @@ struct Item {
     }
 };
 
-__device__ __forceinline__ int items_of(const RopeArgs& a, int n) {
-    return a.rot / (2 * n) + (a.dh - a.rot + 2 * n - 1) / (2 * n);
-}
-
 // The sequence that row t belongs to; false behind the last one.
 __device__ __forceinline__ bool sequence_of(const int* offsets, int B, long long t, int& b) {
     if (B <= 0 || t >= offsets[B]) return false;
@@ -115,10 +112,13 @@ __device__ __forceinline__ bool sequence_of(const int* offsets, int B, long long
 }
 
 template <class E>
-__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int items, int groups) {
-    const long long i = blockIdx.x * 256ll + threadIdx.x;
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, uint32_t items, uint32_t groups) {
+    // (a block's first thread in 64 bits, the threads of a block from it in 32)
+    const uint32_t per_token = items * groups;
+    const long long first = blockIdx.x * 256ll, t0 = first / per_token;
+    const uint32_t i = (uint32_t)(first - t0 * per_token) + threadIdx.x;
     const int item = (int)(i % items), g = (int)(i / items % groups);
-    const long long t = i / ((long long)items * groups);
+    const long long t = t0 + i / per_token;
     if (t >= a.T) return;
     long long position;
     if (a.positions) {
@@ -134,22 +134,39 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int items, int gr
     const E* x = (const E*)a.x + t * a.ld_x;
     E* out = (E*)a.out + t * a.ld_out;
     const int h1 = (int)((long long)a.heads * (g + 1) / groups);
-    for (int h = (int)((long long)a.heads * g / groups); h < h1; h++) {
-        uint4 u0 = *(const uint4*)(x + h * a.dh + it.e0), u1{};
-        if (it.e1 >= 0) u1 = *(const uint4*)(x + h * a.dh + it.e1);
+    int h = (int)((long long)a.heads * g / groups);
+    const int e1 = it.e1 < 0 ? it.e0 : it.e1;                    // (a lone vector is taken twice)
+    // Two heads at a time: their loads before either's stores, which out = x keeps apart.
+    for (; h + 1 < h1; h += 2) {
+        const E* x0 = x + h * a.dh;
+        E* o0 = out + h * a.dh;
+        uint4 u0 = *(const uint4*)(x0 + it.e0), u1 = *(const uint4*)(x0 + e1), v0 = *(const uint4*)(x0 + a.dh + it.e0), v1 = *(const uint4*)(x0 + a.dh + e1);
+        if (it.turns) {
+            it.turn(u0, u1, a.interleaved);
+            it.turn(v0, v1, a.interleaved);
+        }
+        *(uint4*)(o0 + it.e0) = u0;
+        *(uint4*)(o0 + e1) = u1;
+        *(uint4*)(o0 + a.dh + it.e0) = v0;
+        *(uint4*)(o0 + a.dh + e1) = v1;
+    }
+    if (h < h1) {
+        uint4 u0 = *(const uint4*)(x + h * a.dh + it.e0), u1 = *(const uint4*)(x + h * a.dh + e1);
         if (it.turns) it.turn(u0, u1, a.interleaved);
         *(uint4*)(out + h * a.dh + it.e0) = u0;
-        if (it.e1 >= 0) *(uint4*)(out + h * a.dh + it.e1) = u1;
+        *(uint4*)(out + h * a.dh + e1) = u1;
     }
 }
 
-__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int items, int groups) {
+__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, uint32_t items, uint32_t groups) {
     typedef uint16_t E;
     const RopeArgs& r = a.rope;
     const CacheArgs& cache = a.cache;
-    const long long i = blockIdx.x * 256ll + threadIdx.x;
+    const uint32_t per_token = items * groups;
+    const long long block0 = blockIdx.x * 256ll, t0 = block0 / per_token;
+    const uint32_t i = (uint32_t)(block0 - t0 * per_token) + threadIdx.x;
     const int item = (int)(i % items), g = (int)(i / items % groups);
-    const long long t = i / ((long long)items * groups);
+    const long long t = t0 + i / per_token;
     if (t >= r.T) return;
     int b = (int)t;
     long long at = 0;
@@ -188,16 +205,19 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int items,
     }
 }
 
-// Heads go to so many threads each that a launch has about two waves for each SIMD; a thread's sines serve its heads.
-int head_groups(long long threads, int heads) {
-    return (int)std::min<long long>(heads, std::max<long long>(1, (131072 + threads - 1) / threads));
+// Heads go to so many threads each that a launch has about `most` threads; a thread's sines serve its heads.  For positions four
+// waves for each SIMD (40,000 tokens, 8 heads of 64: 17.7 us, with two 20.8, with eight 18.1; 10,000 of 128: 8.9, 8.9, 12.4), for
+// the append, whose threads also find their page, two (67,200 tokens, 8 + 2 heads of 128: 27.8, with four 29.5).
+constexpr long long ROPE_THREADS = 262144, APPEND_THREADS = 131072;
+int head_groups(long long threads, int heads, long long most) {
+    return (int)std::min<long long>(heads, std::max<long long>(1, (most + threads - 1) / threads));
 }
 
 }  // namespace
 
 hipError_t launch_rope(const RopeArgs& a, bool bf16, hipStream_t s) {
     const int n = bf16 ? 8 : 4, items = a.rot / (2 * n) + (a.dh - a.rot + 2 * n - 1) / (2 * n);
-    const int groups = head_groups(a.T * items, a.heads);
+    const int groups = head_groups(a.T * items, a.heads, ROPE_THREADS);
     const long long blocks = (a.T * items * groups + 255) / 256;
     if (bf16) rope_kernel<uint16_t><<<(unsigned)blocks, 256, 0, s>>>(a, items, groups);
     else rope_kernel<float><<<(unsigned)blocks, 256, 0, s>>>(a, items, groups);
@@ -207,7 +227,7 @@ hipError_t launch_rope(const RopeArgs& a, bool bf16, hipStream_t s) {
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s) {
     const RopeArgs& r = a.rope;
     const int items = r.rot / 16 + (r.dh - r.rot + 15) / 16;
-    const int groups = head_groups(r.T * items, r.heads + 2 * a.cache.kv_heads);
+    const int groups = head_groups(r.T * items, r.heads + 2 * a.cache.kv_heads, APPEND_THREADS);
     const long long blocks = (r.T * items * groups + 255) / 256;
     kv_append_kernel<<<(unsigned)blocks, 256, 0, s>>>(a, items, groups);
     return hipGetLastError();

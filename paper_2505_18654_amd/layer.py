@@ -1,4 +1,7 @@
-"""One MTGR encoder layer (Sec. 4.2) built around the attention path, forward and backward.
+"""One MTGR encoder layer (Sec. 4.2) built around the attention path, forward and backward; the feed-forward block that may
+follow it (ffn_fwd), and a layer of causal softmax attention for next-item models (causal_fwd, causal_prompt, causal_step).
+
+The encoder layer:
 
     Xt = GroupLN_in(X)                                   input Group-LN (u = NULL)
     [Q | K | V | U] = silu(Xt W_in + b_in)               the projection MLPs, one fused GEMM
@@ -150,3 +153,95 @@ def ffn_bwd(dx_out: torch.Tensor, ctx: dict, jag: ops.Jagged, P: FfnParams, rng=
                                                residual=dx_out if one_pass else None)
     g["x"] = dx if one_pass else ops.add(dx, dx_out)
     return g
+
+
+@dataclass
+class CausalParams:
+    gamma: torch.Tensor      # [G, d] fp32, of the input Group-LN
+    beta: torch.Tensor       # [G, d] fp32
+    w_qkv: torch.Tensor      # [d, (heads + 2 kv_heads) head_dim] bf16: columns Q | K | V
+    w_out: torch.Tensor      # [heads head_dim, d] bf16
+    b_out: torch.Tensor      # [d] fp32
+
+
+def _qkv(h: torch.Tensor, heads: int, kv_heads: int):
+    a = h.view(h.shape[0], heads + 2 * kv_heads, -1)
+    return a[:, :heads], a[:, heads:heads + kv_heads], a[:, heads + kv_heads:]
+
+
+def causal_fwd(x: torch.Tensor, jag: ops.Jagged, P: CausalParams, heads: int, kv_heads: int,
+               rotary: Optional[ops.Rotary] = None, eps: float = 1e-5, save: bool = True):
+    """A layer of softmax attention over each user's own past, for next-item training (DynamicEmbedding.item_loss), where
+    the encoder layer's mask would show a token its successors:
+
+        [Q | K | V] = GroupLN(X) W_qkv, Q and K rotated by their tokens' positions (`rotary`)
+        X' = X + causal_attention(Q, K, V) W_out + b_out
+
+    Returns (x_out [T, d], ctx for causal_bwd), with save=False (x_out, None)."""
+    T, d = x.shape
+    xt, m, r = ops.gln_fwd(x, None, jag.seg, P.gamma, P.beta, eps)
+    h = ops.gemm(xt, P.w_qkv, "nn")
+    if rotary is not None:
+        qk = h.view(T, heads + 2 * kv_heads, -1)[:, :heads + kv_heads]
+        ops.rope(qk, rotary, offsets=jag.offsets, out=qk)
+    q, k, v = _qkv(h, heads, kv_heads)
+    o = ops.causal_attn_fwd(q, k, v, jag.offsets, save=save)
+    o, lse = o if save else (o, None)
+    x_out = ops.gemm(o.view(T, -1), P.w_out, "nn", bias=P.b_out, residual=x)
+    return x_out, dict(x=x, xt=xt, m=m, r=r, h=h, o=o, lse=lse) if save else None
+
+
+def causal_bwd(dx_out: torch.Tensor, ctx: dict, jag: ops.Jagged, P: CausalParams, heads: int, kv_heads: int,
+               rotary: Optional[ops.Rotary] = None, eps: float = 1e-5, workspace=None) -> dict:
+    """Gradients of causal_fwd: dict with x and every CausalParams field."""
+    x, xt, h, o = (ctx[n] for n in ("x", "xt", "h", "o"))
+    T, d = x.shape
+    g = {"b_out": torch.empty(d, dtype=torch.float32, device=x.device)}
+    g["w_out"] = ops.gemm(o.view(T, -1), dx_out, "tn", colsum=g["b_out"])
+    do = ops.gemm(dx_out, P.w_out, "nt").view_as(o)
+    dh = torch.empty_like(h)
+    ops.causal_attn_bwd(do, *_qkv(h, heads, kv_heads), o, ctx["lse"], jag.offsets, grads=_qkv(dh, heads, kv_heads),
+                        workspace=workspace)
+    if rotary is not None:
+        dqk = dh.view(T, heads + 2 * kv_heads, -1)[:, :heads + kv_heads]
+        ops.rope(dqk, rotary, offsets=jag.offsets, inverse=True, out=dqk)
+    g["w_qkv"] = ops.gemm(xt, dh, "tn")
+    dxt = ops.gemm(dh, P.w_qkv, "nt")
+    # (one pass adds the residual branch's gradient, unless X is a view with gaps between its rows)
+    one_pass = x.is_contiguous() and dx_out.is_contiguous()
+    dx, _, g["gamma"], g["beta"] = ops.gln_bwd(dxt, x, None, jag.seg, P.gamma, ctx["m"], ctx["r"], eps,
+                                               residual=dx_out if one_pass else None)
+    g["x"] = dx if one_pass else ops.add(dx, dx_out)
+    return g
+
+
+def causal_prompt(x: torch.Tensor, jag: ops.Jagged, P: CausalParams, heads: int, kv_heads: int, cache: ops.KvCache,
+                  page_table: torch.Tensor, rotary: Optional[ops.Rotary] = None, eps: float = 1e-5) -> torch.Tensor:
+    """causal_fwd for serving: the tokens of `jag` are whole prompts, whose keys and values also become the first tokens
+    of their sequences in a paged cache, for causal_step."""
+    T, d = x.shape
+    xt, _, _ = ops.gln_fwd(x, None, jag.seg, P.gamma, P.beta, eps)
+    h = ops.gemm(xt, P.w_qkv, "nn")
+    if rotary is not None:
+        qk = h.view(T, heads + 2 * kv_heads, -1)[:, :heads + kv_heads]
+        ops.rope(qk, rotary, offsets=jag.offsets, out=qk)
+    q, k, v = _qkv(h, heads, kv_heads)
+    past = torch.zeros(jag.num_users, dtype=torch.int32, device=x.device)
+    ops.kv_append(cache, page_table, past, k, v, offsets=jag.offsets)
+    o = ops.causal_attn_fwd(q, k, v, jag.offsets)
+    return ops.gemm(o.view(T, -1), P.w_out, "nn", bias=P.b_out, residual=x)
+
+
+def causal_step(x: torch.Tensor, seg: torch.Tensor, P: CausalParams, heads: int, kv_heads: int, cache: ops.KvCache,
+                page_table: torch.Tensor, past: torch.Tensor, rotary: Optional[ops.Rotary] = None,
+                max_len: Optional[int] = None, eps: float = 1e-5, workspace=None) -> torch.Tensor:
+    """One more token of each of B sequences, x [B, d] with segments seg [B] int8: appended to the cache behind past [B]
+    tokens and run against it.  A sequence whose past is negative is left alone (its row of the result means nothing).
+    max_len bounds past + 1 (ops.cache_attn); with `workspace` (ops.cache_attn_workspace) a step can be captured."""
+    B, d = x.shape
+    xt, _, _ = ops.gln_fwd(x, None, seg, P.gamma, P.beta, eps)
+    h = ops.gemm(xt, P.w_qkv, "nn")
+    q, k, v = _qkv(h, heads, kv_heads)
+    ops.kv_append(cache, page_table, past, k, v, q=q, rotary=rotary, q_out=q)
+    o = ops.cache_attn(q, cache, page_table, past + 1, max_len=max_len, workspace=workspace)
+    return ops.gemm(o.view(B, -1), P.w_out, "nn", bias=P.b_out, residual=x)

@@ -1,0 +1,181 @@
+"""The causal layer: its stages against 64-bit values, its gradients against autograd, a training step of it with the item
+loss, and generation token by token against the whole sequence at once."""
+import pytest
+import torch
+
+from paper_2505_18654_amd import layer, ops
+from paper_2505_18654_amd.embedding import DynamicEmbedding
+from tests.block_ref import U, half_step, within
+from tests.causal_ref import causal, rotate
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def jagged(lengths, seed=1):
+    n = sum(lengths)
+    off = torch.zeros(len(lengths) + 1, dtype=torch.int32)
+    off[1:] = torch.cumsum(torch.tensor(lengths), 0)
+    g = torch.Generator().manual_seed(seed)
+    return ops.Jagged(off.cuda(), torch.randint(0, 4, (n,), generator=g).to(torch.int8).cuda(),
+                      torch.zeros(n, dtype=torch.int32).cuda(), max(lengths, default=0))
+
+
+def params(d, heads, kv, dh, seed=2, groups=4):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s, scale=1.0: torch.randn(s, generator=g) * scale  # noqa: E731
+    return layer.CausalParams((1 + r(groups, d, scale=0.1)).cuda(), r(groups, d, scale=0.1).cuda(),
+                              r(d, (heads + 2 * kv) * dh, scale=d ** -0.5).bfloat16().cuda(),
+                              r(heads * dh, d, scale=(heads * dh) ** -0.5).bfloat16().cuda(), r(d, scale=0.1).cuda())
+
+
+def rows(n, d, seed=3):
+    return torch.randn((n, d), generator=torch.Generator().manual_seed(seed)).bfloat16().cuda()
+
+
+def product(a, b):
+    """a b in 64 bits and the bound of its fp32 sums."""
+    a, b = a.double(), b.double()
+    return a @ b, (a.shape[1] + 4) * U * (a.abs() @ b.abs())
+
+
+@pytest.mark.parametrize("lengths, heads, kv, dh, rot", [([5, 0, 130, 1], 4, 2, 64, 64), ([300], 4, 4, 32, 16), ([77, 90], 2, 1, 128, 0)])
+def test_stages(lengths, heads, kv, dh, rot):
+    d, n = 128, sum(lengths)
+    jag, P, x = jagged(lengths), params(d, heads, kv, dh), rows(n, d)
+    r = ops.rotary(rot) if rot else None
+    y, ctx = layer.causal_fwd(x, jag, P, heads, kv, r)
+    torch.cuda.synchronize()
+    h = ctx["h"].view(n, heads + 2 * kv, dh)
+    want, e = product(ctx["xt"], P.w_qkv)
+    want, e = want.view(h.shape), e.view(h.shape)
+    qk = heads + kv
+    within("v", h[:, qk:], want[:, qk:], half_step(h[:, qk:]) + e[:, qk:])
+    if r is not None:
+        pos = torch.cat([torch.arange(m) for m in lengths]).cuda()
+        first = e[:, :qk] + half_step(want[:, :qk]) * (1 + 2.0 ** -7)          # the product, rounded before it is rotated
+        turned, b = rotate(want[:, :qk], r.freqs, pos)
+        spread, _ = rotate(first.abs(), r.freqs, pos)                          # |a cos| + |b sin| <= |a| + |b|
+        half = rot // 2
+        pair = first.clone()
+        pair[..., :half] = pair[..., half:rot] = first[..., :half] + first[..., half:rot]
+        within("q, k", h[:, :qk], turned, half_step(h[:, :qk]) + (pair + b) * (1 + 2.0 ** -6))
+        assert spread.shape == pair.shape
+    else:
+        within("q, k", h[:, :qk], want[:, :qk], half_step(h[:, :qk]) + e[:, :qk])
+    o, _, eo, _ = causal(h[:, :heads], h[:, heads:qk], h[:, qk:], lengths, dh ** -0.5)
+    within("o", ctx["o"], o, half_step(ctx["o"]) + eo * (1 + 2.0 ** -7))
+    z, e = product(ctx["o"].view(n, -1), P.w_out)
+    z = z + P.b_out.double() + x.double()
+    within("x", y, z, half_step(y) + e + 4 * U * (z.abs() + x.double().abs() + P.b_out.double().abs()))
+    assert torch.equal(layer.causal_fwd(x, jag, P, heads, kv, r, save=False)[0], y)
+
+
+def reference(x, seg, P, lengths, heads, kv, freqs, eps=1e-5):
+    """causal_fwd in 64 bits from leaves that autograd follows."""
+    gamma, beta, w, wo, bo = P
+    xt = (x - x.mean(1, keepdim=True)) * torch.rsqrt(x.var(1, unbiased=False, keepdim=True) + eps) * gamma[seg] + beta[seg]
+    h = (xt @ w).view(len(x), heads + 2 * kv, -1)
+    out, a = [], 0
+    for n in lengths:
+        q, k, v = h[a:a + n, :heads], h[a:a + n, heads:heads + kv], h[a:a + n, heads + kv:]
+        angle = torch.arange(n).double()[:, None, None] * freqs
+        c, s, r = angle.cos(), angle.sin(), len(freqs)
+        turn = lambda t: torch.cat([t[..., :r] * c - t[..., r:2 * r] * s, t[..., :r] * s + t[..., r:2 * r] * c, t[..., 2 * r:]], -1)  # noqa: E731
+        q, k = turn(q), turn(k).repeat_interleave(heads // kv, 1)
+        z = torch.einsum("ihd,jhd->hij", q, k) * q.shape[2] ** -0.5
+        p = torch.softmax(z.masked_fill(torch.ones(n, n, dtype=torch.bool).triu(1), -torch.inf), -1)
+        out.append(torch.einsum("hij,jhd->ihd", p, v.repeat_interleave(heads // kv, 1)).reshape(n, -1))
+        a += n
+    return x + torch.cat(out) @ wo + bo
+
+
+def test_gradients():
+    """Against autograd in 64 bits.  At most eight tensors on the way to a gradient are rounded to bf16 (xt, h, rotated h, o,
+    dO, dh, rotated dh, the result), each by at most 2^-8 of itself, next to P and dS: ten times 2^-8 in the 2-norm."""
+    lengths, heads, kv, dh, d = [50, 1, 77], 4, 2, 32, 128
+    n = sum(lengths)
+    jag, P, x, g = jagged(lengths), params(d, heads, kv, dh), rows(n, d), rows(n, d, 9)
+    r = ops.rotary(32)
+    y, ctx = layer.causal_fwd(x, jag, P, heads, kv, r)
+    got = layer.causal_bwd(g, ctx, jag, P, heads, kv, r)
+    names = ("gamma", "beta", "w_qkv", "w_out", "b_out")
+    leaves = [getattr(P, f).double().cpu().requires_grad_() for f in names]
+    xx = x.double().cpu().requires_grad_()
+    want = reference(xx, jag.seg.long().cpu(), leaves, lengths, heads, kv, r.freqs.cpu())
+    (want * g.double().cpu()).sum().backward()
+    for name, t in [("x", xx), *zip(names, leaves)]:
+        err = (got[name].double().cpu() - t.grad).norm() / t.grad.norm()
+        print(f"[causal layer] {name}: {float(err):.4f}", flush=True)
+        assert err <= 10 * 2.0 ** -8, name
+    assert (y.double().cpu() - want.detach()).norm() / want.detach().norm() <= 5 * 2.0 ** -8
+
+
+def test_training_step_with_the_item_loss():
+    """Lookup, causal layer, item loss and back: every gradient finite, and the same bits twice."""
+    lengths, heads, kv, dh, d = [40, 0, 3, 90], 2, 1, 64, 64
+    jag, P = jagged(lengths), params(d, heads, kv, dh)
+    n = sum(lengths)
+    ids = torch.randint(1, 50, (n,), generator=torch.Generator().manual_seed(4)).cuda()
+    labels = torch.arange(1, n + 1)
+    labels[torch.cumsum(torch.tensor([m for m in lengths if m]), 0) - 1] = -1          # the next position, none behind a sequence
+    table = DynamicEmbedding(row_capacity=256, dim=d, dtype=torch.bfloat16)
+    table.values.copy_((0.3 * torch.randn(256, d, generator=torch.Generator().manual_seed(5))).bfloat16())
+    r, out = ops.rotary(64), []
+    for _ in range(2):
+        x, batch = table.lookup(ids, now=1)
+        y, ctx = layer.causal_fwd(x, jag, P, heads, kv, r)
+        loss, saved = table.item_loss(y, batch, labels.cuda())
+        dy, demb = table.item_loss_bwd(torch.full((n,), 1.0 / int((labels >= 0).sum()), device="cuda"), saved)
+        grads = layer.causal_bwd(dy, ctx, jag, P, heads, kv, r)
+        out.append([loss, y, demb, *grads.values()])
+    assert all(torch.isfinite(t.float()).all() for t in out[0]) and all(torch.equal(a, b) for a, b in zip(*out))
+    assert all(float(t.float().abs().sum()) > 0 for t in out[0])
+
+
+def test_generation():
+    """A prompt, then tokens one by one (captured and replayed), against the layer over the whole sequence: both round their
+    own probabilities and outputs, each at most 2 half steps of bf16 before the output product, and are off by its bound."""
+    lengths, steps, heads, kv, dh, d, page = [33, 5, 140], 4, 4, 2, 64, 128, 16
+    B, P, r = 3, params(d, heads, kv, dh), ops.rotary(64, layout="interleaved")
+    whole = jagged([m + steps for m in lengths])
+    xs = rows(sum(lengths) + B * steps, d)
+    want, ctx = layer.causal_fwd(xs, whole, P, heads, kv, r)
+    o = whole.offsets.tolist()
+    prompt_rows = torch.cat([torch.arange(o[b], o[b] + m) for b, m in enumerate(lengths)]).cuda()
+    off = torch.tensor([0, *torch.cumsum(torch.tensor(lengths), 0)], dtype=torch.int32).cuda()
+    jag = ops.Jagged(off, whole.seg[prompt_rows].contiguous(), whole.ts[prompt_rows].contiguous(), max(lengths))
+    room = max(lengths) + steps
+    cache = ops.KvCache.empty(B * -(-room // page) + 2, kv, page, dh)
+    cache.keys.fill_(float("nan"))
+    cache.values.fill_(float("nan"))
+    table = torch.randperm(B * -(-room // page), generator=torch.Generator().manual_seed(1)).view(B, -1).int().cuda()
+    # o of the two ways is off by the bound of the probabilities' rounding and a half step; through the output product
+    h = ctx["h"].view(len(xs), heads + 2 * kv, dh)
+    _, _, eo, _ = causal(h[:, :heads], h[:, heads:heads + kv], h[:, heads + kv:], [m + steps for m in lengths], dh ** -0.5)
+    eo = 2 * (eo * (1 + 2.0 ** -7) + half_step(ctx["o"]) * (1 + 2.0 ** -7))
+    bound = eo.view(len(xs), -1) @ P.w_out.double().abs() + 2 * product(ctx["o"].view(len(xs), -1), P.w_out)[1]
+    bound = bound + 2 * half_step(want) + 8 * U * (want.double().abs() + 1)
+    got = layer.causal_prompt(xs[prompt_rows].contiguous(), jag, P, heads, kv, cache, table, r)
+    within("prompt", got, want[prompt_rows].double(), bound[prompt_rows])
+    past = torch.tensor(lengths, dtype=torch.int32).cuda()
+    x, seg = torch.zeros((B, d), dtype=torch.bfloat16, device="cuda"), torch.zeros(B, dtype=torch.int8, device="cuda")
+    ws = ops.cache_attn_workspace(cache, B, heads, room)
+    layer.causal_step(x, seg, P, heads, kv, cache, table, torch.full_like(past, -1), r, max_len=room, workspace=ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = layer.causal_step(x, seg, P, heads, kv, cache, table, past, r, max_len=room, workspace=ws)
+        past.add_(1)
+    past.copy_(torch.tensor(lengths, dtype=torch.int32))
+    for i in range(steps):
+        at = torch.tensor([o[b] + m + i for b, m in enumerate(lengths)]).cuda()
+        x.copy_(xs[at])
+        seg.copy_(whole.seg[at])
+        graph.replay()
+        torch.cuda.synchronize()
+        within("step", y, want[at].double(), bound[at])
