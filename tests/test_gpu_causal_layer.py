@@ -125,6 +125,7 @@ def test_training_step_with_the_item_loss():
     labels = torch.arange(1, n + 1)
     labels[torch.cumsum(torch.tensor([m for m in lengths if m]), 0) - 1] = -1          # the next position, none behind a sequence
     table = DynamicEmbedding(row_capacity=256, dim=d, dtype=torch.bfloat16)
+    table.lookup(ids, now=1)                                   # (new rows are zeros)
     table.values.copy_((0.3 * torch.randn(256, d, generator=torch.Generator().manual_seed(5))).bfloat16())
     r, out = ops.rotary(64), []
     for _ in range(2):
