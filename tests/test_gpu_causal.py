@@ -66,6 +66,13 @@ def test_long():
     check([5000], 1, 1, 64)
 
 
+# more tiles than the kernels for few take: sequences around the edges of tiles, cut-up long ones among them
+@pytest.mark.parametrize("H, Hk, dh", [(8, 2, 128), (16, 16, 64), (12, 1, 64), (16, 4, 32)])
+def test_batches(H, Hk, dh):
+    check([1, 1500, 0, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 191, 193, 2, 2000, 300], H, Hk, dh, more=5)
+    check([700] * 6 + [64] * 10, H, Hk, dh, wide=2)
+
+
 def test_many_sequences():
     check([3, 1, 0, 7, 2] * 40, 2, 1, 32)
     check([1, 0, 2] * 1700, 1, 1, 32)                    # the search for a tile's sequence takes three steps
