@@ -20,18 +20,19 @@ __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 // Sequence of a slot.  The tiles (of R rows) of sequence b take slots floor(o_b / R) + b on (o: the offsets): at least
 // ceil(n_b / R) of them lie before those of sequence b + 1, so that a tile's sequence follows from the offsets alone,
 // without a plan, and T / R + B slots hold every tile.  The search takes the first entries of 64 ranges at once, a range per
-// lane: two loads one after another for 4,096 sequences.  All lanes get the same result.
+// lane: two loads one after another for 4,096 sequences.  All lanes get the same result.  B >= 1.
 struct Tile {
     int o, n, tile;           // the sequence's first row and length, the tile inside it; no tile: tile < 0
 };
+// begin, end: the sequence's offsets.
 template <int R = BM>
-__device__ __forceinline__ Tile tile_at(const int* offsets, long long T, int b, int slot) {
+__device__ __forceinline__ Tile tile_at(int begin, int end, long long T, int b, int slot) {
     // rows outside 0 .. T-1 are never touched, whatever the offsets hold
-    const int o = (int)min(max((long long)offsets[b], 0ll), T), e = (int)min((long long)offsets[b + 1], T);
+    const int o = (int)min(max((long long)begin, 0ll), T), e = (int)min((long long)end, T);
     Tile t;
     t.o = o;
     t.n = max(e - o, 0);
-    t.tile = slot - offsets[b] / R - b;
+    t.tile = slot - begin / R - b;
     if (t.tile >= (t.n + R - 1) / R) t.tile = -1;
     return t;
 }
@@ -39,15 +40,19 @@ template <int R = BM>
 __device__ __forceinline__ Tile tile_of_slot(const int* offsets, int B, long long T, int slot) {
     const int lane = threadIdx.x & 63;
     int lo = 0, hi = B;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-        const bool before = i < hi && offsets[min(i, B)] / R + i <= slot;
+    for (;;) {
+        const int step = (hi - lo + 63) >> 6, i = lo + lane * step, o = offsets[min(i, B)];
+        const bool before = i < hi && o / R + i <= slot;
         // (offsets that do not ascend leave the range too, as does a slot before the first sequence's)
-        const int k = max(__builtin_popcountll(__ballot(before)), 1) - 1;
-        lo = min(lo + k * step, hi - 1);
+        const int k = max(__builtin_popcountll(__ballot(before)), 1) - 1, b = min(lo + k * step, hi - 1);
+        if (step == 1) {
+            // the next lane holds the sequence's end, but for the last one
+            const int j = b - lo, end = j < 63 ? __builtin_amdgcn_readlane(o, min(j + 1, 63)) : offsets[b + 1];
+            return tile_at<R>(__builtin_amdgcn_readlane(o, j), end, T, b, slot);
+        }
+        lo = __builtin_amdgcn_readfirstlane(b);
         hi = min(lo + step, hi);
     }
-    return tile_at<R>(offsets, T, __builtin_amdgcn_readfirstlane(lo), slot);
 }
 
 // Larger (sum) of this lane's value and that of lane ^ 32, in both.

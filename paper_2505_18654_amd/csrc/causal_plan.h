@@ -49,7 +49,7 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
             if (a.offsets[mid] / BM + mid <= slot) lo = mid;
             else hi = mid;
         }
-        return tile_at(a.offsets, a.T, lo, slot);
+        return tile_at(a.offsets[lo], a.offsets[lo + 1], a.T, lo, slot);
     };
     auto units_of = [&](const Tile& t) { return t.tile < 0 ? 0 : (t.n - t.tile * BM + 31) / 32 * a.group; };
     unsigned long long units = 0;
