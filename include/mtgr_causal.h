@@ -47,7 +47,7 @@ mtgr_status_t mtgr_rope_frequencies(int32_t rot_dim, double base, mtgr_rope_scal
 typedef struct {
     int64_t num_tokens;       /* T, 0 .. 2^31 - 1 */
     int32_t num_seqs;         /* B, used with offsets */
-    int32_t heads;
+    int32_t heads;            /* 1 .. 65535, here and below */
     int32_t head_dim;         /* a multiple of 8, at most 1024 */
     int32_t rot_dim;          /* a multiple of 16, 16 .. head_dim */
     int32_t layout;           /* mtgr_rope_layout_t */
@@ -58,7 +58,7 @@ typedef struct {
     int64_t ld_out;
 } mtgr_rope_problem_t;
 
-/* x, out [T, heads, head_dim]; out may be x.  freqs [rot_dim / 2] fp64 on the device.  The positions are given [T] int32
+/* x, out [T, heads, head_dim]; out may be x, with the same stride.  freqs [rot_dim / 2] fp64 on the device.  The positions are given [T] int32
  * (of any sign), or, where positions is NULL, follow from offsets: those inside each sequence; rows behind the last
  * sequence are then left as they were.  Exactly one of the two is given. */
 mtgr_status_t mtgr_rope(const mtgr_rope_problem_t* p, const void* x, const int32_t* positions, const int32_t* offsets,
@@ -78,7 +78,7 @@ typedef struct {
     int32_t heads;
     int32_t kv_heads;
     int32_t head_dim;
-    int64_t total_tokens;     /* T, 0 .. 2^31 - 1: rows of the tensors, at least offsets[B] */
+    int64_t total_tokens;     /* T, 0 .. 2^30 - 1: rows of the tensors, at least offsets[B]; T heads below 2^35 */
     float scale;              /* positive and finite, in units of log 2 too */
     int32_t reserved;         /* 0 */
     int64_t ld_q;             /* q and dq */
@@ -135,7 +135,7 @@ typedef struct {
 
 /* Appends new tokens to their sequences: rows offsets[b] .. offsets[b+1]-1 of k and v [N, kv_heads, head_dim] become tokens
  * past[b], past[b] + 1, .. of sequence b; offsets NULL: one token per sequence, N = B.  k is rotated on the way by its
- * token's position in the sequence, and q [N, heads, head_dim] is rotated by the same into q_out (which may be q; both NULL
+ * token's position in the sequence, and q [N, heads, head_dim] is rotated by the same into q_out (which may be q, with the same stride; both NULL
  * without q).  past [B] int32; a sequence whose past is negative is left alone (q_out too), as are tokens past the page
  * table's columns and rows behind the last sequence.  Sequences must not share a page that they write. */
 mtgr_status_t mtgr_kv_append(const mtgr_kv_append_problem_t* p, const mtgr_kv_cache_t* cache, const int32_t* page_table,
@@ -143,11 +143,11 @@ mtgr_status_t mtgr_kv_append(const mtgr_kv_append_problem_t* p, const mtgr_kv_ca
                              const double* freqs, void* q_out, mtgr_stream_t stream);
 
 typedef struct {
-    int32_t num_seqs;         /* B */
+    int32_t num_seqs;         /* B, 0 .. 65535; B heads below 2^27 */
     int32_t heads;
     int32_t max_pages;        /* columns of the page table, >= 1 */
     float scale;              /* as in mtgr_causal_problem_t */
-    int64_t max_len;          /* bound of the lengths, known to the host: 0 .. max_pages page_size */
+    int64_t max_len;          /* bound of the lengths, known to the host: 0 .. max_pages page_size, below 2^31 - 4096 */
     int64_t ld_table;
     int64_t ld_q;
     int64_t ld_o;

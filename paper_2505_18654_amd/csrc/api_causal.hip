@@ -31,6 +31,13 @@ mtgr_status_t check_heads(const void* p, const char* name, int64_t ld, int64_t h
     return MTGR_SUCCESS;
 }
 
+// An output that is its input has its stride too: with another one, rows would be read after others were written over them.
+mtgr_status_t check_in_place(const void* in, int64_t ld_in, const void* out, int64_t ld_out, const char* name) {
+    if (in == out && ld_in != ld_out)
+        return fail(MTGR_ERROR_INVALID_ARGUMENT, "%s in place with token strides %lld and %lld", name, (long long)ld_in, (long long)ld_out);
+    return MTGR_SUCCESS;
+}
+
 mtgr_status_t check_array(const void* p, const char* name, size_t align) {
     if (!p) return fail(MTGR_ERROR_NULL_POINTER, "%s is NULL", name);
     if (!aligned(p, align)) return fail(MTGR_ERROR_INVALID_ARGUMENT, "%s is not aligned to its type", name);
@@ -80,7 +87,8 @@ mtgr_status_t check_causal(const mtgr_causal_problem_t* p) {
     if (!p) return fail(MTGR_ERROR_NULL_POINTER, "problem is NULL");
     if (p->num_seqs < 0) return fail(MTGR_ERROR_INVALID_ARGUMENT, "num_seqs = %d", p->num_seqs);
     if (p->reserved != 0) return fail(MTGR_ERROR_INVALID_ARGUMENT, "reserved = %d", p->reserved);
-    CHECK(check_tokens(p->total_tokens, "total_tokens"));
+    if (p->total_tokens < 0 || p->total_tokens >= (1ll << 30))
+        return fail(MTGR_ERROR_INVALID_ARGUMENT, "total_tokens = %lld outside [0, 2^30)", (long long)p->total_tokens);
     CHECK(check_attn(p->heads, p->kv_heads, p->head_dim, p->scale));
     if ((p->total_tokens / 128 + p->num_seqs) * p->heads >= (1ll << 31) ||
         p->total_tokens * p->heads >= (1ll << 35))
@@ -233,6 +241,7 @@ mtgr_status_t mtgr_rope(const mtgr_rope_problem_t* p, const void* x, const int32
     const int esize = p->dtype == MTGR_DTYPE_BF16 ? 2 : 4;
     CHECK(check_heads(x, "x", p->ld_x, p->heads, p->head_dim, esize));
     CHECK(check_heads(out, "out", p->ld_out, p->heads, p->head_dim, esize));
+    CHECK(check_in_place(x, p->ld_x, out, p->ld_out, "x"));
     if ((positions == nullptr) == (offsets == nullptr))
         return fail(positions ? MTGR_ERROR_INVALID_ARGUMENT : MTGR_ERROR_NULL_POINTER, "either positions or offsets is given");
     CHECK(positions ? check_array(positions, "positions", 4) : check_array(offsets, "offsets", 4));
@@ -340,6 +349,7 @@ mtgr_status_t mtgr_kv_append(const mtgr_kv_append_problem_t* p, const mtgr_kv_ca
     if (p->heads > 0) {
         CHECK(check_heads(q, "q", p->ld_q, p->heads, cache->head_dim));
         CHECK(check_heads(q_out, "q_out", p->ld_q_out, p->heads, cache->head_dim));
+        CHECK(check_in_place(q, p->ld_q, q_out, p->ld_q_out, "q"));
     } else if (q || q_out) {
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "q of 0 heads is given");
     }

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 64 ? 4 : 2) void cache_attn_kerne
     auto entry = [&](int key) { return __builtin_amdgcn_readfirstlane(table[min(key >> cache.page_shift, cache.max_pages - 1)]); };
     const int first = c0 + BN * w;
     const int entry0 = entry(first), entry1 = entry(first + 16);
-    const int len = min(max(a.lens[b], 0), a.max_len), c1 = min(c0 + a.chunk, len);
+    const int len = min(max(a.lens[b], 0), a.max_len), c1 = (int)min((long long)c0 + a.chunk, (long long)len);
     if (c0 >= len && split > 0) {
         wait_vmem();
         return;

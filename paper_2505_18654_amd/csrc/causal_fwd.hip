@@ -17,7 +17,8 @@ constexpr int BN = 64;        // keys of a tile
 // Output rows (a bit each, from row qw on) with infinities or NaN once more, a key after the other: P = 0 of the keys behind a
 // query, times an infinite or NaN value there, is NaN in the products.  Such rows are rare, so that this path is slow (about
 // 0.2 us per row and thousand keys) and costs the others one look at their results.  A lane holds features lane, lane + 64 of
-// the row; elements that are finite keep what the products gave.  stat(r, m, inv): a row's reference score and the
+// the row; elements that are finite keep what the products gave, and a row ends once no other could become finite, so
+// that inputs full of NaN, whose first key decides, take no longer.  stat(r, m, inv): a row's reference score and the
 // reciprocal of its sum.  The rows have been written.
 template <int DH, class Stat>
 __device__ void redo_rows(const CausalArgs& a, const Tile& at, int qw, int h, int hk, uint32_t rows, int lane, Stat stat) {
@@ -31,12 +32,20 @@ __device__ void redo_rows(const CausalArgs& a, const Tile& at, int qw, int h, in
         const uint16_t* Q = (const uint16_t*)a.q + (long long)(at.o + i) * a.ld_q + h * DH;
         uint16_t* out = (uint16_t*)a.out + (long long)(at.o + i) * a.ld_o + h * DH;
         float q[F], o[F];
+        bool redo[F];
 #pragma unroll
         for (int f = 0; f < F; f++) {
             q[f] = has ? bf16_to_f32(Q[lane + 64 * f]) : 0.f;
             o[f] = 0.f;
+            redo[f] = has && (out[lane + 64 * f] & 0x7f80) == 0x7f80;
         }
         for (int j = 0; j <= i; j++) {
+            if (j % 16 == 1) {
+                bool open = false;
+#pragma unroll
+                for (int f = 0; f < F; f++) open |= redo[f] && o[f] * 0.f == 0.f;
+                if (!__any(open)) break;
+            }
             const uint16_t* K = (const uint16_t*)a.k + (long long)(at.o + j) * a.ld_k + hk * DH;
             const uint16_t* V = (const uint16_t*)a.v + (long long)(at.o + j) * a.ld_v + hk * DH;
             float s = 0.f;
@@ -48,7 +57,7 @@ __device__ void redo_rows(const CausalArgs& a, const Tile& at, int qw, int h, in
         }
 #pragma unroll
         for (int f = 0; f < F; f++)
-            if (has && (out[lane + 64 * f] & 0x7f80) == 0x7f80) out[lane + 64 * f] = (uint16_t)f32_to_bf16_bits(o[f] * inv);
+            if (redo[f]) out[lane + 64 * f] = (uint16_t)f32_to_bf16_bits(o[f] * inv);
     }
 }
 

@@ -559,10 +559,10 @@ def mtgr_debug_softmax_loss_kernels(problem, backward: bool, labels: Optional[in
 def mtgr_rope_frequencies(rot_dim: int, base: float, scaling: int = MTGR_ROPE_NONE, factor: float = 1.0, trained_len: int = 0,
                           slow: float = 1.0, fast: float = 32.0):
     """(list of rot_dim / 2 frequencies, amplitude), on the host."""
-    freqs, amplitude = (ctypes.c_double * max(int(rot_dim) // 2, 1))(), ctypes.c_float(0.0)
+    freqs, amplitude = (ctypes.c_double * 512)(), ctypes.c_float(0.0)           # (rot_dim is at most 1,024)
     _check(lib().mtgr_rope_frequencies(int(rot_dim), float(base), int(scaling), float(factor), int(trained_len), float(slow),
                                        float(fast), freqs, ctypes.byref(amplitude)))
-    return list(freqs), amplitude.value
+    return list(freqs[:int(rot_dim) // 2]), amplitude.value
 
 
 def mtgr_rope(problem, x, positions, offsets, freqs, out, stream=None) -> None:

@@ -52,7 +52,7 @@ def rope(**kw):
     (dict(ld_x=1 << 22), UNSUPPORTED), (dict(ld_out=128), INVALID), (dict(x=None), NULL), (dict(out=None), NULL),
     (dict(x=FAKE + 8), INVALID), (dict(positions=None), NULL), (dict(offsets=FAKE), INVALID),
     (dict(positions=FAKE + 2), INVALID), (dict(positions=None, offsets=FAKE + 1), INVALID), (dict(freqs=None), NULL),
-    (dict(freqs=FAKE + 4), INVALID),
+    (dict(freqs=FAKE + 4), INVALID), (dict(ld_out=512), INVALID),            # in place with another stride
 ])
 def test_rope_refused(kw, status):
     assert status_of(rope, **kw) == status
@@ -128,8 +128,8 @@ def causal_bwd(**kw):
 @pytest.mark.parametrize("kw, status", [
     (dict(num_seqs=-1), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID), (dict(kv_heads=3), INVALID),
     (dict(kv_heads=8), INVALID), (dict(head_dim=96), UNSUPPORTED), (dict(head_dim=16), UNSUPPORTED),
-    (dict(head_dim=256), UNSUPPORTED), (dict(total_tokens=-1), INVALID), (dict(total_tokens=1 << 31), INVALID),
-    (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID),
+    (dict(head_dim=256), UNSUPPORTED), (dict(total_tokens=-1), INVALID), (dict(total_tokens=1 << 30), INVALID),
+    (dict(total_tokens=1 << 29, heads=64, kv_heads=64), UNSUPPORTED), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID),
     (dict(scale=3e38), INVALID), (dict(reserved=1), INVALID), (dict(num_seqs=2 ** 31 - 1), UNSUPPORTED),
     (dict(ld_q=255), INVALID), (dict(ld_q=260), INVALID), (dict(ld_k=127), INVALID), (dict(ld_v=1 << 22), UNSUPPORTED),
     (dict(ld_o=248), INVALID), (dict(offsets=None), NULL), (dict(offsets=FAKE + 2), INVALID), (dict(q=None), NULL),
@@ -191,6 +191,7 @@ def test_append_cache_refused(kw, status):
     (dict(ld_k=64), INVALID), (dict(ld_v=132), INVALID), (dict(offsets=None), INVALID), (dict(offsets=FAKE + 2), INVALID),
     (dict(page_table=None), NULL), (dict(past=None), NULL), (dict(past=FAKE + 1), INVALID), (dict(k=None), NULL),
     (dict(v=None), NULL), (dict(q=None), NULL), (dict(q_out=None), NULL), (dict(heads=0), INVALID), (dict(freqs=None), NULL),
+    (dict(ld_q=512), INVALID),
 ])
 def test_append_refused(kw, status):
     assert status_of(append, **kw) == status
@@ -215,6 +216,7 @@ def test_cache_attn_cache_refused(kw, status):
 
 @pytest.mark.parametrize("kw, status", [
     (dict(num_seqs=-1), INVALID), (dict(num_seqs=65536), INVALID), (dict(heads=0), INVALID), (dict(heads=3), INVALID),
+    (dict(num_seqs=4096, heads=32768), UNSUPPORTED),
     (dict(max_pages=0), INVALID), (dict(scale=0.0), INVALID), (dict(scale=NAN), INVALID), (dict(max_len=-1), INVALID),
     (dict(max_len=161), INVALID), (dict(max_pages=1 << 30, ld_table=1 << 30, max_len=1 << 31), INVALID), (dict(ld_table=4), INVALID),
     (dict(ld_q=128), INVALID), (dict(ld_o=252), INVALID), (dict(page_table=None), NULL), (dict(page_table=FAKE + 2), INVALID),
@@ -273,3 +275,87 @@ def test_rotation_of_the_definition(layout):
     assert torch.allclose((at(x, 9) * at(y, 4)).sum(), (at(x, 105) * at(y, 100)).sum())
     assert torch.allclose(at(x, 77).norm(), x.norm()) and torch.allclose(at(at(x, 31), -31), x)
     assert torch.equal(at(x, 5)[..., 16:], x[..., 16:])
+
+
+# ------------------------------------------------------------------ the torch-facing checks
+
+def bf(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("call", [
+    lambda: ops.rope(bf(4, 2, 32), ops.rotary(16, device="cpu"), positions=i32(4)),                      # not on the device
+    lambda: ops.rope(torch.zeros(4, 2, 32, dtype=torch.float16), ops.rotary(16, device="cpu"), positions=i32(4)),
+    lambda: ops.causal_attn_fwd(bf(4, 2, 64), bf(4, 2, 64), bf(4, 2, 64), i32(2)),
+    lambda: ops.causal_attn_fwd(bf(4, 128), bf(4, 2, 64), bf(4, 2, 64), i32(2)),
+    lambda: ops.causal_attn_bwd(bf(4, 2, 64), bf(4, 2, 64), bf(4, 2, 64), bf(4, 2, 64), bf(4, 2, 64), torch.zeros(2, 4), i32(2)),
+    lambda: ops.kv_append(ops.KvCache.empty(2, 1, 16, 32, device="cpu"), i32(1, 2), i32(1), bf(1, 1, 32), bf(1, 1, 32)),
+    lambda: ops.cache_attn(bf(1, 2, 32), ops.KvCache.empty(2, 1, 16, 32, device="cpu"), i32(1, 2), i32(1)),
+])
+def test_operands_refused_before_the_library(call):
+    with pytest.raises((ValueError, TypeError)):
+        call()
+
+
+@pytest.fixture
+def on_cpu(monkeypatch):
+    """The checks as if the CPU were the current device; no entry point of the library is reached."""
+    monkeypatch.setattr(ops, "_device", lambda: -1)
+    for name in ("mtgr_rope", "mtgr_causal_attn_fwd", "mtgr_causal_attn_bwd", "mtgr_kv_append", "mtgr_cache_attn"):
+        monkeypatch.setattr(hstu, name, lambda *a, **k: None)
+
+
+ROT = lambda: ops.rotary(16, device="cpu")  # noqa: E731
+CACHE = lambda: ops.KvCache.empty(3, 2, 16, 32, device="cpu")  # noqa: E731
+
+
+def test_operands_accepted(on_cpu):
+    assert ops.rope(bf(4, 2, 32), ROT(), positions=i32(4)).shape == (4, 2, 32)
+    assert ops.causal_attn_fwd(bf(4, 6, 96)[:, :4, :64].contiguous(), bf(4, 2, 64), bf(4, 2, 64), i32(3)).shape == (4, 4, 64)
+    out = ops.kv_append(CACHE(), i32(3, 2), i32(3), bf(3, 2, 32), bf(3, 2, 32), q=bf(3, 4, 32), rotary=ROT())
+    assert out.shape == (3, 4, 32)
+    assert [t.shape for t in ops.cache_attn(bf(3, 4, 32), CACHE(), i32(3, 2), i32(3), save=True)] == [(3, 4, 32), (3, 4)]
+
+
+@pytest.mark.parametrize("call", [
+    lambda: ops.rope(bf(4, 2, 32), ROT()),
+    lambda: ops.rope(bf(4, 2, 32), ROT(), positions=i32(4), offsets=i32(2)),
+    lambda: ops.rope(bf(4, 2, 32), ROT(), positions=i32(5)),
+    lambda: ops.rope(bf(4, 2, 32), ROT(), positions=torch.zeros(4, dtype=torch.int64)),
+    lambda: ops.rope(bf(4, 2, 32), ROT(), offsets=torch.zeros(0, dtype=torch.int32)),
+    lambda: ops.rope(bf(4, 2, 32), ops.Rotary(torch.zeros(8)), positions=i32(4)),
+    lambda: ops.rope(bf(4, 2, 32), ops.Rotary(ROT().freqs, "diagonal"), positions=i32(4)),
+    lambda: ops.rope(bf(4, 2, 64)[..., ::2], ROT(), positions=i32(4)),
+    lambda: ops.rope(bf(4, 2, 64)[..., :32], ROT(), positions=i32(4)),                     # heads with gaps
+    lambda: ops.rope(bf(1, 2, 32).expand(4, 2, 32), ROT(), positions=i32(4)),              # rows that overlap
+    lambda: ops.rope(bf(4, 2, 32), ROT(), positions=i32(4), out=bf(4, 3, 32)),
+    lambda: ops.causal_attn_fwd(bf(4, 2, 64), bf(5, 2, 64), bf(5, 2, 64), i32(2)),
+    lambda: ops.causal_attn_fwd(bf(4, 2, 64), bf(4, 2, 32), bf(4, 2, 32), i32(2)),
+    lambda: ops.causal_attn_fwd(bf(4, 2, 64), bf(4, 2, 64), bf(4, 1, 64), i32(2)),
+    lambda: ops.causal_attn_fwd(bf(4, 2, 64), bf(4, 2, 64), bf(4, 2, 64), i32(2, 2)),
+    lambda: ops.causal_attn_fwd(bf(4, 2, 64), bf(4, 2, 64), bf(4, 2, 64), i32(2), lse=torch.zeros(4, 2)),
+    lambda: ops.causal_attn_bwd(*[bf(4, 2, 64)] * 5, torch.zeros(4, 2), i32(2)),
+    lambda: ops.causal_attn_bwd(*[bf(4, 2, 64)] * 5, torch.zeros(2, 4), i32(2), grads=(bf(4, 3, 64)[:, :2], bf(4, 2, 64), bf(4, 2, 64))),
+    lambda: ops.KvCache(bf(3, 2, 16, 32), bf(3, 2, 16, 64)).struct(-1),
+    lambda: ops.KvCache(bf(3, 2, 16, 64)[..., :32], bf(3, 2, 16, 32)).struct(-1),
+    lambda: ops.KvCache(torch.zeros(3, 2, 16, 32), torch.zeros(3, 2, 16, 32)).struct(-1),
+    lambda: ops.kv_append(CACHE(), i32(3), i32(3), bf(3, 2, 32), bf(3, 2, 32)),
+    lambda: ops.kv_append(CACHE(), i32(3, 2), i32(2), bf(3, 2, 32), bf(3, 2, 32)),
+    lambda: ops.kv_append(CACHE(), i32(3, 2), i32(3), bf(3, 3, 32), bf(3, 3, 32)),
+    lambda: ops.kv_append(CACHE(), i32(3, 2), i32(3), bf(3, 2, 32), bf(4, 2, 32)),
+    lambda: ops.kv_append(CACHE(), i32(3, 2), i32(3), bf(3, 2, 32), bf(3, 2, 32), offsets=i32(3)),
+    lambda: ops.kv_append(CACHE(), i32(3, 2), i32(3), bf(3, 2, 32), bf(3, 2, 32), q_out=bf(3, 2, 32)),
+    lambda: ops.kv_append(CACHE(), i32(3, 2), i32(3), bf(3, 2, 32), bf(3, 2, 32), q=bf(2, 4, 32)),
+    lambda: ops.cache_attn(bf(2, 4, 32), CACHE(), i32(3, 2), i32(3)),
+    lambda: ops.cache_attn(bf(3, 4, 64), CACHE(), i32(3, 2), i32(3)),
+    lambda: ops.cache_attn(bf(3, 4, 32), CACHE(), i32(3, 2), i32(2)),
+    lambda: ops.cache_attn(bf(3, 4, 32), CACHE(), i32(1, 2).expand(3, 2), i32(3)),
+    lambda: ops.cache_attn(bf(3, 4, 32), CACHE(), i32(3, 2).long(), i32(3)),
+])
+def test_operands_that_do_not_fit(on_cpu, call):
+    with pytest.raises(ValueError):
+        call()

@@ -154,6 +154,16 @@ def test_later_tokens_do_not_matter(n, at, dh):
             assert torch.isnan(out2[at:].float()).all()
 
 
+def test_inputs_of_nan_alone():
+    """Nothing is finite and nothing is redone key by key."""
+    for lengths, H in (([6000], 1), ([6000], 8)):
+        q, k, v, _ = batch(lengths, H, 1, 64)
+        v.fill_(float("nan"))
+        out, lse = ops.causal_attn_fwd(q, k, v, offsets_of(lengths), save=True)
+        torch.cuda.synchronize()
+        assert torch.isnan(out.float()).all() and torch.isfinite(lse).all()
+
+
 def test_nothing():
     q, k, v, dout = batch([], 2, 1, 64)
     out, lse = ops.causal_attn_fwd(q, k, v, offsets_of([]), save=True)
