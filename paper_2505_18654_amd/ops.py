@@ -469,49 +469,49 @@ def softmax_loss_bwd(dloss, x, w, targets, lse, bias=None, scale: float = 1.0, g
 
 # ------------------------------------------------------------------ rotary positions, causal attention, paged cache
 
+# (The checks below run on every call and are a large part of its host time, so their way to success is short and what is
+# wrong is said elsewhere.)
+
+def _refuse(name: str, t, what: str):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} is {what}, got {type(t).__name__}")
+    raise ValueError(f"{name} is {what} on the current device, got {list(t.shape)} of {t.dtype}, strides {list(t.stride())}, on {t.device}")
+
+
 def _heads(name: str, t, tokens: Optional[int], heads: Optional[int], dh: Optional[int], dtype, dev: int,
            like: Optional[int] = None) -> int:
     """Checks a [tokens, heads, head_dim] operand (shape, type, device, dense heads, token rows that do not overlap) and
     returns its token stride; None: any size; `like`: the stride that a gradient shares with its primal."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 3:
-        got = f"{list(t.shape)} {t.dtype}" if isinstance(t, torch.Tensor) else type(t).__name__
-        raise ValueError(f"{name} is [tokens, heads, head_dim] of {dtype}, got {got}")
-    n, h, d = t.shape
-    if (tokens is not None and n != tokens) or (heads is not None and h != heads) or (dh is not None and d != dh):
-        raise ValueError(f"{name} is [{tokens}, {heads}, {dh}], got {[n, h, d]}")
-    if t.get_device() != dev:
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
-    ld, sh, se = t.stride()
-    if (se != 1 and d > 1) or (sh != d and h > 1):
-        raise ValueError(f"the heads of {name} are not dense")
-    if n <= 1:
-        ld = h * d
-    elif ld < h * d:
-        raise ValueError(f"the rows of {name} overlap")
-    if like is not None and ld != like:
-        raise ValueError(f"{name} must share the token stride of its primal")
-    return ld
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == 3 and t.get_device() == dev:
+        n, h, d = t.shape
+        ld, sh, se = t.stride()
+        if (tokens is None or n == tokens) and (heads is None or h == heads) and (dh is None or d == dh) and \
+                (se == 1 or d <= 1) and (sh == d or h <= 1):
+            if n <= 1:
+                ld = h * d
+            if ld >= h * d and (like is None or ld == like):
+                return ld
+            _refuse(name, t, "rows that do not overlap" if like is None else "of the token stride of its primal")
+    _refuse(name, t, f"[{tokens or 'tokens'}, {heads or 'heads'}, {dh or 'head_dim'}] of {dtype} with dense heads")
 
 
 def _int32(name: str, t, n: int, dev: int) -> None:
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError(f"{name} is a dense [{n}] of int32")
-    if t.get_device() != dev:
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.get_device() == dev and t.dim() == 1 and
+            t.shape[0] == n and t.is_contiguous()):
+        _refuse(name, t, f"a dense [{n}] of int32")
 
 
 def _sequences(offsets, dev: int) -> int:
-    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.numel() < 1:
-        raise ValueError("offsets is [B + 1] int32")
-    _int32("offsets", offsets, offsets.numel(), dev)
-    return offsets.numel() - 1
+    if not (isinstance(offsets, torch.Tensor) and offsets.dtype is torch.int32 and offsets.get_device() == dev and
+            offsets.dim() == 1 and offsets.shape[0] >= 1 and offsets.is_contiguous()):
+        _refuse("offsets", offsets, "a dense [B + 1] of int32")
+    return offsets.shape[0] - 1
 
 
 def _lse(t, rows: int, cols: int, dev: int) -> None:
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (rows, cols) or not t.is_contiguous():
-        raise ValueError(f"lse is a dense [{rows}, {cols}] of fp32")
-    if t.get_device() != dev:
-        raise ValueError(f"lse is on {t.device}, not on the current device")
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.float32 and t.get_device() == dev and t.shape == (rows, cols) and
+            t.is_contiguous()):
+        _refuse("lse", t, f"a dense [{rows}, {cols}] of fp32")
 
 
 @dataclass
@@ -525,10 +525,9 @@ class Rotary:
 
     def code(self, dev: int) -> int:
         f = self.freqs
-        if not isinstance(f, torch.Tensor) or f.dtype is not torch.float64 or f.dim() != 1 or not f.is_contiguous():
-            raise ValueError("freqs is a dense [rot_dim / 2] of float64")
-        if f.get_device() != dev:
-            raise ValueError(f"freqs is on {f.device}, not on the current device")
+        if not (isinstance(f, torch.Tensor) and f.dtype is torch.float64 and f.get_device() == dev and f.dim() == 1 and
+                f.is_contiguous()):
+            _refuse("freqs", f, "a dense [rot_dim / 2] of float64")
         if self.layout == "half":
             return hstu.MTGR_ROPE_HALF
         if self.layout == "interleaved":
@@ -642,32 +641,26 @@ class KvCache:
 
     def struct(self, dev: int) -> hstu.KvCachePages:
         k, v = self.keys, self.values
-        for t in (k, v):
-            if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.dim() != 4 or not t.is_contiguous():
-                raise ValueError("a cache's keys and values are dense [num_pages, kv_heads, page_size, head_dim] of bf16")
-            if t.get_device() != dev:
-                raise ValueError(f"the cache is on {t.device}, not on the current device")
-        n, h, size, dh = k.shape
-        if v.shape != (n, h, size, dh):
+        for name, t in (("keys", k), ("values", v)):
+            if not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.get_device() == dev and t.dim() == 4 and
+                    t.is_contiguous()):
+                _refuse(name, t, "a cache's dense [num_pages, kv_heads, page_size, head_dim] of bf16")
+        n, h, size, dh = shape = k.shape
+        if v.shape != shape:
             raise ValueError(f"keys {list(k.shape)} and values {list(v.shape)} of the cache differ")
         return hstu.KvCachePages(n, size, h, dh, 0, k.data_ptr(), v.data_ptr())
 
 
 def _page_table(t, dev: int):
     """(num_seqs, max_pages, row stride) of a page table."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.dim() != 2:
-        raise ValueError("page_table is [num_seqs, max_pages] of int32 with dense rows")
-    if t.get_device() != dev:
-        raise ValueError(f"page_table is on {t.device}, not on the current device")
-    B, n = t.shape
-    ld, inner = t.stride()
-    if inner != 1 and n > 1:
-        raise ValueError("page_table is [num_seqs, max_pages] of int32 with dense rows")
-    if B <= 1:
-        ld = n
-    elif ld < n:
-        raise ValueError("the rows of page_table overlap")
-    return B, n, ld
+    if isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.get_device() == dev and t.dim() == 2:
+        B, n = t.shape
+        ld, inner = t.stride()
+        if B <= 1:
+            ld = n
+        if ld >= n and (inner == 1 or n <= 1):
+            return B, n, ld
+    _refuse("page_table", t, "[num_seqs, max_pages] of int32 with dense rows that do not overlap")
 
 
 def kv_append(cache: KvCache, page_table, past, k, v, offsets=None, q=None, rotary: Optional[Rotary] = None, q_out=None):
