@@ -58,9 +58,9 @@ typedef struct {
     int64_t ld_out;
 } mtgr_rope_problem_t;
 
-/* x, out [T, heads, head_dim]; out may be x, with the same stride.  freqs [rot_dim / 2] fp64 on the device.  The positions are given [T] int32
- * (of any sign), or, where positions is NULL, follow from offsets: those inside each sequence; rows behind the last
- * sequence are then left as they were.  Exactly one of the two is given. */
+/* x, out [T, heads, head_dim]; out may be x, with the same stride.  freqs [rot_dim / 2] fp64 on the device.  The positions
+ * are given [T] int32 (of any sign), or, where positions is NULL, follow from offsets: those inside each sequence; rows
+ * behind the last sequence are then left as they were.  Exactly one of the two is given. */
 mtgr_status_t mtgr_rope(const mtgr_rope_problem_t* p, const void* x, const int32_t* positions, const int32_t* offsets,
                         const double* freqs, void* out, mtgr_stream_t stream);
 
@@ -135,9 +135,9 @@ typedef struct {
 
 /* Appends new tokens to their sequences: rows offsets[b] .. offsets[b+1]-1 of k and v [N, kv_heads, head_dim] become tokens
  * past[b], past[b] + 1, .. of sequence b; offsets NULL: one token per sequence, N = B.  k is rotated on the way by its
- * token's position in the sequence, and q [N, heads, head_dim] is rotated by the same into q_out (which may be q, with the same stride; both NULL
- * without q).  past [B] int32; a sequence whose past is negative is left alone (q_out too), as are tokens past the page
- * table's columns and rows behind the last sequence.  Sequences must not share a page that they write. */
+ * token's position in the sequence, and q [N, heads, head_dim] is rotated by the same into q_out (which may be q, with the
+ * same stride; both NULL without q).  past [B] int32; a sequence whose past is negative is left alone (q_out too), as are
+ * tokens past the page table's columns and rows behind the last sequence.  Sequences must not share a page that they write. */
 mtgr_status_t mtgr_kv_append(const mtgr_kv_append_problem_t* p, const mtgr_kv_cache_t* cache, const int32_t* page_table,
                              const int32_t* past, const int32_t* offsets, const void* q, const void* k, const void* v,
                              const double* freqs, void* q_out, mtgr_stream_t stream);

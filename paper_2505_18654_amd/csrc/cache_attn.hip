@@ -5,7 +5,11 @@
 // sum and outputs, and its own LDS tiles, so that no wave waits for another.  A wave copies the next tile's keys while it
 // works on this one's probabilities, and the next values once this one's are used, so that half of its 32 DH bytes of LDS at least
 // are under way at any time.  The waves are joined through LDS, and the chunks of a sequence, where there are several, by a
-// second kernel.  Bound by the read of the cache.
+// second kernel.  Rounded to bf16 are the probabilities (matrix operands) and the result.
+//
+// Bound by the read of the cache: 24 sequences of up to 131,072 tokens, 32 / 8 heads of 128, 4.78 GB in 836 us, 5.7 TB/s (a
+// device copy: 5.14).  Without the copies ahead 1,227 us.  Less to read is bound by each workgroup's chain of length, pages,
+// keys and values, and by the join: one sequence of 100,003 tokens, 6 / 2 heads, 102 MB in 25 us.
 #include "causal_device.h"
 
 namespace mtgr {

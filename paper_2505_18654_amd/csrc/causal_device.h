@@ -9,10 +9,11 @@ namespace causal {
 
 constexpr int BM = 128;       // query rows (dK, dV: keys) of a workgroup
 
-// Up to so many 32-row tiles (of all heads) the kernel for few is the faster one wherever sequences are long, and as fast where
-// they are short: one of 700 tokens, 6 / 2 heads of 128, 9.9 us, the other kernel 17.8; one of 3,000, 8 heads of 128 (752 tiles),
-// 41 and 59; three of 1,000, 8 / 2 heads of 64, 17.6 and 19.5; eight of 500, 4 / 2 of 128 (532), 15.5 and 15.0.  Above: 32 of 320,
-// 4 heads of 64 (1,408), 21.7 and 10.3.
+// Up to so many 32-row tiles (of all heads) the kernels for few are taken.  They win by far wherever a sequence is long, and
+// lose less where all are short, which the host does not know.  Forward, few and other kernel: one of 700 tokens, 6 / 2 heads of
+// 128, 9.9 and 17.8 us; one of 3,000, 8 heads of 128 (752 tiles), 41 and 59; one of 3,000 beside 31 of 10, 4 heads of 64 (540),
+// 19 and 45; 32 of up to 320 (540), 9.5 and 9.0; 20 of 150, 4 / 2 heads of 128 (452), 11.1 and 8.1.  Above: 32 of 320, 4 heads of
+// 64 (1,408), 21.7 and 10.3.
 constexpr long long FEW_TILES = 1024;
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }

@@ -129,8 +129,9 @@ def causal_bwd(**kw):
     (dict(num_seqs=-1), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID), (dict(kv_heads=3), INVALID),
     (dict(kv_heads=8), INVALID), (dict(head_dim=96), UNSUPPORTED), (dict(head_dim=16), UNSUPPORTED),
     (dict(head_dim=256), UNSUPPORTED), (dict(total_tokens=-1), INVALID), (dict(total_tokens=1 << 30), INVALID),
-    (dict(total_tokens=1 << 29, heads=64, kv_heads=64), UNSUPPORTED), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID),
-    (dict(scale=3e38), INVALID), (dict(reserved=1), INVALID), (dict(num_seqs=2 ** 31 - 1), UNSUPPORTED),
+    (dict(total_tokens=1 << 29, heads=64, kv_heads=64), UNSUPPORTED), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID),
+    (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID), (dict(scale=3e38), INVALID), (dict(reserved=1), INVALID),
+    (dict(num_seqs=2 ** 31 - 1), UNSUPPORTED),
     (dict(ld_q=255), INVALID), (dict(ld_q=260), INVALID), (dict(ld_k=127), INVALID), (dict(ld_v=1 << 22), UNSUPPORTED),
     (dict(ld_o=248), INVALID), (dict(offsets=None), NULL), (dict(offsets=FAKE + 2), INVALID), (dict(q=None), NULL),
     (dict(k=None), NULL), (dict(v=FAKE + 2), INVALID), (dict(out=None), NULL), (dict(lse=FAKE + 2), INVALID),

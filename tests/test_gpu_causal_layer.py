@@ -81,17 +81,21 @@ def reference(x, seg, P, lengths, heads, kv, freqs, eps=1e-5):
     gamma, beta, w, wo, bo = P
     xt = (x - x.mean(1, keepdim=True)) * torch.rsqrt(x.var(1, unbiased=False, keepdim=True) + eps) * gamma[seg] + beta[seg]
     h = (xt @ w).view(len(x), heads + 2 * kv, -1)
-    out, a = [], 0
+    out, at = [], 0
     for n in lengths:
-        q, k, v = h[a:a + n, :heads], h[a:a + n, heads:heads + kv], h[a:a + n, heads + kv:]
+        q, k, v = h[at:at + n].split([heads, kv, kv], 1)
         angle = torch.arange(n).double()[:, None, None] * freqs
         c, s, r = angle.cos(), angle.sin(), len(freqs)
-        turn = lambda t: torch.cat([t[..., :r] * c - t[..., r:2 * r] * s, t[..., :r] * s + t[..., r:2 * r] * c, t[..., 2 * r:]], -1)  # noqa: E731
+
+        def turn(t):
+            a, b = t[..., :r], t[..., r:2 * r]
+            return torch.cat([a * c - b * s, a * s + b * c, t[..., 2 * r:]], -1)
+
         q, k = turn(q), turn(k).repeat_interleave(heads // kv, 1)
         z = torch.einsum("ihd,jhd->hij", q, k) * q.shape[2] ** -0.5
         p = torch.softmax(z.masked_fill(torch.ones(n, n, dtype=torch.bool).triu(1), -torch.inf), -1)
         out.append(torch.einsum("hij,jhd->ihd", p, v.repeat_interleave(heads // kv, 1)).reshape(n, -1))
-        a += n
+        at += n
     return x + torch.cat(out) @ wo + bo
 
 
