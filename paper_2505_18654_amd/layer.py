@@ -20,7 +20,7 @@ gradient.  torch only allocates.
 """
 from __future__ import annotations
 
-from dataclasses import dataclass
+from dataclasses import dataclass, fields
 from typing import Optional
 
 import torch
@@ -164,8 +164,12 @@ class CausalParams:
     b_out: torch.Tensor      # [d] fp32
 
 
+def _rows_of_heads(h: torch.Tensor, n: int) -> torch.Tensor:
+    return h.view(h.shape[0], n, h.shape[1] // n)              # (-1 has no size where there are no rows)
+
+
 def _qkv(h: torch.Tensor, heads: int, kv_heads: int):
-    a = h.view(h.shape[0], heads + 2 * kv_heads, -1)
+    a = _rows_of_heads(h, heads + 2 * kv_heads)
     return a[:, :heads], a[:, heads:heads + kv_heads], a[:, heads + kv_heads:]
 
 
@@ -177,17 +181,18 @@ def causal_fwd(x: torch.Tensor, jag: ops.Jagged, P: CausalParams, heads: int, kv
         [Q | K | V] = GroupLN(X) W_qkv, Q and K rotated by their tokens' positions (`rotary`)
         X' = X + causal_attention(Q, K, V) W_out + b_out
 
-    Returns (x_out [T, d], ctx for causal_bwd), with save=False (x_out, None)."""
+    As for every layer here, the sequences hold all rows of x: jag.offsets ends with T.  Returns (x_out [T, d], ctx for
+    causal_bwd), with save=False (x_out, None)."""
     T, d = x.shape
     xt, m, r = ops.gln_fwd(x, None, jag.seg, P.gamma, P.beta, eps)
     h = ops.gemm(xt, P.w_qkv, "nn")
     if rotary is not None:
-        qk = h.view(T, heads + 2 * kv_heads, -1)[:, :heads + kv_heads]
+        qk = _rows_of_heads(h, heads + 2 * kv_heads)[:, :heads + kv_heads]
         ops.rope(qk, rotary, offsets=jag.offsets, out=qk)
     q, k, v = _qkv(h, heads, kv_heads)
     o = ops.causal_attn_fwd(q, k, v, jag.offsets, save=save)
     o, lse = o if save else (o, None)
-    x_out = ops.gemm(o.view(T, -1), P.w_out, "nn", bias=P.b_out, residual=x)
+    x_out = ops.gemm(o.view(T, P.w_out.shape[0]), P.w_out, "nn", bias=P.b_out, residual=x)
     return x_out, dict(x=x, xt=xt, m=m, r=r, h=h, o=o, lse=lse) if save else None
 
 
@@ -196,14 +201,16 @@ def causal_bwd(dx_out: torch.Tensor, ctx: dict, jag: ops.Jagged, P: CausalParams
     """Gradients of causal_fwd: dict with x and every CausalParams field."""
     x, xt, h, o = (ctx[n] for n in ("x", "xt", "h", "o"))
     T, d = x.shape
+    if T == 0:                                                 # (a product over no tokens is refused)
+        return {"x": torch.empty_like(x), **{f.name: torch.zeros_like(getattr(P, f.name)) for f in fields(P)}}
     g = {"b_out": torch.empty(d, dtype=torch.float32, device=x.device)}
-    g["w_out"] = ops.gemm(o.view(T, -1), dx_out, "tn", colsum=g["b_out"])
+    g["w_out"] = ops.gemm(o.view(T, P.w_out.shape[0]), dx_out, "tn", colsum=g["b_out"])
     do = ops.gemm(dx_out, P.w_out, "nt").view_as(o)
     dh = torch.empty_like(h)
     ops.causal_attn_bwd(do, *_qkv(h, heads, kv_heads), o, ctx["lse"], jag.offsets, grads=_qkv(dh, heads, kv_heads),
                         workspace=workspace)
     if rotary is not None:
-        dqk = dh.view(T, heads + 2 * kv_heads, -1)[:, :heads + kv_heads]
+        dqk = _rows_of_heads(dh, heads + 2 * kv_heads)[:, :heads + kv_heads]
         ops.rope(dqk, rotary, offsets=jag.offsets, inverse=True, out=dqk)
     g["w_qkv"] = ops.gemm(xt, dh, "tn")
     dxt = ops.gemm(dh, P.w_qkv, "nt")
@@ -223,13 +230,13 @@ def causal_prompt(x: torch.Tensor, jag: ops.Jagged, P: CausalParams, heads: int,
     xt, _, _ = ops.gln_fwd(x, None, jag.seg, P.gamma, P.beta, eps)
     h = ops.gemm(xt, P.w_qkv, "nn")
     if rotary is not None:
-        qk = h.view(T, heads + 2 * kv_heads, -1)[:, :heads + kv_heads]
+        qk = _rows_of_heads(h, heads + 2 * kv_heads)[:, :heads + kv_heads]
         ops.rope(qk, rotary, offsets=jag.offsets, out=qk)
     q, k, v = _qkv(h, heads, kv_heads)
     past = torch.zeros(jag.num_users, dtype=torch.int32, device=x.device)
     ops.kv_append(cache, page_table, past, k, v, offsets=jag.offsets)
     o = ops.causal_attn_fwd(q, k, v, jag.offsets)
-    return ops.gemm(o.view(T, -1), P.w_out, "nn", bias=P.b_out, residual=x)
+    return ops.gemm(o.view(T, P.w_out.shape[0]), P.w_out, "nn", bias=P.b_out, residual=x)
 
 
 def causal_step(x: torch.Tensor, seg: torch.Tensor, P: CausalParams, heads: int, kv_heads: int, cache: ops.KvCache,
@@ -244,4 +251,4 @@ def causal_step(x: torch.Tensor, seg: torch.Tensor, P: CausalParams, heads: int,
     q, k, v = _qkv(h, heads, kv_heads)
     ops.kv_append(cache, page_table, past, k, v, q=q, rotary=rotary, q_out=q)
     o = ops.cache_attn(q, cache, page_table, past + 1, max_len=max_len, workspace=workspace)
-    return ops.gemm(o.view(B, -1), P.w_out, "nn", bias=P.b_out, residual=x)
+    return ops.gemm(o.view(B, P.w_out.shape[0]), P.w_out, "nn", bias=P.b_out, residual=x)

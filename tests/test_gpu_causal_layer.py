@@ -120,6 +120,26 @@ def test_gradients():
     assert (y.double().cpu() - want.detach()).norm() / want.detach().norm() <= 5 * 2.0 ** -8
 
 
+def test_no_tokens():
+    """A batch whose sequences are all empty, and one without sequences, in training and serving."""
+    heads, kv, dh, d = 4, 2, 32, 128
+    P, r, x = params(d, heads, kv, dh), ops.rotary(32), rows(0, d)
+    for lengths in ([0, 0], []):
+        jag = jagged(lengths)
+        y, ctx = layer.causal_fwd(x, jag, P, heads, kv, r)
+        g = layer.causal_bwd(y, ctx, jag, P, heads, kv, r)
+        assert y.shape == g["x"].shape == (0, d)
+        for f in ("gamma", "beta", "w_qkv", "w_out", "b_out"):
+            assert g[f].dtype == getattr(P, f).dtype and g[f].shape == getattr(P, f).shape and (g[f] == 0).all()
+        cache = ops.KvCache.empty(2, kv, 16, dh)
+        cache.keys.fill_(3.0)
+        table = torch.zeros((len(lengths), 1), dtype=torch.int32, device="cuda")
+        assert layer.causal_prompt(x, jag, P, heads, kv, cache, table, r).shape == (0, d)
+        assert (cache.keys == 3).all()
+    past, seg = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, dtype=torch.int8, device="cuda")
+    assert layer.causal_step(x, seg, P, heads, kv, cache, table, past, r).shape == (0, d)
+
+
 def test_training_step_with_the_item_loss():
     """Lookup, causal layer, item loss and back: every gradient is finite and there, the products' with the same bits twice."""
     lengths, heads, kv, dh, d = [40, 0, 3, 90], 2, 1, 64, 64
