@@ -45,7 +45,7 @@ mtgr_status_t mtgr_rope_frequencies(int32_t rot_dim, double base, mtgr_rope_scal
                                     int64_t trained_len, double slow, double fast, double* freqs, float* amplitude);
 
 typedef struct {
-    int64_t num_tokens;       /* T, 0 .. 2^31 - 1 */
+    int64_t num_tokens;       /* T, 0 .. 2^31 - 1; T times the 32-byte pieces of a head below 2^32 - 256 */
     int32_t num_seqs;         /* B, used with offsets */
     int32_t heads;            /* 1 .. 65535, here and below */
     int32_t head_dim;         /* a multiple of 8, at most 1024 */
@@ -78,7 +78,8 @@ typedef struct {
     int32_t heads;
     int32_t kv_heads;
     int32_t head_dim;
-    int64_t total_tokens;     /* T, 0 .. 2^30 - 1: rows of the tensors, at least offsets[B]; T heads below 2^35 */
+    int64_t total_tokens;     /* T, 0 .. 2^30 - 1: rows of the tensors, at least offsets[B]; (T / 128 + B) heads below
+                                 2^24 - 2^17 */
     float scale;              /* positive and finite, in units of log 2 too */
     int32_t reserved;         /* 0 */
     int64_t ld_q;             /* q and dq */
@@ -119,7 +120,7 @@ typedef struct {
 } mtgr_kv_cache_t;
 
 typedef struct {
-    int64_t num_tokens;       /* N, rows of q, k, v, 0 .. 2^31 - 1 */
+    int64_t num_tokens;       /* N, rows of q, k, v, limited as T of mtgr_rope */
     int32_t num_seqs;         /* B */
     int32_t heads;            /* of q; 0 without q */
     int32_t max_pages;        /* columns of the page table, >= 1 */
@@ -143,7 +144,7 @@ mtgr_status_t mtgr_kv_append(const mtgr_kv_append_problem_t* p, const mtgr_kv_ca
                              const double* freqs, void* q_out, mtgr_stream_t stream);
 
 typedef struct {
-    int32_t num_seqs;         /* B, 0 .. 65535; B heads below 2^27 */
+    int32_t num_seqs;         /* B, 0 .. 65535; B heads below 2^23 */
     int32_t heads;
     int32_t max_pages;        /* columns of the page table, >= 1 */
     float scale;              /* as in mtgr_causal_problem_t */

@@ -11,6 +11,8 @@ namespace {
 using namespace mtgr_api;
 
 constexpr long long MAX_LD = 1ll << 22;        // 32-bit copy offsets over a tile's rows
+// A launch has fewer than 2^32 threads: 2^24 workgroups of 256.  (The dK / dV kernel takes up to 1,024 + kv_heads more than tiles.)
+constexpr long long MAX_THREADS = (1ll << 32) - 256, MAX_TILES = (1ll << 24) - (1ll << 17);
 
 #define CHECK(call)                                  \
     do {                                             \
@@ -72,6 +74,13 @@ mtgr_status_t check_head_dim(int32_t head_dim) {
     return MTGR_SUCCESS;
 }
 
+// A thread takes 32 bytes of a token's heads.
+mtgr_status_t check_threads(int64_t tokens, int32_t head_dim, int esize) {
+    if (tokens * ((head_dim * esize + 31) / 32) >= MAX_THREADS)
+        return fail(MTGR_ERROR_UNSUPPORTED, "problem too large for one launch");
+    return MTGR_SUCCESS;
+}
+
 mtgr_status_t check_attn(int32_t heads, int32_t kv_heads, int32_t head_dim, float scale) {
     if (heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || heads > 65535)
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "heads = %d, kv_heads = %d", heads, kv_heads);
@@ -83,6 +92,8 @@ mtgr_status_t check_attn(int32_t heads, int32_t kv_heads, int32_t head_dim, floa
     return MTGR_SUCCESS;
 }
 
+long long causal_slots(const mtgr_causal_problem_t* p) { return p->total_tokens / 128 + p->num_seqs; }
+
 mtgr_status_t check_causal(const mtgr_causal_problem_t* p) {
     if (!p) return fail(MTGR_ERROR_NULL_POINTER, "problem is NULL");
     if (p->num_seqs < 0) return fail(MTGR_ERROR_INVALID_ARGUMENT, "num_seqs = %d", p->num_seqs);
@@ -90,13 +101,9 @@ mtgr_status_t check_causal(const mtgr_causal_problem_t* p) {
     if (p->total_tokens < 0 || p->total_tokens >= (1ll << 30))
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "total_tokens = %lld outside [0, 2^30)", (long long)p->total_tokens);
     CHECK(check_attn(p->heads, p->kv_heads, p->head_dim, p->scale));
-    if ((p->total_tokens / 128 + p->num_seqs) * p->heads >= (1ll << 31) ||
-        p->total_tokens * p->heads >= (1ll << 35))
-        return fail(MTGR_ERROR_UNSUPPORTED, "problem too large for one launch");
+    if (causal_slots(p) * p->heads >= MAX_TILES) return fail(MTGR_ERROR_UNSUPPORTED, "problem too large for one launch");
     return MTGR_SUCCESS;
 }
-
-long long causal_slots(const mtgr_causal_problem_t* p) { return p->total_tokens / 128 + p->num_seqs; }
 
 // The backward's workspace: - lse / ln 2 and - delta, then the plan with its sums.
 size_t rows_bytes(const mtgr_causal_problem_t* p) { return align256((size_t)p->heads * (size_t)p->total_tokens * 4); }
@@ -120,6 +127,7 @@ mtgr::CausalArgs causal_args(const mtgr_causal_problem_t* p, const int32_t* offs
     a.slots = (int)causal_slots(p);
     a.scale = p->scale;
     a.c = p->scale * 1.4426950408889634f;
+    a.least = mtgr::least_score(a.c);
     a.offsets = offsets;
     a.q = q;
     a.k = k;
@@ -183,7 +191,7 @@ mtgr_status_t check_cache_attn(const mtgr_cache_attn_problem_t* p, const mtgr_kv
     if (p->num_seqs < 0 || p->num_seqs > 65535)
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "num_seqs = %d outside [0, 65535]", p->num_seqs);
     CHECK(check_attn(p->heads, cache->kv_heads, cache->head_dim, p->scale));
-    if ((int64_t)p->num_seqs * p->heads >= (1ll << 27)) return fail(MTGR_ERROR_UNSUPPORTED, "num_seqs heads is not below 2^27");
+    if ((int64_t)p->num_seqs * p->heads >= (1ll << 23)) return fail(MTGR_ERROR_UNSUPPORTED, "num_seqs heads is not below 2^23");
     if (p->max_pages < 1) return fail(MTGR_ERROR_INVALID_ARGUMENT, "max_pages = %d", p->max_pages);
     if (p->max_len < 0 || p->max_len > (int64_t)p->max_pages * cache->page_size || p->max_len >= (1ll << 31) - 4096)
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "max_len = %lld outside [0, max_pages page_size = %lld] or not below 2^31 - 4096",
@@ -239,6 +247,7 @@ mtgr_status_t mtgr_rope(const mtgr_rope_problem_t* p, const void* x, const int32
     CHECK(check_rotation(p->head_dim, p->rot_dim, p->layout, p->amplitude));
     if (p->num_tokens == 0) return ok();
     const int esize = p->dtype == MTGR_DTYPE_BF16 ? 2 : 4;
+    CHECK(check_threads(p->num_tokens, p->head_dim, esize));
     CHECK(check_heads(x, "x", p->ld_x, p->heads, p->head_dim, esize));
     CHECK(check_heads(out, "out", p->ld_out, p->heads, p->head_dim, esize));
     CHECK(check_in_place(x, p->ld_x, out, p->ld_out, "x"));
@@ -341,6 +350,7 @@ mtgr_status_t mtgr_kv_append(const mtgr_kv_append_problem_t* p, const mtgr_kv_ca
         return fail(MTGR_ERROR_INVALID_ARGUMENT, "without offsets, num_tokens = %lld is num_seqs = %d", (long long)p->num_tokens,
                     p->num_seqs);
     if (p->num_tokens == 0 || p->num_seqs == 0) return ok();
+    CHECK(check_threads(p->num_tokens, cache->head_dim, 2));
     CHECK(check_table(page_table, p->ld_table, p->max_pages));
     CHECK(check_array(past, "past", 4));
     if (offsets) CHECK(check_array(offsets, "offsets", 4));
@@ -410,6 +420,7 @@ mtgr_status_t mtgr_cache_attn(const mtgr_cache_attn_problem_t* p, const mtgr_kv_
     a.max_len = (int)p->max_len;
     a.scale = p->scale;
     a.c = p->scale * 1.4426950408889634f;
+    a.least = mtgr::least_score(a.c);
     a.lens = lens;
     a.q = q;
     a.ld_q = p->ld_q;

@@ -111,7 +111,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 64 ? 4 : 2) void cache_attn_kerne
     floatx16 oacc[DBLK];
 #pragma unroll
     for (int d = 0; d < DBLK; d++) oacc[d] = floatx16{};
-    float m = -3.0e38f, l = 0.f;
+    float m = a.least, l = 0.f;
     while (t.k0 < c1) {
         const Keys next = find(t.k0 + BN * WAVES, false);
         const bool more = next.k0 < c1;
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
     const long long row = (long long)b * a.H + h;
     const int len = min(max(a.lens[b], 0), a.max_len), n = max(1, (len + a.chunk - 1) / a.chunk);
     const float2* ml = a.part_ml + row * a.splits;
-    float top = -3.0e38f;
+    float top = a.least;
     for (int i = tid; i < n; i += 256) top = fmaxf(top, ml[i].x);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
@@ -249,7 +249,7 @@ CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_
     long long chunk = (max_len + want - 1) / want;
     chunk = std::min<long long>(std::max<long long>((chunk + 127) / 128 * 128, 128), 2048);
     if (max_len <= 1024) chunk = 1024;
-    while (units * ((max_len + chunk - 1) / chunk) >= (1ll << 31)) chunk *= 2;
+    while (units * ((max_len + chunk - 1) / chunk) >= (1ll << 24)) chunk *= 2;      // (of a launch; units are below 2^23)
     p.chunk = (int)chunk;
     p.splits = (int)std::max<long long>(1, (max_len + chunk - 1) / chunk);
     p.waves = p.splits == 1 && units <= 256 ? 8 : 4;

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256, 2) void causal_fwd_kernel(CausalArgs a) {
     for (int d = 0; d < DBLK; d++) oacc[d] = floatx16{};
     // Scores are taken relative to m, a score that is at most 8 / c below the largest so far: outputs and sums are rescaled
     // only where a score passes it by more, so that probabilities reach 2^8, which bf16 and fp32 hold as well as 1.
-    float m = -3.0e38f, mc = m * a.c, l0 = 0.f, l1 = 0.f;
+    float m = a.least, mc = m * a.c, l0 = 0.f, l1 = 0.f;
     auto mask = [&](floatx16& s) {                               // on the diagonal: element e is key 8 (e / 4) + 4 hh + e % 4
 #pragma unroll
         for (int e = 0; e < 16; e++) s[e] = 8 * (e >> 2) + 4 * hh + (e & 3) > col ? neg_inf() : s[e];
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(512, 2) void causal_fwd_few_kernel(CausalArgs a) {
     floatx16 oacc[DBLK];
 #pragma unroll
     for (int d = 0; d < DBLK; d++) oacc[d] = floatx16{};
-    float m = -3.0e38f, l = 0.f;
+    float m = a.least, l = 0.f;
     for (int j = w; j <= at.tile; j += WAVES) {
         const bool more = j + WAVES <= at.tile;
         wait_vmcnt<NI>();                                        // K(j)

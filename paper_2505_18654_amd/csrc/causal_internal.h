@@ -43,6 +43,10 @@ struct AppendArgs {
 };
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s);
 
+// The reference that scores start from, below all that count: 3e38 in units of log 2, so that least c is finite (an infinite
+// one met scores of minus infinity as NaN).
+inline float least_score(float c) { return -3.0e38f / std::max(c, 1.0f); }
+
 // Work of the dK / dV kernel (causal_plan.h).  An item is a range of the 32-query units that read a tile of 128 keys; a
 // tile of many units is cut into several, which leave fp32 sums that a second kernel adds up.
 struct CausalItem {
@@ -57,6 +61,7 @@ struct CausalArgs {
     long long T;
     int slots;                // tiles of 128 rows, at most
     float scale, c;           // c = scale / ln 2
+    float least;              // least_score(c)
     const int* offsets;
     const void *q, *k, *v, *dout;
     void* out;                // backward: read
@@ -84,7 +89,7 @@ struct CacheAttnArgs {
     int chunk, splits;        // keys of a workgroup, and how many of them a sequence has at most
     int waves;                // of a workgroup: 4 or 8
     int max_len;
-    float scale, c;
+    float scale, c, least;    // as in CausalArgs
     const int* lens;
     const void* q;
     long long ld_q, ld_o;

@@ -109,7 +109,7 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
         CausalItem item;
         item.o = x.t.o;
         item.n = x.t.n;
-        item.tile = x.t.tile;
+        item.tile = part + x.n <= p.parts ? x.t.tile : -1;       // (within p.parts, as below, for offsets that ascend)
         item.parts = x.n;
         item.pad = 0;
         for (int i = 0; i < x.n; i++) {

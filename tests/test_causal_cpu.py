@@ -45,6 +45,7 @@ def rope(**kw):
 
 @pytest.mark.parametrize("kw, status", [
     (dict(num_tokens=-1), INVALID), (dict(num_tokens=1 << 31), INVALID), (dict(num_seqs=-1), INVALID),
+    (dict(num_tokens=1 << 30), UNSUPPORTED), (dict(num_tokens=1 << 29, dtype=1, ld_x=512), UNSUPPORTED),
     (dict(heads=0), INVALID), (dict(heads=65536), INVALID), (dict(head_dim=60), UNSUPPORTED), (dict(head_dim=0), UNSUPPORTED),
     (dict(head_dim=1032), UNSUPPORTED), (dict(rot_dim=0), UNSUPPORTED), (dict(rot_dim=24), UNSUPPORTED),
     (dict(rot_dim=80), UNSUPPORTED), (dict(rot_dim=-16), UNSUPPORTED), (dict(layout=2), INVALID), (dict(dtype=7), UNSUPPORTED),
@@ -131,7 +132,7 @@ def causal_bwd(**kw):
     (dict(head_dim=256), UNSUPPORTED), (dict(total_tokens=-1), INVALID), (dict(total_tokens=1 << 30), INVALID),
     (dict(total_tokens=1 << 29, heads=64, kv_heads=64), UNSUPPORTED), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID),
     (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID), (dict(scale=3e38), INVALID), (dict(reserved=1), INVALID),
-    (dict(num_seqs=2 ** 31 - 1), UNSUPPORTED),
+    (dict(num_seqs=2 ** 31 - 1), UNSUPPORTED), (dict(num_seqs=(1 << 24) - (1 << 17), heads=1, kv_heads=1), UNSUPPORTED),
     (dict(ld_q=255), INVALID), (dict(ld_q=260), INVALID), (dict(ld_k=127), INVALID), (dict(ld_v=1 << 22), UNSUPPORTED),
     (dict(ld_o=248), INVALID), (dict(offsets=None), NULL), (dict(offsets=FAKE + 2), INVALID), (dict(q=None), NULL),
     (dict(k=None), NULL), (dict(v=FAKE + 2), INVALID), (dict(out=None), NULL), (dict(lse=FAKE + 2), INVALID),
@@ -147,6 +148,14 @@ def test_causal_refused(call, kw, status):
 ])
 def test_causal_backward_refused(kw, status):
     assert status_of(causal_bwd, **kw) == status
+
+
+def test_largest_launch():
+    most = (1 << 24) - (1 << 17)
+    assert hstu.mtgr_causal_attn_workspace_size(causal_problem(num_seqs=most - 1, heads=1, kv_heads=1)) > 0
+    p = hstu.CacheAttnProblem(num_seqs=2048, heads=4094, max_pages=1 << 25, scale=0.125, max_len=(1 << 31) - 4097,
+                              ld_table=1 << 25, ld_q=0, ld_o=0)
+    assert hstu.mtgr_cache_attn_workspace_size(p, pages(page_size=4096, kv_heads=4094)) > 0
 
 
 def test_causal_of_nothing():
@@ -192,7 +201,7 @@ def test_append_cache_refused(kw, status):
     (dict(ld_k=64), INVALID), (dict(ld_v=132), INVALID), (dict(offsets=None), INVALID), (dict(offsets=FAKE + 2), INVALID),
     (dict(page_table=None), NULL), (dict(past=None), NULL), (dict(past=FAKE + 1), INVALID), (dict(k=None), NULL),
     (dict(v=None), NULL), (dict(q=None), NULL), (dict(q_out=None), NULL), (dict(heads=0), INVALID), (dict(freqs=None), NULL),
-    (dict(ld_q=512), INVALID),
+    (dict(ld_q=512), INVALID), (dict(num_tokens=1 << 30), UNSUPPORTED),
 ])
 def test_append_refused(kw, status):
     assert status_of(append, **kw) == status
@@ -217,7 +226,7 @@ def test_cache_attn_cache_refused(kw, status):
 
 @pytest.mark.parametrize("kw, status", [
     (dict(num_seqs=-1), INVALID), (dict(num_seqs=65536), INVALID), (dict(heads=0), INVALID), (dict(heads=3), INVALID),
-    (dict(num_seqs=4096, heads=32768), UNSUPPORTED),
+    (dict(num_seqs=4096, heads=32768), UNSUPPORTED), (dict(num_seqs=4096, heads=2048), UNSUPPORTED),
     (dict(max_pages=0), INVALID), (dict(scale=0.0), INVALID), (dict(scale=NAN), INVALID), (dict(max_len=-1), INVALID),
     (dict(max_len=161), INVALID), (dict(max_pages=1 << 30, ld_table=1 << 30, max_len=1 << 31), INVALID), (dict(ld_table=4), INVALID),
     (dict(ld_q=128), INVALID), (dict(ld_o=252), INVALID), (dict(page_table=None), NULL), (dict(page_table=FAKE + 2), INVALID),

@@ -128,6 +128,19 @@ def test_entries_without_a_page(page, bad):
     compare(q, [k[m] for k, m in zip(ks, keep)], [v[m] for v, m in zip(vs, keep)], out, lse, 0.125)
 
 
+@pytest.mark.parametrize("n, gone", [(300, 40), (3000, 2500)])
+@pytest.mark.parametrize("scale", [0.5, 2.0])
+def test_scores_of_minus_infinity(n, gone, scale):
+    """Keys whose scores are minus infinity, whole tiles and chunks of them, weigh nothing."""
+    c, table, ks, vs = make_cache([n], 2, 32, 64)
+    q = heads((1, 4, 64), 9)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    i = torch.arange(gone, device="cuda")
+    c.keys[table[0].long()[i // 32], :, i % 32, 0] = -torch.inf
+    out, lse = ops.cache_attn(q, c, table, lens_of([n]), scale=scale, save=True)
+    compare(q, [ks[0][gone:]], [vs[0][gone:]], out, lse, scale)
+
+
 def test_table_and_output_strides():
     c, table, ks, vs = make_cache([70, 20], 2, 16, 64)
     big = torch.full((2, table.shape[1] + 5), 9999, dtype=torch.int32, device="cuda")

@@ -154,6 +154,21 @@ def test_later_tokens_do_not_matter(n, at, dh):
             assert torch.isnan(out2[at:].float()).all()
 
 
+@pytest.mark.parametrize("H", [2, 128])          # (the kernels for few tiles and for many)
+@pytest.mark.parametrize("scale", [0.5, 2.0])
+def test_scores_of_minus_infinity(H, scale):
+    """Keys whose scores are minus infinity, a block of 32 of them and more before the first other one, weigh nothing."""
+    n, gone = 300, 70
+    q, k, v, _ = batch([n], H, H, 32)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    k[:gone, :, 0] = -torch.inf
+    out, lse = ops.causal_attn_fwd(q, k, v, offsets_of([n]), scale=scale, save=True)
+    want, wl, eo, el = causal(q[gone:], k[gone:], v[gone:], [n - gone], scale)
+    within("out", out[gone:], want, half_step(out[gone:]) + eo * (1 + 2.0 ** -7))       # (adding a zero rounds nothing)
+    within("lse", lse[:, gone:], wl, el)
+    assert torch.isnan(out[:gone].float()).all()
+
+
 def test_inputs_of_nan_alone():
     """Nothing is finite and nothing is redone key by key."""
     for lengths, H in (([6000], 1), ([6000], 8)):
