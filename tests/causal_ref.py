@@ -87,9 +87,12 @@ def causal(q, k, v, lengths, scale):
     return out, lse, eo, el
 
 
+SUMMED = 128       # a sequence's first rows, whose delta is summed from P dP
+
+
 def causal_back(dout, q, k, v, out, lse, lengths, scale, exact_out=False):
     """{name: (gradient, bound)} for given out and lse; exact_out: their 64-bit values, against a kernel that has them
-    rounded."""
+    rounded.  delta is the sum of dO O, in the first rows that of P dP."""
     T, H, dh = q.shape
     group = H // k.shape[1]
     want = {x: torch.zeros(t.shape, dtype=torch.float64, device=q.device) for x, t in (("dq", q), ("dk", k), ("dv", v))}
@@ -109,11 +112,21 @@ def causal_back(dout, q, k, v, out, lse, lengths, scale, exact_out=False):
             p = (z - L).exp().masked_fill(hidden, 0.0)
             dp, size = G @ V.t().contiguous(), G.abs() @ V.abs().t().contiguous()
             delta, dsize = (G * O).sum(1, keepdim=True), (G * O).abs().sum(1, keepdim=True)
-            ds = p * (dp - delta)
             ep = dz + 8 * U * (L.abs() + 1)                                   # of p, relative; the lse's own rounding
-            ed = (dh + 4) * U * (size + dsize) + 2 * U * (dp.abs() + delta.abs())
+            # The kernel's sum of P (dP - delta'), delta' from the rounded out, is off by that of P's and dP's errors and by its
+            # own additions; what the sum of its P is off 1 by multiplies what delta' lacks.
+            first = torch.arange(n, device=q.device)[:, None] < SUMMED
+            soft = torch.softmax(z.masked_fill(hidden, -math.inf), 1)
+            summed = (soft * dp).sum(1, keepdim=True)
+            lacks, near = (summed - delta).abs() + (G.abs() * half_step(O)).sum(1, keepdim=True), soft * (dp - summed).abs()
+            es = (soft * (dh + 4) * U * (size + dsize) + (2 * ep + (n + 8) * U) * near).sum(1, keepdim=True)
+            es = es + (4 * ep.amax(1, keepdim=True) + (n + 16) * U) * lacks          # (the lse's error too)
+            delta = torch.where(first, summed, delta)
+            ds = p * (dp - delta)
+            ed = (dh + 4) * U * (size + dsize) + 2 * U * (dp.abs() + delta.abs()) + torch.where(first, es, 0.0)
             if exact_out:
-                ed = ed + (G.abs() * half_step(O)).sum(1, keepdim=True)       # delta is formed from the rounded out
+                # (delta is formed from the rounded out)
+                ed = ed + torch.where(first, 0.0, (G.abs() * half_step(O)).sum(1, keepdim=True))
                 ep = ep + 4 * U * L.abs()
             e = p * (2 * ep * (dp - delta).abs() + ed) + B16 * ds.abs()       # dS is rounded to bf16
             sums = (H * n + 40) * U
