@@ -152,6 +152,24 @@ def test_table_and_output_strides():
     assert torch.equal(out, ops.cache_attn(q, c, table, lens_of([70, 20]))) and torch.equal(whole[:, 4:], rest)
 
 
+def test_pages_past_32_bits():
+    """The last pages of a cache of 2^32 elements and more, against a small cache."""
+    dh, page, n = 128, 4096, 5000
+    small, table, ks, vs = make_cache([n], 1, page, dh, spare=0)
+    many = (1 << 32) // (page * dh) + 4
+    big = ops.KvCache.empty(many, 1, page, dh)
+    last = torch.tensor([[many - 1, many - 3]], dtype=torch.int32).cuda()
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ops.kv_append(big, last, zero, ks[0], vs[0], offsets=offsets_of([n]))
+    for i in range(2):
+        rows = min(page, n - i * page)
+        for a, b in ((big.keys, small.keys), (big.values, small.values)):
+            assert torch.equal(a[int(last[0, i]), :, :rows], b[int(table[0, i]), :, :rows])
+    q = heads((1, 2, dh), 4)
+    a, b = (ops.cache_attn(q, c, t, lens_of([n]), save=True) for c, t in ((big, last), (small, table)))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 def test_no_sequences():
     c = ops.KvCache.empty(1, 1, 16, 64)
     table = torch.zeros((0, 3), dtype=torch.int32, device="cuda")

@@ -99,6 +99,32 @@ def test_falling_and_rising_scores():
         within("lse", lse, wl, el)
 
 
+@pytest.mark.parametrize("H, lengths", [(2, [500, 600]), (32, [1100])])
+def test_offsets_past_32_bits(H, lengths):
+    """Rows that lie 2^22 - 8 elements apart, the last ones 2^32 elements and more behind the first, against dense ones."""
+    n, ld, dh = sum(lengths), (1 << 22) - 8, 32
+    q, k, v, dout = batch(lengths, H, H, dh)
+    o = offsets_of(lengths)
+    out, lse = ops.causal_attn_fwd(q, k, v, o, save=True)
+    want = ops.causal_attn_bwd(dout, q, k, v, out, lse, o)
+
+    def far():
+        room = torch.empty((n - 1) * ld + 5 * H * dh, dtype=torch.bfloat16, device="cuda")
+        return [room.as_strided((n, H, dh), (ld, dh, 1), i * H * dh) for i in range(5)]
+
+    q2, k2, v2, dout2, out2 = far()
+    for a, b in ((q2, q), (k2, k), (v2, v), (dout2, dout)):
+        a.copy_(b)
+    _, lse2 = ops.causal_attn_fwd(q2, k2, v2, o, save=True, out=out2)
+    assert torch.equal(out2, out) and torch.equal(lse2, lse)
+    grads = far()[:3]
+    ops.causal_attn_bwd(dout2, q2, k2, v2, out2, lse2, o, grads=grads)
+    assert all(torch.equal(a, b) for a, b in zip(grads, want))
+    r = ops.rotary(32)
+    ops.rope(q2, r, offsets=o, out=q2)
+    assert torch.equal(q2, ops.rope(q, r, offsets=o))
+
+
 def test_rows_behind_are_left():
     lengths = [40, 0, 90]
     q, k, v, dout = batch(lengths, 2, 1, 64, more=50)
