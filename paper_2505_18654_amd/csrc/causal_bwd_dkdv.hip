@@ -7,12 +7,16 @@
 //
 // Four products of 60.4 million pairs of 8 heads of 128: 500 .. 550 us, 900 .. 990 TFLOP/s, bound by the matrix cores at the
 // clock that the power limit leaves (busy 53 %).  - delta starts dP's accumulators, so that dS costs one multiplication.
+#include <type_traits>
+
 #include "causal_device.h"
 
 namespace mtgr {
 namespace {
 
 using namespace causal;
+
+constexpr int JOIN_GROUPS = 2048;                            // 8 of a CU
 
 // A wave's sums in the order of its registers, 16 bytes per lane.
 template <int DBLK>
@@ -157,40 +161,70 @@ __global__ __launch_bounds__(256, 2) void causal_dkdv_kernel(CausalArgs a) {
     store_rows<DH>(dv, 1.0f, sO, (uint16_t*)a.dv + (long long)it.o * a.ld_v + hk * DH, a.ld_v, kw, n, lane);
 }
 
-// The sums of a tile's items, added in their order.
+// The sums of a tile's items, added in their order.  A wave takes 32 keys' 32 features of dK or dV, four items' sums at a time, so
+// that a long sequence's first tiles, whose items are many, do not hold up the rest (one of 4,000 tokens, 8 / 1 heads of 128, up
+// to 63 items: the backward 174 us, with 128 keys' 128 features per workgroup 228, 79 of them here).  The workgroups go over what the plan counted.
 template <int DH>
-__global__ __launch_bounds__(256) void causal_dkdv_join_kernel(CausalArgs a) {
-    constexpr int DBLK = DH / 32;
-    __shared__ __align__(16) uint16_t sO[4][32 * DH];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int which = blockIdx.x & 1, hk = (blockIdx.x >> 1) % a.Hk;
-    const CausalItem it = a.joins[(blockIdx.x >> 1) / a.Hk];
-    if (it.tile < 0) return;
-    floatx16 x[DBLK];
+__global__ __launch_bounds__(256) void causal_dkdv_join_kernel(CausalArgs a, int most) {
+    constexpr int DBLK = DH / 32, AHEAD = 4;
+    const int lane = threadIdx.x & 63, units = 8 * DBLK * a.Hk;
+    const int all = min(a.joins[most].parts, most) * units;
+    for (int u = 4 * blockIdx.x + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); u < all; u += 4 * gridDim.x) {
+        const int d = u % DBLK, w = u / DBLK % 4, which = u / (4 * DBLK) % 2, hk = u / (8 * DBLK) % a.Hk;
+        const CausalItem it = a.joins[u / units];
+        if (it.tile < 0) continue;
+        float4 x[4] = {};
+        auto add = [&](int i, auto n_tag) {                      // items i .. i + N - 1, all loads before the first sum
+            constexpr int N = decltype(n_tag)::value;
+            float4 v[N][4];
 #pragma unroll
-    for (int d = 0; d < DBLK; d++) x[d] = floatx16{};
-    for (int i = 0; i < it.parts; i++) {
-        const float4* src = part_of<DBLK>(a.parts, (long long)(it.part + i) * a.Hk + hk, which, w, lane);
+            for (int p = 0; p < N; p++) {
+                const float4* src = part_of<DBLK>(a.parts, (long long)(it.part + i + p) * a.Hk + hk, which, w, lane);
 #pragma unroll
-        for (int d = 0; d < DBLK; d++)
-#pragma unroll
-            for (int g = 0; g < 4; g++) {
-                const float4 v = src[(4 * d + g) * 64];
-                x[d][4 * g] += v.x;
-                x[d][4 * g + 1] += v.y;
-                x[d][4 * g + 2] += v.z;
-                x[d][4 * g + 3] += v.w;
+                for (int g = 0; g < 4; g++) v[p][g] = src[(4 * d + g) * 64];
             }
+#pragma unroll
+            for (int p = 0; p < N; p++)
+#pragma unroll
+                for (int g = 0; g < 4; g++) {
+                    x[g].x += v[p][g].x;
+                    x[g].y += v[p][g].y;
+                    x[g].z += v[p][g].z;
+                    x[g].w += v[p][g].w;
+                }
+        };
+        int i = 0;
+        for (; i + AHEAD <= it.parts; i += AHEAD) add(i, std::integral_constant<int, AHEAD>{});
+        if (it.parts - i == 3) add(i, std::integral_constant<int, 3>{});
+        else if (it.parts - i == 2) add(i, std::integral_constant<int, 2>{});
+        else if (it.parts - i == 1) add(i, std::integral_constant<int, 1>{});
+        // A lane of the lower half takes features 0 .. 15 of its row from both halves, one of the upper half 16 .. 31.
+        const float scale = which ? 1.0f : a.scale;
+        const int row = it.tile * BM + 32 * w + (lane & 31);
+        uint32_t pk[8];
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            pk[2 * g] = pack_bf16x2(x[g].x * scale, x[g].y * scale);
+            pk[2 * g + 1] = pack_bf16x2(x[g].z * scale, x[g].w * scale);
+        }
+        uint4 out[2];
+#pragma unroll
+        for (int g = 0; g < 2; g++) {
+            const auto lo = __builtin_amdgcn_permlane32_swap(pk[2 * g], pk[2 * g + 4], false, false);
+            const auto hi = __builtin_amdgcn_permlane32_swap(pk[2 * g + 1], pk[2 * g + 5], false, false);
+            out[g] = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+        }
+        if (row >= it.n) continue;
+        uint16_t* dst = (uint16_t*)(which ? a.dv : a.dk) + (it.o + row) * (which ? a.ld_v : a.ld_k) + hk * DH + 32 * d + 16 * (lane >> 5);
+        *(uint4*)dst = out[0];
+        *(uint4*)(dst + 8) = out[1];
     }
-    uint16_t* dst = (uint16_t*)(which ? a.dv : a.dk);
-    const long long ld = which ? a.ld_v : a.ld_k;
-    store_rows<DH>(x, which ? 1.0f : a.scale, sO[w], dst + (long long)it.o * ld + hk * DH, ld, it.tile * BM + 32 * w, it.n, lane);
 }
 
 template <int DH>
 hipError_t dkdv(const CausalArgs& a, const CausalPlan& p, hipStream_t s) {
     causal_dkdv_kernel<DH><<<p.items * a.Hk, 256, 0, s>>>(a);
-    if (p.joins > 0) causal_dkdv_join_kernel<DH><<<2 * p.joins * a.Hk, 256, 0, s>>>(a);
+    causal_dkdv_join_kernel<DH><<<std::min(p.joins * a.Hk * (DH / 16), JOIN_GROUPS), 256, 0, s>>>(a, p.joins);
     return hipGetLastError();
 }
 

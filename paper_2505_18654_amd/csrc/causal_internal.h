@@ -68,7 +68,7 @@ struct CausalArgs {
     float* lse;               // [H, T], or NULL in the forward
     float *rows_l, *rows_d;   // [H, T] each: - lse / ln 2 and - delta, from the dQ kernel to the dK / dV kernel
     void *dq, *dk, *dv;
-    CausalItem *items, *joins;       // the dK / dV kernel's plan, from the dQ kernel
+    CausalItem *items, *joins;       // the dK / dV kernel's plan, from the dQ kernel; behind the joins' bound, their number as parts
     float* parts;
     long long ld_q, ld_k, ld_v, ld_o, ld_do;
 };

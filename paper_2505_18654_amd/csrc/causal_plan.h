@@ -1,10 +1,12 @@
 // The dK / dV kernel's work: items of at most about a thousandth of all units, costliest first.
 //
 // A tile of keys is read by all queries from it to its sequence's end, of every query head that shares its key head, so the
-// first tiles of a long sequence are most of the work of a few workgroups.  Cut into items of at most U = max(16, all units
-// / 1024) units, and started costliest first (a counting sort), the workgroups end together: 64 sequences with 68,000 tokens,
-// 8 query heads on 2 of 128, in the batch's order 997 us, costliest first 745, cut as well 538 and 31 for the joins; one of
-// 4,000 tokens, 2 heads (the whole backward), with U of at least 64 172 us, 16 134, 8 the same.  One workgroup of the dQ
+// first tiles of a long sequence are most of the work of a few workgroups.  Cut into items of at most U units and started
+// costliest first (a counting sort), the workgroups end together: 64 sequences with 68,000 tokens, 8 query heads on 2 of 128, in
+// the batch's order 997 us, costliest first 745, cut as well 538 and 31 for the joins.  U is a 1,024th of all units; of little
+// work a 256th, an item for each CU, of at most 16 units (smaller ones cost more in the joins than they end sooner) and at least
+// 8: the whole backward of 700 tokens, 6 / 2 heads of 128, 33 us, with at least 16 37.5, 4 35, 2 41.5; of 1,000, 8 / 1 heads,
+// 42, 45, 49, 49; of two of 2,000 and less, 8 / 2 heads, 70, with 512 items of at most 16 units 83.  One workgroup of the dQ
 // kernel, which runs before, makes the plan.  Which of two items of equal size comes first may differ from run to run; results
 // do not depend on it.
 #pragma once
@@ -14,7 +16,8 @@
 namespace mtgr {
 namespace causal {
 
-constexpr int PLAN_CLASSES = 1024, MOST_ITEMS = 1024, LEAST_UNITS = 16, PLAN_STARTS = 2048;
+constexpr int PLAN_CLASSES = 1024, MOST_ITEMS = 1024, LEAST_UNITS = 8, FEW_ITEMS = 256, PLAN_STARTS = 2048;
+constexpr long long FEW_UNITS = 16;
 
 // The workgroup's THREADS threads; lds: PLAN_LDS ints, 8-byte aligned.
 constexpr int PLAN_LDS = PLAN_CLASSES + PLAN_STARTS + 32;
@@ -63,7 +66,8 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
     long long all = 0;
 #pragma unroll
     for (int i = 0; i < WAVES; i++) all += (long long)sum64[i];
-    const int U = (int)max((all * a.Hk + MOST_ITEMS - 1) / MOST_ITEMS, (long long)LEAST_UNITS);
+    all *= a.Hk;
+    const int U = (int)max(max((all + MOST_ITEMS - 1) / MOST_ITEMS, min(all / FEW_ITEMS, FEW_UNITS)), (long long)LEAST_UNITS);
     auto work = [&](int slot) {
         Work x;
         x.t = tile(slot);
@@ -128,12 +132,15 @@ __device__ __forceinline__ void make_plan(const CausalArgs& a, const CausalPlan&
     CausalItem none{};
     none.tile = -1;
     for (int i = total + tid; i < p.items; i += THREADS) a.items[i] = none;
-    for (int i = *joined + tid; i < p.joins; i += THREADS) a.joins[i] = none;
+    if (tid == 0) {
+        none.parts = *joined;
+        a.joins[p.joins] = none;                                 // how many there are
+    }
 }
 
 }  // namespace causal
 
-// With u units of a key head in all and U = max(16, u Hk / 1024): tiles of more than U units are at most u / U, their items at
+// With u units of a key head in all and U >= max(8, u Hk / 1024): tiles of more than U units are at most u / U, their items at
 // most 2 u / U, all items at most slots + u / U.  A sequence of n tokens has at most (n / 32 + 1) (n / 128 + 1) units per
 // query head.
 inline CausalPlan make_causal_plan(long long T, int B, int H, int Hk, int head_dim) {
@@ -145,7 +152,7 @@ inline CausalPlan make_causal_plan(long long T, int B, int H, int Hk, int head_d
     p.parts = (int)(2 * cuts);
     auto round = [](size_t n) { return (n + 255) & ~(size_t)255; };
     p.joins_ofs = round((size_t)p.items * sizeof(CausalItem));
-    p.parts_ofs = p.joins_ofs + round((size_t)p.joins * sizeof(CausalItem));
+    p.parts_ofs = p.joins_ofs + round((size_t)(p.joins + 1) * sizeof(CausalItem));
     p.bytes = p.parts_ofs + round((size_t)p.parts * Hk * 2 * causal::BM * head_dim * 4);
     return p;
 }
