@@ -282,6 +282,8 @@ __global__ __launch_bounds__(512, 2) void causal_fwd_few_kernel(CausalArgs a) {
     auto issue_v = [&](int j) { copy(a.v, a.ld_v, hk * DH, 32 * j, 1); };
     const bool any = w <= at.tile;
     if (tid == 0) sBad = 0;
+    // (Q through the V tile, as whole lines; a lane's pieces straight from memory, V copied at once: 9.3 -> 10.6 us for 700 tokens,
+    // 6 / 2 heads of 128)
     copy(a.q, a.ld_q, h * DH, q0, 1);
     if (any) issue_k(w);
     if (any) wait_vmcnt<NI>(); else wait_vmem();
