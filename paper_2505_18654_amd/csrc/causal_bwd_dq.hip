@@ -12,7 +12,8 @@
 // S and dP are formed again here, two products beside dQ's own: 440 .. 490 us for 60.4 million pairs of 8 heads of 128 (760 ..
 // 840 TFLOP/s), bound by the matrix cores at the clock that the power limit leaves.  With dS stored by the dK / dV kernel (2
 // bytes a pair, up to 2 GB) and dQ from it, the backward took 915 us instead of 947 there, with heads of 64 (8 sequences of
-// 4,096 tokens, 16 / 2 heads) 1,205 instead of 1,021.
+// 4,096 tokens, 16 / 2 heads) 1,205 instead of 1,021.  A third buffer of keys, copied a tile and a half ahead, changed 1 % for
+// the worse.
 #include <type_traits>
 
 #include "causal_plan.h"
