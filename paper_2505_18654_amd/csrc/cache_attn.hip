@@ -152,6 +152,14 @@ __global__ __launch_bounds__(64 * WAVES, DH == 64 ? 4 : 2) void cache_attn_kerne
             pk[e >> 1] = pack_bf16x2(p0, p1);
         }
         if (more) wait_vmcnt<NI>(); else wait_vmem();            // this tile's values
+        if (t.lo > 0 || t.hi < BN - 1) {
+            // The copies' probabilities are 0, which an infinity in the copied row would turn to NaN.
+#pragma unroll
+            for (int i = 0; i < BN * CPR / 64; i++) {
+                const int row = (lane + 64 * i) / CPR;
+                if (row < t.lo || row > t.hi) *(uint4*)&sT[w][1][8 * (lane + 64 * i)] = make_uint4(0, 0, 0, 0);
+            }
+        }
 #pragma unroll
         for (int kq = 0; kq < 2; kq++) {
             const bf16x8 pb = as_bf16x8(make_uint4(pk[4 * kq], pk[4 * kq + 1], pk[4 * kq + 2], pk[4 * kq + 3]));

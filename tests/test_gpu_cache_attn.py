@@ -301,3 +301,43 @@ def test_generation_step_by_step():
             rk, rqq = ops.rope(ks[b][:n], r, offsets=one), ops.rope(qs[b][:n], r, offsets=one)
             want, _, eo, _ = expect(rqq[-1:], [rk], [vs[b][:n]], dh ** -0.5)
             within("step", out[b], want[0], half_step(out[b]) + eo[0] * (1 + 2.0 ** -7))
+
+
+# ------------------------------------------------------------------ infinite values
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("n", [1, 17, 31, 32, 33, 300, 3000])
+def test_infinite_values_stay_infinite(n, dh):
+    """An infinite value of a sequence's first or last token is the sum, with its sign, of its feature and of no other, wherever
+    the sequence ends in a tile of keys."""
+    for at in {0, n - 1}:
+        c, table, ks, vs = make_cache([n], 2, 16, dh)
+        page, row = int(table[0, at // 16]), at % 16
+        c.values[page, 0, row, 5], c.values[page, 1, row, dh - 1] = torch.inf, -torch.inf
+        q = heads((1, 4, dh), 9)
+        out, lse = ops.cache_attn(q, c, table, lens_of([n]), save=True)
+        assert (out[0, :2, 5] == torch.inf).all() and (out[0, 2:, dh - 1] == -torch.inf).all()
+        want, wl, eo, el = expect(q, ks, vs, dh ** -0.5)             # (of the values without infinities)
+        keep = torch.isfinite(out)
+        assert int((~keep).sum()) == 4
+        within("out", out[keep], want[keep], half_step(out[keep]) + eo[keep] * (1 + 2.0 ** -7))
+        within("lse", lse, wl, el)
+
+
+@pytest.mark.parametrize("page", [16, 32])
+def test_infinite_values_beside_missing_pages(page):
+    """The tokens on either side of a missing page hold an infinity: copies of them stand in for the absent ones."""
+    n, lost = 6 * page, 3
+    c, table, ks, vs = make_cache([n], 2, page, 64)
+    q = heads((1, 4, 64), 9)
+    c.values[int(table[0, lost - 1]), :, page - 1, 3] = torch.inf
+    c.values[int(table[0, lost + 1]), :, 0, 40] = -torch.inf
+    table[0, lost] = -1
+    m = torch.ones(n, dtype=torch.bool, device="cuda")
+    m[lost * page:(lost + 1) * page] = False
+    out = ops.cache_attn(q, c, table, lens_of([n]))
+    assert (out[..., 3] == torch.inf).all() and (out[..., 40] == -torch.inf).all()
+    want, _, eo, _ = expect(q, [ks[0][m]], [vs[0][m]], 0.125)
+    keep = torch.isfinite(out)
+    assert int((~keep).sum()) == 8
+    within("out", out[keep], want[keep], half_step(out[keep]) + eo[keep] * (1 + 2.0 ** -7))
