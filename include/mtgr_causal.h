@@ -93,7 +93,7 @@ typedef struct {
 mtgr_status_t mtgr_causal_attn_fwd(const mtgr_causal_problem_t* p, const int32_t* offsets, const void* q, const void* k,
                                    const void* v, void* out, float* lse, mtgr_stream_t stream);
 
-/* Workspace bytes of the backward pass. */
+/* Workspace bytes of the backward pass; as many or fewer for fewer tokens or sequences. */
 mtgr_status_t mtgr_causal_attn_workspace_size(const mtgr_causal_problem_t* p, size_t* bytes);
 
 /* Gradients for dout [T, heads, head_dim], with out and lse of the forward pass on the same inputs.  The gradients of
@@ -154,6 +154,8 @@ typedef struct {
     int64_t ld_o;
 } mtgr_cache_attn_problem_t;
 
+/* Workspace bytes of a call.  They never fall where num_seqs or max_len rises and the heads stay the same: a workspace for the
+ * largest batch and the longest history serves every smaller one. */
 mtgr_status_t mtgr_cache_attn_workspace_size(const mtgr_cache_attn_problem_t* p, const mtgr_kv_cache_t* cache,
                                              size_t* bytes);
 

@@ -408,7 +408,7 @@ mtgr_status_t mtgr_cache_attn(const mtgr_cache_attn_problem_t* p, const mtgr_kv_
     CHECK(check_heads(out, "out", p->ld_o, p->heads, cache->head_dim));
     if (lse) CHECK(check_array(lse, "lse", 4));
     const mtgr::CacheAttnPlan plan = plan_of(p, cache);
-    CHECK(check_workspace(workspace, workspace_bytes, plan.bytes));
+    CHECK(check_workspace(workspace, workspace_bytes, plan.need));
     mtgr::CacheAttnArgs a{};
     a.cache = cache_args(cache, page_table, p->ld_table, p->max_pages);
     a.B = p->num_seqs;

@@ -252,8 +252,9 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
 CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_len) {
     CacheAttnPlan p{};
     const int group = H / Hk;
-    const long long units = (long long)B * Hk * ((group + QT - 1) / QT);
-    const long long want = ((B > 2 ? 2 * CHUNKS : CHUNKS) + units - 1) / units;      // chunks of a sequence that fill the chip
+    const int per_seq = Hk * ((group + QT - 1) / QT), fill = B > 2 ? 2 * CHUNKS : CHUNKS;
+    const long long units = (long long)B * per_seq;
+    const long long want = (fill + units - 1) / units;                               // chunks of a sequence that fill the chip
     long long chunk = (max_len + want - 1) / want;
     chunk = std::min<long long>(std::max<long long>((chunk + 127) / 128 * 128, 128), 2048);
     if (max_len <= 1024) chunk = 1024;
@@ -261,10 +262,19 @@ CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_
     p.chunk = (int)chunk;
     p.splits = (int)std::max<long long>(1, (max_len + chunk - 1) / chunk);
     p.waves = p.splits == 1 && units <= 256 ? 8 : 4;
+    // The workspace is sized by a bound of (rows, chunks) that rises with B and max_len, so that one for the longest history and
+    // the largest batch serves all others; their number itself falls where chunks grow by a step of 128 keys.  A sequence has at
+    // most `want` chunks, or as many as 2,048 keys each make, and no more than of 128 keys.
+    auto round = [](long long n) { return ((size_t)n + 255) & ~(size_t)255; };
+    const long long rows = (long long)B * H, most = max_len <= 1024 ? 0 : std::min<long long>({
+        rows * ((max_len + 127) / 128),
+        std::max<long long>(rows + (long long)H * (fill - 1) / per_seq, rows * ((max_len + 2047) / 2048)),
+        ((long long)H << 24) / per_seq});                                            // (the launch's bound)
     if (p.splits > 1) {
-        p.part_bytes = ((size_t)B * H * p.splits * head_dim * 4 + 255) & ~(size_t)255;
-        p.bytes = p.part_bytes + (((size_t)B * H * p.splits * 8 + 255) & ~(size_t)255);
+        p.part_bytes = round(rows * p.splits * head_dim * 4);
+        p.need = p.part_bytes + round(rows * p.splits * 8);
     }
+    p.bytes = round(most * head_dim * 4) + round(most * 8);
     return p;
 }
 

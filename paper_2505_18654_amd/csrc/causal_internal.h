@@ -100,7 +100,9 @@ struct CacheAttnArgs {
 };
 struct CacheAttnPlan {
     int chunk, splits, waves;
-    size_t part_bytes, bytes;
+    size_t part_bytes;        // of the chunks' sums
+    size_t need;              // with their maxima and totals
+    size_t bytes;             // of a workspace, at least `need`
 };
 CacheAttnPlan cache_attn_plan(int B, int H, int Hk, int head_dim, long long max_len);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int head_dim, hipStream_t s);

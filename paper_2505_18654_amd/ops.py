@@ -606,7 +606,7 @@ def causal_attn_fwd(q, k, v, offsets, scale: Optional[float] = None, save: bool 
 
 
 def causal_attn_workspace(q, k, offsets) -> torch.Tensor:
-    """A workspace for causal_attn_bwd of these sizes."""
+    """A workspace for causal_attn_bwd of up to so many tokens and sequences."""
     n = hstu.mtgr_causal_attn_workspace_size(_causal_problem(q, k, k, offsets, None, _device()))
     return torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
 
@@ -698,7 +698,7 @@ def kv_append(cache: KvCache, page_table, past, k, v, offsets=None, q=None, rota
 
 
 def cache_attn_workspace(cache: KvCache, num_seqs: int, heads: int, max_len: int) -> torch.Tensor:
-    """A workspace for cache_attn of these sizes."""
+    """A workspace for cache_attn of up to num_seqs sequences and any max_len up to this one."""
     c = cache.struct(_device())
     p = hstu.CacheAttnProblem(num_seqs, heads, -(-max(max_len, 1) // c.page_size), 1.0, max_len, 0, 0, 0)
     n = hstu.mtgr_cache_attn_workspace_size(p, c)

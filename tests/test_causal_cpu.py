@@ -369,3 +369,36 @@ def test_operands_accepted(on_cpu):
 def test_operands_that_do_not_fit(on_cpu, call):
     with pytest.raises(ValueError):
         call()
+
+
+# ------------------------------------------------------------------ workspaces of a session's largest call
+
+@pytest.mark.parametrize("H, Hk, dh", [(8, 2, 128), (1, 1, 32), (33, 1, 64), (70, 2, 64), (32, 8, 128), (24, 24, 64), (600, 300, 32)])
+def test_cache_workspace_of_the_largest_call(H, Hk, dh):
+    """One sized for the longest history and the most sequences is enough for every smaller call."""
+    def size(B, n):
+        p = hstu.CacheAttnProblem(num_seqs=B, heads=H, max_pages=1 << 20, scale=0.125, max_len=n, ld_table=1 << 20, ld_q=0, ld_o=0)
+        return hstu.mtgr_cache_attn_workspace_size(p, pages(page_size=1024, kv_heads=Hk, head_dim=dh))
+
+    lens = sorted({0, 1, 1024, 1025, 8192, 9000, 32768, 32769, 65536, 100003, 1 << 24, (1 << 30) - 1,
+                   *range(900, 40000, 331), *(2 ** i + d for i in range(10, 30) for d in (-1, 0, 1))})
+    batches = [0, 1, 2, 3, 4, 5, 7, 8, 15, 31, 64, 100, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1000, 4096, 10000]
+    before = [0] * len(lens)
+    for B in batches:
+        row = [size(B, n) for n in lens]
+        assert all(a <= b for a, b in zip(row, row[1:])), B
+        assert all(a <= b for a, b in zip(before, row)), B
+        before = row
+
+
+def test_backward_workspace_of_the_largest_call():
+    def size(T, B, H, Hk, dh):
+        return hstu.mtgr_causal_attn_workspace_size(causal_problem(total_tokens=T, num_seqs=B, heads=H, kv_heads=Hk, head_dim=dh,
+                                                                   ld_q=H * dh, ld_k=Hk * dh, ld_v=Hk * dh, ld_o=H * dh, ld_do=H * dh))
+
+    for H, Hk, dh in ((8, 2, 128), (1, 1, 32), (16, 16, 64), (2048, 2048, 32)):
+        before = [0] * 7
+        for T in (0, 1, 31, 128, 129, 700, 3000, 3001, 20000, 70000, 500000):
+            row = [size(T, B, H, Hk, dh) for B in (0, 1, 2, 3, 50, 64, 1000)]
+            assert all(a <= b for a, b in zip(row, row[1:])) and all(a <= b for a, b in zip(before, row)), (H, T)
+            before = row

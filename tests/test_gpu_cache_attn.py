@@ -341,3 +341,22 @@ def test_infinite_values_beside_missing_pages(page):
     keep = torch.isfinite(out)
     assert int((~keep).sum()) == 8
     within("out", out[keep], want[keep], half_step(out[keep]) + eo[keep] * (1 + 2.0 ** -7))
+
+
+@pytest.mark.parametrize("H, Hk, dh, B", [(8, 2, 128, 2), (8, 2, 64, 9), (40, 1, 32, 3)])
+def test_one_workspace_for_a_session(H, Hk, dh, B):
+    """A workspace for the longest history serves every step before, with a tight max_len, and every smaller batch; nothing is
+    written behind it."""
+    lengths = [9000 - 700 * b for b in range(B)]
+    c, table, ks, vs = make_cache(lengths, Hk, 64, dh)
+    n = ops.cache_attn_workspace(c, B, H, 9000).numel()
+    room = torch.full((n + 4096,), 93, dtype=torch.uint8, device="cuda")
+    ws = room[:n]
+    q = heads((B, H, dh), 5)
+    for longest in (1, 1024, 1025, 1152, 1153, 4096, 4097, 8192, 8193, 9000):
+        for m in sorted({1, B // 2, B}):
+            some = [min(longest, x) for x in lengths[:m]]
+            out, lse = ops.cache_attn(q[:m], c, table[:m], lens_of(some), max_len=longest, save=True, workspace=ws)
+            assert (room[n:] == 93).all()
+            if longest in (1153, 8193):
+                compare(q[:m], [k[:x] for k, x in zip(ks, some)], [v[:x] for v, x in zip(vs, some)], out, lse, dh ** -0.5)
