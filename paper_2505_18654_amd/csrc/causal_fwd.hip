@@ -121,14 +121,15 @@ __global__ __launch_bounds__(256, 2) void causal_fwd_kernel(CausalArgs a) {
     };
     auto raise = [&](float top) {
         top = max_halves(top);
-        if (__any(__builtin_fmaf(top, a.c, -mc) > 8.f)) {
-            top = fmaxf(top, m);
-            const float f = __builtin_amdgcn_exp2f((m - top) * a.c);
+        // (each query for itself, so that its bits do not depend on the others of the wave, which see later keys)
+        const bool up = __builtin_fmaf(top, a.c, -mc) > 8.f;
+        if (__any(up)) {
+            const float f = up ? __builtin_amdgcn_exp2f((m - top) * a.c) : 1.f;
             l0 *= f;
             l1 *= f;
 #pragma unroll
             for (int d = 0; d < DBLK; d++) oacc[d] *= f;
-            m = top;
+            m = up ? top : m;
             mc = m * a.c;
         }
     };

@@ -243,3 +243,32 @@ def test_streams_and_graph():
         o2, l2 = ops.causal_attn_fwd(q, k, v, o, save=True)
         g2 = ops.causal_attn_bwd(dout, q, k, v, o2, l2, o)
         assert torch.equal(out, o2) and torch.equal(lse, l2) and all(torch.equal(a, b) for a, b in zip(grads, g2))
+
+
+# ------------------------------------------------------------------ the kernels for few tiles and for many
+
+FEW_TILES = 1024       # tiles of 32 rows, of all heads, that the kernels for few take at most
+SIDES = [(2, "few"), (128, "many")]
+
+
+def on_side(side, lengths, H, more=0):
+    assert ((sum(lengths) + more) // 32 + len(lengths)) * H > FEW_TILES if side == "many" else \
+        ((sum(lengths) + more) // 32 + len(lengths)) * H <= FEW_TILES
+
+
+@pytest.mark.parametrize("H, side", SIDES)
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("n, at", [(300, 250), (300, 33), (270, 1)])
+def test_outputs_keep_their_bits_whatever_follows(n, at, dh, H, side):
+    """Tokens from `at` on of other values and sizes, 60 times the scores among them: outputs and log-sums before are the same."""
+    on_side(side, [n], H)
+    q, k, v, _ = batch([n], H, H // 2, dh)
+    o = offsets_of([n])
+    out, lse = ops.causal_attn_fwd(q, k, v, o, save=True)
+    for size in (0.0, 7.0, 60.0):
+        q2, k2, v2 = q.clone(), k.clone(), v.clone()
+        q2[at:] *= size
+        k2[at:] = k2[at:].flip(0)
+        v2[at:] *= -size
+        out2, lse2 = ops.causal_attn_fwd(q2, k2, v2, o, save=True)
+        assert torch.equal(out2[:at], out[:at]) and torch.equal(lse2[:, :at], lse[:, :at])
