@@ -73,9 +73,9 @@ mtgr_status_t mtgr_rope(const mtgr_rope_problem_t* p, const void* x, const int32
  * head_dim 32, 64 or 128; heads a multiple of kv_heads.  Sums are fp32; probabilities, their gradients and the results are
  * rounded to bf16.  A sequence's results depend on its own tokens alone, and a token's output on tokens up to it alone,
  * whatever the others hold (infinities and NaN too).  Up to rounding, that is: total_tokens, num_seqs and heads choose the
- * kernels, all lengths the pieces that the backward sums shared heads in, and an infinity or NaN up to 31 tokens behind a
- * token the way its feature is summed.  The forward of finite values in a batch of these sizes has the same bits whatever the
- * other sequences and later tokens are.  Rows of outputs behind the last sequence are left as they were. */
+ * kernels, all lengths the pieces that the backward's sums are formed in, and an infinity or NaN up to 31 tokens behind a
+ * token the way that its feature is summed.  But for that, the forward of these sizes gives a token the same bits whatever
+ * the other sequences and later tokens are.  Rows of outputs behind the last sequence are left as they were. */
 typedef struct {
     int32_t num_seqs;         /* B >= 0 */
     int32_t heads;

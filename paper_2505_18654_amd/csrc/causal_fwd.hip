@@ -21,51 +21,185 @@ namespace {
 using namespace causal;
 constexpr int BN = 64;        // keys of a tile
 
-// Output rows (a bit each, from row qw on) with infinities or NaN once more, a key after the other: P = 0 of the keys behind a
-// query, times an infinite or NaN value there, is NaN in the products.  Such rows are rare, so that this path is slow (about
-// 0.2 us per row and thousand keys) and costs the others one look at their results.  A lane holds features lane, lane + 64 of
-// the row; elements that are finite keep what the products gave, and a row ends once no other could become finite, so
-// that inputs full of NaN, whose first key decides, take no longer.  stat(r, m, inv): a row's reference score and the
-// reciprocal of its sum.  The rows have been written.
-template <int DH, class Stat>
-__device__ void redo_rows(const CausalArgs& a, const Tile& at, int qw, int h, int hk, uint32_t rows, int lane, Stat stat) {
-    constexpr int F = (DH + 63) / 64;
-    const bool has = lane < DH;
-    while (rows) {
-        const int r = __builtin_ctz(rows), i = qw + r;
-        rows &= rows - 1;
-        float m, inv;
-        stat(r, m, inv);
-        const uint16_t* Q = (const uint16_t*)a.q + (long long)(at.o + i) * a.ld_q + h * DH;
-        uint16_t* out = (uint16_t*)a.out + (long long)(at.o + i) * a.ld_o + h * DH;
-        float q[F], o[F];
-        bool redo[F];
+// 32 rows from row0 on of columns of a matrix into a wave's swizzled tile; rows behind `last` are copies of it.
+template <int DH>
+__device__ __forceinline__ void copy_rows(uint16_t* tile, const void* src, long long ld, int col0, long long row0, int last, int lane) {
+    constexpr int CPR = DH / 8;
+    const uint16_t* base = (const uint16_t*)src + row0 * ld + col0;
 #pragma unroll
-        for (int f = 0; f < F; f++) {
-            q[f] = has ? bf16_to_f32(Q[lane + 64 * f]) : 0.f;
-            o[f] = 0.f;
-            redo[f] = has && (out[lane + 64 * f] & 0x7f80) == 0x7f80;
-        }
-        for (int j = 0; j <= i; j++) {
-            if (j % 16 == 1) {
-                bool open = false;
-#pragma unroll
-                for (int f = 0; f < F; f++) open |= redo[f] && o[f] * 0.f == 0.f;
-                if (!__any(open)) break;
-            }
-            const uint16_t* K = (const uint16_t*)a.k + (long long)(at.o + j) * a.ld_k + hk * DH;
-            const uint16_t* V = (const uint16_t*)a.v + (long long)(at.o + j) * a.ld_v + hk * DH;
-            float s = 0.f;
-#pragma unroll
-            for (int f = 0; f < F; f++) s = __builtin_fmaf(q[f], has ? bf16_to_f32(K[lane + 64 * f]) : 0.f, s);
-            const float p = bf16_to_f32((uint16_t)f32_to_bf16_bits(__builtin_amdgcn_exp2f((wave_sum(s) - m) * a.c)));
-#pragma unroll
-            for (int f = 0; f < F; f++) o[f] = __builtin_fmaf(p, has ? bf16_to_f32(V[lane + 64 * f]) : 0.f, o[f]);
-        }
-#pragma unroll
-        for (int f = 0; f < F; f++)
-            if (redo[f]) out[lane + 64 * f] = (uint16_t)f32_to_bf16_bits(o[f] * inv);
+    for (int i = 0; i < CPR / 2; i++) {
+        const int row = i * (64 / CPR) + lane / CPR;
+        lds_dma16(lds_address(tile) + i * 1024u, uniform_ptr(base), (uint32_t)(min(row, last) * ld + ((lane % CPR) ^ swz<CPR>(row)) * 8) * 2u);
     }
+}
+
+// A wave's 32 queries against halves of 32 keys, first, first + step, .. below end, `diag` the one on the diagonal: maximum,
+// sum and outputs of a query in a lane.  issue_k and issue_v copy a half into the wave's tiles; those of the first are under way.
+// open(j): whether there is anything left to do behind half j.
+template <int DH, class IssueK, class IssueV, class Open>
+__device__ __forceinline__ void attend_halves(const CausalArgs& a, const uint16_t* sK, const uint16_t* sV, const bf16x8 (&qreg)[DH / 16],
+                                              floatx16 (&oacc)[DH / 32], float& m, float& l, int first, int step, int end, int diag,
+                                              IssueK issue_k, IssueV issue_v, Open open, int lane) {
+    constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, NI = CPR / 2;
+    const int col = lane & 31, hh = lane >> 5;
+    for (int j = first; j < end; j += step) {
+        const bool more = j + step < end;
+        wait_vmcnt<NI>();                                        // K(j)
+        floatx16 s{};
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; kk++)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sK, col, 2 * kk + hh), qreg[kk], s, 0, 0, 0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // it is read
+        if (more) issue_k(j + step);
+        if (j == diag) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) s[e] = 8 * (e >> 2) + 4 * hh + (e & 3) > col ? neg_inf() : s[e];
+        }
+        float top = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; e++) top = fmaxf(top, s[e]);
+        top = fmaxf(max_halves(top), m);
+        if (__any(top > m)) {
+            const float f = __builtin_amdgcn_exp2f((m - top) * a.c);
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DBLK; d++) oacc[d] *= f;
+            m = top;
+        }
+        const float mc = m * a.c;
+        uint32_t pk[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, -mc));
+            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], a.c, -mc));
+            l += p0 + p1;
+            pk[e >> 1] = pack_bf16x2(p0, p1);
+        }
+        if (more) wait_vmcnt<NI>(); else wait_vmem();            // V(j)
+#pragma unroll
+        for (int kq = 0; kq < 2; kq++) {
+            const bf16x8 pb = as_bf16x8(make_uint4(pk[4 * kq], pk[4 * kq + 1], pk[4 * kq + 2], pk[4 * kq + 3]));
+#pragma unroll
+            for (int d = 0; d < DBLK; d++)
+                oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read_tr<CPR>(sV, 16 * kq, 32 * d, lane), pb, oacc[d], 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (!open(j)) break;
+        if (more) issue_v(j + step);
+    }
+}
+
+// Outputs with infinities or NaN among a wave's 32 query rows from q0 on once more.  P = 0 of the keys behind a query, times an
+// infinite or NaN value there, is NaN in the products: of the half on the diagonal alone, and only if it holds such a value.  Its
+// keys are then taken one by one, each by the queries that see it, behind the others' products formed once more; elements that
+// are finite keep what they were.  The rows have been written; sK and sV are tiles of the wave.  8,000 tokens, 8 heads of 128:
+// 194 us, with an infinity in the last token 482, in the middle one 271 (the rows behind show it rightly and are left), in
+// every token 530.
+template <int DH>
+__device__ void redo_rows(const CausalArgs& a, const Tile& at, int q0, int h, int hk, uint16_t* sK, uint16_t* sV, int lane) {
+    constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32;
+    // (opaque, so that the compiler does not keep what it has in common with the loop before in registers across that)
+    asm volatile("" : "+v"(lane));
+    const int col = lane & 31, hh = lane >> 5, n = at.n;
+    uint16_t* row = (uint16_t*)a.out + (long long)(at.o + min(q0 + col, n - 1)) * a.ld_o + h * DH + 4 * hh;
+    auto issue_k = [&](int j) { copy_rows<DH>(sK, a.k, a.ld_k, hk * DH, at.o + 32 * j, n - 1 - 32 * j, lane); };
+    auto issue_v = [&](int j) { copy_rows<DH>(sV, a.v, a.ld_v, hk * DH, at.o + 32 * j, n - 1 - 32 * j, lane); };
+    auto special = [](uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u; };
+    const int diag = q0 / 32;
+    issue_v(diag);
+    copy_rows<DH>(sK, a.q, a.ld_q, h * DH, at.o + q0, n - 1 - q0, lane);
+    uint32_t bad[DBLK];                                          // a bit for each of the lane's elements, as in the accumulators
+#pragma unroll
+    for (int d = 0; d < DBLK; d++) {
+        bad[d] = 0;
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            const uint2 u = *(const uint2*)(row + 32 * d + 8 * g);
+            bad[d] |= (uint32_t)(special(u.x) | special(u.x >> 16) << 1 | special(u.y) << 2 | special(u.y >> 16) << 3) << 4 * g;
+        }
+        if (q0 + col >= n) bad[d] = 0;
+    }
+    wait_vmem();
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < CPR / 2; i++) {
+        const uint4 u = *(const uint4*)&sV[8 * (lane + 64 * i)];
+        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int e = 0; e < 4; e++) any |= special(x[e]) | special(x[e] >> 16);
+    }
+    if (!__any(any)) return;
+    bf16x8 qreg[KSTEPS];
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk++) qreg[kk] = tile_read8<CPR>(sK, col, 2 * kk + hh);
+    wait_lgkm_seen();
+    floatx16 oacc[DBLK];
+#pragma unroll
+    for (int d = 0; d < DBLK; d++) oacc[d] = floatx16{};
+    float m = a.least, l = 0.f;
+    // Once all of these are NaN (inputs full of them), they stay so.
+    auto open = [&](int j) {
+        if (j % 8 != 0) return true;
+        bool some = false;
+#pragma unroll
+        for (int d = 0; d < DBLK; d++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) some |= (bad[d] >> e & 1) != 0 && oacc[d][e] == oacc[d][e];
+        return __any(some) != 0;
+    };
+    if (diag > 0) {
+        issue_k(0);
+        issue_v(0);
+        attend_halves<DH>(a, sK, sV, qreg, oacc, m, l, 0, 1, diag, -1, issue_k, issue_v, open, lane);
+        wait_vmem();
+    }
+    issue_k(diag);
+    issue_v(diag);
+    wait_vmem();
+    floatx16 s{};
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk++)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sK, col, 2 * kk + hh), qreg[kk], s, 0, 0, 0);
+    float top = neg_inf();
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+        if (8 * (e >> 2) + 4 * hh + (e & 3) > col) s[e] = neg_inf();
+        top = fmaxf(top, s[e]);
+    }
+    top = fmaxf(max_halves(top), m);
+    const float f = __builtin_amdgcn_exp2f((m - top) * a.c), mc = top * a.c;
+    l *= f;
+#pragma unroll
+    for (int d = 0; d < DBLK; d++) oacc[d] *= f;
+    // P [query][key] in place of K
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) l += p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * g + e], a.c, -mc));
+        *(uint2*)&sK[32 * col + 8 * g + 4 * hh] = make_uint2(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]));
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+    for (int key = 0; key <= col; key++) {
+        const float p = bf16_to_f32(sK[32 * col + key]);
+#pragma unroll
+        for (int d = 0; d < DBLK; d++)
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const uint2 v = *(const uint2*)&sV[8 * tile_chunk<CPR>(key, 4 * d + g) + 4 * hh];
+                oacc[d][4 * g] = __builtin_fmaf(p, __uint_as_float(v.x << 16), oacc[d][4 * g]);
+                oacc[d][4 * g + 1] = __builtin_fmaf(p, __uint_as_float(v.x & 0xffff0000u), oacc[d][4 * g + 1]);
+                oacc[d][4 * g + 2] = __builtin_fmaf(p, __uint_as_float(v.y << 16), oacc[d][4 * g + 2]);
+                oacc[d][4 * g + 3] = __builtin_fmaf(p, __uint_as_float(v.y & 0xffff0000u), oacc[d][4 * g + 3]);
+            }
+    }
+    const float inv = 1.0f / sum_halves(l);
+#pragma unroll
+    for (int d = 0; d < DBLK; d++)
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+            if (bad[d] >> e & 1) row[32 * d + 8 * (e >> 2) + (e & 3)] = (uint16_t)f32_to_bf16_bits(oacc[d][e] * inv);
 }
 
 template <int DH>
@@ -237,28 +371,26 @@ __global__ __launch_bounds__(256, 2) void causal_fwd_kernel(CausalArgs a) {
     for (int d = 0; d < DBLK; d++)
 #pragma unroll
         for (int e = 0; e < 16; e++) zero = __builtin_fmaf(oacc[d][e], 0.f, zero);
-    const unsigned long long bad = __ballot(zero != 0.f && qi < n);
-    const float inv = 1.0f / l;
+    const bool bad = __any(zero != 0.f && qi < n);
     uint16_t* sO = sKV[0] + w * 32 * DH;
-    store_rows<DH>(oacc, inv, sO, (uint16_t*)a.out + (long long)at.o * a.ld_o + h * DH, a.ld_o, qw, n, lane);
+    store_rows<DH>(oacc, 1.0f / l, sO, (uint16_t*)a.out + (long long)at.o * a.ld_o + h * DH, a.ld_o, qw, n, lane);
     if (bad) {
         wait_vmem();                                             // the rows as they are have been written
-        redo_rows<DH>(a, at, qw, h, hk, (uint32_t)(bad | (bad >> 32)), lane, [&](int r, float& rm, float& ri) {
-            rm = __shfl(m, r, 64);
-            ri = __shfl(inv, r, 64);
-        });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // and their LDS is read
+        redo_rows<DH>(a, at, qw, h, hk, sO, sKV[2] + w * 32 * DH, lane);
     }
 }
 
 // Few query tiles: a workgroup takes 32 query rows of one (sequence, head), and its 8 waves take their halves of 32 keys in
 // turn, each with its own maximum, sum and outputs and its own LDS tiles, joined at the end.  A lone prompt of 700 tokens, 6
-// heads, is 36 workgroups of the kernel above, the last of them 11 tiles one after another.
+// heads, is 36 workgroups of the kernel above, the last of them 11 tiles one after another.  (Heads of 32: registers for three
+// workgroups of a CU, which the rare path at the end would make two.)
 template <int DH>
-__global__ __launch_bounds__(512, 2) void causal_fwd_few_kernel(CausalArgs a) {
+__global__ __launch_bounds__(512, DH == 32 ? 6 : 2) void causal_fwd_few_kernel(CausalArgs a) {
     constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, TILE = 32 * DH, NI = CPR / 2, WAVES = 8;
     __shared__ __align__(16) uint16_t sT[WAVES][2][TILE];        // K and V of each wave; then its outputs
     __shared__ float sML[WAVES][2][32];
-    __shared__ uint32_t sBad;
+    __shared__ int sBad;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, hh = lane >> 5;
     int id = blockIdx.x;
@@ -268,24 +400,13 @@ __global__ __launch_bounds__(512, 2) void causal_fwd_few_kernel(CausalArgs a) {
     const Tile at = tile_of_slot<32>(a.offsets, a.B, a.T, a.slots - 1 - id / a.group);
     if (at.tile < 0) return;
     const int q0 = 32 * at.tile, n = at.n;
-    // 32 rows from row0 on of columns of a matrix; rows behind the sequence are copies of its last one
-    auto copy = [&](const void* src, long long ld, int col0, int row0, int which) {
-        const uint16_t* base = (const uint16_t*)src + (long long)(at.o + row0) * ld + col0;
-        const int last = n - 1 - row0;
-#pragma unroll
-        for (int i = 0; i < NI; i++) {
-            const int row = i * (64 / CPR) + lane / CPR;
-            lds_dma16(lds_address(sT[w][which]) + i * 1024u, uniform_ptr(base),
-                      (uint32_t)(min(row, last) * ld + ((lane % CPR) ^ swz<CPR>(row)) * 8) * 2u);
-        }
-    };
-    auto issue_k = [&](int j) { copy(a.k, a.ld_k, hk * DH, 32 * j, 0); };
-    auto issue_v = [&](int j) { copy(a.v, a.ld_v, hk * DH, 32 * j, 1); };
+    auto issue_k = [&](int j) { copy_rows<DH>(sT[w][0], a.k, a.ld_k, hk * DH, at.o + 32 * j, n - 1 - 32 * j, lane); };
+    auto issue_v = [&](int j) { copy_rows<DH>(sT[w][1], a.v, a.ld_v, hk * DH, at.o + 32 * j, n - 1 - 32 * j, lane); };
     const bool any = w <= at.tile;
     if (tid == 0) sBad = 0;
     // (Q through the V tile, as whole lines; a lane's pieces straight from memory, V copied at once: 9.3 -> 10.6 us for 700 tokens,
     // 6 / 2 heads of 128)
-    copy(a.q, a.ld_q, h * DH, q0, 1);
+    copy_rows<DH>(sT[w][1], a.q, a.ld_q, h * DH, at.o + q0, n - 1 - q0, lane);
     if (any) issue_k(w);
     if (any) wait_vmcnt<NI>(); else wait_vmem();
     bf16x8 qreg[KSTEPS];
@@ -297,50 +418,8 @@ __global__ __launch_bounds__(512, 2) void causal_fwd_few_kernel(CausalArgs a) {
 #pragma unroll
     for (int d = 0; d < DBLK; d++) oacc[d] = floatx16{};
     float m = a.least, l = 0.f;
-    for (int j = w; j <= at.tile; j += WAVES) {
-        const bool more = j + WAVES <= at.tile;
-        wait_vmcnt<NI>();                                        // K(j)
-        floatx16 s{};
-#pragma unroll
-        for (int kk = 0; kk < KSTEPS; kk++)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read8<CPR>(sT[w][0], col, 2 * kk + hh), qreg[kk], s, 0, 0, 0);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // it is read
-        if (more) issue_k(j + WAVES);
-        if (j == at.tile) {
-#pragma unroll
-            for (int e = 0; e < 16; e++) s[e] = 8 * (e >> 2) + 4 * hh + (e & 3) > col ? neg_inf() : s[e];
-        }
-        float top = s[0];
-#pragma unroll
-        for (int e = 1; e < 16; e++) top = fmaxf(top, s[e]);
-        top = fmaxf(max_halves(top), m);
-        if (__any(top > m)) {
-            const float f = __builtin_amdgcn_exp2f((m - top) * a.c);
-            l *= f;
-#pragma unroll
-            for (int d = 0; d < DBLK; d++) oacc[d] *= f;
-            m = top;
-        }
-        const float mc = m * a.c;
-        uint32_t pk[8];
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c, -mc));
-            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], a.c, -mc));
-            l += p0 + p1;
-            pk[e >> 1] = pack_bf16x2(p0, p1);
-        }
-        if (more) wait_vmcnt<NI>(); else wait_vmem();            // V(j)
-#pragma unroll
-        for (int kq = 0; kq < 2; kq++) {
-            const bf16x8 pb = as_bf16x8(make_uint4(pk[4 * kq], pk[4 * kq + 1], pk[4 * kq + 2], pk[4 * kq + 3]));
-#pragma unroll
-            for (int d = 0; d < DBLK; d++)
-                oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_read_tr<CPR>(sT[w][1], 16 * kq, 32 * d, lane), pb, oacc[d], 0, 0, 0);
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more) issue_v(j + WAVES);
-    }
+    attend_halves<DH>(a, sT[w][0], sT[w][1], qreg, oacc, m, l, w, WAVES, at.tile + 1, at.tile, issue_k, issue_v,
+                      [](int) { return true; }, lane);
     l = sum_halves(l);
     if (hh == 0) {
         sML[w][0][col] = m;
@@ -357,15 +436,10 @@ __global__ __launch_bounds__(512, 2) void causal_fwd_few_kernel(CausalArgs a) {
         *(uint2*)((uint16_t*)a.out + (long long)(at.o + qi) * a.ld_o + h * DH + 4 * f) =
             make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
         if (f == 0 && a.lse) a.lse[h * a.T + at.o + qi] = top * a.scale + logf(total);
-        if (o.x * 0.f + o.y * 0.f + o.z * 0.f + o.w * 0.f != 0.f) atomicOr(&sBad, 1u << r);
+        if (o.x * 0.f + o.y * 0.f + o.z * 0.f + o.w * 0.f != 0.f) sBad = 1;
     }
     __syncthreads();
-    if (sBad != 0 && w == 0)
-        redo_rows<DH>(a, at, q0, h, hk, __builtin_amdgcn_readfirstlane(sBad), lane, [&](int r, float& rm, float& ri) {
-            float total;
-            join_parts<DH, WAVES>(sT, sML, r, 0, a.c, rm, total);
-            ri = 1.0f / total;
-        });
+    if (sBad != 0 && w == 0) redo_rows<DH>(a, at, q0, h, hk, sT[0][0], sT[0][1], lane);
 }
 
 template <int DH>

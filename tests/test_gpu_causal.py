@@ -272,3 +272,90 @@ def test_outputs_keep_their_bits_whatever_follows(n, at, dh, H, side):
         v2[at:] *= -size
         out2, lse2 = ops.causal_attn_fwd(q2, k2, v2, o, save=True)
         assert torch.equal(out2[:at], out[:at]) and torch.equal(lse2[:, :at], lse[:, :at])
+
+
+@pytest.mark.parametrize("H, side", SIDES)
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("n, at", [(300, 150), (300, 64), (257, 256), (289, 287)])
+def test_later_values_do_not_matter(n, at, dh, H, side):
+    """Infinities and NaN among a token's values reach its own and later outputs, and of those their feature alone; a NaN in its
+    key reaches them all.  On the kernels for few tiles and for many."""
+    on_side(side, [n], H)
+    q, k, v, _ = batch([n], H, 2, dh)
+    o = offsets_of([n])
+    out, lse = ops.causal_attn_fwd(q, k, v, o, save=True)
+    want, _, eo, _ = causal(q, k, v, [n], dh ** -0.5)
+    lone = heads_of_key(H, 1)
+    for t, bad in ((v, float("nan")), (v, float("inf")), (k, float("nan"))):
+        t2 = t.clone()
+        t2[at, 1, 5] = bad
+        out2, lse2 = ops.causal_attn_fwd(q, k if t is v else t2, t2 if t is v else v, o, save=True)
+        same = torch.ones(n, H, dh, dtype=torch.bool, device="cuda")
+        if t is v:
+            same[at:, lone, 5] = False
+            hit = out2[at:, lone, 5]
+            assert (hit == bad).all() if bad == bad else torch.isnan(hit).all()
+            within("before", out2[:at], want[:at], half_step(out2[:at]) + eo[:at] * (1 + 2.0 ** -7))
+            # (the products' own values but in the half of 32 tokens that holds the infinity)
+            same[at - at % 32:at, lone, 5] = False
+            assert torch.equal(lse2, lse)
+        else:
+            same[at:, lone] = False
+            assert torch.isnan(out2[at:, lone]).all() and torch.equal(lse2[:, :at], lse[:, :at])
+        assert torch.equal(out2[same], out[same])
+
+
+def heads_of_key(H, j, Hk=2):
+    return slice(j * H // Hk, (j + 1) * H // Hk)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("H, side", SIDES)
+def test_infinities_in_several_places(H, side, dh):
+    """Infinities of either sign before, in and behind a row's half: their sum by the definition, NaN where signs meet."""
+    n = 270
+    on_side(side, [n], H)
+    q, k, v, _ = batch([n], H, 2, dh)
+    for at, f, x in ((10, 1, torch.inf), (100, 1, -torch.inf), (101, 2, -torch.inf), (103, 2, -torch.inf), (120, 2, torch.nan),
+                     (200, 3, torch.inf), (201, 3, -torch.inf), (269, 4, torch.inf), (0, 6, -torch.inf)):
+        v[at, :, f] = x
+    out = ops.causal_attn_fwd(q, k, v, offsets_of([n]))
+    row = torch.arange(n, device="cuda")
+    for f, spans in ((1, [(10, torch.inf), (100, torch.nan)]), (2, [(101, -torch.inf), (120, torch.nan)]),
+                     (3, [(200, torch.inf), (201, torch.nan)]), (4, [(269, torch.inf)]), (6, [(0, -torch.inf)])):
+        assert torch.isfinite(out[:spans[0][0], :, f]).all(), f
+        for (a, x), (b, _) in zip(spans, spans[1:] + [(n, 0)]):
+            part = out[(row >= a) & (row < b)][..., f]
+            assert torch.isnan(part).all() if x != x else (part == x).all(), (f, a)
+    rest = [c for c in range(dh) if c not in (1, 2, 3, 4, 6)]
+    v[...] = torch.where(torch.isfinite(v), v, torch.zeros_like(v))
+    want, _, eo, _ = causal(q, k, v, [n], dh ** -0.5)
+    within("rest", out[..., rest], want[..., rest], half_step(out[..., rest]) + eo[..., rest] * (1 + 2.0 ** -7))
+    for f, end in ((1, 10), (2, 101), (3, 200), (4, 269)):
+        within(f"feature {f}", out[:end, :, f], want[:end, :, f], half_step(out[:end, :, f]) + eo[:end, :, f] * (1 + 2.0 ** -7))
+
+
+@pytest.mark.parametrize("n, H, dh", [(2000, 2, 128), (8000, 8, 128)])
+def test_one_infinity_does_not_hold_up_the_pass(n, H, dh):
+    """Its half of 32 tokens is redone by products: the pass takes 4.6 and 2.5 times as long, where keys one by one took 295 and
+    330 times; 25 times is refused."""
+    q, k, v, _ = batch([n], H, 1, dh)
+    o = offsets_of([n])
+
+    def least():
+        t = []
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in "ab")
+            a.record()
+            ops.causal_attn_fwd(q, k, v, o)
+            b.record()
+            b.synchronize()
+            t.append(a.elapsed_time(b))
+        return min(t)
+
+    plain = least()
+    for at in (n - 1, n // 2):
+        v2 = v.clone()
+        v[at, :, 3] = torch.inf
+        assert least() < 25 * plain
+        v = v2
