@@ -360,3 +360,9 @@ def test_one_workspace_for_a_session(H, Hk, dh, B):
             assert (room[n:] == 93).all()
             if longest in (1153, 8193):
                 compare(q[:m], [k[:x] for k, x in zip(ks, some)], [v[:x] for v, x in zip(vs, some)], out, lse, dh ** -0.5)
+
+
+@pytest.mark.parametrize("H, Hk, dh", [(40, 1, 128), (70, 2, 64), (33, 1, 32)])
+def test_many_query_heads_over_several_chunks(H, Hk, dh):
+    """More query heads of a key head than one product has columns, and more keys than one workgroup takes."""
+    check([5000, 1, 0, 2049], H, Hk, dh, 32, max_len=5000)

@@ -359,3 +359,66 @@ def test_one_infinity_does_not_hold_up_the_pass(n, H, dh):
         v[at, :, 3] = torch.inf
         assert least() < 25 * plain
         v = v2
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_other_sequences_do_not_matter_in_large_batches(bad, dh):
+    """As above, on the kernels for many tiles, with sequences of several pieces of the backward's work among them."""
+    lengths, H = [70, 33, 1500, 129, 300, 64], 32
+    on_side("many", lengths, H)
+    q, k, v, dout = batch(lengths, H, 4, dh)
+    o, at = offsets_of(lengths), [0, 70, 103, 1603, 1732, 2032, 2096]
+    out, lse = ops.causal_attn_fwd(q, k, v, o, save=True)
+    grads = ops.causal_attn_bwd(dout, q, k, v, out, lse, o)
+    for hit in ([1], [2], [0, 3, 5]):
+        q2, k2, v2, g2 = (t.clone() for t in (q, k, v, dout))
+        keep = torch.ones(2096, dtype=torch.bool, device="cuda")
+        for i in hit:
+            keep[at[i]:at[i + 1]] = False
+            for t in (q2, k2, v2, g2):
+                t[at[i]:at[i + 1]] = bad
+        out2, lse2 = ops.causal_attn_fwd(q2, k2, v2, o, save=True)
+        grads2 = ops.causal_attn_bwd(g2, q2, k2, v2, out2, lse2, o)
+        for a, b in [(out, out2), *zip(grads, grads2)]:
+            assert torch.equal(a[keep], b[keep])
+        assert torch.equal(lse[:, keep], lse2[:, keep])
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_rows_behind_are_left_in_large_batches(dh):
+    lengths, H = [40, 0, 90, 300], 128
+    on_side("many", lengths, H, 50)
+    q, k, v, dout = batch(lengths, H, 16, dh, more=50)
+    n, o = sum(lengths), offsets_of(lengths)
+    for t in (q, k, v, dout):
+        t[n:] = float("nan")
+    out, lse = torch.full_like(q, 7.0), torch.full((H, n + 50), 7.0, device="cuda")
+    ops.causal_attn_fwd(q, k, v, o, save=True, out=out, lse=lse)
+    assert (out[n:] == 7).all() and (lse[:, n:] == 7).all() and torch.isfinite(out).all()
+    grads = [torch.full_like(t, 7.0) for t in (q, k, v)]
+    ops.causal_attn_bwd(dout, q, k, v, out, lse, o, grads=grads)
+    assert all((g[n:] == 7).all() and torch.isfinite(g).all() for g in grads)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("H, side", SIDES)
+@pytest.mark.parametrize("shape", ["rising", "falling", "steps", "one peak"])
+def test_moving_maximum(shape, H, side, dh):
+    """Scores that pass the reference by more than 2^8 at every second half, never, now and then, or once in the middle: outputs,
+    log-sums and gradients."""
+    n = 350
+    on_side(side, [n], H)
+    q, k, v, dout = batch([n], H, 2, dh)
+    ramp = torch.linspace(0, 40, n)
+    x = {"rising": ramp, "falling": ramp.flip(0), "steps": 9.0 * (torch.arange(n) // 70), "one peak": 40.0 * (torch.arange(n) == 170)}[shape]
+    q[..., 0], k[..., 0] = 8.0 * dh ** 0.5 / 8, x.cuda()[:, None].bfloat16()
+    q[..., 1:] *= 0.25
+    o, s = offsets_of([n]), dh ** -0.5
+    out, lse = ops.causal_attn_fwd(q, k, v, o, save=True)
+    want, wl, eo, el = causal(q, k, v, [n], s)
+    within("out", out, want, half_step(out) + eo * (1 + 2.0 ** -7))
+    within("lse", lse, wl, el)
+    got = dict(zip(("dq", "dk", "dv"), ops.causal_attn_bwd(dout, q, k, v, out, lse, o)))
+    for name, (g, b) in causal_back(dout, q, k, v, out, lse, [n], s).items():
+        within(name, got[name], g, half_step(got[name]) + b * (1 + 2.0 ** -7))
