@@ -247,7 +247,7 @@ def _check(status: int) -> None:
 
 def _ptr(x) -> Optional[int]:
     """Device (or host) address of a tensor, an int address, or None."""
-    return x if x is None or x.__class__ is int else x.data_ptr()
+    return x if x is None or isinstance(x, int) else x.data_ptr()
 
 
 _raw_stream = None

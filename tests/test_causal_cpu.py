@@ -402,3 +402,13 @@ def test_backward_workspace_of_the_largest_call():
             row = [size(T, B, H, Hk, dh) for B in (0, 1, 2, 3, 50, 64, 1000)]
             assert all(a <= b for a, b in zip(row, row[1:])) and all(a <= b for a, b in zip(before, row)), (H, T)
             before = row
+
+
+def test_addresses_of_int_subclasses():
+    """An address may be any int, for every entry point."""
+    class Address(int):
+        pass
+
+    assert hstu._ptr(Address(FAKE)) == FAKE and hstu._ptr(FAKE) == FAKE and hstu._ptr(None) is None
+    assert status_of(rope, x=Address(FAKE), out=Address(FAKE + 8)) == INVALID
+    rope(num_tokens=0, x=Address(FAKE))
