@@ -12,6 +12,9 @@
  * on its stream: calls that can run at the same time (captured graphs too) take one each.
  *
  * Query head h uses key and value head h / (heads / kv_heads).
+ *
+ * The attention's products and sums have to stay in fp32's range: |q . k|, and |v| times 2^8 times the tokens that a token sees,
+ * below 2^127 (the sums of v are divided by those of the probabilities, which reach 2^8, at the end).
  */
 #ifndef MTGR_CAUSAL_H
 #define MTGR_CAUSAL_H

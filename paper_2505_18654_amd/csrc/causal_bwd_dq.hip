@@ -10,10 +10,13 @@
 // up to 100 tokens, 8 / 2 heads of 128: the backward 96 -> 107 us, 64 of up to 3,200: 968 -> 974).
 //
 // S and dP are formed again here, two products beside dQ's own: 440 .. 490 us for 60.4 million pairs of 8 heads of 128 (760 ..
-// 840 TFLOP/s), bound by the matrix cores at the clock that the power limit leaves.  With dS stored by the dK / dV kernel (2
-// bytes a pair, up to 2 GB) and dQ from it, the backward took 915 us instead of 947 there, with heads of 64 (8 sequences of
-// 4,096 tokens, 16 / 2 heads) 1,205 instead of 1,021.  A third buffer of keys, copied a tile and a half ahead, changed 1 % for
-// the worse.
+// 840 TFLOP/s).  The matrix cores are busy 42 % of that and the vector units 33 %, and 29 % of the waves' cycles are waits; the
+// forward and the dK / dV kernel, at the power limit's clock, keep the matrix cores busy 53 % and more.  Each operand from LDS
+// feeds one product here: 24 reads for the 24 products of 32 keys.  With heads of 32 and 64 the elements' arithmetic, which does
+// not shrink with the head, outweighs the products: vector units busy 42 and 41 %, matrix cores 16 and 32 (256 sequences of up to
+// 1,000 tokens, 4 / 1 heads of 32; 8 of up to 4,096, 16 / 2 of 64).  With dS stored by the dK / dV kernel (2 bytes a pair, up to
+// 2 GB) and dQ from it, the backward took 915 us instead of 947 there, with heads of 64 (8 sequences of 4,096 tokens, 16 / 2
+// heads) 1,205 instead of 1,021.  A third buffer of keys, copied a tile and a half ahead, changed 1 % for the worse.
 #include <type_traits>
 
 #include "causal_plan.h"

@@ -23,13 +23,15 @@ constexpr int BN = 64;        // keys of a tile
 
 // 32 rows from row0 on of columns of a matrix into a wave's swizzled tile; rows behind `last` are copies of it.
 template <int DH>
-__device__ __forceinline__ void copy_rows(uint16_t* tile, const void* src, long long ld, int col0, long long row0, int last, int lane) {
+__device__ __forceinline__ void copy_rows(uint16_t* tile, const void* src, long long ld, int col0, long long row0, int last,
+                                          int lane) {
     constexpr int CPR = DH / 8;
     const uint16_t* base = (const uint16_t*)src + row0 * ld + col0;
 #pragma unroll
     for (int i = 0; i < CPR / 2; i++) {
         const int row = i * (64 / CPR) + lane / CPR;
-        lds_dma16(lds_address(tile) + i * 1024u, uniform_ptr(base), (uint32_t)(min(row, last) * ld + ((lane % CPR) ^ swz<CPR>(row)) * 8) * 2u);
+        lds_dma16(lds_address(tile) + i * 1024u, uniform_ptr(base),
+                  (uint32_t)(min(row, last) * ld + ((lane % CPR) ^ swz<CPR>(row)) * 8) * 2u);
     }
 }
 
@@ -37,9 +39,10 @@ __device__ __forceinline__ void copy_rows(uint16_t* tile, const void* src, long 
 // sum and outputs of a query in a lane.  issue_k and issue_v copy a half into the wave's tiles; those of the first are under way.
 // open(j): whether there is anything left to do behind half j.
 template <int DH, class IssueK, class IssueV, class Open>
-__device__ __forceinline__ void attend_halves(const CausalArgs& a, const uint16_t* sK, const uint16_t* sV, const bf16x8 (&qreg)[DH / 16],
-                                              floatx16 (&oacc)[DH / 32], float& m, float& l, int first, int step, int end, int diag,
-                                              IssueK issue_k, IssueV issue_v, Open open, int lane) {
+__device__ __forceinline__ void attend_halves(const CausalArgs& a, const uint16_t* sK, const uint16_t* sV,
+                                              const bf16x8 (&qreg)[DH / 16], floatx16 (&oacc)[DH / 32], float& m, float& l,
+                                              int first, int step, int end, int diag, IssueK issue_k, IssueV issue_v,
+                                              Open open, int lane) {
     constexpr int CPR = DH / 8, KSTEPS = DH / 16, DBLK = DH / 32, NI = CPR / 2;
     const int col = lane & 31, hh = lane >> 5;
     for (int j = first; j < end; j += step) {

@@ -16,7 +16,7 @@ the attention (whose backward goes on through the SiLU of the projection) and th
 input gradient (in the Group-LN's backward).  Q, K, V, U are column views of the
 one [T, 4d] activation, which the kernels take with their token stride, and their gradients are
 written into the same layout, so the backward's input-projection products read one [T, 4d]
-gradient.  torch only allocates.
+gradient.  torch allocates, and in causal_prompt and causal_step it forms the lengths (zeros, past + 1).
 """
 from __future__ import annotations
 
@@ -243,8 +243,9 @@ def causal_step(x: torch.Tensor, seg: torch.Tensor, P: CausalParams, heads: int,
                 page_table: torch.Tensor, past: torch.Tensor, rotary: Optional[ops.Rotary] = None,
                 max_len: Optional[int] = None, eps: float = 1e-5, workspace=None) -> torch.Tensor:
     """One more token of each of B sequences, x [B, d] with segments seg [B] int8: appended to the cache behind past [B]
-    tokens and run against it.  A sequence whose past is negative is left alone (its row of the result means nothing).
-    max_len bounds past + 1 (ops.cache_attn); with `workspace` (ops.cache_attn_workspace) a step can be captured."""
+    tokens and run against it.  A sequence whose past is negative is left alone, as is the cache of one whose row of the page
+    table is full (their rows of the result mean nothing).  max_len bounds past + 1 (ops.cache_attn); with `workspace`
+    (ops.cache_attn_workspace) a step can be captured."""
     B, d = x.shape
     xt, _, _ = ops.gln_fwd(x, None, seg, P.gamma, P.beta, eps)
     h = ops.gemm(xt, P.w_qkv, "nn")

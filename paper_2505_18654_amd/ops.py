@@ -667,7 +667,8 @@ def kv_append(cache: KvCache, page_table, past, k, v, offsets=None, q=None, rota
     """Appends new tokens to a paged cache: rows offsets[b] .. offsets[b + 1] - 1 of k and v [N, kv_heads, head_dim] (without
     offsets: row b) become tokens past[b], past[b] + 1, .. of sequence b.  With `rotary`, k is rotated on the way by its
     position in the sequence, and q [N, heads, head_dim] by the same; returns the rotated q (q_out, which may be q), or None
-    without q.  past [B] int32; a sequence whose past is negative is left alone, with its rows of q_out."""
+    without q.  past [B] int32; a sequence whose past is negative is left alone, with its rows of q_out, as are tokens past the
+    columns of the page table."""
     bf, dev = torch.bfloat16, _device()
     c = cache.struct(dev)
     B, pages, ld_table = _page_table(page_table, dev)
